@@ -291,6 +291,81 @@ sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const
                                       int64_t batch, int64_t heads, int64_t head_dim, void *stream);
 
 /*
+ * What stands between the fused q/k/v projection and the attention of a DiT block: RMS norm of every query and key
+ * head, and rotary positions (the paper names the models of Section 4.1 and leaves both to them).  Per (token, head)
+ * row x of head_dim values, all arithmetic in FP32:
+ *     n = weight * x / sqrt(mean(x^2) + eps)          (no weight: n = x)
+ *     each pair (a, b) of the first R = sum(axis_dims) columns becomes (s (a cos t - b sin t), s (b cos t + a sin t)),
+ *     t = positions[token, axis of the pair] * freqs[pair]  (formed and reduced in FP64);  the other columns keep n
+ * rounded once to BF16.
+ *   q, k      host pointers to the descriptions below (read during the call only); k may be NULL
+ *   x, out    [rows, heads, head_dim] BF16: element (m, h, d) at m * ld + h * head_dim + d; ld a multiple of 8,
+ *             >= heads * head_dim.  out may be x itself with the same pitch (in place); otherwise they do not overlap
+ *   weight    [head_dim] BF16, 8-byte aligned, or NULL for no norm
+ *   rotary    host pointer, NULL: norm only (a weight is then needed).  A token m (0 <= m < rows) takes the positions
+ *             of row m % position_rows, so samples of one geometry share a table.
+ *             Pairs are neighbours (2i, 2i+1) or halves (i, i + R/2); pair i takes freqs[i]; the first axis_dims[0] / 2
+ *             pairs belong to axis 0 and so on.  axis_dims are positive and even, 1 <= axes <= 4, R % 8 == 0, R <= head_dim
+ *   head_dim  32, 64, 128 or 256;  eps >= 0
+ */
+typedef enum { SOL_ROTARY_INTERLEAVED = 0, SOL_ROTARY_HALF = 1 } sol_rotary_layout_t;
+typedef enum {
+    SOL_ROTARY_SCALE_NONE = 0, SOL_ROTARY_SCALE_LINEAR = 1, SOL_ROTARY_SCALE_NTK = 2, SOL_ROTARY_SCALE_YARN = 3
+} sol_rotary_scaling_t;
+typedef struct {
+    const int64_t *positions; /* device, [position_rows, axes] */
+    const double *freqs;      /* device, [R / 2] radians per position */
+    int64_t position_rows, axes, axis_dims[4];
+    sol_rotary_layout_t layout;
+    float scale;              /* s: 1, or the factor that a long-context scaling puts on cosine and sine */
+} sol_rotary_t;
+typedef struct {
+    const void *x;
+    void *out;
+    const void *weight;
+    int64_t heads, ld_in, ld_out;
+} sol_head_tensor_t;
+sol_status_t sol_qk_rotary(const sol_head_tensor_t *q, const sol_head_tensor_t *k, int64_t rows, int64_t head_dim,
+                           const sol_rotary_t *rotary, float eps, void *stream);
+
+/*
+ * Gradients of sol_qk_rotary: from dy = d loss / d out,
+ *     dn = the inverse turn of dy (times s);  without a weight dx = dn, with one, xhat = x / sqrt(mean(x^2) + eps):
+ *     dx = (weight dn - xhat mean(weight dn xhat)) / sqrt(mean(x^2) + eps),   dweight = sum over tokens and heads of dn xhat
+ *   dy, x, dx  laid out as x above; x is the forward call's input, read only when there is a weight (else it may be NULL);
+ *              dx may be dy itself or x itself, with the same pitch
+ *   dweight    [head_dim] FP32, overwritten; needed when there is a weight (NULL without one)
+ *   workspace  device scratch of sol_qk_rotary_backward_workspace_bytes(head_dim) bytes, 256-byte aligned; needed when
+ *              there is a weight.  Two calls that may overlap need one each.
+ * The weight gradients are summed in a fixed order: equal inputs give equal bits.
+ */
+typedef struct {
+    const void *dy, *x;
+    void *dx;
+    const void *weight;
+    float *dweight;
+    int64_t heads, ld_dy, ld_x, ld_dx;
+} sol_head_grad_t;
+size_t sol_qk_rotary_backward_workspace_bytes(int64_t head_dim);
+sol_status_t sol_qk_rotary_backward(const sol_head_grad_t *q, const sol_head_grad_t *k, int64_t rows, int64_t head_dim,
+                                    const sol_rotary_t *rotary, float eps, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/*
+ * Frequencies of one position axis of `dim` rotated columns, computed on the host:
+ *     freqs_out[i] = theta^(-2 i / dim), i < dim / 2        (HOST array of doubles), and *scale_out = 1, scaled for
+ * contexts `factor` times longer than the model was trained on:
+ *   LINEAR  freqs / factor;   NTK  theta replaced by theta * factor^(dim / (dim - 2))  (dim > 2)
+ *   YARN    freqs / factor where a pair turns less than beta_slow times over original_length positions, freqs where it
+ *           turns more than beta_fast times, a linear ramp over the pair index between; *scale_out = 0.1 ln(factor) + 1
+ * dim even and positive, theta > 0, factor >= 1; YARN: theta > 1, original_length > 0, beta_fast >= beta_slow > 0.
+ * A caller with several axes calls it once per axis and lays the results side by side.
+ */
+sol_status_t sol_rotary_frequencies(int64_t dim, double theta, sol_rotary_scaling_t scaling, double factor,
+                                    double original_length, double beta_fast, double beta_slow, double *freqs_out,
+                                    double *scale_out);
+
+/*
  * BF16 linear, the full-precision stage-2 reference (Section 3.4):
  *     Y[m,n] = bf16_rne( sum_k x[m,k] * w[n,k] + bias[n] ),  FP32 accumulate.
  */

@@ -29,7 +29,8 @@ EXPORTS = [
     "mxfp4_linear", "nvfp4_linear_split_out", "nvfp4_quantize_into",
     "nvfp4_quantize_linear_delayed", "sol_roll_tensor_scale", "nvfp4_layernorm_quantize", "sol_attention_bf16", "sol_attention_bf16_joint",
     "sol_attention_nvfp4_out", "mxfp4_linear_quantized_out", "sol_set_wait_limit_cycles", "sol_test_hold_loads",
-    "mxfp4_linear_split_out", "mxfp4_quantize_into",
+    "mxfp4_linear_split_out", "mxfp4_quantize_into", "sol_qk_rotary", "sol_qk_rotary_backward",
+    "sol_qk_rotary_backward_workspace_bytes", "sol_rotary_frequencies",
 ]
 
 _lib = None
@@ -109,6 +110,14 @@ def lib() -> ctypes.CDLL:
     L.mxfp4_linear_split_out.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i32, vp, vp, i64, i64, vp, i64, i64, i64, vp]
     L.mxfp4_quantize_into.restype = i32
     L.mxfp4_quantize_into.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, vp]
+    f32, f64 = ctypes.c_float, ctypes.c_double
+    L.sol_qk_rotary.restype = i32
+    L.sol_qk_rotary.argtypes = [vp, vp, i64, i64, vp, f32, vp]
+    L.sol_qk_rotary_backward.restype = i32
+    L.sol_qk_rotary_backward.argtypes = [vp, vp, i64, i64, vp, f32, vp, sz, vp]
+    L.sol_qk_rotary_backward_workspace_bytes.restype, L.sol_qk_rotary_backward_workspace_bytes.argtypes = sz, [i64]
+    L.sol_rotary_frequencies.restype = i32
+    L.sol_rotary_frequencies.argtypes = [i64, f64, i32, f64, f64, f64, f64, vp, vp]
     L.sol_set_wait_limit_cycles.restype, L.sol_set_wait_limit_cycles.argtypes = i32, [i64]
     L.sol_test_hold_loads.restype, L.sol_test_hold_loads.argtypes = i32, [i32]
     L.sol_last_device_status.restype = i32
@@ -187,6 +196,26 @@ def _guarded(fn):
         finally:
             check_guards(fn.__name__)
     return call
+
+
+def _on_device_of_first(fn):
+    """Run `fn` with the device of its first argument current: its launches, its outputs and its stream (the
+    current one of that device) are then that device's, whichever device the caller has current."""
+    @functools.wraps(fn)
+    def call(first, *args, **kwargs):
+        if not first.is_cuda:
+            raise TypeError(f"{fn.__name__}: expected CUDA tensors")
+        if first.device.index == torch.cuda.current_device():
+            return fn(first, *args, **kwargs)
+        with torch.cuda.device(first.device):
+            return fn(first, *args, **kwargs)
+    return call
+
+
+def _need_on(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the call's first tensor on {device}")
 
 
 def _ptr(t) -> int | None:
@@ -482,6 +511,171 @@ def sol_attention_nvfp4_out(q, k, v, out_tscale: torch.Tensor, dest, dest_col0: 
                                          _token_pitch(v), _ptr(out_tscale), _ptr(dq), _ptr(dsf), dq.shape[1] * 2, dest_col0,
                                          _ptr(amax_out), _stream()), "sol_attention_nvfp4_out")
     return dest
+
+
+ROTARY_INTERLEAVED, ROTARY_HALF = 0, 1
+ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+class Rotary(ctypes.Structure):
+    """sol_rotary_t of the C header."""
+    _fields_ = [("positions", ctypes.c_void_p), ("freqs", ctypes.c_void_p), ("position_rows", ctypes.c_int64),
+                ("axes", ctypes.c_int64), ("axis_dims", ctypes.c_int64 * 4), ("layout", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class HeadTensor(ctypes.Structure):
+    """sol_head_tensor_t of the C header."""
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("heads", ctypes.c_int64),
+                ("ld_in", ctypes.c_int64), ("ld_out", ctypes.c_int64)]
+
+
+class HeadGrad(ctypes.Structure):
+    """sol_head_grad_t of the C header."""
+    _fields_ = [("dy", ctypes.c_void_p), ("x", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+                ("dweight", ctypes.c_void_p), ("heads", ctypes.c_int64), ("ld_dy", ctypes.c_int64), ("ld_x", ctypes.c_int64),
+                ("ld_dx", ctypes.c_int64)]
+
+
+def rotary_frequencies(axis_dims, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                       original_length: float = 0.0, beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda"):
+    """Frequencies of the rotated pairs of all axes, side by side (FP64 on `device`), and the factor on cosine and sine.
+
+    `scaling` = "none" | "linear" | "ntk" | "yarn" stretches them for contexts `factor` times longer than the
+    model was trained on (`original_length` positions: "yarn").
+    """
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROTARY_SCALINGS)}")
+    parts, scale = [], ctypes.c_double(1.0)
+    for d in axis_dims:
+        buf = (ctypes.c_double * max(1, d // 2))()
+        _check(lib().sol_rotary_frequencies(d, float(theta), ROTARY_SCALINGS[scaling], float(factor), float(original_length),
+                                            float(beta_fast), float(beta_slow), buf, ctypes.byref(scale)),
+               "sol_rotary_frequencies")
+        parts += list(buf)[:d // 2]
+    if not parts:
+        raise ValueError("no axes")
+    return torch.tensor(parts, dtype=torch.float64, device=device), scale.value
+
+
+def _head_view(name: str, t: torch.Tensor) -> int:
+    """Checks a [B, S, H, D] BF16 view and returns its token pitch."""
+    if t.dtype != torch.bfloat16 or t.dim() != 4:
+        raise TypeError(f"{name}: expected a [B, S, H, D] bf16 tensor")
+    b, s, h, d = t.shape
+    st = t.stride()
+    if st[3] != 1 or (h > 1 and st[2] != d) or (b > 1 and s > 1 and st[0] != s * st[1]):
+        raise ValueError(f"{name}: heads and head dimension must be contiguous, batches stacked densely")
+    return st[1] if s > 1 else (st[0] if b > 1 else h * d)
+
+
+def _rotary_of(positions, freqs, axis_dims, layout, scale, rows: int, device):
+    if positions is None:
+        if freqs is not None:
+            raise ValueError("freqs without positions")
+        return None
+    if positions.dtype != torch.int64 or positions.dim() != 2 or not positions.is_contiguous():
+        raise TypeError("positions: expected a dense [rows, axes] int64 tensor")
+    if freqs is None or freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+        raise TypeError("freqs: expected a dense 1-D float64 tensor")
+    _need_on(device, positions=positions, freqs=freqs)
+    dims = [2 * freqs.shape[0]] if axis_dims is None else list(axis_dims)
+    if len(dims) != positions.shape[1] or len(dims) > 4 or sum(dims) != 2 * freqs.shape[0]:
+        raise ValueError("axis_dims must name each axis of positions and add up to twice the frequencies")
+    if positions.shape[0] == 0 or rows % positions.shape[0] != 0:
+        raise ValueError("the tokens must be a multiple of the rows of positions")
+    return Rotary(positions.data_ptr(), freqs.data_ptr(), positions.shape[0], len(dims), (ctypes.c_int64 * 4)(*dims), layout, scale)
+
+
+def _norm_weight(name: str, w, d: int, device):
+    if w is not None:
+        if w.dtype != torch.bfloat16 or w.dim() != 1 or w.shape[0] != d or (d > 1 and w.stride(0) != 1):
+            raise TypeError(f"{name}: expected a dense [head_dim] bf16 tensor")
+        _need_on(device, **{name: w})
+
+
+@_on_device_of_first
+def sol_qk_rotary(q, k, positions, freqs, axis_dims=None, layout: int = ROTARY_INTERLEAVED, q_weight=None, k_weight=None,
+                  eps: float = 1e-6, scale: float = 1.0, out=None):
+    """RMS norm of every head of q [B, S, H, D] and k [B, S, Hk, D] (where a weight is given), then rotary positions.
+
+    q and k may be views into a fused projection output; k may be None.  `positions` [R, axes] int64 holds the
+    position of each token (token m of the B * S takes row m % R), or is None for the norm alone; `freqs`, `scale`
+    as from rotary_frequencies; `axis_dims` the rotated columns of each axis (default: one axis).  Returns (q', k');
+    `out` = (q_out, k_out) supplies the destinations, which may be q and k themselves.
+    """
+    B_, S_, H, D = q.shape
+    rows, device = B_ * S_, q.device
+    if k is not None and (k.dim() != 4 or k.shape[0] != B_ or k.shape[1] != S_ or k.shape[3] != D):
+        raise ValueError("k must share q's batch, tokens and head dimension")
+    rot = _rotary_of(positions, freqs, axis_dims, layout, scale, rows, device)
+    heads, outs = [], []
+    for i, (name, x, w) in enumerate((("q", q, q_weight), ("k", k, k_weight))):
+        if x is None:
+            heads.append(None)
+            outs.append(None)
+            continue
+        ld = _head_view(name, x)
+        _norm_weight(name + "_weight", w, D, device)
+        o = out[i] if out is not None else _empty(tuple(x.shape), torch.bfloat16, device)
+        _need_on(device, **{name: x, name + "_out": o})
+        if o.shape != x.shape:
+            raise ValueError(f"{name}'s output must have its shape")
+        heads.append(HeadTensor(x.data_ptr(), o.data_ptr(), _ptr(w), x.shape[2], ld, _head_view(name + "_out", o)))
+        outs.append(o)
+    _check(lib().sol_qk_rotary(ctypes.byref(heads[0]), None if k is None else ctypes.byref(heads[1]), rows, D,
+                               None if rot is None else ctypes.byref(rot), eps, _stream()), "sol_qk_rotary")
+    return outs[0], outs[1]
+
+
+@_on_device_of_first
+def sol_qk_rotary_backward(dq, dk, q, k, positions, freqs, axis_dims=None, layout: int = ROTARY_INTERLEAVED, q_weight=None,
+                           k_weight=None, eps: float = 1e-6, scale: float = 1.0, out=None,
+                           workspace: torch.Tensor | None = None):
+    """Gradients of sol_qk_rotary from those of its outputs: (grad q, grad k, grad q_weight, grad k_weight).
+
+    q and k are the forward call's inputs (needed where there is a weight, else they may be None); dk may be None.
+    Weight gradients are FP32 [D], None without a weight.  `out` = (grad q, grad k) destinations, which may be
+    dq and dk themselves.
+    """
+    B_, S_, H, D = dq.shape
+    rows, device = B_ * S_, dq.device
+    if dk is not None and (dk.dim() != 4 or dk.shape[0] != B_ or dk.shape[1] != S_ or dk.shape[3] != D):
+        raise ValueError("dk must share dq's batch, tokens and head dimension")
+    rot = _rotary_of(positions, freqs, axis_dims, layout, scale, rows, device)
+    grads, dxs, dws = [], [], []
+    for i, (name, dy, x, w) in enumerate((("q", dq, q, q_weight), ("k", dk, k, k_weight))):
+        if dy is None:
+            grads.append(None)
+            dxs.append(None)
+            dws.append(None)
+            continue
+        ld_dy, ld_x, dw = _head_view("d" + name, dy), 0, None
+        _norm_weight(name + "_weight", w, D, device)
+        if w is not None:
+            if x is None or x.shape != dy.shape:
+                raise ValueError(f"{name} must be the forward input, with d{name}'s shape")
+            ld_x = _head_view(name, x)
+            _need_on(device, **{name: x})
+            dw = _empty(D, torch.float32, device)
+        dx = out[i] if out is not None else _empty(tuple(dy.shape), torch.bfloat16, device)
+        _need_on(device, **{"d" + name: dy, name + "_grad": dx})
+        if dx.shape != dy.shape:
+            raise ValueError(f"{name}'s gradient must have its shape")
+        grads.append(HeadGrad(dy.data_ptr(), None if w is None else x.data_ptr(), dx.data_ptr(), _ptr(w), _ptr(dw), dy.shape[2],
+                              ld_dy, ld_x, _head_view(name + "_grad", dx)))
+        dxs.append(dx)
+        dws.append(dw)
+    need = 0
+    if dws[0] is not None or dws[1] is not None:
+        need = lib().sol_qk_rotary_backward_workspace_bytes(D)
+        if workspace is None:
+            workspace = _empty(max(1, need), torch.uint8, device)
+        _need_on(device, workspace=workspace)
+    _check(lib().sol_qk_rotary_backward(ctypes.byref(grads[0]), None if dk is None else ctypes.byref(grads[1]), rows, D,
+                                        None if rot is None else ctypes.byref(rot), eps, _ptr(workspace) if need else None,
+                                        workspace.numel() * workspace.element_size() if need else 0, _stream()),
+           "sol_qk_rotary_backward")
+    return dxs[0], dxs[1], dws[0], dws[1]
 
 
 def mxfp4_scale_bytes(rows: int, K: int, layout: int = SF_SWIZZLED_128x4) -> int:

@@ -3,6 +3,7 @@
 #include "sol_internal.h"
 #include "gemm_common.cuh"
 
+#include <cmath>
 #include <cstddef>
 #include <mutex>
 
@@ -120,6 +121,35 @@ bool shape_ok(int64_t rows, int64_t K) {
     return rows > 0 && K > 0 && K % 32 == 0 && rows <= (1LL << 30) && K <= (1LL << 24) &&
            ceil_div(rows, 128) * ceil_div(K, 256) <= 0x7FFFFFFFLL && ceil_div(rows * (K / 8), 2048) <= 0x7FFFFFFFLL;
 }
+
+// Host description of the rotary positions -> the kernels' form.  Device pointers are not followed.
+sol_status_t make_turn(const sol_rotary_t *r, int64_t head_dim, rotary::Turn *t) {
+    *t = rotary::Turn{};
+    if (r == nullptr) return SOL_OK;
+    if (r->positions == nullptr || r->freqs == nullptr) return SOL_ERR_NULL_POINTER;
+    if (r->axes < 1 || r->axes > 4 || r->position_rows < 1 || r->position_rows > 0x7FFFFFFFLL || !std::isfinite(r->scale))
+        return SOL_ERR_BAD_SHAPE;
+    if (r->layout != SOL_ROTARY_INTERLEAVED && r->layout != SOL_ROTARY_HALF) return SOL_ERR_BAD_LAYOUT;
+    int64_t rot = 0;
+    for (int i = 0; i < 4; ++i) {
+        if (i < r->axes) {
+            if (r->axis_dims[i] <= 0 || r->axis_dims[i] % 2 != 0 || r->axis_dims[i] > head_dim) return SOL_ERR_BAD_SHAPE;
+            rot += r->axis_dims[i];
+        }
+        if (i < 3) t->axis_end[i] = i < r->axes - 1 ? static_cast<int>(rot / 2) : 0x7FFFFFFF;
+    }
+    if (rot % 8 != 0 || rot > head_dim) return SOL_ERR_BAD_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(r->positions) & 7u) || (reinterpret_cast<uintptr_t>(r->freqs) & 7u)) return SOL_ERR_ALIGNMENT;
+    t->positions = r->positions;
+    t->freqs = r->freqs;
+    t->position_rows = static_cast<uint32_t>(r->position_rows);
+    t->axes = static_cast<int>(r->axes);
+    t->rot = static_cast<int>(rot);
+    t->scale = r->scale;
+    return SOL_OK;
+}
+
+bool aligned8(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 
 size_t align256(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
 
@@ -607,6 +637,111 @@ sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const
     const attn::Stream b{second->q, second->k, second->v, second->out, second->seq, second->seq,
                          second->ld_q, second->ld_k, second->ld_v, second->ld_out};
     return attn::launch_attention(&a, b, batch, heads, head_dim, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+sol_status_t sol_qk_rotary(const sol_head_tensor_t *q, const sol_head_tensor_t *k, int64_t rows, int64_t head_dim,
+                           const sol_rotary_t *rot, float eps, void *stream) {
+    if (q == nullptr) return SOL_ERR_NULL_POINTER;
+    if (!rotary::head_dim_ok(head_dim) || rows <= 0 || rows > 0x7FFFFFFFLL || !(eps >= 0.0f)) return SOL_ERR_BAD_SHAPE;
+    rotary::Heads h[2] = {};
+    const sol_head_tensor_t *both[2] = {q, k};
+    for (int i = 0; i < 2; ++i) {
+        const sol_head_tensor_t *s = both[i];
+        if (s == nullptr) continue;
+        if (s->x == nullptr || s->out == nullptr || (rot == nullptr && s->weight == nullptr)) return SOL_ERR_NULL_POINTER;
+        if (s->heads <= 0 || s->heads > 65535 || s->ld_in < s->heads * head_dim || s->ld_out < s->heads * head_dim)
+            return SOL_ERR_BAD_SHAPE;
+        if (!aligned16(s->x) || !aligned16(s->out) || s->ld_in % 8 != 0 || s->ld_out % 8 != 0 || !aligned8(s->weight))
+            return SOL_ERR_ALIGNMENT;
+        h[i] = rotary::Heads{static_cast<const uint16_t *>(s->x), static_cast<uint16_t *>(s->out),
+                             static_cast<const uint16_t *>(s->weight), static_cast<int>(s->heads), s->ld_in, s->ld_out};
+    }
+    rotary::Turn t;
+    sol_status_t st = make_turn(rot, head_dim, &t);
+    if (st != SOL_OK) return st;
+    const DeviceInfo *dev = nullptr;
+    st = check_arch(&dev);
+    if (st != SOL_OK) return st;
+    return rotary::launch_forward(h[0], h[1], t, rows, head_dim, rot != nullptr && rot->layout == SOL_ROTARY_HALF, eps,
+                                  static_cast<cudaStream_t>(stream));
+}
+
+size_t sol_qk_rotary_backward_workspace_bytes(int64_t head_dim) {
+    return rotary::head_dim_ok(head_dim) ? rotary::backward_workspace_bytes(head_dim) : 0;
+}
+
+sol_status_t sol_qk_rotary_backward(const sol_head_grad_t *q, const sol_head_grad_t *k, int64_t rows, int64_t head_dim,
+                                    const sol_rotary_t *rot, float eps, void *workspace, size_t workspace_bytes,
+                                    void *stream) {
+    if (q == nullptr) return SOL_ERR_NULL_POINTER;
+    if (!rotary::head_dim_ok(head_dim) || rows <= 0 || rows > 0x7FFFFFFFLL || !(eps >= 0.0f)) return SOL_ERR_BAD_SHAPE;
+    rotary::Grads g[2] = {};
+    const sol_head_grad_t *both[2] = {q, k};
+    bool weights = false;
+    for (int i = 0; i < 2; ++i) {
+        const sol_head_grad_t *s = both[i];
+        if (s == nullptr) continue;
+        if (s->dy == nullptr || s->dx == nullptr || (rot == nullptr && s->weight == nullptr)) return SOL_ERR_NULL_POINTER;
+        if (s->weight != nullptr && (s->x == nullptr || s->dweight == nullptr)) return SOL_ERR_NULL_POINTER;
+        const int64_t cols = s->heads * head_dim;
+        if (s->heads <= 0 || s->heads > 65535 || s->ld_dy < cols || s->ld_dx < cols || (s->weight != nullptr && s->ld_x < cols))
+            return SOL_ERR_BAD_SHAPE;
+        if (!aligned16(s->dy) || !aligned16(s->dx) || s->ld_dy % 8 != 0 || s->ld_dx % 8 != 0 || !aligned8(s->weight) ||
+            (s->weight != nullptr && (!aligned16(s->x) || s->ld_x % 8 != 0 || (reinterpret_cast<uintptr_t>(s->dweight) & 3u))))
+            return SOL_ERR_ALIGNMENT;
+        weights = weights || s->weight != nullptr;
+        g[i] = rotary::Grads{static_cast<const uint16_t *>(s->dy), static_cast<const uint16_t *>(s->x),
+                             static_cast<uint16_t *>(s->dx), static_cast<const uint16_t *>(s->weight),
+                             s->weight != nullptr ? s->dweight : nullptr, static_cast<int>(s->heads), s->ld_dy, s->ld_x, s->ld_dx};
+    }
+    rotary::Turn t;
+    sol_status_t st = make_turn(rot, head_dim, &t);
+    if (st != SOL_OK) return st;
+    if (weights) {
+        if (workspace == nullptr) return SOL_ERR_NULL_POINTER;
+        if (workspace_bytes < rotary::backward_workspace_bytes(head_dim)) return SOL_ERR_WORKSPACE_TOO_SMALL;
+        if (reinterpret_cast<uintptr_t>(workspace) & 255u) return SOL_ERR_ALIGNMENT;
+    }
+    const DeviceInfo *dev = nullptr;
+    st = check_arch(&dev);
+    if (st != SOL_OK) return st;
+    return rotary::launch_backward(g[0], g[1], t, rows, head_dim, rot != nullptr && rot->layout == SOL_ROTARY_HALF, eps,
+                                   weights ? static_cast<double *>(workspace) : nullptr, static_cast<cudaStream_t>(stream), dev);
+}
+
+sol_status_t sol_rotary_frequencies(int64_t dim, double theta, sol_rotary_scaling_t scaling, double factor,
+                                    double original_length, double beta_fast, double beta_slow, double *freqs_out,
+                                    double *scale_out) {
+    if (freqs_out == nullptr || scale_out == nullptr) return SOL_ERR_NULL_POINTER;
+    if (scaling != SOL_ROTARY_SCALE_NONE && scaling != SOL_ROTARY_SCALE_LINEAR && scaling != SOL_ROTARY_SCALE_NTK &&
+        scaling != SOL_ROTARY_SCALE_YARN)
+        return SOL_ERR_BAD_LAYOUT;
+    if (dim <= 0 || dim % 2 != 0 || dim > 4096 || !(theta > 0.0) || !std::isfinite(theta) || !(factor >= 1.0) || !std::isfinite(factor))
+        return SOL_ERR_BAD_SHAPE;
+    if (scaling == SOL_ROTARY_SCALE_NTK && dim <= 2) return SOL_ERR_BAD_SHAPE;
+    if (scaling == SOL_ROTARY_SCALE_YARN && (!(theta > 1.0) || !(original_length > 0.0) || !std::isfinite(original_length) ||
+                                             !(beta_slow > 0.0) || !(beta_fast >= beta_slow) || !std::isfinite(beta_fast)))
+        return SOL_ERR_BAD_SHAPE;
+    const double d = static_cast<double>(dim);
+    const double base = scaling == SOL_ROTARY_SCALE_NTK ? theta * std::pow(factor, d / (d - 2.0)) : theta;
+    double lo = 0.0, hi = 0.0;
+    if (scaling == SOL_ROTARY_SCALE_YARN) {
+        // the (fractional) pair index that turns `beta` times over the original length
+        auto pair_of = [&](double beta) { return d * std::log(original_length / (beta * 6.283185307179586477)) / (2.0 * std::log(theta)); };
+        lo = std::fmax(std::floor(pair_of(beta_fast)), 0.0);
+        hi = std::fmin(std::ceil(pair_of(beta_slow)), d - 1.0);
+    }
+    for (int64_t i = 0; i < dim / 2; ++i) {
+        double f = std::pow(base, -2.0 * static_cast<double>(i) / d);
+        if (scaling == SOL_ROTARY_SCALE_LINEAR) f /= factor;
+        if (scaling == SOL_ROTARY_SCALE_YARN) {
+            const double ramp = std::fmin(std::fmax((static_cast<double>(i) - lo) / std::fmax(hi - lo, 0.001), 0.0), 1.0);
+            f = f / factor * ramp + f * (1.0 - ramp);
+        }
+        freqs_out[i] = f;
+    }
+    *scale_out = scaling == SOL_ROTARY_SCALE_YARN ? 0.1 * std::log(factor) + 1.0 : 1.0;
+    return SOL_OK;
 }
 
 sol_status_t nvfp4_quantize_linear(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf,

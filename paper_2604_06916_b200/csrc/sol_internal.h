@@ -147,6 +147,40 @@ sol_status_t launch_attention(const Stream *a, const Stream &b, int64_t batch, i
                               const QuantDest *qd, cudaStream_t stream);
 }
 
+// Head norm and rotary positions of q and k (a tensor with no heads is absent).
+namespace rotary {
+struct Heads {
+    const uint16_t *x;
+    uint16_t *out;
+    const uint16_t *weight;   // [head_dim], or null: no norm
+    int heads;
+    int64_t ld_in, ld_out;
+};
+struct Grads {
+    const uint16_t *dy, *x;
+    uint16_t *dx;
+    const uint16_t *weight;
+    float *dweight;
+    int heads;
+    int64_t ld_dy, ld_x, ld_dx;
+};
+struct Turn {
+    const int64_t *positions;   // [position_rows, axes]; token m uses row m % position_rows
+    const double *freqs;        // [rot / 2] radians per position
+    uint32_t position_rows;
+    int axes;
+    int axis_end[3];            // first pair behind axis 0, 1, 2
+    int rot;                    // rotated columns, a multiple of 8; 0: none
+    float scale;
+};
+bool head_dim_ok(int64_t head_dim);
+size_t backward_workspace_bytes(int64_t head_dim);
+sol_status_t launch_forward(const Heads &q, const Heads &k, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
+                            cudaStream_t stream);
+sol_status_t launch_backward(const Grads &q, const Grads &k, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
+                             double *partials, cudaStream_t stream, const DeviceInfo *dev);
+}
+
 // Scale-factor buffer in the chunked layout as a 3-D tensor [row chunk][k chunk][128 x u32]; the box
 // covers `box_k_chunks` k-chunks of `box_row_chunks` row chunks (out-of-range chunks read as zero).
 bool make_tmap_sf(CUtensorMap *out, const void *base, uint64_t chunks_k, uint64_t row_chunks,
