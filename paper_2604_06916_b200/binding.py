@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 import types
 
 import torch
@@ -146,6 +147,7 @@ def _stream() -> int:
 GUARD_BYTES = 4096
 GUARD_BYTE = 0xA5
 _guard_pending: list = []
+_guarding = False        # inside a guarded call
 
 
 def guard_mode() -> bool:
@@ -189,11 +191,14 @@ def check_guards(where: str = "") -> None:
 def _guarded(fn):
     @functools.wraps(fn)
     def call(*args, **kwargs):
+        global _guarding
         if not guard_mode():
             return fn(*args, **kwargs)
+        _guarding = True
         try:
             return fn(*args, **kwargs)
         finally:
+            _guarding = False
             check_guards(fn.__name__)
     return call
 
@@ -205,17 +210,21 @@ def _on_device_of_first(fn):
     def call(first, *args, **kwargs):
         if not first.is_cuda:
             raise TypeError(f"{fn.__name__}: expected CUDA tensors")
-        if first.device.index == torch.cuda.current_device():
+        if first.get_device() == torch.cuda.current_device():
             return fn(first, *args, **kwargs)
         with torch.cuda.device(first.device):
             return fn(first, *args, **kwargs)
     return call
 
 
-def _need_on(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, the call's first tensor on {device}")
+def _raw_stream(index: int) -> int:
+    """Handle of the current stream of device `index` (no Stream object is built)."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _like(x: torch.Tensor) -> torch.Tensor:
+    """A dense output of x's shape and type."""
+    return _empty(tuple(x.shape), x.dtype, x.device) if _guarding else torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 def _ptr(t) -> int | None:
@@ -517,23 +526,11 @@ ROTARY_INTERLEAVED, ROTARY_HALF = 0, 1
 ROTARY_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
-class Rotary(ctypes.Structure):
-    """sol_rotary_t of the C header."""
-    _fields_ = [("positions", ctypes.c_void_p), ("freqs", ctypes.c_void_p), ("position_rows", ctypes.c_int64),
-                ("axes", ctypes.c_int64), ("axis_dims", ctypes.c_int64 * 4), ("layout", ctypes.c_int), ("scale", ctypes.c_float)]
-
-
-class HeadTensor(ctypes.Structure):
-    """sol_head_tensor_t of the C header."""
-    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("heads", ctypes.c_int64),
-                ("ld_in", ctypes.c_int64), ("ld_out", ctypes.c_int64)]
-
-
-class HeadGrad(ctypes.Structure):
-    """sol_head_grad_t of the C header."""
-    _fields_ = [("dy", ctypes.c_void_p), ("x", ctypes.c_void_p), ("dx", ctypes.c_void_p), ("weight", ctypes.c_void_p),
-                ("dweight", ctypes.c_void_p), ("heads", ctypes.c_int64), ("ld_dy", ctypes.c_int64), ("ld_x", ctypes.c_int64),
-                ("ld_dx", ctypes.c_int64)]
+# sol_rotary_t, sol_head_tensor_t and sol_head_grad_t of the C header, packed by the native rules: these calls are a few
+# microseconds of GPU work for short streams, and a packed string costs a quarter of a ctypes structure.
+_ROTARY = struct.Struct("@PPqqqqqqif")
+_HEAD_TENSOR = struct.Struct("@PPPqqq")
+_HEAD_GRAD = struct.Struct("@PPPPPqqqq")
 
 
 def rotary_frequencies(axis_dims, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -557,40 +554,59 @@ def rotary_frequencies(axis_dims, theta: float = 10000.0, scaling: str = "none",
     return torch.tensor(parts, dtype=torch.float64, device=device), scale.value
 
 
-def _head_view(name: str, t: torch.Tensor) -> int:
-    """Checks a [B, S, H, D] BF16 view and returns its token pitch."""
-    if t.dtype != torch.bfloat16 or t.dim() != 4:
+def _head_view(name: str, t: torch.Tensor, shape, index: int) -> int:
+    """Checks a BF16 view of the given [B, S, H, D] on CUDA device `index` and returns its token pitch."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 4:
         raise TypeError(f"{name}: expected a [B, S, H, D] bf16 tensor")
-    b, s, h, d = t.shape
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the call's first tensor on cuda:{index}")
+    b, s, h, d = shape
     st = t.stride()
     if st[3] != 1 or (h > 1 and st[2] != d) or (b > 1 and s > 1 and st[0] != s * st[1]):
         raise ValueError(f"{name}: heads and head dimension must be contiguous, batches stacked densely")
     return st[1] if s > 1 else (st[0] if b > 1 else h * d)
 
 
-def _rotary_of(positions, freqs, axis_dims, layout, scale, rows: int, device):
+def _rotary_of(positions, freqs, axis_dims, layout, scale, rows: int, index: int):
     if positions is None:
         if freqs is not None:
             raise ValueError("freqs without positions")
         return None
-    if positions.dtype != torch.int64 or positions.dim() != 2 or not positions.is_contiguous():
+    if positions.dtype is not torch.int64 or positions.dim() != 2 or not positions.is_contiguous():
         raise TypeError("positions: expected a dense [rows, axes] int64 tensor")
-    if freqs is None or freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
+    if freqs is None or freqs.dtype is not torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous():
         raise TypeError("freqs: expected a dense 1-D float64 tensor")
-    _need_on(device, positions=positions, freqs=freqs)
-    dims = [2 * freqs.shape[0]] if axis_dims is None else list(axis_dims)
-    if len(dims) != positions.shape[1] or len(dims) > 4 or sum(dims) != 2 * freqs.shape[0]:
+    if positions.get_device() != index or freqs.get_device() != index:
+        raise ValueError(f"positions and freqs must be on the first tensor's device, cuda:{index}")
+    pos_rows, axes = positions.shape
+    columns = 2 * freqs.shape[0]
+    dims = (columns,) if axis_dims is None else tuple(axis_dims)
+    if len(dims) != axes or axes > 4 or sum(dims) != columns:
         raise ValueError("axis_dims must name each axis of positions and add up to twice the frequencies")
-    if positions.shape[0] == 0 or rows % positions.shape[0] != 0:
+    if pos_rows == 0 or rows % pos_rows != 0:
         raise ValueError("the tokens must be a multiple of the rows of positions")
-    return Rotary(positions.data_ptr(), freqs.data_ptr(), positions.shape[0], len(dims), (ctypes.c_int64 * 4)(*dims), layout, scale)
+    return _ROTARY.pack(positions.data_ptr(), freqs.data_ptr(), pos_rows, axes, *dims, *(0,) * (4 - axes), layout, scale)
 
 
-def _norm_weight(name: str, w, d: int, device):
-    if w is not None:
-        if w.dtype != torch.bfloat16 or w.dim() != 1 or w.shape[0] != d or (d > 1 and w.stride(0) != 1):
-            raise TypeError(f"{name}: expected a dense [head_dim] bf16 tensor")
-        _need_on(device, **{name: w})
+def _norm_weight(name: str, w, d: int, index: int) -> int:
+    if w is None:
+        return 0
+    if w.dtype is not torch.bfloat16 or w.dim() != 1 or w.shape[0] != d or not w.is_contiguous() or w.get_device() != index:
+        raise TypeError(f"{name}: expected a dense [head_dim] bf16 tensor on the first tensor's device")
+    return w.data_ptr()
+
+
+def _beside(name: str, x, of: str, like):
+    """`like`'s [B, S, ., D] with x's own number of heads."""
+    if like.dim() != 4 or x.dim() != 4:
+        raise TypeError(f"{of} and {name}: expected [B, S, H, D] bf16 tensors")
+    b, s, _, d = like.shape
+    want = (b, s, x.shape[2], d)
+    if x.shape != want:
+        raise ValueError(f"{name} must share {of}'s batch, tokens and head dimension")
+    return want
 
 
 @_on_device_of_first
@@ -603,28 +619,22 @@ def sol_qk_rotary(q, k, positions, freqs, axis_dims=None, layout: int = ROTARY_I
     as from rotary_frequencies; `axis_dims` the rotated columns of each axis (default: one axis).  Returns (q', k');
     `out` = (q_out, k_out) supplies the destinations, which may be q and k themselves.
     """
-    B_, S_, H, D = q.shape
-    rows, device = B_ * S_, q.device
-    if k is not None and (k.dim() != 4 or k.shape[0] != B_ or k.shape[1] != S_ or k.shape[3] != D):
-        raise ValueError("k must share q's batch, tokens and head dimension")
-    rot = _rotary_of(positions, freqs, axis_dims, layout, scale, rows, device)
-    heads, outs = [], []
-    for i, (name, x, w) in enumerate((("q", q, q_weight), ("k", k, k_weight))):
-        if x is None:
-            heads.append(None)
-            outs.append(None)
-            continue
-        ld = _head_view(name, x)
-        _norm_weight(name + "_weight", w, D, device)
-        o = out[i] if out is not None else _empty(tuple(x.shape), torch.bfloat16, device)
-        _need_on(device, **{name: x, name + "_out": o})
-        if o.shape != x.shape:
-            raise ValueError(f"{name}'s output must have its shape")
-        heads.append(HeadTensor(x.data_ptr(), o.data_ptr(), _ptr(w), x.shape[2], ld, _head_view(name + "_out", o)))
-        outs.append(o)
-    _check(lib().sol_qk_rotary(ctypes.byref(heads[0]), None if k is None else ctypes.byref(heads[1]), rows, D,
-                               None if rot is None else ctypes.byref(rot), eps, _stream()), "sol_qk_rotary")
-    return outs[0], outs[1]
+    index = q.get_device()
+    b, s, h, d = shape = _beside("q", q, "q", q)
+    rot = _rotary_of(positions, freqs, axis_dims, layout, scale, b * s, index)
+    oq = _like(q) if out is None else out[0]
+    pq = _HEAD_TENSOR.pack(q.data_ptr(), oq.data_ptr(), _norm_weight("q_weight", q_weight, d, index), h,
+                           _head_view("q", q, shape, index), _head_view("q_out", oq, shape, index))
+    ok = pk = None
+    if k is not None:
+        shape = _beside("k", k, "q", q)
+        ok = _like(k) if out is None else out[1]
+        pk = _HEAD_TENSOR.pack(k.data_ptr(), ok.data_ptr(), _norm_weight("k_weight", k_weight, d, index), shape[2],
+                               _head_view("k", k, shape, index), _head_view("k_out", ok, shape, index))
+    code = lib().sol_qk_rotary(pq, pk, b * s, d, rot, eps, _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_qk_rotary")
+    return oq, ok
 
 
 @_on_device_of_first
@@ -637,44 +647,35 @@ def sol_qk_rotary_backward(dq, dk, q, k, positions, freqs, axis_dims=None, layou
     Weight gradients are FP32 [D], None without a weight.  `out` = (grad q, grad k) destinations, which may be
     dq and dk themselves.
     """
-    B_, S_, H, D = dq.shape
-    rows, device = B_ * S_, dq.device
-    if dk is not None and (dk.dim() != 4 or dk.shape[0] != B_ or dk.shape[1] != S_ or dk.shape[3] != D):
-        raise ValueError("dk must share dq's batch, tokens and head dimension")
-    rot = _rotary_of(positions, freqs, axis_dims, layout, scale, rows, device)
-    grads, dxs, dws = [], [], []
+    index = dq.get_device()
+    b, s, _, d = _beside("dq", dq, "dq", dq)
+    rot = _rotary_of(positions, freqs, axis_dims, layout, scale, b * s, index)
+    packed, dxs, dws = [None, None], [None, None], [None, None]
     for i, (name, dy, x, w) in enumerate((("q", dq, q, q_weight), ("k", dk, k, k_weight))):
         if dy is None:
-            grads.append(None)
-            dxs.append(None)
-            dws.append(None)
             continue
-        ld_dy, ld_x, dw = _head_view("d" + name, dy), 0, None
-        _norm_weight(name + "_weight", w, D, device)
-        if w is not None:
-            if x is None or x.shape != dy.shape:
-                raise ValueError(f"{name} must be the forward input, with d{name}'s shape")
-            ld_x = _head_view(name, x)
-            _need_on(device, **{name: x})
-            dw = _empty(D, torch.float32, device)
-        dx = out[i] if out is not None else _empty(tuple(dy.shape), torch.bfloat16, device)
-        _need_on(device, **{"d" + name: dy, name + "_grad": dx})
-        if dx.shape != dy.shape:
-            raise ValueError(f"{name}'s gradient must have its shape")
-        grads.append(HeadGrad(dy.data_ptr(), None if w is None else x.data_ptr(), dx.data_ptr(), _ptr(w), _ptr(dw), dy.shape[2],
-                              ld_dy, ld_x, _head_view(name + "_grad", dx)))
-        dxs.append(dx)
-        dws.append(dw)
-    need = 0
+        shape = _beside("d" + name, dy, "dq", dq)
+        weight = _norm_weight(name + "_weight", w, d, index)
+        x_ptr = ld_x = dw_ptr = 0
+        if weight:
+            if x is None:
+                raise ValueError(f"{name}: the gradient of a norm needs the forward input")
+            ld_x, x_ptr = _head_view(name, x, shape, index), x.data_ptr()
+            dws[i] = _empty(d, torch.float32, dy.device)
+            dw_ptr = dws[i].data_ptr()
+        dx = dxs[i] = _like(dy) if out is None else out[i]
+        packed[i] = _HEAD_GRAD.pack(dy.data_ptr(), x_ptr, dx.data_ptr(), weight, dw_ptr, shape[2],
+                                    _head_view("d" + name, dy, shape, index), ld_x, _head_view(name + "_grad", dx, shape, index))
+    ws_ptr = ws_bytes = 0
     if dws[0] is not None or dws[1] is not None:
-        need = lib().sol_qk_rotary_backward_workspace_bytes(D)
         if workspace is None:
-            workspace = _empty(max(1, need), torch.uint8, device)
-        _need_on(device, workspace=workspace)
-    _check(lib().sol_qk_rotary_backward(ctypes.byref(grads[0]), None if dk is None else ctypes.byref(grads[1]), rows, D,
-                                        None if rot is None else ctypes.byref(rot), eps, _ptr(workspace) if need else None,
-                                        workspace.numel() * workspace.element_size() if need else 0, _stream()),
-           "sol_qk_rotary_backward")
+            workspace = _empty(max(1, lib().sol_qk_rotary_backward_workspace_bytes(d)), torch.uint8, dq.device)
+        elif workspace.get_device() != index or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a dense tensor on the first tensor's device")
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    code = lib().sol_qk_rotary_backward(packed[0], packed[1], b * s, d, rot, eps, ws_ptr, ws_bytes, _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_qk_rotary_backward")
     return dxs[0], dxs[1], dws[0], dws[1]
 
 

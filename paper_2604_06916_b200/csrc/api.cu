@@ -643,7 +643,7 @@ sol_status_t sol_qk_rotary(const sol_head_tensor_t *q, const sol_head_tensor_t *
                            const sol_rotary_t *rot, float eps, void *stream) {
     if (q == nullptr) return SOL_ERR_NULL_POINTER;
     if (!rotary::head_dim_ok(head_dim) || rows <= 0 || rows > 0x7FFFFFFFLL || !(eps >= 0.0f)) return SOL_ERR_BAD_SHAPE;
-    rotary::Heads h[2] = {};
+    rotary::Heads2 heads{};
     const sol_head_tensor_t *both[2] = {q, k};
     for (int i = 0; i < 2; ++i) {
         const sol_head_tensor_t *s = both[i];
@@ -653,7 +653,7 @@ sol_status_t sol_qk_rotary(const sol_head_tensor_t *q, const sol_head_tensor_t *
             return SOL_ERR_BAD_SHAPE;
         if (!aligned16(s->x) || !aligned16(s->out) || s->ld_in % 8 != 0 || s->ld_out % 8 != 0 || !aligned8(s->weight))
             return SOL_ERR_ALIGNMENT;
-        h[i] = rotary::Heads{static_cast<const uint16_t *>(s->x), static_cast<uint16_t *>(s->out),
+        heads.h[i] = rotary::Heads{static_cast<const uint16_t *>(s->x), static_cast<uint16_t *>(s->out),
                              static_cast<const uint16_t *>(s->weight), static_cast<int>(s->heads), s->ld_in, s->ld_out};
     }
     rotary::Turn t;
@@ -662,8 +662,8 @@ sol_status_t sol_qk_rotary(const sol_head_tensor_t *q, const sol_head_tensor_t *
     const DeviceInfo *dev = nullptr;
     st = check_arch(&dev);
     if (st != SOL_OK) return st;
-    return rotary::launch_forward(h[0], h[1], t, rows, head_dim, rot != nullptr && rot->layout == SOL_ROTARY_HALF, eps,
-                                  static_cast<cudaStream_t>(stream));
+    return rotary::launch_forward(heads, t, rows, head_dim, rot != nullptr && rot->layout == SOL_ROTARY_HALF, eps,
+                                  static_cast<cudaStream_t>(stream), dev);
 }
 
 size_t sol_qk_rotary_backward_workspace_bytes(int64_t head_dim) {
@@ -675,7 +675,7 @@ sol_status_t sol_qk_rotary_backward(const sol_head_grad_t *q, const sol_head_gra
                                     void *stream) {
     if (q == nullptr) return SOL_ERR_NULL_POINTER;
     if (!rotary::head_dim_ok(head_dim) || rows <= 0 || rows > 0x7FFFFFFFLL || !(eps >= 0.0f)) return SOL_ERR_BAD_SHAPE;
-    rotary::Grads g[2] = {};
+    rotary::Grads2 grads{};
     const sol_head_grad_t *both[2] = {q, k};
     bool weights = false;
     for (int i = 0; i < 2; ++i) {
@@ -690,7 +690,7 @@ sol_status_t sol_qk_rotary_backward(const sol_head_grad_t *q, const sol_head_gra
             (s->weight != nullptr && (!aligned16(s->x) || s->ld_x % 8 != 0 || (reinterpret_cast<uintptr_t>(s->dweight) & 3u))))
             return SOL_ERR_ALIGNMENT;
         weights = weights || s->weight != nullptr;
-        g[i] = rotary::Grads{static_cast<const uint16_t *>(s->dy), static_cast<const uint16_t *>(s->x),
+        grads.g[i] = rotary::Grads{static_cast<const uint16_t *>(s->dy), static_cast<const uint16_t *>(s->x),
                              static_cast<uint16_t *>(s->dx), static_cast<const uint16_t *>(s->weight),
                              s->weight != nullptr ? s->dweight : nullptr, static_cast<int>(s->heads), s->ld_dy, s->ld_x, s->ld_dx};
     }
@@ -705,7 +705,7 @@ sol_status_t sol_qk_rotary_backward(const sol_head_grad_t *q, const sol_head_gra
     const DeviceInfo *dev = nullptr;
     st = check_arch(&dev);
     if (st != SOL_OK) return st;
-    return rotary::launch_backward(g[0], g[1], t, rows, head_dim, rot != nullptr && rot->layout == SOL_ROTARY_HALF, eps,
+    return rotary::launch_backward(grads, t, rows, head_dim, rot != nullptr && rot->layout == SOL_ROTARY_HALF, eps,
                                    weights ? static_cast<double *>(workspace) : nullptr, static_cast<cudaStream_t>(stream), dev);
 }
 

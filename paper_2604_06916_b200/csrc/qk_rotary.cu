@@ -8,14 +8,20 @@
 // The gradients: dn = the inverse turn of dy (times s), dx = (w dn - xhat mean(w dn xhat)) / rms, and
 // dw = sum over rows of dn xhat with xhat = x / rms.
 //
-// HBM bound: 4 bytes per element forward, 6 backward.  A warp owns one token and a few heads of it; a lane
-// owns the same eight columns of each of those heads (in the half layout four and their four partners), so
-// angles are formed once per warp, each by one lane, and handed round by shuffles; all loads of a warp are
-// issued before the angle arithmetic, which runs in their shadow.
+// HBM bound: 4 bytes per element forward, 6 backward.  A warp owns one token and walks its heads; a lane owns the
+// same eight columns of every head (in the half layout four and their four partners), so the angles are formed once
+// per token and tensor, each by one lane, and handed round by shuffles while the first heads' loads are under way.
+// Four heads per lane are loaded before any is used.  Where tokens are few, up to one warp per four-head group shares a
+// token.  Measured (B200, q and k of 24 heads x 128 from a fused projection, norm and three axes): forward, 8 x 4608
+// tokens, 143 us = 6.3 TB/s, 97 % of the copy rate (one warp per token and eight heads, with its index divisions and
+// angles for each: 195 us).  Gradients, 2 x 4608 tokens, 66 us = 5.1 TB/s, 78 %: 113 registers hold both tensors'
+// loads, sixteen warps per SM wait for memory 2.4 cycles per issued instruction.  Two heads per lane with 24 warps
+// take 74 us, with the next ones prefetched 73 us.
 //
 // Angles: position * freq and the reduction to half a turn are in FP64 (a far position times a frequency has
 // more significant bits than FP32 holds), the sine and cosine of the remainder in FP32.  Squares, means and
 // products are FP32; the only rounding to 16 bits is the output's.
+#include "ptx.cuh"
 #include "quant_math.cuh"
 #include "sol_internal.h"
 
@@ -28,6 +34,8 @@ using qmath::bf16_lo;
 
 constexpr int kWarps = 8;
 constexpr int kUnroll = 4;      // heads per lane in flight
+constexpr int kUnrollBack = 4;  // the same in the gradients, which hold two tensors
+constexpr int kBackResident = 2;   // blocks of the gradients' kernel per SM
 
 // Lanes of a head: kD / 8; a warp holds kRep heads at a time.
 template <int kD>
@@ -71,21 +79,54 @@ __device__ __forceinline__ void store8(uint16_t *row, int c0, int c1, uint4 v) {
         *reinterpret_cast<uint2 *>(row + c1) = make_uint2(v.z, v.w);
     }
 }
-__device__ __forceinline__ void unpack8(uint4 v, float (&f)[8]) {
-    f[0] = bf16_lo(v.x), f[1] = bf16_hi(v.x), f[2] = bf16_lo(v.y), f[3] = bf16_hi(v.y);
-    f[4] = bf16_lo(v.z), f[5] = bf16_hi(v.z), f[6] = bf16_lo(v.w), f[7] = bf16_hi(v.w);
-}
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-}
-// Members of the slot's pair i (0..3) among its eight values.
+// A slot's eight values as four two-lane FP32 registers, the pairs' first members, then their second ones
+// (a0 a1, a2 a3, b0 b1, b2 b3): in this order the turn and everything else is two-lane arithmetic in both layouts.
+struct Slot {
+    uint64_t v[4];
+};
 template <bool kHalf>
-__device__ __forceinline__ constexpr int first_of(int i) { return kHalf ? i : 2 * i; }
+__device__ __forceinline__ Slot unpack(uint4 r) {
+    using qmath::f32x2;
+    if (kHalf)
+        return {{f32x2(bf16_lo(r.x), bf16_hi(r.x)), f32x2(bf16_lo(r.y), bf16_hi(r.y)), f32x2(bf16_lo(r.z), bf16_hi(r.z)),
+                 f32x2(bf16_lo(r.w), bf16_hi(r.w))}};
+    return {{f32x2(bf16_lo(r.x), bf16_lo(r.y)), f32x2(bf16_lo(r.z), bf16_lo(r.w)), f32x2(bf16_hi(r.x), bf16_hi(r.y)),
+             f32x2(bf16_hi(r.z), bf16_hi(r.w))}};
+}
 template <bool kHalf>
-__device__ __forceinline__ constexpr int second_of(int i) { return kHalf ? i + 4 : 2 * i + 1; }
+__device__ __forceinline__ uint4 pack(const Slot &s) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) qmath::f32x2_split(s.v[i], f[2 * i], f[2 * i + 1]);
+    if (kHalf) return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    return make_uint4(pack_bf16(f[0], f[4]), pack_bf16(f[1], f[5]), pack_bf16(f[2], f[6]), pack_bf16(f[3], f[7]));
+}
+// Memory column of value `e` of a slot (0..3: first members, 4..7: second ones).
+template <bool kHalf>
+__device__ __forceinline__ int column_of(int e, int c0, int c1) {
+    if (kHalf) return e < 4 ? c0 + e : c1 + e - 4;
+    return c0 + 2 * (e & 3) + (e >> 2);
+}
+__device__ __forceinline__ uint64_t twice(float f) { return qmath::f32x2(f, f); }
+__device__ __forceinline__ float sum_lanes(uint64_t v) {
+    float a, b;
+    qmath::f32x2_split(v, a, b);
+    return a + b;
+}
+// (a, b) -> (a c - b s, b c + a s) for the slot's four pairs.
+struct Angles {
+    uint64_t c[2], s[2], ns[2];   // ns = -s
+};
+__device__ __forceinline__ void turn(Slot &x, const uint64_t *c, const uint64_t *s, const uint64_t *ns) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint64_t a = x.v[i], b = x.v[i + 2];
+        x.v[i] = qmath::fma2(a, c[i], qmath::mul2(b, ns[i]));
+        x.v[i + 2] = qmath::fma2(b, c[i], qmath::mul2(a, s[i]));
+    }
+}
 
 // The slot's columns of a norm weight (read by every warp: cached).
-template <bool kHalf>
 __device__ __forceinline__ uint4 load_weight(const uint16_t *w, int c0, int c1) {
     const uint2 a = __ldg(reinterpret_cast<const uint2 *>(w + c0)), b = __ldg(reinterpret_cast<const uint2 *>(w + c1));
     return make_uint4(a.x, a.y, b.x, b.y);
@@ -101,7 +142,7 @@ __device__ __forceinline__ float head_sum(float v) {
 
 // Cosine and sine (times the scale) of the four pairs of this lane's slot at row m.  Called by whole warps.
 template <int kD>
-__device__ __forceinline__ void angles(const Turn &t, int64_t m, int lane, float (&cs)[4], float (&sn)[4]) {
+__device__ __forceinline__ Angles angles(const Turn &t, int64_t m, int lane) {
     using S = Shape<kD>;
     const int slot = lane % S::kLanes, rep = lane / S::kLanes;
     const int64_t *pos = t.positions + static_cast<int64_t>(static_cast<uint32_t>(m) % t.position_rows) * t.axes;
@@ -118,210 +159,240 @@ __device__ __forceinline__ void angles(const Turn &t, int64_t m, int lane, float
             mc[j] *= t.scale, ms[j] *= t.scale;
         }
     }
+    float cs[4], sn[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int src = slot + S::kLanes * (i / S::kPairs);
         cs[i] = __shfl_sync(0xFFFFFFFFu, mc[i % S::kPairs], src);
         sn[i] = __shfl_sync(0xFFFFFFFFu, ms[i % S::kPairs], src);
     }
+    using qmath::f32x2;
+    return {{f32x2(cs[0], cs[1]), f32x2(cs[2], cs[3])}, {f32x2(sn[0], sn[1]), f32x2(sn[2], sn[3])},
+            {f32x2(-sn[0], -sn[1]), f32x2(-sn[2], -sn[3])}};
 }
 
+// A warp takes one token and every `parts`-th group of its heads; blockIdx.y picks q or k.
 template <int kD, bool kHalf>
 __global__ void __launch_bounds__(32 * kWarps)
-forward_kernel(const Heads q, const Heads k, const Turn t, uint32_t rows, int groups, float eps) {
+forward_kernel(const Heads2 both, const Turn t, uint32_t rows, int parts_log2, float eps) {
     using S = Shape<kD>;
     const int lane = threadIdx.x & 31;
-    const uint64_t task = static_cast<uint64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-    const uint32_t m = static_cast<uint32_t>(task / static_cast<uint32_t>(groups));
+    const Heads d = blockIdx.y == 0 ? both.h[0] : both.h[1];
+    const uint32_t task = blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const uint32_t m = task >> parts_log2;
     if (m >= rows) return;
-    const int first = static_cast<int>(task % static_cast<uint32_t>(groups)) * S::kHeads + lane / S::kLanes;
     int c0, c1;
     columns<kHalf>(lane % S::kLanes, t.rot, c0, c1);
+    int h = static_cast<int>(task & ((1u << parts_log2) - 1u)) * S::kHeads + lane / S::kLanes;
+    const int step = S::kHeads << parts_log2;
+    const int heads = d.heads;
+    const uint16_t *x = d.x + m * d.ld_in;
+    uint16_t *out = d.out + m * d.ld_out;
     uint4 raw[kUnroll];
+    auto fetch = [&]() {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int h = first + u * S::kRep;
-        raw[u] = make_uint4(0, 0, 0, 0);
-        if (h < q.heads) raw[u] = load8<kHalf>(q.x + m * q.ld_in + h * kD, c0, c1);
-        else if (h < q.heads + k.heads) raw[u] = load8<kHalf>(k.x + m * k.ld_in + (h - q.heads) * kD, c0, c1);
-    }
-    float cs[4], sn[4];
-    const bool turned = t.rot > 0;
-    if (turned) angles<kD>(t, m, lane, cs, sn);
+        for (int u = 0; u < kUnroll; ++u)
+            raw[u] = h + u * S::kRep < heads ? load8<kHalf>(x + (h + u * S::kRep) * kD, c0, c1) : make_uint4(0, 0, 0, 0);
+    };
+    fetch();
+    Angles an;
+    if (t.rot > 0) an = angles<kD>(t, m, lane);
     const bool mine = c0 < t.rot;    // this lane's columns are rotated ones (a slot is wholly inside or outside)
+    const bool norm = d.weight != nullptr;
+    Slot w;
+    if (norm) w = unpack<kHalf>(load_weight(d.weight, c0, c1));
+    for (; h - lane / S::kLanes < heads; h += step) {
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-        const int h = first + u * S::kRep;
-        const bool is_q = h < q.heads, live = h < q.heads + k.heads;
-        const uint16_t *w = is_q ? q.weight : k.weight;
-        float f[8];
-        unpack8(raw[u], f);
-        float ss = 0.0f;
+        for (int u = 0; u < kUnroll; ++u) {
+            Slot f = unpack<kHalf>(raw[u]);
+            if (norm) {   // uniform over the warp
+                uint64_t ss = qmath::mul2(f.v[0], f.v[0]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
-        ss = head_sum<S::kLanes>(ss);
-        if (w != nullptr) {
-            const float r = 1.0f / sqrtf(fmaf(ss, 1.0f / kD, eps));
-            float g[8];
-            unpack8(load_weight<kHalf>(w, c0, c1), g);
+                for (int e = 1; e < 4; ++e) ss = qmath::fma2(f.v[e], f.v[e], ss);
+                const uint64_t r = twice(rsqrtf(fmaf(head_sum<S::kLanes>(sum_lanes(ss)), 1.0f / kD, eps)));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] *= r * g[e];
-        }
-        if (mine) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float a = f[first_of<kHalf>(i)], b = f[second_of<kHalf>(i)];
-                f[first_of<kHalf>(i)] = fmaf(a, cs[i], -(b * sn[i]));
-                f[second_of<kHalf>(i)] = fmaf(b, cs[i], a * sn[i]);
+                for (int e = 0; e < 4; ++e) f.v[e] = qmath::mul2(f.v[e], qmath::mul2(r, w.v[e]));
             }
+            if (mine) turn(f, an.c, an.s, an.ns);
+            raw[u] = pack<kHalf>(f);
         }
-        if (live) {
-            uint16_t *out = is_q ? q.out + m * q.ld_out + h * kD : k.out + m * k.ld_out + (h - q.heads) * kD;
-            store8<kHalf>(out, c0, c1, pack8(f));
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (h + u * S::kRep < heads) store8<kHalf>(out + (h + u * S::kRep) * kD, c0, c1, raw[u]);
+        if (h - lane / S::kLanes + step < heads) {
+            h += step;
+            fetch();
+            h -= step;
         }
     }
 }
 
-// Gradients.  Blocks stay and walk the (token, head group) tasks; a task is all of q or all of k, so that the two
-// weight gradients collect in registers: per lane over its tasks, per block over the lanes and warps that share a
-// column (FP64, fixed order), and reduce_weight_grads adds the blocks up.  No atomics: the result depends on
-// nothing but the shape.
+// Gradients.  blockIdx.y picks q or k; blocks stay and walk the (token, part of its heads) tasks, so that the weight
+// gradient collects in registers: per lane over its tasks, per block over the lanes and warps that share a column
+// (FP64, fixed order), and reduce_weight_grads adds the blocks up.  No atomics: the result depends on nothing but
+// the shape.
 template <int kD, bool kHalf>
-__global__ void __launch_bounds__(32 * kWarps)
-backward_kernel(const Grads q, const Grads k, const Turn t, uint32_t rows, int groups_q, int groups_k, float eps,
-                double *__restrict__ partials) {
+__global__ void __launch_bounds__(32 * kWarps, kBackResident)
+backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int parts_log2, float eps, double *__restrict__ partials) {
     using S = Shape<kD>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Grads d = blockIdx.y == 0 ? both.g[0] : both.g[1];
     int c0, c1;
     columns<kHalf>(lane % S::kLanes, t.rot, c0, c1);
     const bool mine = c0 < t.rot;
-    const uint32_t groups = static_cast<uint32_t>(groups_q + groups_k);
-    const uint64_t tasks = static_cast<uint64_t>(rows) * groups;
-    float acc[2][8] = {};
+    const bool norm = d.weight != nullptr;
+    const int heads = d.heads, step = (S::kRep * kUnrollBack) << parts_log2;
+    Slot w, acc{};    // 0.0f in both lanes
+    if (norm) w = unpack<kHalf>(load_weight(d.weight, c0, c1));
+    const uint64_t tasks = static_cast<uint64_t>(rows) << parts_log2;
     for (uint64_t task = static_cast<uint64_t>(blockIdx.x) * kWarps + warp; task < tasks;
          task += static_cast<uint64_t>(gridDim.x) * kWarps) {
-        const uint32_t m = static_cast<uint32_t>(task / groups);
-        const int g = static_cast<int>(task - static_cast<uint64_t>(m) * groups);
-        const bool is_q = g < groups_q;
-        const Grads &d = is_q ? q : k;
-        const int first = (is_q ? g : g - groups_q) * S::kHeads + lane / S::kLanes;
-        const bool norm = d.weight != nullptr;
-        uint4 raw_dy[kUnroll], raw_x[kUnroll];
+        const uint32_t m = static_cast<uint32_t>(task >> parts_log2);
+        const uint16_t *dy = d.dy + m * d.ld_dy, *x = d.x + m * d.ld_x;
+        uint16_t *dx = d.dx + m * d.ld_dx;
+        int h = static_cast<int>(task & ((1u << parts_log2) - 1u)) * (S::kRep * kUnrollBack) + lane / S::kLanes;
+        uint4 raw_dy[kUnrollBack], raw_x[kUnrollBack];
+        auto fetch = [&]() {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int h = first + u * S::kRep;
-            raw_dy[u] = raw_x[u] = make_uint4(0, 0, 0, 0);
-            if (h < d.heads) {
-                raw_dy[u] = load8<kHalf>(d.dy + m * d.ld_dy + h * kD, c0, c1);
-                if (norm) raw_x[u] = load8<kHalf>(d.x + m * d.ld_x + h * kD, c0, c1);
-            }
-        }
-        float cs[4], sn[4], w[8];
-        if (t.rot > 0) angles<kD>(t, m, lane, cs, sn);
-        if (norm) unpack8(load_weight<kHalf>(d.weight, c0, c1), w);
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int h = first + u * S::kRep;
-            float dn[8];
-            unpack8(raw_dy[u], dn);
-            if (mine) {   // the inverse turn
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float a = dn[first_of<kHalf>(i)], b = dn[second_of<kHalf>(i)];
-                    dn[first_of<kHalf>(i)] = fmaf(a, cs[i], b * sn[i]);
-                    dn[second_of<kHalf>(i)] = fmaf(b, cs[i], -(a * sn[i]));
+            for (int u = 0; u < kUnrollBack; ++u) {
+                raw_dy[u] = raw_x[u] = make_uint4(0, 0, 0, 0);
+                if (h + u * S::kRep < heads) {
+                    raw_dy[u] = load8<kHalf>(dy + (h + u * S::kRep) * kD, c0, c1);
+                    if (norm) raw_x[u] = load8<kHalf>(x + (h + u * S::kRep) * kD, c0, c1);
                 }
             }
-            if (norm) {   // uniform over the warp
-                float x[8];
-                unpack8(raw_x[u], x);
-                float ss = 0.0f, dot = 0.0f;
+        };
+        fetch();
+        Angles an;
+        if (t.rot > 0) an = angles<kD>(t, m, lane);
+        for (; h - lane / S::kLanes < heads; h += step) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    ss = fmaf(x[e], x[e], ss);
-                    dot = fmaf(dn[e] * w[e], x[e], dot);
-                }
-                ss = head_sum<S::kLanes>(ss);
-                dot = head_sum<S::kLanes>(dot);
-                const float r = 1.0f / sqrtf(fmaf(ss, 1.0f / kD, eps));
-                const float mean = dot * r * (1.0f / kD);       // mean of w dn xhat
-                const bool live = h < d.heads;
+            for (int u = 0; u < kUnrollBack; ++u) {
+                Slot dn = unpack<kHalf>(raw_dy[u]);
+                if (mine) turn(dn, an.c, an.ns, an.s);   // the inverse turn
+                if (norm) {   // uniform over the warp
+                    const Slot x8 = unpack<kHalf>(raw_x[u]);
+                    Slot prod;    // dn x
+                    uint64_t ss = 0, dot = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float xhat = x[e] * r;
-                    const float c = live ? dn[e] * xhat : 0.0f;
-                    if (is_q) acc[0][e] += c;
-                    else acc[1][e] += c;
-                    dn[e] = r * fmaf(dn[e], w[e], -(xhat * mean));
+                    for (int e = 0; e < 4; ++e) {
+                        prod.v[e] = qmath::mul2(dn.v[e], x8.v[e]);
+                        ss = qmath::fma2(x8.v[e], x8.v[e], ss);
+                        dot = qmath::fma2(prod.v[e], w.v[e], dot);
+                    }
+                    const float r = rsqrtf(fmaf(head_sum<S::kLanes>(sum_lanes(ss)), 1.0f / kD, eps));
+                    const float mean = head_sum<S::kLanes>(sum_lanes(dot)) * r * (1.0f / kD);       // mean of w dn xhat
+                    const uint64_t r2 = twice(r), back = twice(-(r * r * mean));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {   // heads that do not exist were read as zeros: they add nothing
+                        acc.v[e] = qmath::fma2(prod.v[e], r2, acc.v[e]);
+                        dn.v[e] = qmath::fma2(qmath::mul2(dn.v[e], w.v[e]), r2, qmath::mul2(x8.v[e], back));
+                    }
                 }
+                raw_dy[u] = pack<kHalf>(dn);
             }
-            if (h < d.heads) store8<kHalf>(d.dx + m * d.ld_dx + h * kD, c0, c1, pack8(dn));
+#pragma unroll
+            for (int u = 0; u < kUnrollBack; ++u)
+                if (h + u * S::kRep < heads) store8<kHalf>(dx + (h + u * S::kRep) * kD, c0, c1, raw_dy[u]);
+            if (h - lane / S::kLanes + step < heads) {
+                h += step;
+                fetch();
+                h -= step;
+            }
         }
     }
     if (partials == nullptr) return;
     // lanes that hold the same columns, then the warps, then one FP64 value per column and block
-    __shared__ float part[kWarps][2][kD];
+    __shared__ float part[kWarps][kD];
+    float sums[8];
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
+    for (int e = 0; e < 4; ++e) qmath::f32x2_split(acc.v[e], sums[2 * e], sums[2 * e + 1]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float v = acc[s][e];
+    for (int e = 0; e < 8; ++e) {
 #pragma unroll
-            for (int o = S::kLanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-            if (lane < S::kLanes) part[warp][s][e < 4 ? c0 + e : c1 + e - 4] = v;
-        }
+        for (int o = S::kLanes; o < 32; o <<= 1) sums[e] += __shfl_xor_sync(0xFFFFFFFFu, sums[e], o);
+        if (lane < S::kLanes) part[warp][column_of<kHalf>(e, c0, c1)] = sums[e];
+    }
     __syncthreads();
-    for (int c = threadIdx.x; c < 2 * kD; c += 32 * kWarps) {
+    for (int c = threadIdx.x; c < kD; c += 32 * kWarps) {
         double v = 0.0;
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) v += part[i][c / kD][c % kD];
-        partials[static_cast<int64_t>(blockIdx.x) * (2 * kD) + c] = v;
+        for (int i = 0; i < kWarps; ++i) v += part[i][c];
+        partials[(static_cast<int64_t>(blockIdx.x) * 2 + blockIdx.y) * kD + c] = v;
     }
 }
 
 // dw[c] = sum of the blocks' partials, in block order within each of the strips that the threads take.
-constexpr int kReduceStrips = 8;
+constexpr int kReduceStrips = 16;
 template <int kD>
 __global__ void __launch_bounds__(32 * kReduceStrips)
 reduce_weight_grads(const double *__restrict__ partials, int blocks, float *dw_q, float *dw_k) {
     __shared__ double part[kReduceStrips][32];
+    float *dw = blockIdx.y == 0 ? dw_q : dw_k;
+    ptx::grid_dependency_wait();
+    if (dw == nullptr) return;
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), strip = threadIdx.x >> 5;
     double v = 0.0;
 #pragma unroll 8
-    for (int b = strip; b < blocks; b += kReduceStrips) v += partials[static_cast<int64_t>(b) * (2 * kD) + c];
+    for (int b = strip; b < blocks; b += kReduceStrips) v += partials[(static_cast<int64_t>(b) * 2 + blockIdx.y) * kD + c];
     part[strip][threadIdx.x & 31] = v;
     __syncthreads();
     if (strip != 0) return;
 #pragma unroll
     for (int i = 1; i < kReduceStrips; ++i) v += part[i][threadIdx.x & 31];
-    float *dw = c < kD ? dw_q : dw_k;
-    if (dw != nullptr) dw[c % kD] = static_cast<float>(v);
+    dw[c] = static_cast<float>(v);
 }
 
-constexpr int kMaxBackwardBlocks = 1024;
+constexpr int kMaxBackwardBlocks = 1024;   // per tensor
+
+// Warps that share a token, as a power of two: one where the tokens alone fill the GPU's warps, up to one per group of
+// heads where they are few.
+template <int kD>
+int split_of(int64_t rows, int heads, int64_t fill) {
+    int log2 = 0;
+    while ((rows << log2) < fill && (Shape<kD>::kHeads << log2) < heads) ++log2;
+    return log2;
+}
 
 template <int kD>
-sol_status_t forward(const Heads &q, const Heads &k, const Turn &t, int64_t rows, bool half, float eps, cudaStream_t stream) {
-    const int groups = static_cast<int>(ceil_div(q.heads + k.heads, Shape<kD>::kHeads));
-    const int64_t blocks = ceil_div(rows * groups, kWarps);
-    if (blocks > 0x7FFFFFFFLL) return SOL_ERR_BAD_SHAPE;
+sol_status_t forward(const Heads2 &h, const Turn &t, int64_t rows, bool half, float eps, cudaStream_t stream, const DeviceInfo *dev) {
+    const int heads = h.h[0].heads > h.h[1].heads ? h.h[0].heads : h.h[1].heads;
+    const int split = split_of<kD>(rows, heads, 16LL * dev->sm_count);
+    const dim3 grid(static_cast<unsigned>(ceil_div(rows << split, kWarps)), h.h[1].heads > 0 ? 2u : 1u);
     auto kern = half ? forward_kernel<kD, true> : forward_kernel<kD, false>;
-    kern<<<static_cast<unsigned>(blocks), 32 * kWarps, 0, stream>>>(q, k, t, static_cast<uint32_t>(rows), groups, eps);
+    kern<<<grid, 32 * kWarps, 0, stream>>>(h, t, static_cast<uint32_t>(rows), split, eps);
     return launch_status();
 }
 
 template <int kD>
-sol_status_t backward(const Grads &q, const Grads &k, const Turn &t, int64_t rows, bool half, float eps, double *partials,
-                      cudaStream_t stream, const DeviceInfo *dev) {
-    const int gq = static_cast<int>(ceil_div(q.heads, Shape<kD>::kHeads)), gk = static_cast<int>(ceil_div(k.heads, Shape<kD>::kHeads));
-    const int64_t want = ceil_div(rows * (gq + gk), kWarps);
-    const int64_t most = 4 * dev->sm_count < kMaxBackwardBlocks ? 4 * dev->sm_count : kMaxBackwardBlocks;
-    const int blocks = static_cast<int>(want < most ? want : most);
+sol_status_t backward(const Grads2 &g, const Turn &t, int64_t rows, bool half, float eps, double *partials, cudaStream_t stream,
+                      const DeviceInfo *dev) {
+    const int heads = g.g[0].heads > g.g[1].heads ? g.g[0].heads : g.g[1].heads;
+    const int split = split_of<kD>(rows, heads, 16LL * dev->sm_count);
+    const int64_t want = ceil_div(rows << split, kWarps);
+    const unsigned tensors = g.g[1].heads > 0 ? 2u : 1u;
+    int64_t most = kBackResident * dev->sm_count / tensors;   // all blocks resident at once
+    if (most > kMaxBackwardBlocks) most = kMaxBackwardBlocks;
+    const dim3 grid(static_cast<unsigned>(want < most ? want : most), tensors);
     auto kern = half ? backward_kernel<kD, true> : backward_kernel<kD, false>;
-    kern<<<blocks, 32 * kWarps, 0, stream>>>(q, k, t, static_cast<uint32_t>(rows), gq, gk, eps, partials);
+    kern<<<grid, 32 * kWarps, 0, stream>>>(g, t, static_cast<uint32_t>(rows), split, eps, partials);
     const sol_status_t st = launch_status();
     if (st != SOL_OK || partials == nullptr) return st;
-    reduce_weight_grads<kD><<<2 * kD / 32, 32 * kReduceStrips, 0, stream>>>(partials, blocks, q.dweight, k.dweight);
+    // the few blocks of the sum are set up while the last blocks of the gradients drain (programmatic launch)
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(kD / 32, grid.y);
+    cfg.blockDim = dim3(32 * kReduceStrips);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, reduce_weight_grads<kD>, static_cast<const double *>(partials), static_cast<int>(grid.x),
+                           g.g[0].dweight, g.g[1].dweight) != cudaSuccess) {
+        cudaGetLastError();
+        return SOL_ERR_CUDA;
+    }
     return launch_status();
 }
 
@@ -331,24 +402,24 @@ size_t backward_workspace_bytes(int64_t head_dim) { return sizeof(double) * 2 * 
 
 bool head_dim_ok(int64_t d) { return d == 32 || d == 64 || d == 128 || d == 256; }
 
-sol_status_t launch_forward(const Heads &q, const Heads &k, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
-                            cudaStream_t stream) {
+sol_status_t launch_forward(const Heads2 &h, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
+                            cudaStream_t stream, const DeviceInfo *dev) {
     switch (head_dim) {
-        case 32: return forward<32>(q, k, t, rows, half, eps, stream);
-        case 64: return forward<64>(q, k, t, rows, half, eps, stream);
-        case 128: return forward<128>(q, k, t, rows, half, eps, stream);
-        case 256: return forward<256>(q, k, t, rows, half, eps, stream);
+        case 32: return forward<32>(h, t, rows, half, eps, stream, dev);
+        case 64: return forward<64>(h, t, rows, half, eps, stream, dev);
+        case 128: return forward<128>(h, t, rows, half, eps, stream, dev);
+        case 256: return forward<256>(h, t, rows, half, eps, stream, dev);
     }
     return SOL_ERR_BAD_SHAPE;
 }
 
-sol_status_t launch_backward(const Grads &q, const Grads &k, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
+sol_status_t launch_backward(const Grads2 &g, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
                              double *partials, cudaStream_t stream, const DeviceInfo *dev) {
     switch (head_dim) {
-        case 32: return backward<32>(q, k, t, rows, half, eps, partials, stream, dev);
-        case 64: return backward<64>(q, k, t, rows, half, eps, partials, stream, dev);
-        case 128: return backward<128>(q, k, t, rows, half, eps, partials, stream, dev);
-        case 256: return backward<256>(q, k, t, rows, half, eps, partials, stream, dev);
+        case 32: return backward<32>(g, t, rows, half, eps, partials, stream, dev);
+        case 64: return backward<64>(g, t, rows, half, eps, partials, stream, dev);
+        case 128: return backward<128>(g, t, rows, half, eps, partials, stream, dev);
+        case 256: return backward<256>(g, t, rows, half, eps, partials, stream, dev);
     }
     return SOL_ERR_BAD_SHAPE;
 }

@@ -164,6 +164,8 @@ struct Grads {
     int heads;
     int64_t ld_dy, ld_x, ld_dx;
 };
+struct Heads2 { Heads h[2]; };   // q, k
+struct Grads2 { Grads g[2]; };
 struct Turn {
     const int64_t *positions;   // [position_rows, axes]; token m uses row m % position_rows
     const double *freqs;        // [rot / 2] radians per position
@@ -175,9 +177,9 @@ struct Turn {
 };
 bool head_dim_ok(int64_t head_dim);
 size_t backward_workspace_bytes(int64_t head_dim);
-sol_status_t launch_forward(const Heads &q, const Heads &k, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
-                            cudaStream_t stream);
-sol_status_t launch_backward(const Grads &q, const Grads &k, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
+sol_status_t launch_forward(const Heads2 &h, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
+                            cudaStream_t stream, const DeviceInfo *dev);
+sol_status_t launch_backward(const Grads2 &g, const Turn &t, int64_t rows, int64_t head_dim, bool half, float eps,
                              double *partials, cudaStream_t stream, const DeviceInfo *dev);
 }
 

@@ -94,15 +94,14 @@ def test_entry_points_refuse_bad_arguments(B):
     def rot(**kw):
         d = dict(positions=p, freqs=p, position_rows=4, axes=1, axis_dims=(64,), layout=0, scale=1.0)
         d.update(kw)
-        dims = (ctypes.c_int64 * 4)(*d["axis_dims"])
-        return B.Rotary(d["positions"], d["freqs"], d["position_rows"], d["axes"], dims, d["layout"], d["scale"])
+        dims = d["axis_dims"] + (0,) * (4 - len(d["axis_dims"]))
+        return B._ROTARY.pack(d["positions"] or 0, d["freqs"] or 0, d["position_rows"], d["axes"], *dims, d["layout"], d["scale"])
 
     def heads(x=p, out=p, weight=None, heads=2, ld_in=128, ld_out=128):
-        return B.HeadTensor(x, out, weight, heads, ld_in, ld_out)
+        return B._HEAD_TENSOR.pack(x or 0, out or 0, weight or 0, heads, ld_in, ld_out)
 
     def fwd(q=None, k=None, rows=4, D=64, r=None, eps=1e-6, no_q=False, no_rot=False):
-        return L.sol_qk_rotary(None if no_q else ctypes.byref(q or heads()), None if k is None else ctypes.byref(k), rows, D,
-                               None if no_rot else ctypes.byref(r or rot()), eps, None)
+        return L.sol_qk_rotary(None if no_q else q or heads(), k, rows, D, None if no_rot else r or rot(), eps, None)
 
     assert fwd(no_q=True) == NULLP
     assert fwd(q=heads(x=None)) == NULLP and fwd(k=heads(out=None)) == NULLP
@@ -124,11 +123,11 @@ def test_entry_points_refuse_bad_arguments(B):
     assert need > 0 and L.sol_qk_rotary_backward_workspace_bytes(48) == 0
 
     def grad(dy=p, x=p, dx=p, weight=p, dweight=p, heads=2, ld_dy=128, ld_x=128, ld_dx=128):
-        return B.HeadGrad(dy, x, dx, weight, dweight, heads, ld_dy, ld_x, ld_dx)
+        return B._HEAD_GRAD.pack(dy or 0, x or 0, dx or 0, weight or 0, dweight or 0, heads, ld_dy, ld_x, ld_dx)
 
     def bwd(q=None, k=None, rows=4, D=64, r=None, eps=1e-6, ws=p, size=need, no_q=False, no_rot=False):
-        return L.sol_qk_rotary_backward(None if no_q else ctypes.byref(q or grad()), None if k is None else ctypes.byref(k), rows,
-                                        D, None if no_rot else ctypes.byref(r or rot()), eps, ws, size, None)
+        return L.sol_qk_rotary_backward(None if no_q else q or grad(), k, rows, D, None if no_rot else r or rot(), eps, ws,
+                                        size, None)
 
     assert bwd(no_q=True) == NULLP and bwd(q=grad(dy=None)) == NULLP and bwd(q=grad(dx=None)) == NULLP
     assert bwd(q=grad(x=None)) == NULLP and bwd(q=grad(dweight=None)) == NULLP and bwd(ws=None) == NULLP
@@ -146,16 +145,20 @@ def test_binding_refuses_before_the_library(B):
         B.sol_qk_rotary(q, None, pos, f)
     with pytest.raises(TypeError):
         B.sol_qk_rotary_backward(q, None, None, None, pos, f)
-    assert B._head_view("q", q) == 128 and B._head_view("q", q[:, :, :1]) == 128
+    shape = (1, 4, 2, 64)
+    assert B._head_view("q", q, shape, -1) == 128 and B._head_view("q", q[:, :, :1], (1, 4, 1, 64), -1) == 128
     with pytest.raises(TypeError):
-        B._head_view("q", q.float())
+        B._head_view("q", q.float(), shape, -1)
     with pytest.raises(ValueError):
-        B._head_view("q", q.transpose(1, 2))
+        B._head_view("q", q, (1, 4, 4, 64), -1)
     with pytest.raises(ValueError):
-        B._head_view("q", torch.zeros((2, 8, 2, 64), dtype=torch.bfloat16)[:, :4])   # batches not densely stacked
-    cpu = torch.device("cpu")
-    assert B._rotary_of(None, None, None, 0, 1.0, 4, cpu) is None
+        B._head_view("q", q, shape, 0)                               # another device
+    with pytest.raises(ValueError):
+        B._head_view("q", q.transpose(1, 2), (1, 2, 4, 64), -1)
+    with pytest.raises(ValueError):                                  # batches not densely stacked
+        B._head_view("q", torch.zeros((2, 8, 2, 64), dtype=torch.bfloat16)[:, :4], (2, 4, 2, 64), -1)
+    assert B._rotary_of(None, None, None, 0, 1.0, 4, -1) is None and B._rotary_of(pos, f, None, 0, 1.0, 8, -1) is not None
     for bad in [(pos.int(), f, None), (pos[:, 0], f, None), (pos, f.float(), None), (pos, None, None), (None, f, None),
                 (pos, f, [32, 32]), (pos, f, [32]), (pos[:3], f, None)]:
         with pytest.raises((TypeError, ValueError)):
-            B._rotary_of(*bad, 0, 1.0, 4, cpu)
+            B._rotary_of(*bad, 0, 1.0, 4, -1)
