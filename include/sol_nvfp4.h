@@ -61,7 +61,7 @@ typedef enum {
 } sol_status_t;
 
 typedef enum { SOL_SF_ROW_MAJOR = 0, SOL_SF_SWIZZLED_128x4 = 1 } sol_sf_layout_t;
-typedef enum { SOL_ACT_NONE = 0, SOL_ACT_GELU_TANH = 1 } sol_activation_t;
+typedef enum { SOL_ACT_NONE = 0, SOL_ACT_GELU_TANH = 1, SOL_ACT_SILU = 2 } sol_activation_t;
 
 /* Static, human-readable name of a status (host pointer, never NULL). */
 const char *sol_status_string(sol_status_t status);
@@ -289,6 +289,24 @@ typedef struct {
 } sol_attention_stream_t;
 sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const sol_attention_stream_t *second,
                                       int64_t batch, int64_t heads, int64_t head_dim, void *stream);
+
+/*
+ * Linear of a few BF16 rows against a weight in NVFP4 or MXFP4, x kept in 16 bits (weight-only: the rollout models'
+ * modulation and embedding linears, whose rows are samples; the paper quantizes both operands of the token linears):
+ *     y[m,n] = bf16_rne( T * sum_k act(x[m,k]) * code[n,k] * scale[n, block of k] + bias[n] )      (MXFP4: T = 1)
+ *   x_bf16      [M, K] BF16, pitch ldx;  wq, wsf  as written by nvfp4_quantize_weight / mxfp4_quantize with
+ *               SOL_SF_SWIZZLED_128x4;  w_tscale one float (device);  bias_bf16 [N] or NULL;  y_bf16 [M, N], pitch ldy
+ *   activation  applied to x: SOL_ACT_NONE or SOL_ACT_SILU (x / (1 + exp(-x)), FP32), SOL_ERR_BAD_LAYOUT otherwise
+ *   M >= 1 (the weight is read once per 32 rows), N % 8 == 0, K % 32 == 0, K <= 24576
+ * Sums are FP32 and in a fixed order.  Before the product act(x) is scaled by a power of two per row and slice of K and
+ * held in FP16: BF16 values down to 2^-29 of the slice's largest are kept exactly (an activation's result to 11 bits).
+ */
+sol_status_t nvfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf, const float *w_tscale,
+                          const void *bias_bf16, sol_activation_t activation, void *y_bf16, int64_t ldy, int64_t M,
+                          int64_t N, int64_t K, void *stream);
+sol_status_t mxfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf, const void *bias_bf16,
+                          sol_activation_t activation, void *y_bf16, int64_t ldy, int64_t M, int64_t N, int64_t K,
+                          void *stream);
 
 /*
  * What stands between the fused q/k/v projection and the attention of a DiT block: RMS norm of every query and key
