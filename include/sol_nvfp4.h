@@ -297,16 +297,19 @@ sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const
  *   x_bf16      [M, K] BF16, pitch ldx;  wq, wsf  as written by nvfp4_quantize_weight / mxfp4_quantize with
  *               SOL_SF_SWIZZLED_128x4;  w_tscale one float (device);  bias_bf16 [N] or NULL;  y_bf16 [M, N], pitch ldy
  *   activation  applied to x: SOL_ACT_NONE or SOL_ACT_SILU (x / (1 + exp(-x)), FP32), SOL_ERR_BAD_LAYOUT otherwise
- *   M >= 1 (the weight is read once per 32 rows), N % 8 == 0, K % 32 == 0, K <= 24576
- * Sums are FP32 and in a fixed order.  Before the product act(x) is scaled by a power of two per row and slice of K and
- * held in FP16: BF16 values down to 2^-29 of the slice's largest are kept exactly (an activation's result to 11 bits).
+ *   workspace   device scratch of at least sol_matvec_workspace_bytes(M, K) bytes, 256-byte aligned; holds x in the
+ *               products' layout; contents undefined after.  Two calls that may overlap need one each.
+ *   M >= 1 (the weight is read once per 64 rows), N % 8 == 0, K % 32 == 0
+ * Two launches.  Sums are FP32 and in a fixed order.  Before the product act(x) is scaled by a power of two per row and
+ * held in FP16: BF16 values down to 2^-29 of the row's largest are kept exactly (an activation's result to 11 bits).
  */
+size_t sol_matvec_workspace_bytes(int64_t M, int64_t K);
 sol_status_t nvfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf, const float *w_tscale,
                           const void *bias_bf16, sol_activation_t activation, void *y_bf16, int64_t ldy, int64_t M,
-                          int64_t N, int64_t K, void *stream);
+                          int64_t N, int64_t K, void *workspace, size_t workspace_bytes, void *stream);
 sol_status_t mxfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf, const void *bias_bf16,
                           sol_activation_t activation, void *y_bf16, int64_t ldy, int64_t M, int64_t N, int64_t K,
-                          void *stream);
+                          void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * What stands between the fused q/k/v projection and the attention of a DiT block: RMS norm of every query and key

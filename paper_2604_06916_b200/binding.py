@@ -32,6 +32,7 @@ EXPORTS = [
     "sol_attention_nvfp4_out", "mxfp4_linear_quantized_out", "sol_set_wait_limit_cycles", "sol_test_hold_loads",
     "mxfp4_linear_split_out", "mxfp4_quantize_into", "sol_qk_rotary", "sol_qk_rotary_backward",
     "sol_qk_rotary_backward_workspace_bytes", "sol_rotary_frequencies", "nvfp4_matvec", "mxfp4_matvec",
+    "sol_matvec_workspace_bytes",
 ]
 
 _lib = None
@@ -113,8 +114,9 @@ def lib() -> ctypes.CDLL:
     L.mxfp4_quantize_into.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, vp]
     f32, f64 = ctypes.c_float, ctypes.c_double
     L.nvfp4_matvec.restype = L.mxfp4_matvec.restype = i32
-    L.nvfp4_matvec.argtypes = [vp, i64, vp, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp]
-    L.mxfp4_matvec.argtypes = [vp, i64, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp]
+    L.nvfp4_matvec.argtypes = [vp, i64, vp, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, sz, vp]
+    L.mxfp4_matvec.argtypes = [vp, i64, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, sz, vp]
+    L.sol_matvec_workspace_bytes.restype, L.sol_matvec_workspace_bytes.argtypes = sz, [i64, i64]
     L.sol_qk_rotary.restype = i32
     L.sol_qk_rotary.argtypes = [vp, vp, i64, i64, vp, f32, vp]
     L.sol_qk_rotary_backward.restype = i32
@@ -525,16 +527,20 @@ def sol_attention_nvfp4_out(q, k, v, out_tscale: torch.Tensor, dest, dest_col0: 
     return dest
 
 
-def _matvec_args(x, wq, wsf, bias, out, blocks_per_chunk: int):
-    """Checks of a weight-only product; returns (M, N, K, ldx, out, ldy).  `blocks_per_chunk`: K of a scale chunk."""
+def matvec_workspace_bytes(M: int, K: int) -> int:
+    return lib().sol_matvec_workspace_bytes(M, K)
+
+
+def _matvec(entry: str, x, wq, wsf, w_tscale, bias, activation: int, out, workspace, blocks_per_chunk: int):
+    """Checks and the call of a weight-only product; `blocks_per_chunk`: columns of K that a scale chunk spans."""
     index = x.get_device()
     if x.dtype is not torch.bfloat16 or x.dim() != 2 or x.stride(1) != 1:
         raise TypeError("x: expected a 2-D CUDA bf16 tensor with contiguous rows")
     if wq.dtype is not torch.uint8 or wq.dim() != 2 or not wq.is_contiguous() or wsf.dtype is not torch.uint8 or not wsf.is_contiguous():
         raise TypeError("weights: expected dense uint8 nibbles [N, K/2] and a dense uint8 scale buffer")
-    (M, K), N = x.shape, wq.shape[0]
-    if wq.shape[1] * 2 != K:
-        raise ValueError(f"x has {K} columns, the weight {wq.shape[1] * 2}")
+    (M, K), (N, packed) = x.shape, wq.shape
+    if packed * 2 != K:
+        raise ValueError(f"x has {K} columns, the weight {packed * 2}")
     if wsf.numel() < (N + 127) // 128 * ((K + blocks_per_chunk - 1) // blocks_per_chunk) * 512:
         raise ValueError("scale buffer too small for the weight's chunked scales")
     if bias is not None and (bias.dtype is not torch.bfloat16 or bias.dim() != 1 or bias.shape[0] != N or not bias.is_contiguous()):
@@ -543,34 +549,38 @@ def _matvec_args(x, wq, wsf, bias, out, blocks_per_chunk: int):
         out = _empty((M, N), torch.bfloat16, x.device)
     elif out.dtype is not torch.bfloat16 or out.dim() != 2 or out.shape != (M, N) or out.stride(1) != 1:
         raise TypeError("out: expected a [M, N] bf16 tensor with contiguous rows")
-    if wq.get_device() != index or wsf.get_device() != index or out.get_device() != index or (bias is not None and bias.get_device() != index):
-        raise ValueError("all tensors must be on x's device")
+    if workspace is None:
+        workspace = _empty(max(1, lib().sol_matvec_workspace_bytes(M, K)), torch.uint8, x.device)
+    elif not workspace.is_contiguous():
+        raise TypeError("workspace: expected a dense tensor")
+    for t in (wq, wsf, w_tscale, bias, out, workspace):
+        if t is not None and t.get_device() != index:
+            raise ValueError("all tensors must be on x's device")
     # a single row has no pitch of its own
-    return M, N, K, (x.stride(0) if M > 1 else max(K, 8)), out, (out.stride(0) if M > 1 else max(N, 8))
+    args = [x.data_ptr(), x.stride(0) if M > 1 else K, wq.data_ptr(), wsf.data_ptr(), _ptr(bias), activation, out.data_ptr(),
+            out.stride(0) if M > 1 else N, M, N, K, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(index)]
+    if w_tscale is not None:
+        args.insert(4, w_tscale.data_ptr())
+    code = getattr(lib(), entry)(*args)
+    if code:
+        raise SolError(code, entry)
+    return out
 
 
 @_on_device_of_first
-def nvfp4_matvec(x, wq, wsf, w_tscale, bias=None, activation: int = ACT_NONE, out: torch.Tensor | None = None):
+def nvfp4_matvec(x, wq, wsf, w_tscale, bias=None, activation: int = ACT_NONE, out: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None):
     """Y = act(X) . dequant(W)^T + bias for a few BF16 rows: x is not quantized.  `activation`: ACT_NONE or ACT_SILU, on x."""
-    M, N, K, ldx, out, ldy = _matvec_args(x, wq, wsf, bias, out, 64)
-    if w_tscale.dtype is not torch.float32 or w_tscale.get_device() != x.get_device() or w_tscale.numel() < 1:
-        raise TypeError("w_tscale: expected a float32 tensor on x's device")
-    code = lib().nvfp4_matvec(x.data_ptr(), ldx, wq.data_ptr(), wsf.data_ptr(), w_tscale.data_ptr(), _ptr(bias), activation,
-                              out.data_ptr(), ldy, M, N, K, _raw_stream(x.get_device()))
-    if code:
-        raise SolError(code, "nvfp4_matvec")
-    return out
+    if w_tscale.dtype is not torch.float32 or w_tscale.numel() < 1:
+        raise TypeError("w_tscale: expected a float32 tensor")
+    return _matvec("nvfp4_matvec", x, wq, wsf, w_tscale, bias, activation, out, workspace, 64)
 
 
 @_on_device_of_first
-def mxfp4_matvec(x, wq, wsf, bias=None, activation: int = ACT_NONE, out: torch.Tensor | None = None):
+def mxfp4_matvec(x, wq, wsf, bias=None, activation: int = ACT_NONE, out: torch.Tensor | None = None,
+                 workspace: torch.Tensor | None = None):
     """The same against an MXFP4 weight (no tensor scale)."""
-    M, N, K, ldx, out, ldy = _matvec_args(x, wq, wsf, bias, out, 128)
-    code = lib().mxfp4_matvec(x.data_ptr(), ldx, wq.data_ptr(), wsf.data_ptr(), _ptr(bias), activation, out.data_ptr(), ldy,
-                              M, N, K, _raw_stream(x.get_device()))
-    if code:
-        raise SolError(code, "mxfp4_matvec")
-    return out
+    return _matvec("mxfp4_matvec", x, wq, wsf, None, bias, activation, out, workspace, 128)
 
 
 ROTARY_INTERLEAVED, ROTARY_HALF = 0, 1

@@ -640,34 +640,39 @@ sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const
 }
 
 namespace {
+bool matvec_shape_ok(int64_t M, int64_t K) { return shape_ok(M, K) && M <= (1LL << 18); }
+
 sol_status_t matvec_entry(const void *x, int64_t ldx, const void *wq, const void *wsf, const float *wts, const void *bias,
-                          sol_activation_t act, void *y, int64_t ldy, int64_t M, int64_t N, int64_t K, void *stream) {
-    if (x == nullptr || wq == nullptr || wsf == nullptr || y == nullptr) return SOL_ERR_NULL_POINTER;
+                          sol_activation_t act, void *y, int64_t ldy, int64_t M, int64_t N, int64_t K, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+    if (x == nullptr || wq == nullptr || wsf == nullptr || y == nullptr || workspace == nullptr) return SOL_ERR_NULL_POINTER;
     if (act != SOL_ACT_NONE && act != SOL_ACT_SILU) return SOL_ERR_BAD_LAYOUT;
-    if (!shape_ok(M, K) || !shape_ok(N, K) || M > (1LL << 18) || N > (1LL << 22) || N % 8 != 0 || K > matvec::max_k() || ldx < K ||
-        ldy < N)
-        return SOL_ERR_BAD_SHAPE;
+    if (!matvec_shape_ok(M, K) || !shape_ok(N, K) || N > (1LL << 22) || N % 8 != 0 || ldx < K || ldy < N) return SOL_ERR_BAD_SHAPE;
     if (!aligned16(x) || !aligned16(wq) || !aligned16(wsf) || !aligned16(y) || !aligned16(bias) || ldx % 8 != 0 || ldy % 8 != 0 ||
-        (reinterpret_cast<uintptr_t>(wts) & 3u))
+        (reinterpret_cast<uintptr_t>(wts) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
         return SOL_ERR_ALIGNMENT;
+    if (workspace_bytes < matvec::workspace_bytes(M, K)) return SOL_ERR_WORKSPACE_TOO_SMALL;
     const DeviceInfo *dev = nullptr;
     const sol_status_t st = check_arch(&dev);
     if (st != SOL_OK) return st;
-    return matvec::launch_matvec(x, ldx, wq, wsf, wts, bias, y, ldy, M, N, K, act == SOL_ACT_SILU, static_cast<cudaStream_t>(stream), dev);
+    return matvec::launch_matvec(x, ldx, wq, wsf, wts, bias, y, ldy, M, N, K, act == SOL_ACT_SILU, workspace,
+                                 static_cast<cudaStream_t>(stream));
 }
 }  // namespace
 
+size_t sol_matvec_workspace_bytes(int64_t M, int64_t K) { return matvec_shape_ok(M, K) ? matvec::workspace_bytes(M, K) : 0; }
+
 sol_status_t nvfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf, const float *w_tscale,
                           const void *bias_bf16, sol_activation_t activation, void *y_bf16, int64_t ldy, int64_t M,
-                          int64_t N, int64_t K, void *stream) {
+                          int64_t N, int64_t K, void *workspace, size_t workspace_bytes, void *stream) {
     if (w_tscale == nullptr) return SOL_ERR_NULL_POINTER;
-    return matvec_entry(x_bf16, ldx, wq, wsf, w_tscale, bias_bf16, activation, y_bf16, ldy, M, N, K, stream);
+    return matvec_entry(x_bf16, ldx, wq, wsf, w_tscale, bias_bf16, activation, y_bf16, ldy, M, N, K, workspace, workspace_bytes, stream);
 }
 
 sol_status_t mxfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf, const void *bias_bf16,
                           sol_activation_t activation, void *y_bf16, int64_t ldy, int64_t M, int64_t N, int64_t K,
-                          void *stream) {
-    return matvec_entry(x_bf16, ldx, wq, wsf, nullptr, bias_bf16, activation, y_bf16, ldy, M, N, K, stream);
+                          void *workspace, size_t workspace_bytes, void *stream) {
+    return matvec_entry(x_bf16, ldx, wq, wsf, nullptr, bias_bf16, activation, y_bf16, ldy, M, N, K, workspace, workspace_bytes, stream);
 }
 
 sol_status_t sol_qk_rotary(const sol_head_tensor_t *q, const sol_head_tensor_t *k, int64_t rows, int64_t head_dim,

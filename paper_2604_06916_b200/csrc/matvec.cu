@@ -4,15 +4,14 @@
 // once for a handful of rows, so the weight's bytes are the floor (0.5625 or 0.53 B per element) and the activations
 // stay in 16 bits -- no quantizer, no scale pass over x.
 //
-// One CTA takes 128 output columns (a row group of the chunked scale layout) and a slice of K; a cluster of up to eight
-// CTAs covers K and adds its partial sums through distributed shared memory in rank order.  A warp owns sixteen of
-// the 128 weight rows (four neighbours of each 32-row quarter, so that its scale bytes are contiguous), and its
-// lanes load their weights straight into the A fragments of mma.m16n8k16: the order of K inside a product is free as
-// long as x follows it, so lane t of a quad takes 32 consecutive codes (16 bytes) of its two rows per 128 columns,
-// i.e. whole scale blocks, and x is laid out in shared memory in the order in which the B fragments want it.
-// Codes become FP16 by the hardware conversion, are multiplied by their block's scale, and enter the tensor core:
-// dequantizing, not the products, is the work here (measured: 23 T codes/s for the conversion alone, 15 T codes/s with
-// scale and mma, against 11.6 T codes/s that HBM delivers; unpacking into BF16 with integer operations: 9 T).
+// Two launches.  prepare_x turns x (after the activation) into FP16 once, in the shared-memory image of the products'
+// operand; the products' kernel is launched along with it (programmatic launch) and waits for it only where x enters.
+// One CTA takes 128 output columns (a row group of the chunked scale layout) and a slice of K, one CTA per SM; where the
+// columns leave SMs free, a cluster of up to eight CTAs shares K, each adds up its share of the 128 columns in rank order.
+// The weight is the M = 128 operand of tcgen05.mma kind::f16 and comes from tensor memory: codes, scales and x
+// stream into a ring of 256-column stages by TMA and bulk copies, a thread per weight row converts the codes to FP16
+// (cvt.e2m1x2), multiplies by the block scales and leaves them in its TMEM lane; x is the N operand (16 to 64 rows).
+// Four warpgroups convert: two share an even stage, two an odd one, while the products of the stage before run.
 //
 // Number formats.  code * block scale has at most six significant bits: exact in FP16 for NVFP4 (2^-10 .. 2688).  MXFP4
 // scales are powers of two of any size: they are taken relative to the largest one of the row's slice, 2^13 for that
@@ -22,7 +21,7 @@
 // rounded to FP16's 11 bits.  Sums are FP32.
 #include <cuda_fp16.h>
 
-#include "ptx.cuh"
+#include "gemm_common.cuh"
 #include "quant_math.cuh"
 #include "sol_internal.h"
 
@@ -30,44 +29,61 @@ namespace sol {
 namespace matvec {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
+using gemm::wait_bounded;
+
+constexpr int kConvWarps = 16;       // four warpgroups
+constexpr int kProducer = kConvWarps, kIssuer = kConvWarps + 1;
+constexpr int kThreads = 32 * (kConvWarps + 2);
 constexpr int kRows = 128;           // weight rows of a CTA
-constexpr int kStepK = 128;          // K of a step: 32 codes per lane and row
-constexpr int kRing = 4;             // steps whose weights are in registers or on their way
+constexpr int kStageK = 256;         // K of a stage: 128 bytes of codes per row
+constexpr int kMaxStages = 8;
+constexpr int kCodeBytes = kRows * kStageK / 2;
+constexpr int kSfBytes = kRows * kStageK / 16;
 constexpr int kMaxCluster = 8;
-constexpr int kPartPitch = kRows + 4;
 constexpr int kXExp = 14;            // exponent of the largest scaled |x|
 constexpr int kMxExp = 13;           // exponent of the largest relative MXFP4 scale
+constexpr int kMaxXRows = 64;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kColA = 0, kColABuf = 128, kColD = 256;   // A: two buffers of a stage; D: up to 64 columns
+constexpr int kFull = 0, kXFull = kFull + kMaxStages, kEmpty = kXFull + kMaxStages, kAFull = kEmpty + kMaxStages, kAEmpty = kAFull + 2,
+              kDone = kAEmpty + 2, kBars = kDone + 1;
+constexpr int kMaxSmem = 232448;     // per block
 
 struct Params {
-    const uint16_t *x;
-    const uint8_t *wq;
+    const uint8_t *ximage;   // FP16 x: [row chunk][64 columns of K][x_rows][128 bytes, 128-byte swizzle], K padded to stages
+    const float *x_back;     // per row: what undoes its scaling
     const uint8_t *wsf;
     const float *wts;        // null: MXFP4
     const uint16_t *bias;    // null: none
     uint16_t *y;
-    int64_t ldx, ldy;
-    int M, N, K;
-    int steps, per_cta;      // 128-column steps of K, and those of one CTA
+    uint32_t *status;
+    int64_t ldy;
+    int M, N;
+    int x_rows;              // rows of x in a CTA: 16, 32, 48 or 64
+    int stages, per_cta;     // 256-column stages of K, and those of one CTA
+    int ring;                // stages in shared memory
     int chunks_k;            // scale chunks per row group
-    int silu;
 };
 
-__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t (&h)[4]) {
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
-        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
-        : "r"(w));
+__host__ __device__ constexpr int stage_x_bytes(int x_rows) { return x_rows * (2 * kStageK); }
+// Shared memory: the code ring, the x ring, the scale ring, the cluster's partial sums [rank][x row][own columns], barriers.
+__host__ __device__ constexpr int smem_bytes(int x_rows, int ring) {
+    return ring * (kCodeBytes + kSfBytes + stage_x_bytes(x_rows)) + x_rows * kRows * 4 + 8 * kBars + 16;
 }
-__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
-    uint32_t d;
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-    return d;
+
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t s, uint32_t *h) {
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t.reg .b32 t0, t1, t2, t3;\n\t"
+        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 t0, b0;\n\t"
+        "cvt.rn.f16x2.e2m1x2 t1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 t2, b2;\n\t"
+        "cvt.rn.f16x2.e2m1x2 t3, b3;\n\t"
+        "mul.rn.f16x2 %0, t0, %5;\n\t"
+        "mul.rn.f16x2 %1, t1, %5;\n\t"
+        "mul.rn.f16x2 %2, t2, %5;\n\t"
+        "mul.rn.f16x2 %3, t3, %5;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w), "r"(s));
 }
 __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t pair) {
     uint32_t d;
@@ -80,15 +96,24 @@ __device__ __forceinline__ uint32_t mx_scale_half2(int below) {
     const uint32_t h = e > 0 ? static_cast<uint32_t>(e) << 10 : (e > -10 ? 1u << (9 + e) : 0u);
     return h | h << 16;
 }
-__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float ld_cluster(uint32_t cluster_addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
     return v;
+}
+__device__ __forceinline__ void st_cluster(uint32_t cluster_addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+
+// A bounded wait of a whole warp: if it runs out for one lane, every lane gives up, so the warp stays together.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status, uint32_t code) {
+    return __all_sync(0xFFFFFFFFu, wait_bounded(bar, parity, abort_flag, status, code));
 }
 
 __device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
@@ -106,267 +131,379 @@ __device__ __forceinline__ void activate8(uint4 r, int act, float (&f)[8]) {
     }
 }
 
-// Shared memory: x of the slice (kTiles * 8 rows, pitch per_cta * 256 + 64 bytes), partial sums, row scales, x scales.
-__host__ __device__ constexpr int x_pitch(int per_cta) { return per_cta * (2 * kStepK) + 64; }
-constexpr int smem_bytes(int tiles, int per_cta) {
-    return 8 * tiles * x_pitch(per_cta) + 8 * tiles * kPartPitch * 4 + kRows * 4 + 8 * tiles * 4;
+// x -> scaled FP16 in the products' layout.  A block per row (rows behind the last are zeros), a thread per eight columns.
+constexpr int kPrepThreads = 512;
+__global__ void __launch_bounds__(kPrepThreads)
+prepare_x(const uint16_t *__restrict__ x, int64_t ldx, int M, int K, int x_rows, int stages, int act, uint8_t *__restrict__ image,
+          float *__restrict__ x_back) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the products' CTAs may start loading weights
+    __shared__ uint32_t warp_max[kPrepThreads / 32];
+    const int m = blockIdx.x, chunks = stages * (kStageK / 8), live = K / 8;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    const uint16_t *row = x + m * ldx;
+    constexpr int kHeld = 2;                  // chunks per thread kept from the first pass (rows up to 8192 columns)
+    float f[kHeld][8], most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+        const int c = threadIdx.x + j * kPrepThreads;
+        activate8(m < M && c < live ? __ldg(reinterpret_cast<const uint4 *>(row + 8 * c)) : zero, act, f[j]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[j][e]));
+    }
+    for (int c = threadIdx.x + kHeld * kPrepThreads; c < live; c += kPrepThreads) {
+        float v[8];
+        activate8(m < M ? __ldg(reinterpret_cast<const uint4 *>(row + 8 * c)) : zero, act, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
+    }
+    uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
+    if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = bits;
+    __syncthreads();
+    bits = __reduce_max_sync(0xFFFFFFFFu, warp_max[threadIdx.x & (kPrepThreads / 32 - 1)]);
+    // 2^(kXExp - e) with e the exponent of the largest element, held to what FP32 can scale by
+    const int e = min(max(static_cast<int>(bits >> 23) - 127, -100), 127);
+    const float up = __uint_as_float(static_cast<uint32_t>(127 + kXExp - e) << 23);
+    if (threadIdx.x == 0) x_back[m] = bits ? __uint_as_float(static_cast<uint32_t>(127 - kXExp + e) << 23) : 0.0f;
+    const int r = m % x_rows;
+    uint8_t *to = image + static_cast<int64_t>(m / x_rows) * (4 * stages) * (x_rows * 128) + r * 128;
+    auto put = [&](int c, const float (&v)[8]) {
+        uint32_t h[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const __half2 pair = __floats2half2_rn(v[2 * q] * up, v[2 * q + 1] * up);
+            h[q] = *reinterpret_cast<const uint32_t *>(&pair);
+        }
+        *reinterpret_cast<uint4 *>(to + static_cast<int64_t>(c >> 3) * (x_rows * 128) + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+    };
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j)
+        if (threadIdx.x + j * kPrepThreads < chunks) put(threadIdx.x + j * kPrepThreads, f[j]);
+    for (int c = threadIdx.x + kHeld * kPrepThreads; c < chunks; c += kPrepThreads) {
+        float v[8];
+        activate8(m < M && c < live ? __ldg(reinterpret_cast<const uint4 *>(row + 8 * c)) : zero, act, v);
+        put(c, v);
+    }
 }
 
-template <bool kMx, int kTiles>
-__global__ void __launch_bounds__(kThreads, 2)
-matvec_kernel(const Params p) {
-    constexpr int kM = 8 * kTiles;              // rows of x in this CTA
-    constexpr int kAccs = kTiles == 1 ? 2 : 1;  // independent sums per tile: one chain of products would wait on itself
-    extern __shared__ __align__(16) uint8_t smem[];
-    const int pitch = x_pitch(p.per_cta);
-    float *part = reinterpret_cast<float *>(smem + kM * pitch);
-    int *row_ref = reinterpret_cast<int *>(part + kM * kPartPitch);
-    float *x_back = reinterpret_cast<float *>(row_ref + kRows);
+template <bool kMx>
+__global__ void __launch_bounds__(kThreads, 1)
+matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
+    constexpr int kChunksPerStage = kMx ? 2 : 4;      // 512-byte scale chunks of a stage
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const uint32_t base = ptx::smem_u32(smem_raw);
+    const uint32_t x_bytes = static_cast<uint32_t>(stage_x_bytes(p.x_rows));
+    const uint32_t s_code = base, s_x = s_code + p.ring * kCodeBytes, s_sf = s_x + p.ring * x_bytes;
+    const uint32_t s_part = s_sf + p.ring * kSfBytes, bar_base = s_part + p.x_rows * kRows * 4;
+    uint8_t *bar_gen = smem_raw + (bar_base - base);
+    const float *part = reinterpret_cast<const float *>(smem_raw + (s_part - base));
+    uint32_t *tmem_ptr = reinterpret_cast<uint32_t *>(bar_gen + 8 * kBars);
+    volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(bar_gen + 8 * kBars + 4);
+    auto bar = [&](int i) { return bar_base + 8u * i; };
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const uint32_t rank = ptx::cluster_ctarank();
-    const int group = blockIdx.y, m0 = blockIdx.z * kM;
-    const int step0 = static_cast<int>(rank) * p.per_cta;
-    const int steps = min(p.per_cta, p.steps - step0);
-    const int ra = 4 * warp + (g & 3) + 32 * (g >> 2);          // this lane's rows of the group: ra and ra + 64
-    const int64_t na = static_cast<int64_t>(group) * kRows + ra;
-    const bool live_a = na < p.N, live_b = na + 64 < p.N;
-    const uint8_t *qa = p.wq + na * (p.K / 2) + 16 * t, *qb = qa + static_cast<int64_t>(32) * p.K;   // 64 rows of K / 2 bytes
-    const uint8_t *sf = p.wsf + static_cast<int64_t>(group) * p.chunks_k * 512 + (ra & 31) * 16 + (ra >> 5) * 4;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x, ranks = gridDim.x;   // the cluster is the grid's x extent
+    const int group = blockIdx.y, m0 = blockIdx.z * p.x_rows;
+    const int stage0 = rank * p.per_cta;
+    const int stages = min(p.per_cta, p.stages - stage0);
+    const bool aligned = (base & 1023u) == 0;         // what the swizzled operand layout needs
 
-    uint4 wa[kRing], wb[kRing];
-    uint32_t sa[kRing], sb[kRing];
-    auto fetch = [&](int s, uint4 &a, uint4 &b, uint32_t &fa, uint32_t &fb) {
-        const int k = (step0 + s) * kStepK + 32 * t;
-        a = b = make_uint4(0, 0, 0, 0);
-        fa = fb = 0;
-        if (s < steps && k < p.K) {
-            if (live_a) a = __ldcs(reinterpret_cast<const uint4 *>(qa + (step0 + s) * (kStepK / 2)));
-            if (live_b) b = __ldcs(reinterpret_cast<const uint4 *>(qb + (step0 + s) * (kStepK / 2)));
-            if (kMx) {
-                const uint8_t *c = sf + static_cast<int64_t>(step0 + s) * 512 + t;
-                fa = __ldg(c);
-                fb = __ldg(c + 8);
-            } else {
-                const uint8_t *c = sf + static_cast<int64_t>(2 * (step0 + s) + (t >> 1)) * 512 + 2 * (t & 1);
-                fa = __ldg(reinterpret_cast<const uint16_t *>(c));
-                fb = __ldg(reinterpret_cast<const uint16_t *>(c + 8));
-            }
-        }
+    auto load_codes = [&](int s) {
+        const int st = s % p.ring, chunk0 = (stage0 + s) * kChunksPerStage;
+        const uint32_t sf_bytes = 512u * static_cast<uint32_t>(min(kChunksPerStage, p.chunks_k - chunk0));
+        ptx::mbar_arrive_expect_tx(bar(kFull + st), kCodeBytes + sf_bytes);
+        ptx::tma_load_2d(s_code + st * kCodeBytes, &tm_w, (stage0 + s) * (kStageK / 2), group * kRows, bar(kFull + st));
+        ptx::bulk_load_1d(s_sf + st * kSfBytes, p.wsf + (static_cast<int64_t>(group) * p.chunks_k + chunk0) * 512, sf_bytes, bar(kFull + st));
     };
-#pragma unroll
-    for (int i = 0; i < kRing; ++i) fetch(i, wa[i], wb[i], sa[i], sb[i]);
-
-    // ---- x: a warp per row; largest magnitude of the slice, then scaled halves in fragment order
-    const int chunks = steps * (kStepK / 8), live_chunks = min(chunks, (p.K - step0 * kStepK) / 8);
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    uint4 xr[kTiles][2];
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-        const int m = warp + 8 * i;
-        const uint16_t *row = p.x + (m0 + m) * p.ldx + step0 * kStepK;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int c = lane + 32 * j;
-            xr[i][j] = m0 + m < p.M && c < live_chunks ? __ldg(reinterpret_cast<const uint4 *>(row + 8 * c)) : zero;
+    auto load_x = [&](int s) {
+        const int st = s % p.ring;
+        ptx::mbar_arrive_expect_tx(bar(kXFull + st), x_bytes);
+        ptx::bulk_load_1d(s_x + st * x_bytes, p.ximage + (static_cast<int64_t>(blockIdx.z) * p.stages + stage0 + s) * x_bytes, x_bytes, bar(kXFull + st));
+    };
+    const int first = min(stages, p.ring);
+    if (warp == kProducer && aligned) {
+        if (ptx::elect_one()) {
+            ptx::prefetch_tmap(&tm_w);
+            for (int i = 0; i < p.ring; ++i) {
+                ptx::mbar_init(bar(kFull + i), 1);
+                ptx::mbar_init(bar(kXFull + i), 1);
+                ptx::mbar_init(bar(kEmpty + i), 1);
+            }
+            for (int i = 0; i < 2; ++i) {
+                ptx::mbar_init(bar(kAFull + i), kConvWarps / 2);
+                ptx::mbar_init(bar(kAEmpty + i), 1);
+            }
+            ptx::mbar_init(bar(kDone), 1);
+            *abort_flag = 0;
+            ptx::fence_mbar_init();
+            ptx::fence_proxy_async_smem();
+            for (int s = 0; s < first; ++s) load_codes(s);
         }
+        __syncwarp();
     }
-    if (kMx && threadIdx.x < kRows) {   // largest scale exponent of each row's slice
-        const uint8_t *c = p.wsf + (static_cast<int64_t>(group) * p.chunks_k + step0) * 512 + (threadIdx.x & 31) * 16 + (threadIdx.x >> 5) * 4;
+    if (warp == kIssuer && aligned) {
+        ptx::tmem_alloc(ptx::smem_u32(tmem_ptr), kTmemCols);
+        ptx::tmem_relinquish();
+    }
+    if (!aligned && threadIdx.x == 0) atomicExch(p.status, 0xC00u);
+    int ref = 0;        // MXFP4: largest scale exponent of this thread's row and slice
+    if (kMx && warp < kConvWarps) {
+        const uint8_t *c = p.wsf + (static_cast<int64_t>(group) * p.chunks_k + stage0 * kChunksPerStage) * 512 + lane * 16 + (warp & 3) * 4;
+        const int n = min(stages * kChunksPerStage, p.chunks_k - stage0 * kChunksPerStage);
         uint32_t most = 0;
-        for (int s = 0; s < steps; ++s) most = __vmaxu4(most, __ldg(reinterpret_cast<const uint32_t *>(c + s * 512)));
-        row_ref[threadIdx.x] = static_cast<int>(max(max(most & 255u, most >> 8 & 255u), max(most >> 16 & 255u, most >> 24)));
+#pragma unroll 8
+        for (int i = 0; i < n; ++i) most = __vmaxu4(most, __ldg(reinterpret_cast<const uint32_t *>(c + i * 512)));
+        ref = static_cast<int>(max(max(most & 255u, most >> 8 & 255u), max(most >> 16 & 255u, most >> 24)));
     }
-#pragma unroll
-    for (int i = 0; i < kTiles; ++i) {
-        const int m = warp + 8 * i;
-        const uint16_t *row = p.x + (m0 + m) * p.ldx + step0 * kStepK;
-        const bool live = m0 + m < p.M;
-        float f[2][8], most = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            activate8(xr[i][j], p.silu, f[j]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[j][e]));
-        }
-        for (int c = lane + 64; c < live_chunks; c += 32) {   // slices beyond 512 columns
-            float v[8];
-            activate8(live ? __ldg(reinterpret_cast<const uint4 *>(row + 8 * c)) : zero, p.silu, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
-        }
-        const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
-        // 2^(kXExp - e) with e the exponent of the largest element, held to what FP32 can scale by
-        const int e = max(static_cast<int>(bits >> 23) - 127, -100);
-        const float up = __uint_as_float(static_cast<uint32_t>(127 + kXExp - min(e, 127)) << 23);
-        if (lane == 0) x_back[m] = bits ? __uint_as_float(static_cast<uint32_t>(127 - kXExp + min(e, 127)) << 23) : 0.0f;
-        auto put = [&](int c, const float (&v)[8]) {
-            // eight columns of lane t' = (c % 16) / 4, word c % 4 of its sixteen bytes
-            __half2 h[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) h[q] = __floats2half2_rn(v[2 * q] * up, v[2 * q + 1] * up);
-            uint8_t *to = smem + m * pitch + (c >> 4) * (2 * kStepK) + ((c & 3) * 4 + ((c & 15) >> 2)) * 16;
-            *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(h);
-        };
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            if (lane + 32 * j < chunks) put(lane + 32 * j, f[j]);
-        for (int c = lane + 64; c < chunks; c += 32) {
-            float v[8];
-            activate8(live && c < live_chunks ? __ldg(reinterpret_cast<const uint4 *>(row + 8 * c)) : zero, p.silu, v);
-            put(c, v);
-        }
-    }
+    ptx::tc_fence_before_sync();
     __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = aligned ? *tmem_ptr : 0;
+    ptx::cluster_arrive();       // this CTA runs: the others may write their sums into it (awaited before the first such write)
 
-    // ---- products
-    float acc[kTiles][kAccs][4] = {};
-    const int ref_a = kMx ? row_ref[ra] : 0, ref_b = kMx ? row_ref[ra + 64] : 0;
-    const uint32_t xs = ptx::smem_u32(smem) + g * pitch + t * 16;
-    auto multiply = [&](int s, const uint4 &a, const uint4 &b, uint32_t fa, uint32_t fb) {
-        const uint32_t wa4[4] = {a.x, a.y, a.z, a.w}, wb4[4] = {b.x, b.y, b.z, b.w};
-        uint32_t sca[2], scb[2];    // scale pairs of the lane's first and second sixteen codes
-        if (kMx) {
-            sca[0] = sca[1] = mx_scale_half2(ref_a - static_cast<int>(fa));
-            scb[0] = scb[1] = mx_scale_half2(ref_b - static_cast<int>(fb));
-        } else {
-            const uint32_t ha = e4m3x2_to_half2(fa), hb = e4m3x2_to_half2(fb);
-            sca[0] = __byte_perm(ha, ha, 0x1010);
-            sca[1] = __byte_perm(ha, ha, 0x3232);
-            scb[0] = __byte_perm(hb, hb, 0x1010);
-            scb[1] = __byte_perm(hb, hb, 0x3232);
-        }
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            uint32_t ha[4], hb[4];
-            codes_to_half(wa4[w], ha);
-            codes_to_half(wb4[w], hb);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                ha[i] = mul_half2(ha[i], sca[w >> 1]);
-                hb[i] = mul_half2(hb[i], scb[w >> 1]);
-            }
-#pragma unroll
-            for (int n = 0; n < kTiles; ++n) {
-                const uint4 xb = ptx::lds128(xs + n * 8 * pitch + s * (2 * kStepK) + w * 64);
-                mma_f16(acc[n][0], ha[0], hb[0], ha[1], hb[1], xb.x, xb.y);
-                mma_f16(acc[n][kAccs - 1], ha[2], hb[2], ha[3], hb[3], xb.z, xb.w);
+    if (!aligned) {
+    } else if (warp == kProducer) {
+        // ------------------------------------------------------------ loads
+        if (ptx::elect_one()) {
+            ptx::grid_dependency_wait();       // x is prepared
+            for (int s = 0; s < first; ++s) load_x(s);
+            for (int s = first; s < stages; ++s) {
+                if (!wait_bounded(bar(kEmpty + s % p.ring), static_cast<uint32_t>(s / p.ring - 1) & 1u, abort_flag, p.status, 0xC10u)) break;
+                load_codes(s);
+                load_x(s);
             }
         }
-    };
-    for (int s = 0; s < steps; s += kRing) {
+        __syncwarp();
+    } else if (warp == kIssuer) {
+        // ------------------------------------------------------------ products
+        if (ptx::elect_one()) {
+            const uint32_t idesc = (1u << 4) | (static_cast<uint32_t>(p.x_rows >> 3) << 17) | (static_cast<uint32_t>(kRows >> 4) << 24);
+            bool ok = true;
+            for (int s = 0; s < stages; ++s) {
+                const int st = s % p.ring, buf = s & 1;
+                ok = wait_bounded(bar(kXFull + st), static_cast<uint32_t>(s / p.ring) & 1u, abort_flag, p.status, 0xC20u) &&
+                     wait_bounded(bar(kAFull + buf), static_cast<uint32_t>(s >> 1) & 1u, abort_flag, p.status, 0xC21u);
+                if (!ok) break;
+                ptx::tc_fence_after_sync();
 #pragma unroll
-        for (int i = 0; i < kRing; ++i) {
-            if (s + i < steps) {
-                multiply(s + i, wa[i], wb[i], sa[i], sb[i]);
-                fetch(s + i + kRing, wa[i], wb[i], sa[i], sb[i]);
+                for (int i = 0; i < 16; ++i) {
+                    const uint64_t b = ptx::smem_desc_sw128(s_x + st * x_bytes + (i >> 2) * (p.x_rows * 128)) + 2u * (i & 3);
+                    ptx::mma_bf16_a_tmem(tmem + kColD, tmem + kColA + buf * kColABuf + 8 * i, b, idesc, s > 0 || i > 0);
+                }
+                ptx::tc_commit(bar(kAEmpty + buf));
+                ptx::tc_commit(bar(kEmpty + st));      // the codes were read before they became A
+            }
+            if (ok) ptx::tc_commit(bar(kDone));
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------ codes -> FP16 in TMEM: thread = weight row
+        const int half = (warp >> 2) & 1, odd = warp >> 3;
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t t_a = tmem + kColA + odd * kColABuf + half * (kColABuf / 2) + lanes;
+        bool ok = true;
+        for (int s = odd; s < stages; s += 2) {
+            const int st = s % p.ring;
+            if (!warp_wait(bar(kFull + st), static_cast<uint32_t>(s / p.ring) & 1u, abort_flag, p.status, 0xC40u | st)) {
+                ok = false;
+                break;
+            }
+            uint4 q[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                q[c] = ptx::lds128(s_code + st * kCodeBytes + row * 128 + (((4 * half + c) ^ (row & 7)) << 4));
+            uint32_t sf[2] = {0, 0};
+            const uint32_t sf_at = s_sf + st * kSfBytes + lane * 16 + (warp & 3) * 4;
+#pragma unroll
+            for (int c = 0; c < kChunksPerStage / 2; ++c) {   // chunks behind the last are not loaded: their codes are zeros
+                const int chunk = half * (kChunksPerStage / 2) + c;
+                if ((stage0 + s) * kChunksPerStage + chunk < p.chunks_k) sf[c] = lds32(sf_at + chunk * 512);
+            }
+            uint32_t h[2][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {          // 32 codes: two NVFP4 blocks or one MXFP4 block
+                uint32_t s0, s1;
+                if (kMx) {
+                    s0 = s1 = mx_scale_half2(ref - static_cast<int>(sf[0] >> (8 * c) & 255u));
+                } else {
+                    const uint32_t pair = e4m3x2_to_half2(sf[c >> 1] >> (16 * (c & 1)));
+                    s0 = __byte_perm(pair, pair, 0x1010);
+                    s1 = __byte_perm(pair, pair, 0x3232);
+                }
+                uint32_t *to = &h[c >> 1][16 * (c & 1)];
+                codes_to_half(q[c].x, s0, to);
+                codes_to_half(q[c].y, s0, to + 4);
+                codes_to_half(q[c].z, s1, to + 8);
+                codes_to_half(q[c].w, s1, to + 12);
+            }
+            if (s > 1 && !warp_wait(bar(kAEmpty + odd), static_cast<uint32_t>((s >> 1) - 1) & 1u, abort_flag, p.status, 0xC50u | odd)) {
+                ok = false;
+                break;
+            }
+            ptx::tc_fence_after_sync();
+            ptx::tmem_st_32x32(t_a, h[0]);
+            ptx::tmem_st_32x32(t_a + 32, h[1]);
+            ptx::tc_wait_st();
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(kAFull + odd));
+        }
+        // ------------------------------------------------------------ this slice's sums, to the rank that owns the column
+        ok = ok && warp_wait(bar(kDone), 0, abort_flag, p.status, 0xC60u);
+        ptx::cluster_wait();
+        if (ok) {
+            ptx::tc_fence_after_sync();
+            const int own = kRows / ranks;
+            const uint32_t to = ptx::map_to_cta(s_part + (rank * p.x_rows * own + row % own) * 4, row / own);
+            for (int c = 8 * (warp >> 2); c < p.x_rows; c += 32) {
+                uint32_t d[8];
+                tmem_ld_32x8(tmem + kColD + lanes + c, d);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float v = __uint_as_float(d[e]);
+                    if (kMx) v = scalbnf(v, ref - 127 - kMxExp);
+                    st_cluster(to + (c + e) * own * 4, v);
+                }
             }
         }
     }
+    if (!aligned || warp >= kConvWarps) ptx::cluster_wait();
+    ptx::tc_fence_before_sync();
 
-    // ---- sums of the slices: every CTA leaves its own, then adds a share of the outputs over the cluster in rank order
-#pragma unroll
-    for (int n = 0; n < kTiles; ++n) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int m = 8 * n + 2 * t + (e & 1), r = ra + (e >> 1) * 64;
-            float v = acc[n][0][e];
-            if (kAccs == 2) v += acc[n][kAccs - 1][e];
-            v *= x_back[m];
-            if (kMx) v = scalbnf(v, ((e >> 1) ? ref_b : ref_a) - 127 - kMxExp);
-            part[m * kPartPitch + r] = v;
-        }
-    }
-    ptx::cluster_sync();
-    const uint32_t ranks = static_cast<uint32_t>(gridDim.x);
+    // ---------------------------------------------------------------- own columns: sum over the ranks, scale, bias, store
+    const int own = kRows / ranks, live = min(p.x_rows, p.M - m0);
     const float T = kMx ? 1.0f : __ldg(p.wts);
-    const uint32_t mine = ptx::smem_u32(part);
-    for (uint32_t i = rank * kThreads + threadIdx.x; i < kM * (kRows / 2); i += ranks * kThreads) {
-        const int m = static_cast<int>(i) / (kRows / 2), r = 2 * (static_cast<int>(i) % (kRows / 2));
-        const int n = group * kRows + r;
-        if (m0 + m >= p.M || n >= p.N) continue;
+    ptx::cluster_sync();
+    for (int i = threadIdx.x; i < live * (own / 2); i += kThreads) {
+        const int m = i / (own / 2), r = 2 * (i % (own / 2));
+        const int n = group * kRows + rank * own + r;
+        if (n >= p.N) continue;
         float v0 = 0.0f, v1 = 0.0f;
-        for (uint32_t c = 0; c < ranks; ++c) {
-            const uint32_t at = ptx::map_to_cta(mine + (m * kPartPitch + r) * 4, c);
-            v0 += ld_cluster(at);
-            v1 += ld_cluster(at + 4);
+        for (int c = 0; c < ranks; ++c) {
+            const float2 v = *reinterpret_cast<const float2 *>(part + (c * p.x_rows + m) * own + r);
+            v0 += v.x;
+            v1 += v.y;
         }
+        const float back = __ldcg(p.x_back + m0 + m);
         uint32_t b2 = 0;
         if (p.bias != nullptr) b2 = __ldg(reinterpret_cast<const uint32_t *>(p.bias + n));
-        const float y0 = fmaf(v0, T, qmath::bf16_lo(b2)), y1 = fmaf(v1, T, qmath::bf16_hi(b2));
+        const float y0 = fmaf(v0 * back, T, qmath::bf16_lo(b2)), y1 = fmaf(v1 * back, T, qmath::bf16_hi(b2));
         uint32_t o;
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(y1), "f"(y0));
         *reinterpret_cast<uint32_t *>(p.y + (m0 + m) * p.ldy + n) = o;
     }
-    ptx::cluster_sync();   // no CTA leaves while another may still read its sums
+    if (warp == kIssuer && aligned) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, kTmemCols);
+    }
 }
 
-template <bool kMx, int kTiles>
-sol_status_t launch(const Params &p, int ranks, cudaStream_t stream) {
-    auto kern = matvec_kernel<kMx, kTiles>;
-    const int smem = smem_bytes(kTiles, p.per_cta);
+int x_rows_of(int64_t M) { return M >= kMaxXRows ? kMaxXRows : static_cast<int>(16 * ceil_div(M, 16)); }
+int ring_of(int x_rows) {
+    int ring = kMaxStages;
+    while (smem_bytes(x_rows, ring) > kMaxSmem) --ring;
+    return ring;
+}
+
+// Most clusters of `ranks` CTAs that the device holds at once (one CTA per SM; clusters do not span GPCs).
+template <bool kMx>
+int resident_clusters(int dev, int ranks) {
+    static int known[64][kMaxCluster + 1] = {};
+    if (known[dev][ranks] == 0) {
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3(static_cast<unsigned>(ranks));
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = kMaxSmem;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim = {static_cast<unsigned>(ranks), 1, 1};
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, matvec_kernel<kMx>, &cfg) != cudaSuccess || n < 1) {
+            cudaGetLastError();
+            n = 1;
+        }
+        known[dev][ranks] = n;
+    }
+    return known[dev][ranks];
+}
+
+template <bool kMx>
+sol_status_t launch(const void *x, int64_t ldx, bool silu, void *workspace, const CUtensorMap &tm_w, Params &p, int64_t K, cudaStream_t stream) {
+    auto kern = matvec_kernel<kMx>;
     static bool configured[64] = {};
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SOL_ERR_CUDA;
     if (!configured[dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024) != cudaSuccess) return SOL_ERR_CUDA;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) != cudaSuccess) return SOL_ERR_CUDA;
         configured[dev] = true;
     }
+    // K is shared by the largest cluster (of two, four or eight CTAs) that still runs in one wave.
+    const int64_t groups = ceil_div(p.N, kRows), row_chunks = ceil_div(p.M, p.x_rows);
+    int ranks = 1;
+    while (2 * ranks <= kMaxCluster && 2 * ranks <= p.stages && groups * row_chunks <= resident_clusters<kMx>(dev, 2 * ranks)) ranks *= 2;
+    p.per_cta = static_cast<int>(ceil_div(p.stages, ranks));
+    while (ranks > 1 && (ranks - 1) * p.per_cta >= p.stages) {    // every rank needs a stage
+        ranks /= 2;
+        p.per_cta = static_cast<int>(ceil_div(p.stages, ranks));
+    }
+    uint8_t *image = static_cast<uint8_t *>(workspace);
+    float *x_back = reinterpret_cast<float *>(image + row_chunks * p.stages * stage_x_bytes(p.x_rows));
+    p.ximage = image;
+    p.x_back = x_back;
+    prepare_x<<<static_cast<unsigned>(row_chunks * p.x_rows), kPrepThreads, 0, stream>>>(
+        static_cast<const uint16_t *>(x), ldx, p.M, static_cast<int>(K), p.x_rows, p.stages, silu ? 1 : 0, image, x_back);
+    const sol_status_t st = launch_status();
+    if (st != SOL_OK) return st;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(ranks), static_cast<unsigned>(ceil_div(p.N, kRows)), static_cast<unsigned>(ceil_div(p.M, 8 * kTiles)));
+    cfg.gridDim = dim3(static_cast<unsigned>(ranks), static_cast<unsigned>(groups), static_cast<unsigned>(row_chunks));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem_bytes(p.x_rows, p.ring));
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim = {static_cast<unsigned>(ranks), 1, 1};
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kern, p) != cudaSuccess) {
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, kern, tm_w, static_cast<const Params &>(p)) != cudaSuccess) {
         cudaGetLastError();
         return SOL_ERR_CUDA;
     }
     return launch_status();
 }
 
-template <bool kMx>
-sol_status_t launch_rows(const Params &p, int ranks, cudaStream_t stream) {
-    if (p.M <= 8) return launch<kMx, 1>(p, ranks, stream);
-    if (p.M <= 16) return launch<kMx, 2>(p, ranks, stream);
-    if (p.M <= 24) return launch<kMx, 3>(p, ranks, stream);
-    return launch<kMx, 4>(p, ranks, stream);
-}
-
 }  // namespace
 
-int max_k() { return 24576; }
+size_t workspace_bytes(int64_t M, int64_t K) {
+    const int x_rows = x_rows_of(M);
+    const int64_t chunks = ceil_div(M, x_rows);
+    return static_cast<size_t>(chunks * ceil_div(K, kStageK) * stage_x_bytes(x_rows) + chunks * x_rows * 4);
+}
 
 sol_status_t launch_matvec(const void *x, int64_t ldx, const void *wq, const void *wsf, const float *wts, const void *bias, void *y,
-                           int64_t ldy, int64_t M, int64_t N, int64_t K, bool silu, cudaStream_t stream, const DeviceInfo *dev) {
+                           int64_t ldy, int64_t M, int64_t N, int64_t K, bool silu, void *workspace, cudaStream_t stream) {
     Params p{};
-    p.x = static_cast<const uint16_t *>(x);
-    p.wq = static_cast<const uint8_t *>(wq);
     p.wsf = static_cast<const uint8_t *>(wsf);
     p.wts = wts;
     p.bias = static_cast<const uint16_t *>(bias);
     p.y = static_cast<uint16_t *>(y);
-    p.ldx = ldx;
+    p.status = device_status_word();
     p.ldy = ldy;
     p.M = static_cast<int>(M);
     p.N = static_cast<int>(N);
-    p.K = static_cast<int>(K);
-    p.steps = static_cast<int>(ceil_div(K, kStepK));
+    p.stages = static_cast<int>(ceil_div(K, kStageK));
     p.chunks_k = static_cast<int>(ceil_div(K, wts != nullptr ? 64 : 128));
-    p.silu = silu ? 1 : 0;
-    // Slices of four steps (what a CTA's registers hold at once), shorter where that leaves SMs without a CTA, longer
-    // where the cluster is full.
-    const int64_t groups = ceil_div(N, kRows);
-    int per = kRing;
-    while (per > 1 && groups * ceil_div(p.steps, per) < dev->sm_count && ceil_div(p.steps, per - 1) <= kMaxCluster) --per;
-    if (ceil_div(p.steps, per) > kMaxCluster) per = static_cast<int>(ceil_div(p.steps, kMaxCluster));
-    p.per_cta = per;
-    const int ranks = static_cast<int>(ceil_div(p.steps, per));
-    return wts != nullptr ? launch_rows<false>(p, ranks, stream) : launch_rows<true>(p, ranks, stream);
+    p.x_rows = x_rows_of(M);
+    p.ring = ring_of(p.x_rows);
+    CUtensorMap tm_w;
+    if (!make_tmap_2d(&tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, wq, static_cast<uint64_t>(K / 2), static_cast<uint64_t>(N),
+                      static_cast<uint64_t>(K / 2), kStageK / 2, kRows, CU_TENSOR_MAP_SWIZZLE_128B))
+        return SOL_ERR_CUDA;
+    return wts != nullptr ? launch<false>(x, ldx, silu, workspace, tm_w, p, K, stream) : launch<true>(x, ldx, silu, workspace, tm_w, p, K, stream);
 }
 
 }  // namespace matvec

@@ -185,9 +185,9 @@ sol_status_t launch_backward(const Grads2 &g, const Turn &t, int64_t rows, int64
 
 // Few BF16 rows against a 4-bit weight (wts null: MXFP4).
 namespace matvec {
-int max_k();
+size_t workspace_bytes(int64_t M, int64_t K);
 sol_status_t launch_matvec(const void *x, int64_t ldx, const void *wq, const void *wsf, const float *wts, const void *bias, void *y,
-                           int64_t ldy, int64_t M, int64_t N, int64_t K, bool silu, cudaStream_t stream, const DeviceInfo *dev);
+                           int64_t ldy, int64_t M, int64_t N, int64_t K, bool silu, void *workspace, cudaStream_t stream);
 }
 
 // Scale-factor buffer in the chunked layout as a 3-D tensor [row chunk][k chunk][128 x u32]; the box

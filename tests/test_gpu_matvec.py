@@ -68,7 +68,7 @@ def rows(M, K, seed, pad=0):
 
 
 SHAPES = [(1, 8, 32), (1, 128, 128), (2, 136, 96), (3, 1000, 160), (8, 256, 512), (9, 264, 544), (16, 128, 1056), (17, 640, 2240),
-          (24, 72, 320), (25, 128, 4128), (32, 2432, 1216), (33, 200, 640), (64, 512, 1024), (70, 88, 256), (5, 128, 24576), (32, 136, 15360)]
+          (24, 72, 320), (25, 128, 4128), (32, 2432, 1216), (33, 200, 640), (64, 512, 1024), (70, 88, 256), (5, 128, 24576), (32, 136, 15360), (48, 64, 32), (130, 40, 288)]
 
 
 @pytest.mark.parametrize("fmt", ["nv", "mx"])
@@ -191,6 +191,27 @@ def test_repeatable_on_another_stream_and_captured(B, fmt, M, N, K):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_workspaces_of_two_streams_and_a_small_one(B):
+    # two calls at once, each with a workspace of its own; and one that is too small is refused
+    W = Weight("nv", 4096, 1024, 31)
+    a, b = rows(8, 1024, 41), rows(20, 1024, 42)
+    wa, wb = W.call(B, a), W.call(B, b)
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for i in range(20):
+        with torch.cuda.stream(s1):
+            got.append((W.call(B, a), wa))
+        with torch.cuda.stream(s2):
+            got.append((W.call(B, b), wb))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in got)
+    ws = torch.empty(B.matvec_workspace_bytes(8, 1024), dtype=torch.uint8, device="cuda")
+    assert torch.equal(B.nvfp4_matvec(a, W.q, W.sf, W.ts, workspace=ws), wa)
+    with pytest.raises(B.SolError):
+        B.nvfp4_matvec(a, W.q, W.sf, W.ts, workspace=ws[:-256])
 
 
 def test_weight_beyond_32_bit_offsets(B):

@@ -37,13 +37,14 @@ def test_entry_points_refuse_bad_arguments(B):
     L = B.lib()
     buf = ctypes.create_string_buffer(4096)
     p = (ctypes.addressof(buf) + 255) & ~255   # aligned fake pointer, never dereferenced
-    NULLP, SHAPE, ALIGN, LAYOUT = 1, 2, 3, 8
+    NULLP, SHAPE, ALIGN, WS, LAYOUT = 1, 2, 3, 4, 8
+    big = 1 << 40
 
-    def nv(x=p, ldx=64, wq=p, wsf=p, ts=p, bias=None, act=0, y=p, ldy=8, M=4, N=8, K=64):
-        return L.nvfp4_matvec(x, ldx, wq, wsf, ts, bias, act, y, ldy, M, N, K, None)
+    def nv(x=p, ldx=64, wq=p, wsf=p, ts=p, bias=None, act=0, y=p, ldy=8, M=4, N=8, K=64, ws=p, size=big):
+        return L.nvfp4_matvec(x, ldx, wq, wsf, ts, bias, act, y, ldy, M, N, K, ws, size, None)
 
-    def mx(x=p, ldx=64, wq=p, wsf=p, bias=None, act=0, y=p, ldy=8, M=4, N=8, K=64):
-        return L.mxfp4_matvec(x, ldx, wq, wsf, bias, act, y, ldy, M, N, K, None)
+    def mx(x=p, ldx=64, wq=p, wsf=p, bias=None, act=0, y=p, ldy=8, M=4, N=8, K=64, ws=p, size=big):
+        return L.mxfp4_matvec(x, ldx, wq, wsf, bias, act, y, ldy, M, N, K, ws, size, None)
 
     assert nv(ts=None) == NULLP
     assert nv(ts=p + 2) == ALIGN
@@ -55,7 +56,13 @@ def test_entry_points_refuse_bad_arguments(B):
         assert f(act=1) == LAYOUT and f(act=3) == LAYOUT                    # GELU is an output activation elsewhere
         assert f(M=0) == SHAPE and f(N=12, ldy=16) == SHAPE and f(K=48) == SHAPE and f(N=0) == SHAPE
         assert f(ldx=56) == SHAPE and f(N=16) == SHAPE                      # pitches too small
-        assert f(K=24608, ldx=24608) == SHAPE and f(M=(1 << 18) + 1) == SHAPE
+        assert f(M=(1 << 18) + 1) == SHAPE and f(N=1 << 23, ldy=1 << 23) == SHAPE
+        assert f(ws=None) == NULLP and f(ws=p + 128) == ALIGN
+        assert f(size=L.sol_matvec_workspace_bytes(4, 64) - 1) == WS
+    assert L.sol_matvec_workspace_bytes(0, 64) == 0 and L.sol_matvec_workspace_bytes(4, 48) == 0
+    # x padded to sixteen rows and 256 columns in FP16, and a float per row
+    assert L.sol_matvec_workspace_bytes(4, 64) == 16 * 256 * 2 + 16 * 4
+    assert L.sol_matvec_workspace_bytes(65, 544) == 128 * 768 * 2 + 128 * 4
     # the input activation is refused where an output activation is asked for
     assert L.nvfp4_linear_quantized_out(p, p, p, p, p, p, None, 2, p, p, p, None, 4, 64, 64, None) == LAYOUT
 
@@ -67,14 +74,12 @@ def test_binding_refuses_before_the_library(B):
         B.nvfp4_matvec(x, wq, wsf, torch.ones(1))
     with pytest.raises(TypeError):
         B.mxfp4_matvec(x, wq, wsf)
-    ok = B._matvec_args(x, wq, wsf, None, None, 64)
-    assert ok[:4] == (2, 8, 64, 64) and ok[5] == 8
-    assert B._matvec_args(x[:1].expand(1, 64), wq, wsf, None, None, 64)[3] == 64
     bad = [dict(x=x.float()), dict(x=x[0]), dict(x=x.t()), dict(wq=wq.int()), dict(wq=wq[:, ::2]), dict(wq=wq[:, :16].contiguous()),
            dict(wsf=wsf[:256]), dict(wsf=wsf.int()), dict(bias=torch.zeros(8)), dict(bias=torch.zeros(4, dtype=torch.bfloat16)),
-           dict(out=torch.zeros((2, 8))), dict(out=torch.zeros((2, 16), dtype=torch.bfloat16))]
+           dict(out=torch.zeros((2, 8))), dict(out=torch.zeros((2, 16), dtype=torch.bfloat16)),
+           dict(workspace=torch.zeros((4, 4), dtype=torch.uint8)[:, :2])]
     for kw in bad:
-        args = dict(x=x, wq=wq, wsf=wsf, bias=None, out=None)
+        args = dict(x=x, wq=wq, wsf=wsf, bias=None, out=None, workspace=None)
         args.update(kw)
         with pytest.raises((TypeError, ValueError)):
-            B._matvec_args(args["x"], args["wq"], args["wsf"], args["bias"], args["out"], 64)
+            B._matvec("mxfp4_matvec", args["x"], args["wq"], args["wsf"], None, args["bias"], 0, args["out"], args["workspace"], 64)
