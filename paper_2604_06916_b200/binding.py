@@ -213,9 +213,10 @@ def _on_device_of_first(fn):
     current one of that device) are then that device's, whichever device the caller has current."""
     @functools.wraps(fn)
     def call(first, *args, **kwargs):
-        if not first.is_cuda:
+        index = first.get_device()
+        if index < 0:
             raise TypeError(f"{fn.__name__}: expected CUDA tensors")
-        if first.get_device() == torch.cuda.current_device():
+        if index == torch._C._cuda_getDevice():
             return fn(first, *args, **kwargs)
         with torch.cuda.device(first.device):
             return fn(first, *args, **kwargs)
@@ -225,6 +226,13 @@ def _on_device_of_first(fn):
 def _raw_stream(index: int) -> int:
     """Handle of the current stream of device `index` (no Stream object is built)."""
     return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _new(x: torch.Tensor, shape, dtype=None) -> torch.Tensor:
+    """An output on x's device (of x's type unless one is given)."""
+    if _guarding:
+        return _empty(shape, x.dtype if dtype is None else dtype, x.device)
+    return x.new_empty(shape) if dtype is None else x.new_empty(shape, dtype=dtype)
 
 
 def _like(x: torch.Tensor) -> torch.Tensor:
@@ -531,8 +539,8 @@ def matvec_workspace_bytes(M: int, K: int) -> int:
     return lib().sol_matvec_workspace_bytes(M, K)
 
 
-def _matvec(entry: str, x, wq, wsf, w_tscale, bias, activation: int, out, workspace, blocks_per_chunk: int):
-    """Checks and the call of a weight-only product; `blocks_per_chunk`: columns of K that a scale chunk spans."""
+def _matvec(entry, name: str, x, wq, wsf, w_tscale, bias, activation: int, out, workspace, scale_columns: int):
+    """Checks and the call of a weight-only product; `scale_columns`: columns of K that a scale chunk spans."""
     index = x.get_device()
     if x.dtype is not torch.bfloat16 or x.dim() != 2 or x.stride(1) != 1:
         raise TypeError("x: expected a 2-D CUDA bf16 tensor with contiguous rows")
@@ -541,29 +549,34 @@ def _matvec(entry: str, x, wq, wsf, w_tscale, bias, activation: int, out, worksp
     (M, K), (N, packed) = x.shape, wq.shape
     if packed * 2 != K:
         raise ValueError(f"x has {K} columns, the weight {packed * 2}")
-    if wsf.numel() < (N + 127) // 128 * ((K + blocks_per_chunk - 1) // blocks_per_chunk) * 512:
+    if wsf.numel() < (N + 127) // 128 * ((K + scale_columns - 1) // scale_columns) * 512:
         raise ValueError("scale buffer too small for the weight's chunked scales")
-    if bias is not None and (bias.dtype is not torch.bfloat16 or bias.dim() != 1 or bias.shape[0] != N or not bias.is_contiguous()):
-        raise TypeError("bias: expected a dense [N] bf16 tensor")
+    if wq.get_device() != index or wsf.get_device() != index:
+        raise ValueError("the weight must be on x's device")
+    if bias is not None and (bias.dtype is not torch.bfloat16 or bias.dim() != 1 or bias.shape[0] != N or not bias.is_contiguous()
+                             or bias.get_device() != index):
+        raise TypeError("bias: expected a dense [N] bf16 tensor on x's device")
     if out is None:
-        out = _empty((M, N), torch.bfloat16, x.device)
-    elif out.dtype is not torch.bfloat16 or out.dim() != 2 or out.shape != (M, N) or out.stride(1) != 1:
-        raise TypeError("out: expected a [M, N] bf16 tensor with contiguous rows")
+        out, ldy = _new(x, (M, N)), N
+    elif out.dtype is not torch.bfloat16 or out.dim() != 2 or out.shape != (M, N) or out.stride(1) != 1 or out.get_device() != index:
+        raise TypeError("out: expected a [M, N] bf16 tensor with contiguous rows on x's device")
+    else:
+        ldy = out.stride(0) if M > 1 else N      # a single row has no pitch of its own
     if workspace is None:
-        workspace = _empty(max(1, lib().sol_matvec_workspace_bytes(M, K)), torch.uint8, x.device)
-    elif not workspace.is_contiguous():
-        raise TypeError("workspace: expected a dense tensor")
-    for t in (wq, wsf, w_tscale, bias, out, workspace):
-        if t is not None and t.get_device() != index:
-            raise ValueError("all tensors must be on x's device")
-    # a single row has no pitch of its own
-    args = [x.data_ptr(), x.stride(0) if M > 1 else K, wq.data_ptr(), wsf.data_ptr(), _ptr(bias), activation, out.data_ptr(),
-            out.stride(0) if M > 1 else N, M, N, K, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(index)]
-    if w_tscale is not None:
-        args.insert(4, w_tscale.data_ptr())
-    code = getattr(lib(), entry)(*args)
+        workspace = _new(wq, max(1, lib().sol_matvec_workspace_bytes(M, K)))
+    elif not workspace.is_contiguous() or workspace.get_device() != index:
+        raise TypeError("workspace: expected a dense tensor on x's device")
+    tail = (None if bias is None else bias.data_ptr(), activation, out.data_ptr(), ldy, M, N, K, workspace.data_ptr(),
+            workspace.nbytes, _raw_stream(index))
+    ldx = x.stride(0) if M > 1 else K
+    if w_tscale is None:
+        code = entry(x.data_ptr(), ldx, wq.data_ptr(), wsf.data_ptr(), *tail)
+    else:
+        if w_tscale.dtype is not torch.float32 or w_tscale.numel() < 1 or w_tscale.get_device() != index:
+            raise TypeError("w_tscale: expected a float32 tensor on x's device")
+        code = entry(x.data_ptr(), ldx, wq.data_ptr(), wsf.data_ptr(), w_tscale.data_ptr(), *tail)
     if code:
-        raise SolError(code, entry)
+        raise SolError(code, name)
     return out
 
 
@@ -571,16 +584,16 @@ def _matvec(entry: str, x, wq, wsf, w_tscale, bias, activation: int, out, worksp
 def nvfp4_matvec(x, wq, wsf, w_tscale, bias=None, activation: int = ACT_NONE, out: torch.Tensor | None = None,
                  workspace: torch.Tensor | None = None):
     """Y = act(X) . dequant(W)^T + bias for a few BF16 rows: x is not quantized.  `activation`: ACT_NONE or ACT_SILU, on x."""
-    if w_tscale.dtype is not torch.float32 or w_tscale.numel() < 1:
-        raise TypeError("w_tscale: expected a float32 tensor")
-    return _matvec("nvfp4_matvec", x, wq, wsf, w_tscale, bias, activation, out, workspace, 64)
+    if w_tscale is None:
+        raise TypeError("w_tscale: expected a float32 tensor on x's device")
+    return _matvec(lib().nvfp4_matvec, "nvfp4_matvec", x, wq, wsf, w_tscale, bias, activation, out, workspace, 64)
 
 
 @_on_device_of_first
 def mxfp4_matvec(x, wq, wsf, bias=None, activation: int = ACT_NONE, out: torch.Tensor | None = None,
                  workspace: torch.Tensor | None = None):
     """The same against an MXFP4 weight (no tensor scale)."""
-    return _matvec("mxfp4_matvec", x, wq, wsf, None, bias, activation, out, workspace, 128)
+    return _matvec(lib().mxfp4_matvec, "mxfp4_matvec", x, wq, wsf, None, bias, activation, out, workspace, 128)
 
 
 ROTARY_INTERLEAVED, ROTARY_HALF = 0, 1
@@ -722,7 +735,7 @@ def sol_qk_rotary_backward(dq, dk, q, k, positions, freqs, axis_dims=None, layou
             if x is None:
                 raise ValueError(f"{name}: the gradient of a norm needs the forward input")
             ld_x, x_ptr = _head_view(name, x, shape, index), x.data_ptr()
-            dws[i] = _empty(d, torch.float32, dy.device)
+            dws[i] = _new(dy, d, torch.float32)
             dw_ptr = dws[i].data_ptr()
         dx = dxs[i] = _like(dy) if out is None else out[i]
         packed[i] = _HEAD_GRAD.pack(dy.data_ptr(), x_ptr, dx.data_ptr(), weight, dw_ptr, shape[2],
@@ -730,10 +743,10 @@ def sol_qk_rotary_backward(dq, dk, q, k, positions, freqs, axis_dims=None, layou
     ws_ptr = ws_bytes = 0
     if dws[0] is not None or dws[1] is not None:
         if workspace is None:
-            workspace = _empty(max(1, lib().sol_qk_rotary_backward_workspace_bytes(d)), torch.uint8, dq.device)
+            workspace = _new(dq, max(1, lib().sol_qk_rotary_backward_workspace_bytes(d)), torch.uint8)
         elif workspace.get_device() != index or not workspace.is_contiguous():
             raise ValueError("workspace: expected a dense tensor on the first tensor's device")
-        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.nbytes
     code = lib().sol_qk_rotary_backward(packed[0], packed[1], b * s, d, rot, eps, ws_ptr, ws_bytes, _raw_stream(index))
     if code:
         raise SolError(code, "sol_qk_rotary_backward")

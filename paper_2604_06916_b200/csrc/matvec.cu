@@ -36,7 +36,7 @@ constexpr int kProducer = kConvWarps, kIssuer = kConvWarps + 1;
 constexpr int kThreads = 32 * (kConvWarps + 2);
 constexpr int kRows = 128;           // weight rows of a CTA
 constexpr int kStageK = 256;         // K of a stage: 128 bytes of codes per row
-constexpr int kMaxStages = 8;
+constexpr int kMaxStages = 4;
 constexpr int kCodeBytes = kRows * kStageK / 2;
 constexpr int kSfBytes = kRows * kStageK / 16;
 constexpr int kMaxCluster = 8;
@@ -44,10 +44,11 @@ constexpr int kXExp = 14;            // exponent of the largest scaled |x|
 constexpr int kMxExp = 13;           // exponent of the largest relative MXFP4 scale
 constexpr int kMaxXRows = 64;
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kColA = 0, kColABuf = 128, kColD = 256;   // A: two buffers of a stage; D: up to 64 columns
+constexpr uint32_t kColA = 0, kColABuf = 128, kColD = 256;   // A: two buffers of a stage; D: kSums of 64 columns
+constexpr int kSums = 4;             // sums that products take in turn: one alone would wait for itself
 constexpr int kFull = 0, kXFull = kFull + kMaxStages, kEmpty = kXFull + kMaxStages, kAFull = kEmpty + kMaxStages, kAEmpty = kAFull + 2,
               kDone = kAEmpty + 2, kBars = kDone + 1;
-constexpr int kMaxSmem = 232448;     // per block
+constexpr int kMaxSmem = 232448 - 1024;   // dynamic, beside row_most
 
 struct Params {
     const uint8_t *ximage;   // FP16 x: [row chunk][64 columns of K][x_rows][128 bytes, 128-byte swizzle], K padded to stages
@@ -190,6 +191,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     constexpr int kChunksPerStage = kMx ? 2 : 4;      // 512-byte scale chunks of a stage
     extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ uint8_t row_most[kMx ? 4 : 1][kRows];
+    __shared__ float back[kMaxXRows];
     const uint32_t base = ptx::smem_u32(smem_raw);
     const uint32_t x_bytes = static_cast<uint32_t>(stage_x_bytes(p.x_rows));
     const uint32_t s_code = base, s_x = s_code + p.ring * kCodeBytes, s_sf = s_x + p.ring * x_bytes;
@@ -249,16 +252,21 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     if (kMx && warp < kConvWarps) {
         const uint8_t *c = p.wsf + (static_cast<int64_t>(group) * p.chunks_k + stage0 * kChunksPerStage) * 512 + lane * 16 + (warp & 3) * 4;
         const int n = min(stages * kChunksPerStage, p.chunks_k - stage0 * kChunksPerStage);
-        uint32_t most = 0;
+        uint32_t most = 0;    // the four warpgroups read a quarter of the row's words each
 #pragma unroll 8
-        for (int i = 0; i < n; ++i) most = __vmaxu4(most, __ldg(reinterpret_cast<const uint32_t *>(c + i * 512)));
+        for (int i = warp >> 2; i < n; i += 4) most = __vmaxu4(most, __ldg(reinterpret_cast<const uint32_t *>(c + i * 512)));
         ref = static_cast<int>(max(max(most & 255u, most >> 8 & 255u), max(most >> 16 & 255u, most >> 24)));
+        row_most[warp >> 2][(warp & 3) * 32 + lane] = static_cast<uint8_t>(ref);
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
+    if (kMx && warp < kConvWarps) {
+        const int row = (warp & 3) * 32 + lane;
+        ref = max(max(row_most[0][row], row_most[1][row]), max(row_most[2][row], row_most[3][row]));
+    }
     const uint32_t tmem = aligned ? *tmem_ptr : 0;
-    ptx::cluster_arrive();       // this CTA runs: the others may write their sums into it (awaited before the first such write)
+    if (ranks > 1) ptx::cluster_arrive();       // this CTA runs: the others may write their sums into it (awaited before the first such write)
 
     if (!aligned) {
     } else if (warp == kProducer) {
@@ -287,7 +295,7 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const uint64_t b = ptx::smem_desc_sw128(s_x + st * x_bytes + (i >> 2) * (p.x_rows * 128)) + 2u * (i & 3);
-                    ptx::mma_bf16_a_tmem(tmem + kColD, tmem + kColA + buf * kColABuf + 8 * i, b, idesc, s > 0 || i > 0);
+                    ptx::mma_bf16_a_tmem(tmem + kColD + (i % kSums) * kMaxXRows, tmem + kColA + buf * kColABuf + 8 * i, b, idesc, s > 0 || i >= kSums);
                 }
                 ptx::tc_commit(bar(kAEmpty + buf));
                 ptx::tc_commit(bar(kEmpty + st));      // the codes were read before they became A
@@ -350,45 +358,47 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
         }
         // ------------------------------------------------------------ this slice's sums, to the rank that owns the column
         ok = ok && warp_wait(bar(kDone), 0, abort_flag, p.status, 0xC60u);
-        ptx::cluster_wait();
+        if (ranks > 1) ptx::cluster_wait();
         if (ok) {
+            if (threadIdx.x < p.x_rows) back[threadIdx.x] = __ldcg(p.x_back + m0 + threadIdx.x);   // written before x was loaded
             ptx::tc_fence_after_sync();
             const int own = kRows / ranks;
             const uint32_t to = ptx::map_to_cta(s_part + (rank * p.x_rows * own + row % own) * 4, row / own);
             for (int c = 8 * (warp >> 2); c < p.x_rows; c += 32) {
-                uint32_t d[8];
-                tmem_ld_32x8(tmem + kColD + lanes + c, d);
+                uint32_t d[kSums][8];
+#pragma unroll
+                for (int i = 0; i < kSums; ++i) tmem_ld_32x8(tmem + kColD + i * kMaxXRows + lanes + c, d[i]);
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    float v = __uint_as_float(d[e]);
+                    float v = __uint_as_float(d[0][e]);
+#pragma unroll
+                    for (int i = 1; i < kSums; ++i) v += __uint_as_float(d[i][e]);
                     if (kMx) v = scalbnf(v, ref - 127 - kMxExp);
                     st_cluster(to + (c + e) * own * 4, v);
                 }
             }
         }
     }
-    if (!aligned || warp >= kConvWarps) ptx::cluster_wait();
+    if (ranks > 1 && (!aligned || warp >= kConvWarps)) ptx::cluster_wait();
     ptx::tc_fence_before_sync();
 
     // ---------------------------------------------------------------- own columns: sum over the ranks, scale, bias, store
-    const int own = kRows / ranks, live = min(p.x_rows, p.M - m0);
+    const int own = kRows / ranks, pairs = own / 2, live = min(p.x_rows, p.M - m0);
+    const int r = 2 * (threadIdx.x % pairs), n = group * kRows + rank * own + r;
     const float T = kMx ? 1.0f : __ldg(p.wts);
-    ptx::cluster_sync();
-    for (int i = threadIdx.x; i < live * (own / 2); i += kThreads) {
-        const int m = i / (own / 2), r = 2 * (i % (own / 2));
-        const int n = group * kRows + rank * own + r;
-        if (n >= p.N) continue;
+    uint32_t b2 = 0;
+    if (p.bias != nullptr && n < p.N) b2 = __ldg(reinterpret_cast<const uint32_t *>(p.bias + n));
+    if (ranks > 1) ptx::cluster_sync();
+    else __syncthreads();
+    for (int m = threadIdx.x / pairs; m < live && warp < kConvWarps && n < p.N; m += 32 * kConvWarps / pairs) {
         float v0 = 0.0f, v1 = 0.0f;
         for (int c = 0; c < ranks; ++c) {
             const float2 v = *reinterpret_cast<const float2 *>(part + (c * p.x_rows + m) * own + r);
             v0 += v.x;
             v1 += v.y;
         }
-        const float back = __ldcg(p.x_back + m0 + m);
-        uint32_t b2 = 0;
-        if (p.bias != nullptr) b2 = __ldg(reinterpret_cast<const uint32_t *>(p.bias + n));
-        const float y0 = fmaf(v0 * back, T, qmath::bf16_lo(b2)), y1 = fmaf(v1 * back, T, qmath::bf16_hi(b2));
+        const float y0 = fmaf(v0 * back[m], T, qmath::bf16_lo(b2)), y1 = fmaf(v1 * back[m], T, qmath::bf16_hi(b2));
         uint32_t o;
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(y1), "f"(y0));
         *reinterpret_cast<uint32_t *>(p.y + (m0 + m) * p.ldy + n) = o;

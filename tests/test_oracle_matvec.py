@@ -82,4 +82,4 @@ def test_binding_refuses_before_the_library(B):
         args = dict(x=x, wq=wq, wsf=wsf, bias=None, out=None, workspace=None)
         args.update(kw)
         with pytest.raises((TypeError, ValueError)):
-            B._matvec("mxfp4_matvec", args["x"], args["wq"], args["wsf"], None, args["bias"], 0, args["out"], args["workspace"], 64)
+            B._matvec(None, "mxfp4_matvec", args["x"], args["wq"], args["wsf"], None, args["bias"], 0, args["out"], args["workspace"], 64)
