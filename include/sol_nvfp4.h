@@ -291,6 +291,39 @@ sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const
                                       int64_t batch, int64_t heads, int64_t head_dim, void *stream);
 
 /*
+ * Block-sparse attention for the explore phase (no counterpart in the paper, whose attention is dense): each block of
+ * 256 queries of each head attends to a list of key blocks of 128 tokens.
+ *
+ * sol_select_blocks chooses the lists by a cheap score, per batch element and head:
+ *     score[i][j] = mean(query rows of block i) . mean(key rows of block j)           (FP64)
+ *     list[i] = the `count` key blocks of highest score, ascending; the first keep_first blocks are kept whatever their
+ *     score (text tokens in front); among equal scores the lower index
+ *   q  [batch, seq_q, heads, head_dim] BF16, token pitch ld_q as in sol_attention_bf16;  k  the same with heads_kv heads;
+ *      query head h reads key head h / (heads / heads_kv)
+ *   kv_lens      [batch] int32 (device) or NULL: keys of a batch element that exist (held to [0, seq_kv]); means are taken over
+ *                them and blocks without any are not chosen
+ *   block_lists  [batch, heads, ceil(seq_q / 256), count] int32, -1 behind the last;  counts the lists' lengths
+ *   scores       same shape as block_lists, FP32 scores of the chosen blocks (-inf behind the last), or NULL
+ *   workspace    sol_select_blocks_workspace_bytes(...) bytes of device scratch, 256-byte aligned (one per call that may overlap)
+ *   head_dim 64 or 128, seq_kv <= 1048576, 1 <= count <= 8192, keep_first <= count.  Inputs must be finite.
+ *
+ * sol_attention_blocks computes softmax(q k^T / sqrt(head_dim)) v over the keys of the listed blocks (rounding as
+ * sol_attention_bf16).  Any lists will do: entries outside [0, ceil(keys / 128)) are skipped, the order is free, a block
+ * listed twice counts twice, a row of queries whose list names no existing key gets zeros.  A count is held to [0, max_blocks].
+ *   block_lists [batch, heads, ceil(seq_q / 256), max_blocks];  out as in sol_attention_bf16, no alias of an input
+ */
+size_t sol_select_blocks_workspace_bytes(int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv,
+                                         int64_t head_dim);
+sol_status_t sol_select_blocks(const void *q, const void *k, int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads,
+                               int64_t heads_kv, int64_t head_dim, int64_t ld_q, int64_t ld_k, int64_t count, int64_t keep_first,
+                               const int32_t *kv_lens, int32_t *block_lists, int32_t *counts, float *scores, void *workspace,
+                               size_t workspace_bytes, void *stream);
+sol_status_t sol_attention_blocks(const void *q, const void *k, const void *v, void *out, int64_t batch, int64_t seq_q,
+                                  int64_t seq_kv, int64_t heads, int64_t heads_kv, int64_t head_dim, int64_t ld_q,
+                                  int64_t ld_k, int64_t ld_v, int64_t ld_out, const int32_t *block_lists,
+                                  const int32_t *counts, int64_t max_blocks, const int32_t *kv_lens, void *stream);
+
+/*
  * Linear of a few BF16 rows against a weight in NVFP4 or MXFP4, x kept in 16 bits (weight-only: the rollout models'
  * modulation and embedding linears, whose rows are samples; the paper quantizes both operands of the token linears):
  *     y[m,n] = bf16_rne( T * sum_k act(x[m,k]) * code[n,k] * scale[n, block of k] + bias[n] )      (MXFP4: T = 1)

@@ -32,7 +32,7 @@ EXPORTS = [
     "sol_attention_nvfp4_out", "mxfp4_linear_quantized_out", "sol_set_wait_limit_cycles", "sol_test_hold_loads",
     "mxfp4_linear_split_out", "mxfp4_quantize_into", "sol_qk_rotary", "sol_qk_rotary_backward",
     "sol_qk_rotary_backward_workspace_bytes", "sol_rotary_frequencies", "nvfp4_matvec", "mxfp4_matvec",
-    "sol_matvec_workspace_bytes",
+    "sol_matvec_workspace_bytes", "sol_select_blocks", "sol_select_blocks_workspace_bytes", "sol_attention_blocks",
 ]
 
 _lib = None
@@ -117,6 +117,11 @@ def lib() -> ctypes.CDLL:
     L.nvfp4_matvec.argtypes = [vp, i64, vp, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, sz, vp]
     L.mxfp4_matvec.argtypes = [vp, i64, vp, vp, vp, i32, vp, i64, i64, i64, i64, vp, sz, vp]
     L.sol_matvec_workspace_bytes.restype, L.sol_matvec_workspace_bytes.argtypes = sz, [i64, i64]
+    L.sol_select_blocks_workspace_bytes.restype, L.sol_select_blocks_workspace_bytes.argtypes = sz, [i64] * 6
+    L.sol_select_blocks.restype = i32
+    L.sol_select_blocks.argtypes = [vp, vp] + [i64] * 10 + [vp, vp, vp, vp, vp, sz, vp]
+    L.sol_attention_blocks.restype = i32
+    L.sol_attention_blocks.argtypes = [vp, vp, vp, vp] + [i64] * 10 + [vp, vp, i64, vp, vp]
     L.sol_qk_rotary.restype = i32
     L.sol_qk_rotary.argtypes = [vp, vp, i64, i64, vp, f32, vp]
     L.sol_qk_rotary_backward.restype = i32
@@ -751,6 +756,84 @@ def sol_qk_rotary_backward(dq, dk, q, k, positions, freqs, axis_dims=None, layou
     if code:
         raise SolError(code, "sol_qk_rotary_backward")
     return dxs[0], dxs[1], dws[0], dws[1]
+
+
+QUERY_BLOCK, KEY_BLOCK = 256, 128
+
+
+def _kv_of(q, k, index: int):
+    """Shapes of q [B, Sq, H, D] and k [B, Skv, Hk, D] and their token pitches."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise TypeError("q and k: expected [B, S, H, D] bf16 tensors")
+    B_, Sq, H, D = q.shape
+    b, Skv, Hk, d = k.shape
+    if b != B_ or d != D or Hk == 0 or H % Hk != 0:
+        raise ValueError("k must share q's batch and head dimension, and its heads must divide q's")
+    return B_, Sq, Skv, H, Hk, D, _head_view("q", q, q.shape, index), _head_view("k", k, k.shape, index)
+
+
+def _lens_ptr(kv_lens, B_: int, index: int) -> int | None:
+    if kv_lens is None:
+        return None
+    if kv_lens.dtype is not torch.int32 or kv_lens.shape != (B_,) or not kv_lens.is_contiguous() or kv_lens.get_device() != index:
+        raise TypeError("kv_lens: expected a dense [B] int32 tensor on q's device")
+    return kv_lens.data_ptr()
+
+
+@_on_device_of_first
+def sol_select_blocks(q, k, count: int, keep_first: int = 0, kv_lens=None, with_scores: bool = False,
+                      workspace: torch.Tensor | None = None):
+    """Key blocks (128 tokens) of highest mean-pooled score for each query block (256 tokens) of each head.
+
+    q [B, Sq, H, D], k [B, Skv, Hk, D] (D = 64 or 128, Hk divides H).  Returns (blocks [B, H, ceil(Sq / 256), count]
+    int32, ascending, -1 behind the last; counts [B, H, ceil(Sq / 256)] int32) and, `with_scores`, the chosen
+    blocks' FP32 scores.  The first `keep_first` blocks are always kept; `kv_lens` [B] int32 limits the keys that exist.
+    """
+    index = q.get_device()
+    B_, Sq, Skv, H, Hk, D, ld_q, ld_k = _kv_of(q, k, index)
+    lens = _lens_ptr(kv_lens, B_, index)
+    nq = (Sq + QUERY_BLOCK - 1) // QUERY_BLOCK
+    if not 0 < count <= 8192:
+        raise ValueError("count must be between 1 and 8192")
+    blocks = _new(q, (B_, H, nq, count), torch.int32)
+    counts = _new(q, (B_, H, nq), torch.int32)
+    scores = _new(q, (B_, H, nq, count), torch.float32) if with_scores else None
+    if workspace is None:
+        workspace = _new(q, max(1, lib().sol_select_blocks_workspace_bytes(B_, Sq, Skv, H, Hk, D)), torch.uint8)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise TypeError("workspace: expected a dense tensor on q's device")
+    code = lib().sol_select_blocks(q.data_ptr(), k.data_ptr(), B_, Sq, Skv, H, Hk, D, ld_q, ld_k, count, keep_first, lens,
+                                   blocks.data_ptr(), counts.data_ptr(), None if scores is None else scores.data_ptr(),
+                                   workspace.data_ptr(), workspace.nbytes, _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_select_blocks")
+    return (blocks, counts, scores) if with_scores else (blocks, counts)
+
+
+@_on_device_of_first
+def sol_attention_blocks(q, k, v, blocks, counts, kv_lens=None, out: torch.Tensor | None = None):
+    """Attention of each 256-query block of each head over its listed 128-key blocks (as from sol_select_blocks).
+
+    q [B, Sq, H, D], k and v [B, Skv, Hk, D]; blocks [B, H, ceil(Sq / 256), n] int32, counts [B, H, ceil(Sq / 256)] int32.
+    Entries that name no existing block are skipped; a query whose list names no key gets zeros.  Returns [B, Sq, H, D].
+    """
+    index = q.get_device()
+    B_, Sq, Skv, H, Hk, D, ld_q, ld_k = _kv_of(q, k, index)
+    ld_v = _head_view("v", v, k.shape, index)
+    nq = (Sq + QUERY_BLOCK - 1) // QUERY_BLOCK
+    if blocks.dtype is not torch.int32 or blocks.dim() != 4 or blocks.shape[:3] != (B_, H, nq) or not blocks.is_contiguous() \
+            or blocks.get_device() != index:
+        raise TypeError("blocks: expected a dense [B, H, ceil(Sq / 256), n] int32 tensor on q's device")
+    if counts.dtype is not torch.int32 or counts.shape != (B_, H, nq) or not counts.is_contiguous() or counts.get_device() != index:
+        raise TypeError("counts: expected a dense [B, H, ceil(Sq / 256)] int32 tensor on q's device")
+    if out is None:
+        out = _like(q)
+    code = lib().sol_attention_blocks(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B_, Sq, Skv, H, Hk, D, ld_q, ld_k, ld_v,
+                                      _head_view("out", out, q.shape, index), blocks.data_ptr(), counts.data_ptr(), blocks.shape[3],
+                                      _lens_ptr(kv_lens, B_, index), _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_attention_blocks")
+    return out
 
 
 def mxfp4_scale_bytes(rows: int, K: int, layout: int = SF_SWIZZLED_128x4) -> int:

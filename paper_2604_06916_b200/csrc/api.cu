@@ -585,7 +585,7 @@ sol_status_t sol_attention_bf16(const void *q, const void *k, const void *v, voi
     sol_status_t st = check_arch(&dev);
     if (st != SOL_OK) return st;
     const attn::Stream b{q, k, v, out, seq_q, seq_kv, ld_q, ld_k, ld_v, ld_out};
-    return attn::launch_attention(nullptr, b, batch, heads, head_dim, nullptr, static_cast<cudaStream_t>(stream));
+    return attn::launch_attention(nullptr, b, batch, heads, head_dim, nullptr, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 sol_status_t sol_attention_nvfp4_out(const void *q, const void *k, const void *v, int64_t batch, int64_t seq_q,
@@ -610,7 +610,7 @@ sol_status_t sol_attention_nvfp4_out(const void *q, const void *k, const void *v
     if (st != SOL_OK) return st;
     const attn::Stream b{q, k, v, nullptr, seq_q, seq_kv, ld_q, ld_k, ld_v, cols};
     const attn::QuantDest qd{q_dest, sf_dest, out_tscale, reinterpret_cast<uint32_t *>(amax_out), dest_K, dest_col0};
-    return attn::launch_attention(nullptr, b, batch, heads, head_dim, &qd, static_cast<cudaStream_t>(stream));
+    return attn::launch_attention(nullptr, b, batch, heads, head_dim, &qd, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const sol_attention_stream_t *second,
@@ -636,7 +636,61 @@ sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const
                          first->ld_q, first->ld_k, first->ld_v, first->ld_out};
     const attn::Stream b{second->q, second->k, second->v, second->out, second->seq, second->seq,
                          second->ld_q, second->ld_k, second->ld_v, second->ld_out};
-    return attn::launch_attention(&a, b, batch, heads, head_dim, nullptr, static_cast<cudaStream_t>(stream));
+    return attn::launch_attention(&a, b, batch, heads, head_dim, nullptr, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+bool blocks_shape_ok(int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv, int64_t head_dim) {
+    return (head_dim == 64 || head_dim == 128) && batch > 0 && batch <= 65535 && heads > 0 && heads <= 65535 && heads_kv > 0 &&
+           heads % heads_kv == 0 && seq_q > 0 && seq_q <= (1LL << 24) && seq_kv > 0 && seq_kv <= blocks::kMaxKeyBlocks * blocks::kKeyBlock;
+}
+}  // namespace
+
+size_t sol_select_blocks_workspace_bytes(int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv,
+                                         int64_t head_dim) {
+    return blocks_shape_ok(batch, seq_q, seq_kv, heads, heads_kv, head_dim)
+               ? blocks::select_workspace_bytes(batch, seq_q, seq_kv, heads, heads_kv, head_dim) : 0;
+}
+
+sol_status_t sol_select_blocks(const void *q, const void *k, int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads,
+                               int64_t heads_kv, int64_t head_dim, int64_t ld_q, int64_t ld_k, int64_t count, int64_t keep_first,
+                               const int32_t *kv_lens, int32_t *block_lists, int32_t *counts, float *scores, void *workspace,
+                               size_t workspace_bytes, void *stream) {
+    if (q == nullptr || k == nullptr || block_lists == nullptr || counts == nullptr || workspace == nullptr) return SOL_ERR_NULL_POINTER;
+    if (!blocks_shape_ok(batch, seq_q, seq_kv, heads, heads_kv, head_dim) || ld_q < heads * head_dim || ld_k < heads_kv * head_dim ||
+        count < 1 || count > blocks::kMaxKeyBlocks || keep_first < 0 || keep_first > count)
+        return SOL_ERR_BAD_SHAPE;
+    if (!aligned16(q) || !aligned16(k) || ld_q % 8 != 0 || ld_k % 8 != 0 || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+        (reinterpret_cast<uintptr_t>(kv_lens) & 3u) || (reinterpret_cast<uintptr_t>(block_lists) & 3u) ||
+        (reinterpret_cast<uintptr_t>(counts) & 3u) || (reinterpret_cast<uintptr_t>(scores) & 3u))
+        return SOL_ERR_ALIGNMENT;
+    if (workspace_bytes < blocks::select_workspace_bytes(batch, seq_q, seq_kv, heads, heads_kv, head_dim)) return SOL_ERR_WORKSPACE_TOO_SMALL;
+    const DeviceInfo *dev = nullptr;
+    const sol_status_t st = check_arch(&dev);
+    if (st != SOL_OK) return st;
+    return blocks::launch_select(q, k, batch, seq_q, seq_kv, heads, heads_kv, head_dim, ld_q, ld_k, count, keep_first, kv_lens,
+                                 block_lists, counts, scores, workspace, static_cast<cudaStream_t>(stream));
+}
+
+sol_status_t sol_attention_blocks(const void *q, const void *k, const void *v, void *out, int64_t batch, int64_t seq_q, int64_t seq_kv,
+                                  int64_t heads, int64_t heads_kv, int64_t head_dim, int64_t ld_q, int64_t ld_k, int64_t ld_v,
+                                  int64_t ld_out, const int32_t *block_lists, const int32_t *counts, int64_t max_blocks,
+                                  const int32_t *kv_lens, void *stream) {
+    if (q == nullptr || k == nullptr || v == nullptr || out == nullptr || block_lists == nullptr || counts == nullptr)
+        return SOL_ERR_NULL_POINTER;
+    if (!blocks_shape_ok(batch, seq_q, seq_kv, heads, heads_kv, head_dim) || max_blocks < 1 || max_blocks > blocks::kMaxKeyBlocks ||
+        ld_q < heads * head_dim || ld_out < heads * head_dim || ld_k < heads_kv * head_dim || ld_v < heads_kv * head_dim)
+        return SOL_ERR_BAD_SHAPE;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || ld_q % 8 != 0 || ld_k % 8 != 0 || ld_v % 8 != 0 ||
+        ld_out % 8 != 0 || (reinterpret_cast<uintptr_t>(kv_lens) & 3u) || (reinterpret_cast<uintptr_t>(block_lists) & 3u) ||
+        (reinterpret_cast<uintptr_t>(counts) & 3u))
+        return SOL_ERR_ALIGNMENT;
+    const DeviceInfo *dev = nullptr;
+    const sol_status_t st = check_arch(&dev);
+    if (st != SOL_OK) return st;
+    const attn::Stream b{q, k, v, out, seq_q, seq_kv, ld_q, ld_k, ld_v, ld_out};
+    const attn::BlockLists lists{block_lists, counts, kv_lens, max_blocks, heads_kv};
+    return attn::launch_attention(nullptr, b, batch, heads, head_dim, nullptr, &lists, static_cast<cudaStream_t>(stream));
 }
 
 namespace {

@@ -18,6 +18,10 @@
 // tensor pipe works for one tile while the other is in its softmax.  TMEM: S_t/P_t and O_t, 128
 // columns each.  The epilogue divides by l and leaves through TMA stores (staged where Q_t was).
 //
+// Over listed key blocks (kListed) the tiles are the entries of a list per query block: a warp copies the entries that
+// name existing keys into shared memory while Q loads, and tile j is the j-th of them; a list without any leaves
+// zeros.  A key / value head may serve several query heads.
+//
 // Warps: 0 = TMA producer, 1 = TMEM owner and MMA issuer, 2..5 and 6..9 = softmax / epilogue of query
 // tile 0 and 1 (one warp per TMEM lane quadrant).  Every mbarrier wait is bounded.
 #include "gemm_common.cuh"
@@ -38,6 +42,8 @@ constexpr int kStages = 2;              // K ring and V ring
 constexpr int kThreads = 32 * (2 + 4 * kQTiles);
 constexpr float kLazyLog2 = 8.0f;       // slack of the softmax reference maximum, in powers of two
 constexpr int smem_bytes(int head_dim) { return (kQTiles + 2 * kStages) * (head_dim / 64) * kBox + 256; }
+constexpr int list_bytes(int64_t max_blocks) { return static_cast<int>((2 * max_blocks + 15) / 16 * 16); }   // 16-bit block numbers
+static_assert(smem_bytes(128) + list_bytes(blocks::kMaxKeyBlocks) <= 232448, "shared memory budget with a list");
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 128, kColTile = 256;   // per query tile; P overwrites columns [0, 64) of S
 static_assert(smem_bytes(128) <= 232448, "shared memory budget");
@@ -64,6 +70,12 @@ struct Params {
     int dest_pitch;        // dest_K / 2
     int dest_col0;         // first destination column of head 0
     int dest_chunks_k;     // dest_K / 64
+    // listed key blocks (kListed)
+    const int32_t *blocks;
+    const int32_t *counts;
+    const int32_t *kv_lens;   // null: every batch element has seq_kv keys
+    int max_blocks;
+    int group;             // query heads per key / value head
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -83,7 +95,8 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, ui
 // kD: head dimension, 64 or 128 (a tile of kD columns is kD / 64 boxes of [128 rows][64 BF16]).
 // kQuantOut: the output leaves as the next linear's NVFP4 activations (h = bf16(O / l), then the
 // quantizer's FP32 sequence per 16 columns) instead of BF16 -- one stream only.
-template <int kD, bool kQuantOut>
+// kListed: over the listed key blocks -- one stream, BF16 output.
+template <int kD, bool kQuantOut, bool kListed>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constant__ CUtensorMap tm_ka,
                  const __grid_constant__ CUtensorMap tm_va, const __grid_constant__ CUtensorMap tm_oa,
@@ -111,7 +124,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int q0_joint = blockIdx.x * (kQTiles * kBQ), head = blockIdx.y, batch = blockIdx.z;
-    const int n_tiles = (p.seq_kv + kBKV - 1) / kBKV;
+    uint16_t *list = reinterpret_cast<uint16_t *>(smem_raw + (sV + kStages * kTile - smem_base) + 256);
+    uint32_t *list_len = tmem_ptr_smem + 2;
+    const int kv_len = !kListed || p.kv_lens == nullptr ? p.seq_kv : min(max(__ldg(p.kv_lens + batch), 0), p.seq_kv);
     // the CTA's queries come from one stream (the split is a multiple of the CTA's 256 rows)
     const bool q_in_a = q0_joint < p.q_split;
     const CUtensorMap *tm_q = q_in_a ? &tm_qa : &tm_qb;
@@ -128,6 +143,21 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         ptx::prefetch_tmap(&tm_kb);
         ptx::prefetch_tmap(&tm_vb);
     }
+    if (kListed && warp == 2) {   // the entries that name existing keys, in their order
+        const int64_t row = (static_cast<int64_t>(batch) * gridDim.y + head) * gridDim.x + blockIdx.x;
+        const int32_t *from = p.blocks + row * p.max_blocks;
+        const int named = min(max(__ldg(p.counts + row), 0), p.max_blocks);
+        const int existing = (kv_len + kBKV - 1) / kBKV;
+        int kept = 0;
+        for (int i0 = 0; i0 < named; i0 += 32) {
+            const int e = i0 + lane < named ? __ldg(from + i0 + lane) : -1;
+            const bool keep = e >= 0 && e < existing;
+            const uint32_t mask = __ballot_sync(0xFFFFFFFFu, keep);
+            if (keep) list[kept + __popc(mask & ((1u << lane) - 1u))] = static_cast<uint16_t>(e);
+            kept += __popc(mask);
+        }
+        if (lane == 0) *list_len = static_cast<uint32_t>(kept);
+    }
     if (warp == 1) {
         ptx::tmem_alloc(ptx::smem_u32(tmem_ptr_smem), kTmemCols);
         ptx::tmem_relinquish();
@@ -136,11 +166,13 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_ptr_smem;
+    const int n_tiles = kListed ? static_cast<int>(*list_len) : (p.seq_kv + kBKV - 1) / kBKV;
+    auto first_key = [&](int j) { return kListed ? list[j] * kBKV : j * kBKV; };   // of tile j
 
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer
         if (ptx::elect_one()) {
-            const int x0 = head * kD;
+            const int x0 = head * kD, x0_kv = kListed ? head / p.group * kD : x0;
             ptx::mbar_arrive_expect_tx(bar(kQFull), kQTiles * kTile);
 #pragma unroll
             for (int t = 0; t < kQTiles; ++t) {
@@ -156,18 +188,18 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                 ptx::mbar_arrive_expect_tx(bar(kKFull + st), kTile);
                 // key tile j of the joint sequence: stream a up to the split (a multiple of the tile), then stream b
                 const bool kv_in_a = j * kBKV < p.kv_split;
-                const int kv0 = kv_in_a ? j * kBKV : j * kBKV - p.kv_split;
+                const int kv0 = kListed || kv_in_a ? first_key(j) : j * kBKV - p.kv_split;
                 const CUtensorMap *tm_k = kv_in_a ? &tm_ka : &tm_kb;
                 const CUtensorMap *tm_v = kv_in_a ? &tm_va : &tm_vb;
 #pragma unroll
                 for (int bx = 0; bx < kBoxes; ++bx)
-                    ptx::tma_load_3d(sK + st * kTile + bx * kBox, tm_k, x0 + 64 * bx, kv0, batch, bar(kKFull + st));
+                    ptx::tma_load_3d(sK + st * kTile + bx * kBox, tm_k, x0_kv + 64 * bx, kv0, batch, bar(kKFull + st));
                 if (!wait_bounded(bar(kVEmpty + st), par ^ 1u, abort_flag, p.status, 0xB20u | st)) break;
                 ATTN_TRACE(11, j);
                 ptx::mbar_arrive_expect_tx(bar(kVFull + st), kTile);
 #pragma unroll
                 for (int bx = 0; bx < kBoxes; ++bx)
-                    ptx::tma_load_3d(sV + st * kTile + bx * kBox, tm_v, x0 + 64 * bx, kv0, batch, bar(kVFull + st));
+                    ptx::tma_load_3d(sV + st * kTile + bx * kBox, tm_v, x0_kv + 64 * bx, kv0, batch, bar(kVFull + st));
             }
         }
         __syncwarp();
@@ -195,7 +227,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                                          idesc_pv, acc || i > 0);
                 }
             };
-            bool ok = wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xB30u) &&
+            bool ok = wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xB30u) && (!kListed || n_tiles > 0) &&
                       wait_bounded(bar(kKFull), 0, abort_flag, p.status, 0xB31u);
             if (ok) {
                 ptx::tc_fence_after_sync();
@@ -262,7 +294,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
             for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_lane + kColS + 32 * c, s[c]);
             ptx::tmem_ld_wait();
             if (tracer) ATTN_TRACE(5, j);
-            const int valid = p.seq_kv - j * kBKV;              // keys of this tile that exist (>= 1)
+            const int valid = kv_len - first_key(j);            // keys of this tile that exist (>= 1)
             if (valid < kBKV) {  // the last tile of a ragged sequence: keys that do not exist score -inf
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
@@ -327,7 +359,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
             if (lane == 0) ptx::mbar_arrive(bar(kPFull + t));
             if (tracer) ATTN_TRACE(9, j);
         }
-        if (ok && wait_bounded(bar(kPvDone + t), 0, abort_flag, p.status, 0xBA0u | t)) {
+        const bool empty = kListed && n_tiles == 0;            // no products: Q's place is free once Q has arrived
+        if (ok && (empty ? wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xBB0u | t)
+                         : wait_bounded(bar(kPvDone + t), 0, abort_flag, p.status, 0xBA0u | t))) {
             ptx::tc_fence_after_sync();
             const float inv = 1.0f / l;
             if constexpr (kQuantOut) {
@@ -395,8 +429,10 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                 for (int q = 0; q < 4; ++q) {
                     uint32_t w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                    for (int e = 0; e < 4; ++e) {
                         w[e] = pack_bf16(__uint_as_float(o[8 * q + 2 * e]) * inv, __uint_as_float(o[8 * q + 2 * e + 1]) * inv);
+                        if (kListed && empty) w[e] = 0;        // O was never written
+                    }
                     const int ch = c * 4 + q;
                     sts128(o_row + (ch >> 3) * kBox + ((static_cast<uint32_t>(ch & 7) ^ sw) << 4), w[0], w[1], w[2], w[3]);
                 }
@@ -427,20 +463,26 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 }  // namespace
 
 sol_status_t launch_attention(const Stream *a, const Stream &b, int64_t batch, int64_t heads, int64_t head_dim,
-                              const QuantDest *qd, cudaStream_t stream) {
+                              const QuantDest *qd, const BlockLists *lists, cudaStream_t stream) {
     CUtensorMap tm[8];
     const uint64_t cols = static_cast<uint64_t>(heads) * static_cast<uint64_t>(head_dim);
-    auto make = [&](CUtensorMap *t, const void *base, int64_t seq, int64_t ld, uint32_t box_rows) {
-        return make_tmap_3d_bf16(t, base, cols, static_cast<uint64_t>(seq), static_cast<uint64_t>(batch),
+    const uint64_t cols_kv = lists != nullptr ? static_cast<uint64_t>(lists->heads_kv) * static_cast<uint64_t>(head_dim) : cols;
+    auto make = [&](CUtensorMap *t, const void *base, int64_t seq, int64_t ld, uint32_t box_rows, uint64_t columns) {
+        return make_tmap_3d_bf16(t, base, columns, static_cast<uint64_t>(seq), static_cast<uint64_t>(batch),
                                  static_cast<uint64_t>(ld) * 2, static_cast<uint64_t>(seq) * ld * 2, 64, box_rows);
     };
     auto make4 = [&](CUtensorMap *t, const Stream &s) {
         // a quantized destination has no BF16 output tensor: the (unused) output map is a copy of the query map
-        return make(t, s.q, s.seq_q, s.ld_q, kBQ) && make(t + 1, s.k, s.seq_kv, s.ld_k, kBKV) &&
-               make(t + 2, s.v, s.seq_kv, s.ld_v, kBKV) &&
-               (qd != nullptr ? make(t + 3, s.q, s.seq_q, s.ld_q, 32) : make(t + 3, s.out, s.seq_q, s.ld_out, 32));
+        return make(t, s.q, s.seq_q, s.ld_q, kBQ, cols) && make(t + 1, s.k, s.seq_kv, s.ld_k, kBKV, cols_kv) &&
+               make(t + 2, s.v, s.seq_kv, s.ld_v, kBKV, cols_kv) &&
+               (qd != nullptr ? make(t + 3, s.q, s.seq_q, s.ld_q, 32, cols) : make(t + 3, s.out, s.seq_q, s.ld_out, 32, cols));
     };
-    if (!make4(tm + 4, b) || !make4(tm, a != nullptr ? *a : b)) return SOL_ERR_CUDA;  // one stream: the a maps are never used
+    if (!make4(tm + 4, b)) return SOL_ERR_CUDA;
+    if (a == nullptr) {  // one stream: the a maps are never used
+        for (int i = 0; i < 4; ++i) tm[i] = tm[4 + i];
+    } else if (!make4(tm, *a)) {
+        return SOL_ERR_CUDA;
+    }
     Params p{};
     p.q_split = a != nullptr ? static_cast<int>(a->seq_q) : 0;
     p.kv_split = a != nullptr ? static_cast<int>(a->seq_kv) : 0;
@@ -457,16 +499,25 @@ sol_status_t launch_attention(const Stream *a, const Stream &b, int64_t batch, i
         p.dest_col0 = static_cast<int>(qd->dest_col0);
         p.dest_chunks_k = static_cast<int>(qd->dest_K / 64);
     }
-    const bool quant = qd != nullptr, wide = head_dim == 128;
-    auto kern = wide ? (quant ? attention_kernel<128, true> : attention_kernel<128, false>)
-                     : (quant ? attention_kernel<64, true> : attention_kernel<64, false>);
-    const int smem = smem_bytes(static_cast<int>(head_dim));
-    static bool configured[4][64] = {};
+    if (lists != nullptr) {
+        p.blocks = lists->blocks;
+        p.counts = lists->counts;
+        p.kv_lens = lists->kv_lens;
+        p.max_blocks = static_cast<int>(lists->max_blocks);
+        p.group = static_cast<int>(heads / lists->heads_kv);
+    }
+    const bool quant = qd != nullptr, wide = head_dim == 128, listed = lists != nullptr;
+    auto kern = wide ? (listed ? attention_kernel<128, false, true> : quant ? attention_kernel<128, true, false> : attention_kernel<128, false, false>)
+                     : (listed ? attention_kernel<64, false, true> : quant ? attention_kernel<64, true, false> : attention_kernel<64, false, false>);
+    const int fixed = smem_bytes(static_cast<int>(head_dim));
+    const int smem = fixed + (listed ? list_bytes(lists->max_blocks) : 0);
+    const int smem_most = fixed + (listed ? list_bytes(blocks::kMaxKeyBlocks) : 0);
+    static bool configured[6][64] = {};
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SOL_ERR_CUDA;
-    const int slot = (wide ? 2 : 0) + (quant ? 1 : 0);
+    const int slot = (wide ? 3 : 0) + (listed ? 2 : quant ? 1 : 0);
     if (!configured[slot][dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_most) != cudaSuccess)
             return SOL_ERR_CUDA;
         configured[slot][dev] = true;
     }

@@ -135,6 +135,12 @@ struct Stream {   // one token stream of an attention call: [batch, seq, heads, 
     void *out;
     int64_t seq_q, seq_kv, ld_q, ld_k, ld_v, ld_out;
 };
+struct BlockLists {  // key blocks that each query block of each head attends to
+    const int32_t *blocks;   // [batch, heads, ceil(seq_q / 256), max_blocks]
+    const int32_t *counts;   // [batch, heads, ceil(seq_q / 256)]
+    const int32_t *kv_lens;  // [batch] keys that exist, or null
+    int64_t max_blocks, heads_kv;
+};
 struct QuantDest {   // NVFP4 destination of the output: columns [dest_col0, dest_col0 + heads * head_dim) of a [rows, dest_K] tensor
     void *q, *sf;
     const float *tscale;
@@ -142,9 +148,20 @@ struct QuantDest {   // NVFP4 destination of the output: columns [dest_col0, des
     int64_t dest_K, dest_col0;
 };
 // Attention over the concatenation (a, then b) of two token streams, or over b alone when a is null;
-// with `qd` (one stream only) the output is quantized into `qd` instead of written as BF16.
+// with `qd` (one stream only) the output is quantized into `qd` instead of written as BF16; with `lists` (one stream
+// only, BF16 output) over the listed key blocks.
 sol_status_t launch_attention(const Stream *a, const Stream &b, int64_t batch, int64_t heads, int64_t head_dim,
-                              const QuantDest *qd, cudaStream_t stream);
+                              const QuantDest *qd, const BlockLists *lists, cudaStream_t stream);
+}
+
+// Selection of key blocks for block-sparse attention.
+namespace blocks {
+constexpr int kQueryBlock = 256, kKeyBlock = 128;
+constexpr int kMaxKeyBlocks = 8192;
+size_t select_workspace_bytes(int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv, int64_t head_dim);
+sol_status_t launch_select(const void *q, const void *k, int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv,
+                           int64_t head_dim, int64_t ld_q, int64_t ld_k, int64_t count, int64_t keep_first, const int32_t *kv_lens,
+                           int32_t *blocks, int32_t *counts, float *scores, void *workspace, cudaStream_t stream);
 }
 
 // Head norm and rotary positions of q and k (a tensor with no heads is absent).
