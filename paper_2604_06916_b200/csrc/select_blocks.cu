@@ -17,8 +17,9 @@ namespace blocks {
 namespace {
 
 constexpr int kPoolWarps = 8;
-constexpr int kPoolColumns = 256;      // columns of a pooling CTA: 16 bytes per lane
-constexpr int kRowsInFlight = 8;       // rows a warp loads before it adds any
+constexpr int kWarpColumns = 256;      // columns of a pooling warp: 16 bytes per lane
+constexpr int kWarpRows = 64;          // rows of a pooling warp
+constexpr int kRowsInFlight = 16;      // rows a warp loads before it adds any
 
 // FP64 of the two BF16 halves of a word, times 2^-896 (upper words; the lower ones are zero).
 __device__ __forceinline__ double scaled_hi(uint32_t w) {
@@ -45,51 +46,67 @@ __device__ __forceinline__ int valid_rows(const int32_t *lens, int b, int seq) {
     return lens == nullptr ? seq : min(max(__ldg(lens + b), 0), seq);
 }
 
+// (volatile: all loads of a batch are issued before the first addition, which the compiler otherwise trades for registers)
+__device__ __forceinline__ uint4 load_once(const uint16_t *p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// A CTA's warps lie side by side along the columns (long contiguous pieces of each row) and, a block's 64-row parts, below
+// each other.
 __global__ void __launch_bounds__(32 * kPoolWarps)
 pool_kernel(const PoolParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ double part[kPoolWarps][kPoolColumns];
+    __shared__ double part[kPoolWarps][kWarpColumns];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.y;
     const bool is_q = static_cast<int>(blockIdx.x) < p.q_ctas;
     const PoolTensor t = is_q ? p.q : p.k;
     const int unit = is_q ? blockIdx.x : blockIdx.x - p.q_ctas;
-    const int blk = unit / t.column_chunks, c0 = unit % t.column_chunks * kPoolColumns;
+    const int parts = t.rows_per_block / kWarpRows, side = kPoolWarps / parts;      // warps below, and beside each other
+    const int blk = unit / t.column_chunks, c0 = (unit % t.column_chunks * side + warp % side) * kWarpColumns;
     const int columns = t.heads << p.head_dim_log2;
     const int row0 = blk * t.rows_per_block, rows = min(t.rows_per_block, valid_rows(t.lens, b, t.seq) - row0);
+    const int first = warp / side * kWarpRows, last = min(rows, first + kWarpRows);
     const int c = c0 + 8 * lane;
     const bool live = c < columns;       // columns are a multiple of 64: a lane is wholly inside or outside
     const uint16_t *x = t.x + b * t.batch_stride + static_cast<int64_t>(row0) * t.ld + c;
     double acc[8] = {};
-    for (int r0 = warp; r0 < rows; r0 += kPoolWarps * kRowsInFlight) {
-        uint4 v[kRowsInFlight];
+    auto add = [&](const uint4 &v) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < kRowsInFlight; ++i) {
-            const int r = r0 + i * kPoolWarps;
-            v[i] = live && r < rows ? __ldg(reinterpret_cast<const uint4 *>(x + r * t.ld)) : make_uint4(0, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) {
+            acc[2 * e] += scaled_lo(w[e]);
+            acc[2 * e + 1] += scaled_hi(w[e]);
         }
+    };
+    if (live) {
+        int r = first;
+        for (; r + kRowsInFlight <= last; r += kRowsInFlight) {
+            uint4 v[kRowsInFlight];
 #pragma unroll
-        for (int i = 0; i < kRowsInFlight; ++i) {
-            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            for (int i = 0; i < kRowsInFlight; ++i) v[i] = load_once(x + (r + i) * t.ld);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                acc[2 * e] += scaled_lo(w[e]);
-                acc[2 * e + 1] += scaled_hi(w[e]);
-            }
+            for (int i = 0; i < kRowsInFlight; ++i) add(v[i]);
         }
+        for (; r < last; ++r) add(__ldcs(reinterpret_cast<const uint4 *>(x + r * t.ld)));
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) part[warp][8 * lane + e] = acc[e];
+    for (int e = 0; e < 8; ++e) part[warp][32 * e + lane] = acc[e];    // column 8 * lane + e: no bank is hit twice
     __syncthreads();
-    const int col = c0 + threadIdx.x;
-    if (col >= columns) return;
-    double sum = 0.0;
+    if (warp >= side) return;
 #pragma unroll
-    for (int w = 0; w < kPoolWarps; ++w) sum += part[w][threadIdx.x];
-    const double mean = rows > 0 ? sum * 0x1p896 / static_cast<double>(rows) : 0.0;
-    const int head = col >> p.head_dim_log2, d = col & ((1 << p.head_dim_log2) - 1);
-    const int64_t bh = static_cast<int64_t>(b) * t.heads + head;
-    if (t.transposed) t.out[((bh << p.head_dim_log2) + d) * t.blocks + blk] = mean;
-    else t.out[((bh * t.blocks + blk) << p.head_dim_log2) + d] = mean;
+    for (int e = 0; e < 8; ++e) {
+        const int col = c + e;
+        if (!live) break;
+        double sum = 0.0;
+        for (int i = 0; i < parts; ++i) sum += part[i * side + warp][32 * e + lane];
+        const double mean = rows > 0 ? sum * 0x1p896 / static_cast<double>(rows) : 0.0;
+        const int head = col >> p.head_dim_log2, d = col & ((1 << p.head_dim_log2) - 1);
+        const int64_t bh = static_cast<int64_t>(b) * t.heads + head;
+        if (t.transposed) t.out[((bh << p.head_dim_log2) + d) * t.blocks + blk] = mean;
+        else t.out[((bh * t.blocks + blk) << p.head_dim_log2) + d] = mean;
+    }
 }
 
 struct SelectParams {
@@ -98,68 +115,112 @@ struct SelectParams {
     int32_t *blocks, *counts;
     float *scores;            // null: not asked for
     int heads, group, q_blocks, k_blocks, seq_kv, head_dim, count, keep_first;
+    int parts;                // of head_dim, summed by different warps
 };
 
-// A warp per query block: scores of all key blocks as ordered 64-bit keys in shared memory, the smallest kept key by a
-// binary search over its bits, the list by ballots.
-__global__ void select_kernel(const SelectParams p) {
-    extern __shared__ unsigned long long keys_all[];
+// A CTA takes kRows query blocks of one head (the key means are read once for all of them).  Scores: a warp takes 32 key
+// blocks, a lane per key block, and where key blocks are few a part of head_dim; the parts are added in order.  They become
+// ordered 64-bit keys in shared memory, and a warp per query block finds the smallest kept key -- by counting, for every
+// key, the keys before it where these are few, else by a binary search over the bits -- and writes the list by ballots.
+constexpr int kSelectWarps = 8;
+constexpr int kParts = 4;                  // of head_dim
+constexpr int kMaxSplit = 256;             // key blocks up to which head_dim is split: beyond, the key blocks alone occupy the warps
+constexpr int kMaxRanked = 96;             // key blocks up to which keys are counted: there it costs what 64 passes of the search do
+constexpr int kManyRows = 4;
+constexpr int kMaxShared = 1024;           // key blocks up to which a CTA takes kManyRows query blocks
+template <int kRows>
+__global__ void __launch_bounds__(32 * kSelectWarps)
+select_kernel(const SelectParams p) {
+    extern __shared__ __align__(16) double shared[];
+    double *means = shared;                                             // [head_dim][kRows]
+    double *sums = shared + p.head_dim * kRows;                         // [parts][kRows][k_blocks]; part 0 becomes the keys
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int qb = blockIdx.x * (blockDim.x >> 5) + warp, head = blockIdx.y, b = blockIdx.z;
-    if (qb >= p.q_blocks) return;
-    unsigned long long *keys = keys_all + static_cast<int64_t>(warp) * p.k_blocks;
-    ptx::grid_dependency_wait();
+    const int qb0 = blockIdx.x * kRows, head = blockIdx.y, b = blockIdx.z;
     const int valid = (valid_rows(p.kv_lens, b, p.seq_kv) + kKeyBlock - 1) / kKeyBlock;     // a prefix of the key blocks
-    const int64_t row = (static_cast<int64_t>(b) * p.heads + head) * p.q_blocks + qb;
-    const double *q = p.pq + row * p.head_dim;
+    const int64_t row0 = (static_cast<int64_t>(b) * p.heads + head) * p.q_blocks + qb0;
     const double *k = p.pk + (static_cast<int64_t>(b) * (p.heads / p.group) + head / p.group) * p.head_dim * p.k_blocks;
-    auto score_of_key = [](unsigned long long key) {
-        const unsigned long long bits = key >> 63 ? key & 0x7FFFFFFFFFFFFFFFull : ~key;
-        return __longlong_as_double(static_cast<long long>(bits));
+    auto key_of = [](double s) {
+        const unsigned long long bits = static_cast<unsigned long long>(__double_as_longlong(s + 0.0));   // -0 is 0
+        return bits >> 63 ? ~bits : bits | 0x8000000000000000ull;
     };
-    for (int j0 = 0; j0 < valid; j0 += 32) {
-        const int j = j0 + lane;
-        double s = 0.0;
-        if (j < valid) {
+    auto score_of = [](unsigned long long key) {
+        return __longlong_as_double(static_cast<long long>(key >> 63 ? key & 0x7FFFFFFFFFFFFFFFull : ~key));
+    };
+    ptx::grid_dependency_wait();
+    for (int i = threadIdx.x; i < kRows * p.head_dim; i += 32 * kSelectWarps) {
+        const int r = i / p.head_dim, d = i % p.head_dim;
+        means[d * kRows + r] = qb0 + r < p.q_blocks ? p.pq[(row0 + r) * p.head_dim + d] : 0.0;
+    }
+    __syncthreads();
+    const int depth = p.head_dim / p.parts;
+    for (int item = warp; item < (valid + 31) / 32 * p.parts; item += kSelectWarps) {
+        const int j = item / p.parts * 32 + lane, part = item % p.parts;
+        if (j >= valid) continue;
+        const double *kd = k + static_cast<int64_t>(part * depth) * p.k_blocks + j, *qd = means + part * depth * kRows;
+        double s[kRows] = {};
 #pragma unroll 8
-            for (int d = 0; d < p.head_dim; ++d) s = fma(__ldcg(q + d), __ldcg(k + static_cast<int64_t>(d) * p.k_blocks + j), s);
-            const unsigned long long bits = static_cast<unsigned long long>(__double_as_longlong(s + 0.0));   // -0 is 0
-            keys[j] = bits >> 63 ? ~bits : bits | 0x8000000000000000ull;
+        for (int d = 0; d < depth; ++d) {
+            const double kv = kd[static_cast<int64_t>(d) * p.k_blocks];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) s[r] = fma(qd[d * kRows + r], kv, s[r]);
         }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) sums[(part * kRows + r) * p.k_blocks + j] = s[r];
+    }
+    __syncthreads();
+    const int qb = qb0 + warp;
+    if (warp >= kRows || qb >= p.q_blocks) return;
+    const int64_t row = row0 + warp;
+    unsigned long long *keys = reinterpret_cast<unsigned long long *>(sums) + static_cast<int64_t>(warp) * p.k_blocks;
+    for (int j = lane; j < valid; j += 32) {
+        double s = sums[warp * p.k_blocks + j];
+        for (int i = 1; i < p.parts; ++i) s += sums[(i * kRows + warp) * p.k_blocks + j];
+        keys[j] = key_of(s);
     }
     __syncwarp();
-    const int forced = min(p.keep_first, min(valid, p.count)), wanted = min(p.count, valid);
-    // among the blocks behind the forced ones: the largest key that at least `wanted - forced` of them reach
+    const int forced = min(p.keep_first, min(valid, p.count)), wanted = min(p.count, valid), open = wanted - forced;
+    // the largest key that at least `open` of the blocks behind the forced ones reach, and how many lie above it
     unsigned long long cut = 0;
-    if (wanted < valid && wanted > forced) {
+    int above = 0;
+    if (valid > kMaxRanked && open > 0) {
         for (int bit = 63; bit >= 0; --bit) {
             const unsigned long long trial = cut | 1ull << bit;
             int reach = 0;
             for (int j0 = forced; j0 < valid; j0 += 32)
                 reach += __popc(__ballot_sync(0xFFFFFFFFu, j0 + lane < valid && keys[j0 + lane] >= trial));
-            if (reach >= wanted - forced) cut = trial;
+            if (reach >= open) cut = trial;
         }
+        for (int j0 = forced; j0 < valid; j0 += 32)
+            above += __popc(__ballot_sync(0xFFFFFFFFu, j0 + lane < valid && keys[j0 + lane] > cut));
     }
-    int above = 0;      // blocks strictly above the cut; the rest of the list are the lowest-numbered ones at it
-    for (int j0 = forced; j0 < valid; j0 += 32)
-        above += __popc(__ballot_sync(0xFFFFFFFFu, j0 + lane < valid && keys[j0 + lane] > cut));
-    int at_cut = wanted - forced - above, written = 0;
     int32_t *list = p.blocks + row * p.count;
     float *out_scores = p.scores == nullptr ? nullptr : p.scores + row * p.count;
+    const uint32_t below = (1u << lane) - 1u;
+    int written = 0, ties_left = open - above;
     for (int j0 = 0; j0 < valid; j0 += 32) {
         const int j = j0 + lane;
-        const bool behind = j < valid && j >= forced && wanted > forced;
-        const bool tie = behind && keys[j] == cut;
-        const uint32_t ties = __ballot_sync(0xFFFFFFFFu, tie), below = (1u << lane) - 1u;
-        const bool take = j < forced || (behind && keys[j] > cut) || (tie && __popc(ties & below) < at_cut);
+        bool take = j < forced, tie = false;
+        if (j >= forced && j < valid && open > 0) {
+            const unsigned long long mine = keys[j];
+            if (valid <= kMaxRanked) {
+                int before = 0;
+                for (int i = forced; i < valid; ++i) before += keys[i] > mine || (keys[i] == mine && i < j);
+                take = before < open;
+            } else {
+                take = mine > cut;
+                tie = mine == cut;
+            }
+        }
+        const uint32_t ties = __ballot_sync(0xFFFFFFFFu, tie);      // taken from the lowest, as far as there is room
+        take = take || (tie && __popc(ties & below) < ties_left);
+        ties_left -= min(max(ties_left, 0), __popc(ties));
         const uint32_t taken = __ballot_sync(0xFFFFFFFFu, take);
         if (take) {
             const int at = written + __popc(taken & below);
             list[at] = j;
-            if (out_scores != nullptr) out_scores[at] = static_cast<float>(score_of_key(keys[j]));
+            if (out_scores != nullptr) out_scores[at] = static_cast<float>(score_of(keys[j]));
         }
         written += __popc(taken);
-        at_cut -= min(at_cut, __popc(ties));
     }
     for (int i = written + lane; i < p.count; i += 32) {
         list[i] = -1;
@@ -168,8 +229,34 @@ __global__ void select_kernel(const SelectParams p) {
     if (lane == 0) p.counts[row] = written;
 }
 
-constexpr int kSelectWarps = 4;
-constexpr int kMaxSelectSmem = kMaxKeyBlocks * 8;
+size_t select_smem(int rows, int parts, int64_t head_dim, int nk) { return sizeof(double) * rows * (head_dim + static_cast<size_t>(parts) * nk); }
+constexpr int kMaxSelectSmem = 8 * (128 + kMaxKeyBlocks);      // one row over the most key blocks
+
+template <int kRows>
+sol_status_t launch_scores(const SelectParams &p, int64_t batch, cudaStream_t stream) {
+    static bool configured[64] = {};
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SOL_ERR_CUDA;
+    if (!configured[dev]) {
+        if (cudaFuncSetAttribute(select_kernel<kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSelectSmem) != cudaSuccess) return SOL_ERR_CUDA;
+        configured[dev] = true;
+    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(ceil_div(p.q_blocks, kRows)), static_cast<unsigned>(p.heads), static_cast<unsigned>(batch));
+    cfg.blockDim = dim3(32 * kSelectWarps);
+    cfg.dynamicSmemBytes = select_smem(kRows, p.parts, p.head_dim, p.k_blocks);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, select_kernel<kRows>, p) != cudaSuccess) {
+        cudaGetLastError();
+        return SOL_ERR_CUDA;
+    }
+    return launch_status();
+}
 
 }  // namespace
 
@@ -184,9 +271,9 @@ sol_status_t launch_select(const void *q, const void *k, int64_t batch, int64_t 
     double *pq = static_cast<double *>(workspace), *pk = pq + batch * heads * nq * head_dim;
     PoolParams pool{};
     pool.q = PoolTensor{static_cast<const uint16_t *>(q), pq, nullptr, ld_q, seq_q * ld_q, static_cast<int>(seq_q), static_cast<int>(heads), nq,
-                        kQueryBlock, static_cast<int>(ceil_div(heads * head_dim, kPoolColumns)), false};
+                        kQueryBlock, static_cast<int>(ceil_div(heads * head_dim, kWarpColumns * kPoolWarps * kWarpRows / kQueryBlock)), false};
     pool.k = PoolTensor{static_cast<const uint16_t *>(k), pk, kv_lens, ld_k, seq_kv * ld_k, static_cast<int>(seq_kv), static_cast<int>(heads_kv), nk,
-                        kKeyBlock, static_cast<int>(ceil_div(heads_kv * head_dim, kPoolColumns)), true};
+                        kKeyBlock, static_cast<int>(ceil_div(heads_kv * head_dim, kWarpColumns * kPoolWarps * kWarpRows / kKeyBlock)), true};
     pool.q_ctas = nq * pool.q.column_chunks;
     pool.head_dim_log2 = head_dim == 128 ? 7 : 6;
     const int64_t ctas = pool.q_ctas + static_cast<int64_t>(nk) * pool.k.column_chunks;
@@ -210,30 +297,8 @@ sol_status_t launch_select(const void *q, const void *k, int64_t batch, int64_t 
     p.head_dim = static_cast<int>(head_dim);
     p.count = static_cast<int>(count);
     p.keep_first = static_cast<int>(keep_first);
-    // several query blocks per CTA share the key means in L1 as long as their keys leave room for more CTAs
-    const int warps = nk <= 512 ? kSelectWarps : 1;
-    static bool configured[64] = {};
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SOL_ERR_CUDA;
-    if (!configured[dev]) {
-        if (cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSelectSmem) != cudaSuccess) return SOL_ERR_CUDA;
-        configured[dev] = true;
-    }
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(ceil_div(nq, warps)), static_cast<unsigned>(heads), static_cast<unsigned>(batch));
-    cfg.blockDim = dim3(static_cast<unsigned>(32 * warps));
-    cfg.dynamicSmemBytes = static_cast<size_t>(warps) * nk * sizeof(double);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, select_kernel, static_cast<const SelectParams &>(p)) != cudaSuccess) {
-        cudaGetLastError();
-        return SOL_ERR_CUDA;
-    }
-    return launch_status();
+    p.parts = nk <= kMaxSplit ? kParts : 1;
+    return nk <= kMaxShared ? launch_scores<kManyRows>(p, batch, stream) : launch_scores<1>(p, batch, stream);
 }
 
 }  // namespace blocks
