@@ -134,6 +134,15 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     const int q0 = q_in_a ? q0_joint : q0_joint - p.q_split;                 // row within its stream
     const int q_rows = q_in_a ? p.q_split : p.seq_q - p.q_split;             // rows of that stream
 
+    auto load_q = [&]() {
+        ptx::mbar_arrive_expect_tx(bar(kQFull), kQTiles * kTile);
+#pragma unroll
+        for (int t = 0; t < kQTiles; ++t) {
+#pragma unroll
+            for (int bx = 0; bx < kBoxes; ++bx)
+                ptx::tma_load_3d(sQ + t * kTile + bx * kBox, tm_q, head * kD + 64 * bx, q0 + t * kBQ, batch, bar(kQFull));
+        }
+    };
     if (threadIdx.x == 0) {
         for (int i = 0; i < kNumBars; ++i) ptx::mbar_init(bar(i), (i == kPFull || i == kPFull + 1) ? 4 : 1);
         *abort_flag = 0;
@@ -142,15 +151,18 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         ptx::prefetch_tmap(tm_o);
         ptx::prefetch_tmap(&tm_kb);
         ptx::prefetch_tmap(&tm_vb);
+        if (kListed) load_q();        // the list takes a while: Q need not wait for it
     }
     if (kListed && warp == 2) {   // the entries that name existing keys, in their order
         const int64_t row = (static_cast<int64_t>(batch) * gridDim.y + head) * gridDim.x + blockIdx.x;
         const int32_t *from = p.blocks + row * p.max_blocks;
+        int next = lane < p.max_blocks ? __ldg(from + lane) : -1;       // not after the count: one latency, not two
         const int named = min(max(__ldg(p.counts + row), 0), p.max_blocks);
         const int existing = (kv_len + kBKV - 1) / kBKV;
         int kept = 0;
         for (int i0 = 0; i0 < named; i0 += 32) {
-            const int e = i0 + lane < named ? __ldg(from + i0 + lane) : -1;
+            const int e = i0 + lane < named ? next : -1;
+            if (i0 + 32 + lane < named) next = __ldg(from + i0 + 32 + lane);
             const bool keep = e >= 0 && e < existing;
             const uint32_t mask = __ballot_sync(0xFFFFFFFFu, keep);
             if (keep) list[kept + __popc(mask & ((1u << lane) - 1u))] = static_cast<uint16_t>(e);
@@ -173,13 +185,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         // ------------------------------------------------------------ TMA producer
         if (ptx::elect_one()) {
             const int x0 = head * kD, x0_kv = kListed ? head / p.group * kD : x0;
-            ptx::mbar_arrive_expect_tx(bar(kQFull), kQTiles * kTile);
-#pragma unroll
-            for (int t = 0; t < kQTiles; ++t) {
-#pragma unroll
-                for (int bx = 0; bx < kBoxes; ++bx)
-                    ptx::tma_load_3d(sQ + t * kTile + bx * kBox, tm_q, x0 + 64 * bx, q0 + t * kBQ, batch, bar(kQFull));
-            }
+            if (!kListed) load_q();
             for (int j = 0; j < n_tiles; ++j) {
                 const int st = j & 1;
                 const uint32_t par = static_cast<uint32_t>(j >> 1) & 1u;
