@@ -151,7 +151,10 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         ptx::prefetch_tmap(tm_o);
         ptx::prefetch_tmap(&tm_kb);
         ptx::prefetch_tmap(&tm_vb);
-        if (kListed) load_q();        // the list takes a while: Q need not wait for it
+        if (kListed) {                // the list takes a while: Q need not wait for it
+            ptx::fence_proxy_async_smem();
+            load_q();
+        }
     }
     if (kListed && warp == 2) {   // the entries that name existing keys, in their order
         const int64_t row = (static_cast<int64_t>(batch) * gridDim.y + head) * gridDim.x + blockIdx.x;
