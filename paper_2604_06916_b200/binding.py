@@ -161,7 +161,7 @@ _guarding = False        # inside a guarded call
 
 
 def guard_mode() -> bool:
-    return os.environ.get("SOL_NVFP4_GUARD", "0") not in ("", "0")
+    return "SOL_NVFP4_GUARD" in os.environ and os.environ["SOL_NVFP4_GUARD"] not in ("", "0")
 
 
 def _empty(shape, dtype, device) -> torch.Tensor:
@@ -215,16 +215,21 @@ def _guarded(fn):
 
 def _on_device_of_first(fn):
     """Run `fn` with the device of its first argument current: its launches, its outputs and its stream (the
-    current one of that device) are then that device's, whichever device the caller has current."""
+    current one of that device) are then that device's, whichever device the caller has current.  The guard bands are
+    checked here as well, in one wrapper: these calls are a few microseconds of GPU work at their smallest."""
+    guarded = _guarded(fn)
+
     @functools.wraps(fn)
     def call(first, *args, **kwargs):
         index = first.get_device()
         if index < 0:
             raise TypeError(f"{fn.__name__}: expected CUDA tensors")
+        run = guarded if guard_mode() else fn
         if index == torch._C._cuda_getDevice():
-            return fn(first, *args, **kwargs)
+            return run(first, *args, **kwargs)
         with torch.cuda.device(first.device):
-            return fn(first, *args, **kwargs)
+            return run(first, *args, **kwargs)
+    call._guards_itself = True
     return call
 
 
@@ -633,19 +638,24 @@ def rotary_frequencies(axis_dims, theta: float = 10000.0, scaling: str = "none",
     return torch.tensor(parts, dtype=torch.float64, device=device), scale.value
 
 
-def _head_view(name: str, t: torch.Tensor, shape, index: int) -> int:
-    """Checks a BF16 view of the given [B, S, H, D] on CUDA device `index` and returns its token pitch."""
+def _head_pitch(name: str, t: torch.Tensor, index: int) -> int:
+    """Checks a BF16 view [B, S, H, D] on CUDA device `index` and returns its token pitch."""
     if t.dtype is not torch.bfloat16 or t.dim() != 4:
         raise TypeError(f"{name}: expected a [B, S, H, D] bf16 tensor")
-    if t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.get_device() != index:
         raise ValueError(f"{name} is on {t.device}, the call's first tensor on cuda:{index}")
-    b, s, h, d = shape
-    st = t.stride()
-    if st[3] != 1 or (h > 1 and st[2] != d) or (b > 1 and s > 1 and st[0] != s * st[1]):
+    b, s, h, d = t.shape
+    sb, ss, sh, sd = t.stride()
+    if sd != 1 or (sh != d and h > 1) or (b > 1 and s > 1 and sb != s * ss):
         raise ValueError(f"{name}: heads and head dimension must be contiguous, batches stacked densely")
-    return st[1] if s > 1 else (st[0] if b > 1 else h * d)
+    return ss if s > 1 else (sb if b > 1 else h * d)
+
+
+def _head_view(name: str, t: torch.Tensor, shape, index: int) -> int:
+    """The same for a view that must have the given shape."""
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return _head_pitch(name, t, index)
 
 
 def _rotary_of(positions, freqs, axis_dims, layout, scale, rows: int, index: int):
@@ -677,17 +687,6 @@ def _norm_weight(name: str, w, d: int, index: int) -> int:
     return w.data_ptr()
 
 
-def _beside(name: str, x, of: str, like):
-    """`like`'s [B, S, ., D] with x's own number of heads."""
-    if like.dim() != 4 or x.dim() != 4:
-        raise TypeError(f"{of} and {name}: expected [B, S, H, D] bf16 tensors")
-    b, s, _, d = like.shape
-    want = (b, s, x.shape[2], d)
-    if x.shape != want:
-        raise ValueError(f"{name} must share {of}'s batch, tokens and head dimension")
-    return want
-
-
 @_on_device_of_first
 def sol_qk_rotary(q, k, positions, freqs, axis_dims=None, layout: int = ROTARY_INTERLEAVED, q_weight=None, k_weight=None,
                   eps: float = 1e-6, scale: float = 1.0, out=None):
@@ -699,18 +698,27 @@ def sol_qk_rotary(q, k, positions, freqs, axis_dims=None, layout: int = ROTARY_I
     `out` = (q_out, k_out) supplies the destinations, which may be q and k themselves.
     """
     index = q.get_device()
-    b, s, h, d = shape = _beside("q", q, "q", q)
-    rot = _rotary_of(positions, freqs, axis_dims, layout, scale, b * s, index)
-    oq = _like(q) if out is None else out[0]
-    pq = _HEAD_TENSOR.pack(q.data_ptr(), oq.data_ptr(), _norm_weight("q_weight", q_weight, d, index), h,
-                           _head_view("q", q, shape, index), _head_view("q_out", oq, shape, index))
+    ld = _head_pitch("q", q, index)
+    b, s, h, d = q.shape
+    rows = b * s
+    rot = _rotary_of(positions, freqs, axis_dims, layout, scale, rows, index)
+    if out is None:
+        oq, ld_out = _like(q), h * d
+    else:
+        oq, ld_out = out[0], _head_view("q_out", out[0], q.shape, index)
+    pq = _HEAD_TENSOR.pack(q.data_ptr(), oq.data_ptr(), _norm_weight("q_weight", q_weight, d, index), h, ld, ld_out)
     ok = pk = None
     if k is not None:
-        shape = _beside("k", k, "q", q)
-        ok = _like(k) if out is None else out[1]
-        pk = _HEAD_TENSOR.pack(k.data_ptr(), ok.data_ptr(), _norm_weight("k_weight", k_weight, d, index), shape[2],
-                               _head_view("k", k, shape, index), _head_view("k_out", ok, shape, index))
-    code = lib().sol_qk_rotary(pq, pk, b * s, d, rot, eps, _raw_stream(index))
+        ld = _head_pitch("k", k, index)
+        bk, sk, hk, dk = k.shape
+        if bk != b or sk != s or dk != d:
+            raise ValueError("k must share q's batch, tokens and head dimension")
+        if out is None:
+            ok, ld_out = _like(k), hk * d
+        else:
+            ok, ld_out = out[1], _head_view("k_out", out[1], k.shape, index)
+        pk = _HEAD_TENSOR.pack(k.data_ptr(), ok.data_ptr(), _norm_weight("k_weight", k_weight, d, index), hk, ld, ld_out)
+    code = lib().sol_qk_rotary(pq, pk, rows, d, rot, eps, _raw_stream(index))
     if code:
         raise SolError(code, "sol_qk_rotary")
     return oq, ok
@@ -727,24 +735,31 @@ def sol_qk_rotary_backward(dq, dk, q, k, positions, freqs, axis_dims=None, layou
     dq and dk themselves.
     """
     index = dq.get_device()
-    b, s, _, d = _beside("dq", dq, "dq", dq)
+    ld = _head_pitch("dq", dq, index)
+    b, s, _, d = dq.shape
     rot = _rotary_of(positions, freqs, axis_dims, layout, scale, b * s, index)
     packed, dxs, dws = [None, None], [None, None], [None, None]
-    for i, (name, dy, x, w) in enumerate((("q", dq, q, q_weight), ("k", dk, k, k_weight))):
+    for i, name, dy, x, w in ((0, "q", dq, q, q_weight), (1, "k", dk, k, k_weight)):
         if dy is None:
             continue
-        shape = _beside("d" + name, dy, "dq", dq)
+        if i:
+            ld = _head_pitch("dk", dy, index)
+            if dy.shape[0] != b or dy.shape[1] != s or dy.shape[3] != d:
+                raise ValueError("dk must share dq's batch, tokens and head dimension")
+        h = dy.shape[2]
         weight = _norm_weight(name + "_weight", w, d, index)
         x_ptr = ld_x = dw_ptr = 0
         if weight:
             if x is None:
                 raise ValueError(f"{name}: the gradient of a norm needs the forward input")
-            ld_x, x_ptr = _head_view(name, x, shape, index), x.data_ptr()
+            ld_x, x_ptr = _head_view(name, x, dy.shape, index), x.data_ptr()
             dws[i] = _new(dy, d, torch.float32)
             dw_ptr = dws[i].data_ptr()
-        dx = dxs[i] = _like(dy) if out is None else out[i]
-        packed[i] = _HEAD_GRAD.pack(dy.data_ptr(), x_ptr, dx.data_ptr(), weight, dw_ptr, shape[2],
-                                    _head_view("d" + name, dy, shape, index), ld_x, _head_view(name + "_grad", dx, shape, index))
+        if out is None:
+            dxs[i], ld_dx = _like(dy), h * d
+        else:
+            dxs[i], ld_dx = out[i], _head_view(name + "_grad", out[i], dy.shape, index)
+        packed[i] = _HEAD_GRAD.pack(dy.data_ptr(), x_ptr, dxs[i].data_ptr(), weight, dw_ptr, h, ld, ld_x, ld_dx)
     ws_ptr = ws_bytes = 0
     if dws[0] is not None or dws[1] is not None:
         if workspace is None:
@@ -763,13 +778,12 @@ QUERY_BLOCK, KEY_BLOCK = 256, 128
 
 def _kv_of(q, k, index: int):
     """Shapes of q [B, Sq, H, D] and k [B, Skv, Hk, D] and their token pitches."""
-    if q.dim() != 4 or k.dim() != 4:
-        raise TypeError("q and k: expected [B, S, H, D] bf16 tensors")
+    ld_q, ld_k = _head_pitch("q", q, index), _head_pitch("k", k, index)
     B_, Sq, H, D = q.shape
     b, Skv, Hk, d = k.shape
     if b != B_ or d != D or Hk == 0 or H % Hk != 0:
         raise ValueError("k must share q's batch and head dimension, and its heads must divide q's")
-    return B_, Sq, Skv, H, Hk, D, _head_view("q", q, q.shape, index), _head_view("k", k, k.shape, index)
+    return B_, Sq, Skv, H, Hk, D, ld_q, ld_k
 
 
 def _lens_ptr(kv_lens, B_: int, index: int) -> int | None:
@@ -827,9 +841,11 @@ def sol_attention_blocks(q, k, v, blocks, counts, kv_lens=None, out: torch.Tenso
     if counts.dtype is not torch.int32 or counts.shape != (B_, H, nq) or not counts.is_contiguous() or counts.get_device() != index:
         raise TypeError("counts: expected a dense [B, H, ceil(Sq / 256)] int32 tensor on q's device")
     if out is None:
-        out = _like(q)
+        out, ld_out = _like(q), H * D
+    else:
+        ld_out = _head_view("out", out, q.shape, index)
     code = lib().sol_attention_blocks(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), B_, Sq, Skv, H, Hk, D, ld_q, ld_k, ld_v,
-                                      _head_view("out", out, q.shape, index), blocks.data_ptr(), counts.data_ptr(), blocks.shape[3],
+                                      ld_out, blocks.data_ptr(), counts.data_ptr(), blocks.shape[3],
                                       _lens_ptr(kv_lens, B_, index), _raw_stream(index))
     if code:
         raise SolError(code, "sol_attention_blocks")
@@ -1032,6 +1048,6 @@ def sol_test_hold_loads(on: bool) -> None:
 # every public entry checks the guard bands of what it allocated (a no-op outside guard mode)
 for _name, _fn in list(globals().items()):
     if (isinstance(_fn, types.FunctionType) and _fn.__module__ == __name__ and not _name.startswith("_")
-            and _name not in ("lib", "guard_mode", "check_guards", "status_string")):
+            and _name not in ("lib", "guard_mode", "check_guards", "status_string") and not hasattr(_fn, "_guards_itself")):
         globals()[_name] = _guarded(_fn)
 del _name, _fn
