@@ -331,10 +331,11 @@ sol_status_t sol_attention_blocks(const void *q, const void *k, const void *v, v
  *               SOL_SF_SWIZZLED_128x4;  w_tscale one float (device);  bias_bf16 [N] or NULL;  y_bf16 [M, N], pitch ldy
  *   activation  applied to x: SOL_ACT_NONE or SOL_ACT_SILU (x / (1 + exp(-x)), FP32), SOL_ERR_BAD_LAYOUT otherwise
  *   workspace   device scratch of at least sol_matvec_workspace_bytes(M, K) bytes, 256-byte aligned; holds x in the
- *               products' layout; contents undefined after.  Two calls that may overlap need one each.
+ *               products' layout; contents undefined after.  Two calls that may overlap need one each.  The size is 0, and
+ *               NULL will do, for up to four rows of up to 3072 columns, which every block prepares for itself
  *   M >= 1 (the weight is read once per 64 rows), N % 8 == 0, K % 32 == 0
- * Two launches.  Sums are FP32 and in a fixed order.  Before the product act(x) is scaled by a power of two per row and
- * held in FP16: BF16 values down to 2^-29 of the row's largest are kept exactly (an activation's result to 11 bits).
+ * Two launches, one where no workspace is needed.  Sums are FP32 and in a fixed order.  Before the product act(x) is
+ * scaled by a power of two per row (and slice of K) and held in FP16: BF16 values down to 2^-29 of the row's largest are kept exactly (an activation's result to 11 bits).
  */
 size_t sol_matvec_workspace_bytes(int64_t M, int64_t K);
 sol_status_t nvfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf, const float *w_tscale,

@@ -572,12 +572,17 @@ def _matvec(entry, name: str, x, wq, wsf, w_tscale, bias, activation: int, out, 
         raise TypeError("out: expected a [M, N] bf16 tensor with contiguous rows on x's device")
     else:
         ldy = out.stride(0) if M > 1 else N      # a single row has no pitch of its own
+    ws_ptr, ws_bytes = None, 0
     if workspace is None:
-        workspace = _new(wq, max(1, lib().sol_matvec_workspace_bytes(M, K)))
+        ws_bytes = lib().sol_matvec_workspace_bytes(M, K)
+        if ws_bytes:
+            workspace = _new(wq, ws_bytes)
+            ws_ptr = workspace.data_ptr()
     elif not workspace.is_contiguous() or workspace.get_device() != index:
         raise TypeError("workspace: expected a dense tensor on x's device")
-    tail = (None if bias is None else bias.data_ptr(), activation, out.data_ptr(), ldy, M, N, K, workspace.data_ptr(),
-            workspace.nbytes, _raw_stream(index))
+    else:
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.nbytes
+    tail = (None if bias is None else bias.data_ptr(), activation, out.data_ptr(), ldy, M, N, K, ws_ptr, ws_bytes, _raw_stream(index))
     ldx = x.stride(0) if M > 1 else K
     if w_tscale is None:
         code = entry(x.data_ptr(), ldx, wq.data_ptr(), wsf.data_ptr(), *tail)

@@ -699,13 +699,15 @@ bool matvec_shape_ok(int64_t M, int64_t K) { return shape_ok(M, K) && M <= (1LL 
 sol_status_t matvec_entry(const void *x, int64_t ldx, const void *wq, const void *wsf, const float *wts, const void *bias,
                           sol_activation_t act, void *y, int64_t ldy, int64_t M, int64_t N, int64_t K, void *workspace,
                           size_t workspace_bytes, void *stream) {
-    if (x == nullptr || wq == nullptr || wsf == nullptr || y == nullptr || workspace == nullptr) return SOL_ERR_NULL_POINTER;
+    if (x == nullptr || wq == nullptr || wsf == nullptr || y == nullptr) return SOL_ERR_NULL_POINTER;
     if (act != SOL_ACT_NONE && act != SOL_ACT_SILU) return SOL_ERR_BAD_LAYOUT;
     if (!matvec_shape_ok(M, K) || !shape_ok(N, K) || N > (1LL << 22) || N % 8 != 0 || ldx < K || ldy < N) return SOL_ERR_BAD_SHAPE;
     if (!aligned16(x) || !aligned16(wq) || !aligned16(wsf) || !aligned16(y) || !aligned16(bias) || ldx % 8 != 0 || ldy % 8 != 0 ||
         (reinterpret_cast<uintptr_t>(wts) & 3u) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
         return SOL_ERR_ALIGNMENT;
-    if (workspace_bytes < matvec::workspace_bytes(M, K)) return SOL_ERR_WORKSPACE_TOO_SMALL;
+    const size_t need = matvec::workspace_bytes(M, K);
+    if (need > 0 && workspace == nullptr) return SOL_ERR_NULL_POINTER;
+    if (workspace_bytes < need) return SOL_ERR_WORKSPACE_TOO_SMALL;
     const DeviceInfo *dev = nullptr;
     const sol_status_t st = check_arch(&dev);
     if (st != SOL_OK) return st;

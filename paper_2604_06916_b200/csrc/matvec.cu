@@ -48,9 +48,12 @@ constexpr uint32_t kColA = 0, kColABuf = 128, kColD = 256;   // A: two buffers o
 constexpr int kSums = 4;             // sums that products take in turn: one alone would wait for itself
 constexpr int kFull = 0, kXFull = kFull + kMaxStages, kEmpty = kXFull + kMaxStages, kAFull = kEmpty + kMaxStages, kAEmpty = kAFull + 2,
               kDone = kAEmpty + 2, kBars = kDone + 1;
-constexpr int kMaxSmem = 232448 - 1024;   // dynamic, beside row_most
+constexpr int kMaxSmem = 232448 - 1024;   // dynamic, beside the static arrays
 
 struct Params {
+    const uint16_t *x;       // few rows: prepared by every CTA for its slice (kInline)
+    int64_t ldx;
+    int K, act;
     const uint8_t *ximage;   // FP16 x: [row chunk][64 columns of K][x_rows][128 bytes, 128-byte swizzle], K padded to stages
     const float *x_back;     // per row: what undoes its scaling
     const uint8_t *wsf;
@@ -68,9 +71,14 @@ struct Params {
 
 __host__ __device__ constexpr int stage_x_bytes(int x_rows) { return x_rows * (2 * kStageK); }
 // Shared memory: the code ring, the x ring, the scale ring, the cluster's partial sums [rank][x row][own columns], barriers.
-__host__ __device__ constexpr int smem_bytes(int x_rows, int ring) {
-    return ring * (kCodeBytes + kSfBytes + stage_x_bytes(x_rows)) + x_rows * kRows * 4 + 8 * kBars + 16;
+// `x_stages`: stages of x held at once, the ring's or (kInline) the slice's.
+__host__ __device__ constexpr int smem_bytes(int x_rows, int ring, int x_stages) {
+    return ring * (kCodeBytes + kSfBytes) + x_stages * stage_x_bytes(x_rows) + x_rows * kRows * 4 + 8 * kBars + 16;
 }
+constexpr int kXWarps = kConvWarps / 2;   // warps that prepare x there
+constexpr int kInlineRows = 4;       // rows of x up to which every CTA prepares its slice itself, in one launch
+constexpr int kInlineStages = 12;    // ... of K up to so many stages
+constexpr bool prepared_inline(int64_t M, int64_t K) { return M <= kInlineRows && K <= kInlineStages * kStageK; }
 
 __device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t s, uint32_t *h) {
     asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t.reg .b32 t0, t1, t2, t3;\n\t"
@@ -102,6 +110,9 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
     return v;
 }
+__device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 __device__ __forceinline__ void st_cluster(uint32_t cluster_addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
 }
@@ -132,6 +143,30 @@ __device__ __forceinline__ void activate8(uint4 r, int act, float (&f)[8]) {
     }
 }
 
+// 2^(kXExp - e) with e the exponent of the largest element (FP32 bits), held to what FP32 can scale by; and its inverse.
+__device__ __forceinline__ float scale_up(uint32_t bits) {
+    return __uint_as_float(static_cast<uint32_t>(127 + kXExp - min(max(static_cast<int>(bits >> 23) - 127, -100), 127)) << 23);
+}
+__device__ __forceinline__ float scale_back(uint32_t bits) {
+    return bits ? __uint_as_float(static_cast<uint32_t>(127 - kXExp + min(max(static_cast<int>(bits >> 23) - 127, -100), 127)) << 23) : 0.0f;
+}
+__device__ __forceinline__ float largest8(const float (&v)[8], float most) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
+    return most;
+}
+__device__ __forceinline__ uint4 to_half8(const float (&v)[8], float up) {
+    uint32_t h[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const __half2 pair = __floats2half2_rn(v[2 * q] * up, v[2 * q + 1] * up);
+        h[q] = *reinterpret_cast<const uint32_t *>(&pair);
+    }
+    return make_uint4(h[0], h[1], h[2], h[3]);
+}
+// Place of eight columns (chunk c of the slice) of row r in the image: a box of [x_rows][128 bytes] per 64 columns.
+__device__ __forceinline__ int image_offset(int c, int r, int x_rows) { return (c >> 3) * (x_rows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
+
 // x -> scaled FP16 in the products' layout.  A block per row (rows behind the last are zeros), a thread per eight columns.
 constexpr int kPrepThreads = 512;
 __global__ void __launch_bounds__(kPrepThreads)
@@ -148,34 +183,21 @@ prepare_x(const uint16_t *__restrict__ x, int64_t ldx, int M, int K, int x_rows,
     for (int j = 0; j < kHeld; ++j) {
         const int c = threadIdx.x + j * kPrepThreads;
         activate8(m < M && c < live ? __ldg(reinterpret_cast<const uint4 *>(row + 8 * c)) : zero, act, f[j]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(f[j][e]));
+        most = largest8(f[j], most);
     }
     for (int c = threadIdx.x + kHeld * kPrepThreads; c < live; c += kPrepThreads) {
         float v[8];
         activate8(m < M ? __ldg(reinterpret_cast<const uint4 *>(row + 8 * c)) : zero, act, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
+        most = largest8(v, most);
     }
     uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
     if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = bits;
     __syncthreads();
     bits = __reduce_max_sync(0xFFFFFFFFu, warp_max[threadIdx.x & (kPrepThreads / 32 - 1)]);
-    // 2^(kXExp - e) with e the exponent of the largest element, held to what FP32 can scale by
-    const int e = min(max(static_cast<int>(bits >> 23) - 127, -100), 127);
-    const float up = __uint_as_float(static_cast<uint32_t>(127 + kXExp - e) << 23);
-    if (threadIdx.x == 0) x_back[m] = bits ? __uint_as_float(static_cast<uint32_t>(127 - kXExp + e) << 23) : 0.0f;
-    const int r = m % x_rows;
-    uint8_t *to = image + static_cast<int64_t>(m / x_rows) * (4 * stages) * (x_rows * 128) + r * 128;
-    auto put = [&](int c, const float (&v)[8]) {
-        uint32_t h[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const __half2 pair = __floats2half2_rn(v[2 * q] * up, v[2 * q + 1] * up);
-            h[q] = *reinterpret_cast<const uint32_t *>(&pair);
-        }
-        *reinterpret_cast<uint4 *>(to + static_cast<int64_t>(c >> 3) * (x_rows * 128) + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-    };
+    const float up = scale_up(bits);
+    if (threadIdx.x == 0) x_back[m] = scale_back(bits);
+    uint8_t *to = image + static_cast<int64_t>(m / x_rows) * (4 * stages) * (x_rows * 128);
+    auto put = [&](int c, const float (&v)[8]) { *reinterpret_cast<uint4 *>(to + image_offset(c, m % x_rows, x_rows)) = to_half8(v, up); };
 #pragma unroll
     for (int j = 0; j < kHeld; ++j)
         if (threadIdx.x + j * kPrepThreads < chunks) put(threadIdx.x + j * kPrepThreads, f[j]);
@@ -186,16 +208,17 @@ prepare_x(const uint16_t *__restrict__ x, int64_t ldx, int M, int K, int x_rows,
     }
 }
 
-template <bool kMx>
+template <bool kMx, bool kInline>
 __global__ void __launch_bounds__(kThreads, 1)
 matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     constexpr int kChunksPerStage = kMx ? 2 : 4;      // 512-byte scale chunks of a stage
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ uint8_t row_most[kMx ? 4 : 1][kRows];
     __shared__ float back[kMaxXRows];
+    __shared__ uint32_t warp_most[kXWarps];
     const uint32_t base = ptx::smem_u32(smem_raw);
     const uint32_t x_bytes = static_cast<uint32_t>(stage_x_bytes(p.x_rows));
-    const uint32_t s_code = base, s_x = s_code + p.ring * kCodeBytes, s_sf = s_x + p.ring * x_bytes;
+    const uint32_t s_code = base, s_x = s_code + p.ring * kCodeBytes, s_sf = s_x + (kInline ? p.per_cta : p.ring) * x_bytes;
     const uint32_t s_part = s_sf + p.ring * kSfBytes, bar_base = s_part + p.x_rows * kRows * 4;
     uint8_t *bar_gen = smem_raw + (bar_base - base);
     const float *part = reinterpret_cast<const float *>(smem_raw + (s_part - base));
@@ -223,12 +246,25 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
         ptx::bulk_load_1d(s_x + st * x_bytes, p.ximage + (static_cast<int64_t>(blockIdx.z) * p.stages + stage0 + s) * x_bytes, x_bytes, bar(kXFull + st));
     };
     const int first = min(stages, p.ring);
+    // few rows of x: the second half of the converting warps prepares them; their loads go out ahead of the codes'
+    constexpr int kHeld = kInlineStages * (kStageK / 8) * kInlineRows / (32 * kXWarps);
+    const int me = warp - kConvWarps / 2;
+    const int per_row = kXWarps >> (p.M > 2 ? 2 : p.M - 1), m = me / per_row;     // warps of a row: 8, 4 or 2
+    const int chunks = stages * (kStageK / 8), live = min(chunks, (p.K - stage0 * kStageK) / 8), step = 32 * per_row;
+    const int at = (me % per_row) * 32 + lane, id = me * 32 + lane;
+    uint4 raw[kInline ? kHeld : 1];
+    if (kInline && me >= 0 && me < kXWarps) {
+        const uint16_t *xrow = p.x + m * p.ldx + stage0 * kStageK;
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+            raw[j] = m < p.M && at + j * step < live ? __ldg(reinterpret_cast<const uint4 *>(xrow + 8 * (at + j * step))) : make_uint4(0, 0, 0, 0);
+    }
     if (warp == kProducer && aligned) {
         if (ptx::elect_one()) {
             ptx::prefetch_tmap(&tm_w);
             for (int i = 0; i < p.ring; ++i) {
                 ptx::mbar_init(bar(kFull + i), 1);
-                ptx::mbar_init(bar(kXFull + i), 1);
+                ptx::mbar_init(bar(kXFull + i), kInline ? kXWarps : 1);
                 ptx::mbar_init(bar(kEmpty + i), 1);
             }
             for (int i = 0; i < 2; ++i) {
@@ -272,12 +308,14 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     } else if (warp == kProducer) {
         // ------------------------------------------------------------ loads
         if (ptx::elect_one()) {
-            ptx::grid_dependency_wait();       // x is prepared
-            for (int s = 0; s < first; ++s) load_x(s);
+            if (!kInline) {
+                ptx::grid_dependency_wait();       // x is prepared
+                for (int s = 0; s < first; ++s) load_x(s);
+            }
             for (int s = first; s < stages; ++s) {
                 if (!wait_bounded(bar(kEmpty + s % p.ring), static_cast<uint32_t>(s / p.ring - 1) & 1u, abort_flag, p.status, 0xC10u)) break;
                 load_codes(s);
-                load_x(s);
+                if (!kInline) load_x(s);
             }
         }
         __syncwarp();
@@ -288,13 +326,13 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
             bool ok = true;
             for (int s = 0; s < stages; ++s) {
                 const int st = s % p.ring, buf = s & 1;
-                ok = wait_bounded(bar(kXFull + st), static_cast<uint32_t>(s / p.ring) & 1u, abort_flag, p.status, 0xC20u) &&
+                ok = wait_bounded(bar(kXFull + (kInline ? 0 : st)), kInline ? 0u : static_cast<uint32_t>(s / p.ring) & 1u, abort_flag, p.status, 0xC20u) &&
                      wait_bounded(bar(kAFull + buf), static_cast<uint32_t>(s >> 1) & 1u, abort_flag, p.status, 0xC21u);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const uint64_t b = ptx::smem_desc_sw128(s_x + st * x_bytes + (i >> 2) * (p.x_rows * 128)) + 2u * (i & 3);
+                    const uint64_t b = ptx::smem_desc_sw128(s_x + (kInline ? s : st) * x_bytes + (i >> 2) * (p.x_rows * 128)) + 2u * (i & 3);
                     ptx::mma_bf16_a_tmem(tmem + kColD + (i % kSums) * kMaxXRows, tmem + kColA + buf * kColABuf + 8 * i, b, idesc, s > 0 || i >= kSums);
                 }
                 ptx::tc_commit(bar(kAEmpty + buf));
@@ -310,6 +348,36 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t t_a = tmem + kColA + odd * kColABuf + half * (kColABuf / 2) + lanes;
         bool ok = true;
+        if (kInline && odd) {
+            // this slice of x, while the other two warpgroups convert the first stage: the warps of a row find its largest
+            // element, every thread scales and places its columns
+            for (int i = id; i < chunks * (p.x_rows - kInlineRows); i += 32 * kXWarps)      // rows that never exist
+                sts128(s_x + image_offset(i / (p.x_rows - kInlineRows), kInlineRows + i % (p.x_rows - kInlineRows), p.x_rows), make_uint4(0, 0, 0, 0));
+            float f[8], most = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                if (j * step >= live) break;
+                activate8(raw[j], p.act, f);
+                most = largest8(f, most);
+            }
+            const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));
+            if (lane == 0) warp_most[me] = bits;
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kXWarps) : "memory");
+            uint32_t row_bits = 0;
+            for (int i = 0; i < per_row; ++i) row_bits = max(row_bits, warp_most[m * per_row + i]);
+            const float up = scale_up(row_bits);
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) {
+                if (at + j * step >= chunks) break;
+                activate8(raw[j], p.act, f);
+                sts128(s_x + image_offset(at + j * step, m, p.x_rows), to_half8(f, up));
+            }
+            for (int i = id; i < chunks * (kInlineRows - kXWarps / per_row); i += 32 * kXWarps)     // rows without warps
+                sts128(s_x + image_offset(i % chunks, kXWarps / per_row + i / chunks, p.x_rows), make_uint4(0, 0, 0, 0));
+            ptx::fence_proxy_async_smem();      // the tensor core reads x through the async proxy
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(kXFull));
+        }
         for (int s = odd; s < stages; s += 2) {
             const int st = s % p.ring;
             if (!warp_wait(bar(kFull + st), static_cast<uint32_t>(s / p.ring) & 1u, abort_flag, p.status, 0xC40u | st)) {
@@ -357,10 +425,20 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
             if (lane == 0) ptx::mbar_arrive(bar(kAFull + odd));
         }
         // ------------------------------------------------------------ this slice's sums, to the rank that owns the column
+        float x_back[kInlineRows];
         ok = ok && warp_wait(bar(kDone), 0, abort_flag, p.status, 0xC60u);
+        if (kInline) ok = ok && warp_wait(bar(kXFull), 0, abort_flag, p.status, 0xC61u);    // long complete: warp_most is in view
         if (ranks > 1) ptx::cluster_wait();
         if (ok) {
-            if (threadIdx.x < p.x_rows) back[threadIdx.x] = __ldcg(p.x_back + m0 + threadIdx.x);   // written before x was loaded
+            if (!kInline && threadIdx.x < p.x_rows) back[threadIdx.x] = __ldcg(p.x_back + m0 + threadIdx.x);   // written before x was loaded
+            if (kInline) {     // what undoes the slice's own scaling of each row
+#pragma unroll
+                for (int r = 0; r < kInlineRows; ++r) {
+                    uint32_t bits = 0;
+                    for (int i = r * per_row; i < (r + 1) * per_row && i < kXWarps; ++i) bits = max(bits, warp_most[i]);
+                    x_back[r] = scale_back(bits);
+                }
+            }
             ptx::tc_fence_after_sync();
             const int own = kRows / ranks;
             const uint32_t to = ptx::map_to_cta(s_part + (rank * p.x_rows * own + row % own) * 4, row / own);
@@ -375,6 +453,7 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
 #pragma unroll
                     for (int i = 1; i < kSums; ++i) v += __uint_as_float(d[i][e]);
                     if (kMx) v = scalbnf(v, ref - 127 - kMxExp);
+                    if (kInline) v *= c == 0 && e < kInlineRows ? x_back[e % kInlineRows] : 0.0f;    // every slice has its own scale
                     st_cluster(to + (c + e) * own * 4, v);
                 }
             }
@@ -384,24 +463,25 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     ptx::tc_fence_before_sync();
 
     // ---------------------------------------------------------------- own columns: sum over the ranks, scale, bias, store
-    const int own = kRows / ranks, pairs = own / 2, live = min(p.x_rows, p.M - m0);
+    const int own = kRows / ranks, pairs = own / 2, rows = min(p.x_rows, p.M - m0);
     const int r = 2 * (threadIdx.x % pairs), n = group * kRows + rank * own + r;
     const float T = kMx ? 1.0f : __ldg(p.wts);
     uint32_t b2 = 0;
     if (p.bias != nullptr && n < p.N) b2 = __ldg(reinterpret_cast<const uint32_t *>(p.bias + n));
     if (ranks > 1) ptx::cluster_sync();
     else __syncthreads();
-    for (int m = threadIdx.x / pairs; m < live && warp < kConvWarps && n < p.N; m += 32 * kConvWarps / pairs) {
+    for (int i = threadIdx.x / pairs; i < rows && warp < kConvWarps && n < p.N; i += 32 * kConvWarps / pairs) {
         float v0 = 0.0f, v1 = 0.0f;
         for (int c = 0; c < ranks; ++c) {
-            const float2 v = *reinterpret_cast<const float2 *>(part + (c * p.x_rows + m) * own + r);
+            const float2 v = *reinterpret_cast<const float2 *>(part + (c * p.x_rows + i) * own + r);
             v0 += v.x;
             v1 += v.y;
         }
-        const float y0 = fmaf(v0 * back[m], T, qmath::bf16_lo(b2)), y1 = fmaf(v1 * back[m], T, qmath::bf16_hi(b2));
+        const float scale = kInline ? 1.0f : back[i];
+        const float y0 = fmaf(v0 * scale, T, qmath::bf16_lo(b2)), y1 = fmaf(v1 * scale, T, qmath::bf16_hi(b2));
         uint32_t o;
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(y1), "f"(y0));
-        *reinterpret_cast<uint32_t *>(p.y + (m0 + m) * p.ldy + n) = o;
+        *reinterpret_cast<uint32_t *>(p.y + (m0 + i) * p.ldy + n) = o;
     }
     if (warp == kIssuer && aligned) {
         ptx::tc_fence_after_sync();
@@ -412,12 +492,12 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
 int x_rows_of(int64_t M) { return M >= kMaxXRows ? kMaxXRows : static_cast<int>(16 * ceil_div(M, 16)); }
 int ring_of(int x_rows) {
     int ring = kMaxStages;
-    while (smem_bytes(x_rows, ring) > kMaxSmem) --ring;
+    while (smem_bytes(x_rows, ring, ring) > kMaxSmem) --ring;
     return ring;
 }
 
 // Most clusters of `ranks` CTAs that the device holds at once (one CTA per SM; clusters do not span GPCs).
-template <bool kMx>
+template <bool kMx, bool kInline>
 int resident_clusters(int dev, int ranks) {
     static int known[64][kMaxCluster + 1] = {};
     if (known[dev][ranks] == 0) {
@@ -431,7 +511,7 @@ int resident_clusters(int dev, int ranks) {
         cfg.attrs = attr;
         cfg.numAttrs = 1;
         int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, matvec_kernel<kMx>, &cfg) != cudaSuccess || n < 1) {
+        if (cudaOccupancyMaxActiveClusters(&n, matvec_kernel<kMx, kInline>, &cfg) != cudaSuccess || n < 1) {
             cudaGetLastError();
             n = 1;
         }
@@ -440,37 +520,34 @@ int resident_clusters(int dev, int ranks) {
     return known[dev][ranks];
 }
 
-template <bool kMx>
-sol_status_t launch(const void *x, int64_t ldx, bool silu, void *workspace, const CUtensorMap &tm_w, Params &p, int64_t K, cudaStream_t stream) {
-    auto kern = matvec_kernel<kMx>;
+// K is shared by the largest cluster (of two, four or eight CTAs) that still runs in one wave.
+template <bool kMx, bool kInline>
+bool share_k(Params &p, int &ranks) {
+    auto kern = matvec_kernel<kMx, kInline>;
     static bool configured[64] = {};
     int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SOL_ERR_CUDA;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
     if (!configured[dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) != cudaSuccess) return SOL_ERR_CUDA;
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem) != cudaSuccess) return false;
         configured[dev] = true;
     }
-    // K is shared by the largest cluster (of two, four or eight CTAs) that still runs in one wave.
-    const int64_t groups = ceil_div(p.N, kRows), row_chunks = ceil_div(p.M, p.x_rows);
-    int ranks = 1;
-    while (2 * ranks <= kMaxCluster && 2 * ranks <= p.stages && groups * row_chunks <= resident_clusters<kMx>(dev, 2 * ranks)) ranks *= 2;
+    const int64_t ctas = ceil_div(p.N, kRows) * ceil_div(p.M, p.x_rows);
+    ranks = 1;
+    while (2 * ranks <= kMaxCluster && 2 * ranks <= p.stages && ctas <= resident_clusters<kMx, kInline>(dev, 2 * ranks)) ranks *= 2;
     p.per_cta = static_cast<int>(ceil_div(p.stages, ranks));
     while (ranks > 1 && (ranks - 1) * p.per_cta >= p.stages) {    // every rank needs a stage
         ranks /= 2;
         p.per_cta = static_cast<int>(ceil_div(p.stages, ranks));
     }
-    uint8_t *image = static_cast<uint8_t *>(workspace);
-    float *x_back = reinterpret_cast<float *>(image + row_chunks * p.stages * stage_x_bytes(p.x_rows));
-    p.ximage = image;
-    p.x_back = x_back;
-    prepare_x<<<static_cast<unsigned>(row_chunks * p.x_rows), kPrepThreads, 0, stream>>>(
-        static_cast<const uint16_t *>(x), ldx, p.M, static_cast<int>(K), p.x_rows, p.stages, silu ? 1 : 0, image, x_back);
-    const sol_status_t st = launch_status();
-    if (st != SOL_OK) return st;
+    return true;
+}
+
+template <bool kMx, bool kInline>
+sol_status_t launch_products(const CUtensorMap &tm_w, const Params &p, int ranks, cudaStream_t stream) {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(ranks), static_cast<unsigned>(groups), static_cast<unsigned>(row_chunks));
+    cfg.gridDim = dim3(static_cast<unsigned>(ranks), static_cast<unsigned>(ceil_div(p.N, kRows)), static_cast<unsigned>(ceil_div(p.M, p.x_rows)));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = static_cast<size_t>(smem_bytes(p.x_rows, p.ring));
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem_bytes(p.x_rows, p.ring, kInline ? p.per_cta : p.ring));
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -478,17 +555,41 @@ sol_status_t launch(const void *x, int64_t ldx, bool silu, void *workspace, cons
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, kern, tm_w, static_cast<const Params &>(p)) != cudaSuccess) {
+    cfg.numAttrs = kInline ? 1 : 2;
+    if (cudaLaunchKernelEx(&cfg, matvec_kernel<kMx, kInline>, tm_w, p) != cudaSuccess) {
         cudaGetLastError();
         return SOL_ERR_CUDA;
     }
     return launch_status();
 }
 
+template <bool kMx>
+sol_status_t launch(const void *x, int64_t ldx, bool silu, void *workspace, const CUtensorMap &tm_w, Params &p, int64_t K, cudaStream_t stream) {
+    int ranks = 1;
+    if (prepared_inline(p.M, K)) {
+        if (!share_k<kMx, true>(p, ranks)) return SOL_ERR_CUDA;
+        p.x = static_cast<const uint16_t *>(x);
+        p.ldx = ldx;
+        p.K = static_cast<int>(K);
+        p.act = silu ? 1 : 0;
+        return launch_products<kMx, true>(tm_w, p, ranks, stream);
+    }
+    if (!share_k<kMx, false>(p, ranks)) return SOL_ERR_CUDA;
+    const int64_t row_chunks = ceil_div(p.M, p.x_rows);
+    uint8_t *image = static_cast<uint8_t *>(workspace);
+    float *x_back = reinterpret_cast<float *>(image + row_chunks * p.stages * stage_x_bytes(p.x_rows));
+    p.ximage = image;
+    p.x_back = x_back;
+    prepare_x<<<static_cast<unsigned>(row_chunks * p.x_rows), kPrepThreads, 0, stream>>>(
+        static_cast<const uint16_t *>(x), ldx, p.M, static_cast<int>(K), p.x_rows, p.stages, silu ? 1 : 0, image, x_back);
+    const sol_status_t st = launch_status();
+    return st != SOL_OK ? st : launch_products<kMx, false>(tm_w, p, ranks, stream);
+}
+
 }  // namespace
 
 size_t workspace_bytes(int64_t M, int64_t K) {
+    if (prepared_inline(M, K)) return 0;
     const int x_rows = x_rows_of(M);
     const int64_t chunks = ceil_div(M, x_rows);
     return static_cast<size_t>(chunks * ceil_div(K, kStageK) * stage_x_bytes(x_rows) + chunks * x_rows * 4);

@@ -68,7 +68,7 @@ def rows(M, K, seed, pad=0):
 
 
 SHAPES = [(1, 8, 32), (1, 128, 128), (2, 136, 96), (3, 1000, 160), (8, 256, 512), (9, 264, 544), (16, 128, 1056), (17, 640, 2240),
-          (24, 72, 320), (25, 128, 4128), (32, 2432, 1216), (33, 200, 640), (64, 512, 1024), (70, 88, 256), (5, 128, 24576), (32, 136, 15360), (48, 64, 32), (130, 40, 288)]
+          (24, 72, 320), (25, 128, 4128), (32, 2432, 1216), (33, 200, 640), (64, 512, 1024), (70, 88, 256), (5, 128, 24576), (32, 136, 15360), (48, 64, 32), (130, 40, 288), (1, 9216, 3072), (4, 4104, 3072), (2, 72, 2240), (3, 16, 992), (4, 256, 3104), (1, 40000, 64)]
 
 
 @pytest.mark.parametrize("fmt", ["nv", "mx"])

@@ -57,11 +57,13 @@ def test_entry_points_refuse_bad_arguments(B):
         assert f(M=0) == SHAPE and f(N=12, ldy=16) == SHAPE and f(K=48) == SHAPE and f(N=0) == SHAPE
         assert f(ldx=56) == SHAPE and f(N=16) == SHAPE                      # pitches too small
         assert f(M=(1 << 18) + 1) == SHAPE and f(N=1 << 23, ldy=1 << 23) == SHAPE
-        assert f(ws=None) == NULLP and f(ws=p + 128) == ALIGN
-        assert f(size=L.sol_matvec_workspace_bytes(4, 64) - 1) == WS
+        assert f(M=8, ws=None) == NULLP and f(ws=p + 128) == ALIGN
+        assert f(M=8, size=L.sol_matvec_workspace_bytes(8, 64) - 1) == WS
     assert L.sol_matvec_workspace_bytes(0, 64) == 0 and L.sol_matvec_workspace_bytes(4, 48) == 0
     # x padded to sixteen rows and 256 columns in FP16, and a float per row
-    assert L.sol_matvec_workspace_bytes(4, 64) == 16 * 256 * 2 + 16 * 4
+    assert L.sol_matvec_workspace_bytes(8, 64) == 16 * 256 * 2 + 16 * 4
+    assert L.sol_matvec_workspace_bytes(4, 3072) == 0 and L.sol_matvec_workspace_bytes(5, 3072) > 0      # the blocks' own
+    assert L.sol_matvec_workspace_bytes(1, 3104) == 16 * 3328 * 2 + 16 * 4
     assert L.sol_matvec_workspace_bytes(65, 544) == 128 * 768 * 2 + 128 * 4
     # the input activation is refused where an output activation is asked for
     assert L.nvfp4_linear_quantized_out(p, p, p, p, p, p, None, 2, p, p, p, None, 4, 64, 64, None) == LAYOUT
