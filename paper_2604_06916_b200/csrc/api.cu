@@ -669,7 +669,7 @@ sol_status_t sol_select_blocks(const void *q, const void *k, int64_t batch, int6
     const sol_status_t st = check_arch(&dev);
     if (st != SOL_OK) return st;
     return blocks::launch_select(q, k, batch, seq_q, seq_kv, heads, heads_kv, head_dim, ld_q, ld_k, count, keep_first, kv_lens,
-                                 block_lists, counts, scores, workspace, static_cast<cudaStream_t>(stream));
+                                 block_lists, counts, scores, workspace, static_cast<cudaStream_t>(stream), dev);
 }
 
 sol_status_t sol_attention_blocks(const void *q, const void *k, const void *v, void *out, int64_t batch, int64_t seq_q, int64_t seq_kv,

@@ -17,9 +17,8 @@ namespace blocks {
 namespace {
 
 constexpr int kPoolWarps = 8;
-constexpr int kWarpColumns = 256;      // columns of a pooling warp: 16 bytes per lane
-constexpr int kWarpRows = 64;          // rows of a pooling warp
-constexpr int kRowsInFlight = 16;      // rows a warp loads before it adds any
+constexpr int kColumns = 256;          // columns of a pooling unit: 16 bytes per lane
+constexpr int kBatch = 8;              // rows of a warp's batch: one is on its way while the one before is added
 
 // FP64 of the two BF16 halves of a word, times 2^-896 (upper words; the lower ones are zero).
 __device__ __forceinline__ double scaled_hi(uint32_t w) {
@@ -33,12 +32,11 @@ struct PoolTensor {
     const int32_t *lens;      // per batch element, or null
     int64_t ld, batch_stride; // elements
     int seq, heads, blocks, rows_per_block, column_chunks;
-    bool transposed;
 };
 
 struct PoolParams {
     PoolTensor q, k;
-    int q_ctas;               // CTAs of q along x; the rest pool k
+    int q_units, k_units;
     int head_dim_log2;
 };
 
@@ -53,61 +51,103 @@ __device__ __forceinline__ uint4 load_once(const uint16_t *p) {
     return v;
 }
 
-// A CTA's warps lie side by side along the columns (long contiguous pieces of each row) and, a block's 64-row parts, below
-// each other.
-__global__ void __launch_bounds__(32 * kPoolWarps)
+// A block of rows by 256 columns.  Its rows go to the warps in turn, a batch at a time.
+struct Unit {
+    const uint16_t *x;      // this lane's first column in the block's first row, or null: no such column
+    int64_t ld;
+    int rows, batches;      // rows that exist; batches of each warp
+    int b, blk, c0;         // sample, block, first column
+    bool is_q;
+};
+__device__ __forceinline__ Unit unit_of(const PoolParams &p, int at, int lane) {
+    Unit u;
+    u.is_q = at < p.q_units;
+    const PoolTensor &t = u.is_q ? p.q : p.k;
+    const uint32_t unit = static_cast<uint32_t>(u.is_q ? at : at - p.q_units), line = unit / static_cast<uint32_t>(t.column_chunks);
+    u.c0 = static_cast<int>(unit - line * t.column_chunks) * kColumns;
+    u.b = static_cast<int>(line / static_cast<uint32_t>(t.blocks));
+    u.blk = static_cast<int>(line) - u.b * t.blocks;
+    const int c = u.c0 + 8 * lane, row0 = u.blk * t.rows_per_block;
+    u.x = c < t.heads << p.head_dim_log2 ? t.x + u.b * t.batch_stride + static_cast<int64_t>(row0) * t.ld + c : nullptr;
+    u.ld = t.ld;
+    u.rows = min(t.rows_per_block, valid_rows(t.lens, u.b, t.seq) - row0);
+    u.batches = t.rows_per_block / (kPoolWarps * kBatch);
+    return u;
+}
+
+// Blocks stay and walk the units, loads running ahead over the units' borders: without that all warps of the GPU load at
+// once and then add at once.
+__global__ void __launch_bounds__(32 * kPoolWarps, 2)
 pool_kernel(const PoolParams p) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ double part[kPoolWarps][kWarpColumns];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, b = blockIdx.y;
-    const bool is_q = static_cast<int>(blockIdx.x) < p.q_ctas;
-    const PoolTensor t = is_q ? p.q : p.k;
-    const int unit = is_q ? blockIdx.x : blockIdx.x - p.q_ctas;
-    const int parts = t.rows_per_block / kWarpRows, side = kPoolWarps / parts;      // warps below, and beside each other
-    const int blk = unit / t.column_chunks, c0 = (unit % t.column_chunks * side + warp % side) * kWarpColumns;
-    const int columns = t.heads << p.head_dim_log2;
-    const int row0 = blk * t.rows_per_block, rows = min(t.rows_per_block, valid_rows(t.lens, b, t.seq) - row0);
-    const int first = warp / side * kWarpRows, last = min(rows, first + kWarpRows);
-    const int c = c0 + 8 * lane;
-    const bool live = c < columns;       // columns are a multiple of 64: a lane is wholly inside or outside
-    const uint16_t *x = t.x + b * t.batch_stride + static_cast<int64_t>(row0) * t.ld + c;
-    double acc[8] = {};
-    auto add = [&](const uint4 &v) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    __shared__ double part[2][kPoolWarps][kColumns];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int units = p.q_units + p.k_units;
+    auto fetch = [&](const Unit &u, int batch, uint4 (&v)[kBatch]) {
+        const int first = (batch * kPoolWarps + warp) * kBatch;
+        if (u.x == nullptr || first + kBatch > u.rows) {     // no columns, or a block's ragged end
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            acc[2 * e] += scaled_lo(w[e]);
-            acc[2 * e + 1] += scaled_hi(w[e]);
+            for (int i = 0; i < kBatch; ++i)
+                v[i] = u.x != nullptr && first + i < u.rows ? load_once(u.x + (first + i) * u.ld) : make_uint4(0, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) v[i] = load_once(u.x + (first + i) * u.ld);
         }
     };
-    if (live) {
-        int r = first;
-        for (; r + kRowsInFlight <= last; r += kRowsInFlight) {
-            uint4 v[kRowsInFlight];
+    double acc[8];
+    auto add_all = [&](const uint4 (&v)[kBatch]) {
 #pragma unroll
-            for (int i = 0; i < kRowsInFlight; ++i) v[i] = load_once(x + (r + i) * t.ld);
+        for (int i = 0; i < kBatch; ++i) {
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
 #pragma unroll
-            for (int i = 0; i < kRowsInFlight; ++i) add(v[i]);
+            for (int e = 0; e < 4; ++e) {
+                acc[2 * e] += scaled_lo(w[e]);
+                acc[2 * e + 1] += scaled_hi(w[e]);
+            }
         }
-        for (; r < last; ++r) add(__ldcs(reinterpret_cast<const uint4 *>(x + r * t.ld)));
-    }
+    };
+    int at = blockIdx.x, buf = 0;
+    if (at >= units) return;
+    Unit u = unit_of(p, at, lane);
+    uint4 now[kBatch], next[kBatch];
+    fetch(u, 0, now);
+    while (at < units) {
+        const int following = at + gridDim.x;
+        Unit v = u;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) part[warp][32 * e + lane] = acc[e];    // column 8 * lane + e: no bank is hit twice
-    __syncthreads();
-    if (warp >= side) return;
+        for (int e = 0; e < 8; ++e) acc[e] = 0.0;
+        for (int batch = 0; batch < u.batches; batch += 2) {       // two or four batches
+            fetch(u, batch + 1, next);
+            add_all(now);
+            if (batch + 2 < u.batches) {
+                fetch(u, batch + 2, now);
+            } else if (following < units) {
+                v = unit_of(p, following, lane);
+                fetch(v, 0, now);
+            }
+            add_all(next);
+        }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int col = c + e;
-        if (!live) break;
-        double sum = 0.0;
-        for (int i = 0; i < parts; ++i) sum += part[i * side + warp][32 * e + lane];
-        const double mean = rows > 0 ? sum * 0x1p896 / static_cast<double>(rows) : 0.0;
-        const int head = col >> p.head_dim_log2, d = col & ((1 << p.head_dim_log2) - 1);
-        const int64_t bh = static_cast<int64_t>(b) * t.heads + head;
-        if (t.transposed) t.out[((bh << p.head_dim_log2) + d) * t.blocks + blk] = mean;
-        else t.out[((bh * t.blocks + blk) << p.head_dim_log2) + d] = mean;
+        for (int e = 0; e < 8; ++e) part[buf][warp][32 * e + lane] = acc[e];    // column 8 * lane + e: no bank is hit twice
+        __syncthreads();
+        const PoolTensor &t = u.is_q ? p.q : p.k;
+        const int col = u.c0 + 8 * lane + warp;    // a warp takes one of the eight columns of each lane
+        if (col < t.heads << p.head_dim_log2) {
+            double sum = 0.0;
+#pragma unroll
+            for (int w = 0; w < kPoolWarps; ++w) sum += part[buf][w][32 * warp + lane];
+            const double mean = u.rows > 0 ? sum * 0x1p896 / static_cast<double>(u.rows) : 0.0;
+            const int head = col >> p.head_dim_log2, d = col & ((1 << p.head_dim_log2) - 1);
+            const int64_t bh = static_cast<int64_t>(u.b) * t.heads + head;
+            if (u.is_q) t.out[((bh * t.blocks + u.blk) << p.head_dim_log2) + d] = mean;
+            else t.out[((bh << p.head_dim_log2) + d) * t.blocks + u.blk] = mean;
+        }
+        u = v;
+        at = following;
+        buf ^= 1;      // the sums of this unit may still be read when the next one's are written
     }
 }
+static_assert(kPoolWarps == 8 && kKeyBlock % (2 * kPoolWarps * kBatch) == 0 && kQueryBlock % (2 * kPoolWarps * kBatch) == 0, "pairs of batches");
 
 struct SelectParams {
     const double *pq, *pk;
@@ -158,7 +198,7 @@ select_kernel(const SelectParams p) {
         if (j >= valid) continue;
         const double *kd = k + static_cast<int64_t>(part * depth) * p.k_blocks + j, *qd = means + part * depth * kRows;
         double s[kRows] = {};
-#pragma unroll 8
+#pragma unroll 16
         for (int d = 0; d < depth; ++d) {
             const double kv = kd[static_cast<int64_t>(d) * p.k_blocks];
 #pragma unroll
@@ -183,12 +223,24 @@ select_kernel(const SelectParams p) {
     unsigned long long cut = 0;
     int above = 0;
     if (valid > kMaxRanked && open > 0) {
-        for (int bit = 63; bit >= 0; --bit) {
+        // bits that all upper halves share need no pass, and no further one once exactly `open` keys reach the trial
+        uint32_t least = 0xFFFFFFFFu, most = 0;
+        for (int j = forced + lane; j < valid; j += 32) {
+            const uint32_t upper = static_cast<uint32_t>(keys[j] >> 32);
+            least = min(least, upper);
+            most = max(most, upper);
+        }
+        least = __reduce_min_sync(0xFFFFFFFFu, least);
+        most = __reduce_max_sync(0xFFFFFFFFu, most);
+        int bit = 63 - __clz(least ^ most);                       // 31 where they agree in all 32
+        cut = static_cast<unsigned long long>(most) << 32 >> bit >> 1 << bit << 1;     // the shared bits (a shift by 64 is none)
+        for (; bit >= 0; --bit) {
             const unsigned long long trial = cut | 1ull << bit;
             int reach = 0;
             for (int j0 = forced; j0 < valid; j0 += 32)
                 reach += __popc(__ballot_sync(0xFFFFFFFFu, j0 + lane < valid && keys[j0 + lane] >= trial));
             if (reach >= open) cut = trial;
+            if (reach == open) break;
         }
         for (int j0 = forced; j0 < valid; j0 += 32)
             above += __popc(__ballot_sync(0xFFFFFFFFu, j0 + lane < valid && keys[j0 + lane] > cut));
@@ -266,19 +318,21 @@ size_t select_workspace_bytes(int64_t batch, int64_t seq_q, int64_t seq_kv, int6
 
 sol_status_t launch_select(const void *q, const void *k, int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv,
                            int64_t head_dim, int64_t ld_q, int64_t ld_k, int64_t count, int64_t keep_first, const int32_t *kv_lens,
-                           int32_t *blocks, int32_t *counts, float *scores, void *workspace, cudaStream_t stream) {
+                           int32_t *blocks, int32_t *counts, float *scores, void *workspace, cudaStream_t stream, const DeviceInfo *dev) {
     const int nq = static_cast<int>(ceil_div(seq_q, kQueryBlock)), nk = static_cast<int>(ceil_div(seq_kv, kKeyBlock));
     double *pq = static_cast<double *>(workspace), *pk = pq + batch * heads * nq * head_dim;
     PoolParams pool{};
     pool.q = PoolTensor{static_cast<const uint16_t *>(q), pq, nullptr, ld_q, seq_q * ld_q, static_cast<int>(seq_q), static_cast<int>(heads), nq,
-                        kQueryBlock, static_cast<int>(ceil_div(heads * head_dim, kWarpColumns * kPoolWarps * kWarpRows / kQueryBlock)), false};
+                        kQueryBlock, static_cast<int>(ceil_div(heads * head_dim, kColumns))};
     pool.k = PoolTensor{static_cast<const uint16_t *>(k), pk, kv_lens, ld_k, seq_kv * ld_k, static_cast<int>(seq_kv), static_cast<int>(heads_kv), nk,
-                        kKeyBlock, static_cast<int>(ceil_div(heads_kv * head_dim, kWarpColumns * kPoolWarps * kWarpRows / kKeyBlock)), true};
-    pool.q_ctas = nq * pool.q.column_chunks;
+                        kKeyBlock, static_cast<int>(ceil_div(heads_kv * head_dim, kColumns))};
+    const int64_t q_units = batch * nq * pool.q.column_chunks, k_units = batch * nk * pool.k.column_chunks;
+    if (q_units + k_units > 0x3FFFFFFFLL) return SOL_ERR_BAD_SHAPE;
+    pool.q_units = static_cast<int>(q_units);
+    pool.k_units = static_cast<int>(k_units);
     pool.head_dim_log2 = head_dim == 128 ? 7 : 6;
-    const int64_t ctas = pool.q_ctas + static_cast<int64_t>(nk) * pool.k.column_chunks;
-    if (ctas > 0x7FFFFFFFLL) return SOL_ERR_BAD_SHAPE;
-    pool_kernel<<<dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(batch)), 32 * kPoolWarps, 0, stream>>>(pool);
+    const int64_t resident = 2LL * dev->sm_count;
+    pool_kernel<<<static_cast<unsigned>(q_units + k_units < resident ? q_units + k_units : resident), 32 * kPoolWarps, 0, stream>>>(pool);
     const sol_status_t st = launch_status();
     if (st != SOL_OK) return st;
 

@@ -161,7 +161,7 @@ constexpr int kMaxKeyBlocks = 8192;
 size_t select_workspace_bytes(int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv, int64_t head_dim);
 sol_status_t launch_select(const void *q, const void *k, int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv,
                            int64_t head_dim, int64_t ld_q, int64_t ld_k, int64_t count, int64_t keep_first, const int32_t *kv_lens,
-                           int32_t *blocks, int32_t *counts, float *scores, void *workspace, cudaStream_t stream);
+                           int32_t *blocks, int32_t *counts, float *scores, void *workspace, cudaStream_t stream, const DeviceInfo *dev);
 }
 
 // Head norm and rotary positions of q and k (a tensor with no heads is absent).

@@ -74,6 +74,26 @@ def test_selection_over_many_blocks(B):
     check_select(B, q, k, 700, 1)
 
 
+def test_many_blocks_of_both_signs_equal_or_nearly(B):
+    # the search over the keys' bits: signs apart, all upper halves alike, exact ties across the cut
+    q, k, _ = make(1, 256, 128 * 200, 1, 1, 64, 4)
+    q[:] = 0
+    q[..., 0] = 1.0
+    k[:] = 0
+    k[0, ::128, 0, 0] = torch.linspace(-3, 3, 200, device="cuda").to(torch.bfloat16)      # one row per block decides its mean
+    for count in (1, 7, 100, 199, 200):
+        check_select(B, q, k, count)
+    k[0, ::128, 0, 0] = 1.0                                          # all equal
+    check_select(B, q, k, 50, 3)
+    k[0, 1::128, 0, 0] = torch.arange(200, device="cuda").to(torch.bfloat16) * 2.0 ** -40   # apart by 2^-40 only
+    check_select(B, q, k, 50)
+    k[0, 1::128, 0, 0] = (torch.arange(200, device="cuda") // 9).to(torch.bfloat16) * 2.0 ** -40
+    for count in (5, 9, 14, 197):
+        check_select(B, q, k, count, 2)
+    k[0, ::128, 0, 0] = -1.0
+    check_select(B, q, k, 14)
+
+
 def test_equal_scores_go_to_the_lower_index(B):
     q, k, _ = make(1, 300, 1280, 2, 2, 64, 5)
     k = k[:, :128].repeat(1, 10, 1, 1)                          # ten equal blocks
