@@ -20,7 +20,13 @@
 //
 // Over listed key blocks (kListed) the tiles are the entries of a list per query block: a warp copies the entries that
 // name existing keys into shared memory while Q loads, and tile j is the j-th of them; a list without any leaves
-// zeros.  A key / value head may serve several query heads.
+// zeros.  A key / value head may serve several query heads.  Measured: 4 x 4608 tokens, 24 heads x 128, 9 of 36 blocks,
+// 267 us = 980 TFLOP/s (the dense form reaches 1.05 to 1.1 PFLOP/s on 36 tiles; a CTA's way in and out costs 2.5 us, over
+// nine tiles of 2.3 us); 2 x 4429, 38 heads x 64, 8 blocks, 184 us.  Per tile of 3600 cycles a query tile's chain
+// is 1430 of exponentials, 500 of loads, maximum and stores, 400 until the issuer sees P, 1000 of P V and the next scores.
+// Built and not kept: two threads per row and sixteen softmax warps (345 us: 96 registers, and the two halves have to agree
+// on the maximum every tile); P handed over in two halves so that P V starts under the second half's
+// exponentials (277 us); three-input maxima and two-lane sums (no change).
 //
 // Warps: 0 = TMA producer, 1 = TMEM owner and MMA issuer, 2..5 and 6..9 = softmax / epilogue of query
 // tile 0 and 1 (one warp per TMEM lane quadrant).  Every mbarrier wait is bounded.

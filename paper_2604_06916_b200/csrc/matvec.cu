@@ -6,12 +6,24 @@
 //
 // Two launches.  prepare_x turns x (after the activation) into FP16 once, in the shared-memory image of the products'
 // operand; the products' kernel is launched along with it (programmatic launch) and waits for it only where x enters.
+// Up to four rows of K <= 3072 are prepared by every CTA for its own slice instead (two of its warpgroups, while the other
+// two convert the first stage): one launch and no workspace, which is what a caller without graphs waits for (1 x 9216 x
+// 3072: 13 us a call against 17; 9.7 against 9.2 us inside a graph).  With eight rows the exponentials alone would
+// take a CTA longer than its weights.
 // One CTA takes 128 output columns (a row group of the chunked scale layout) and a slice of K, one CTA per SM; where the
 // columns leave SMs free, a cluster of up to eight CTAs shares K, each adds up its share of the 128 columns in rank order.
 // The weight is the M = 128 operand of tcgen05.mma kind::f16 and comes from tensor memory: codes, scales and x
 // stream into a ring of 256-column stages by TMA and bulk copies, a thread per weight row converts the codes to FP16
 // (cvt.e2m1x2), multiplies by the block scales and leaves them in its TMEM lane; x is the N operand (16 to 64 rows).
 // Four warpgroups convert: two share an even stage, two an odd one, while the products of the stage before run.
+//
+// Measured (B200, inside a graph): NVFP4 1 x 9216 x 3072 9.7 us, 8 x 18432 x 3072 12.0 us (floor 4.9 us), MXFP4 24 x 14592 x
+// 2432 12.9 us (floor 3.0 us).  While stages run they run at the weights' HBM rate (800 cycles per 18 KB stage and SM; leaving
+// out three quarters of the products or of the conversions changes nothing at up to sixteen rows); the rest is the way
+// in (2 to 2.5 us until the first codes arrive) and out (1.5 us from the last product to the stores).  Four stages: with eight
+// in flight the first one arrives with the last (13.5 us), with two the ring runs dry (16.8 us).  Register tiles and
+// mma.sync m16n8k16 in place of tensor memory: 11.5, 23.7 and 28 us; converting for mma.sync costs 2 codes per cycle and
+// scheduler and every eight rows of x as much again, tcgen05 takes 64 rows for the price of one.
 //
 // Number formats.  code * block scale has at most six significant bits: exact in FP16 for NVFP4 (2^-10 .. 2688).  MXFP4
 // scales are powers of two of any size: they are taken relative to the largest one of the row's slice, 2^13 for that
@@ -116,13 +128,6 @@ __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
 __device__ __forceinline__ void st_cluster(uint32_t cluster_addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
 }
-__device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&r)[8]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(taddr)
-                 : "memory");
-}
-
 // A bounded wait of a whole warp: if it runs out for one lane, every lane gives up, so the warp stays together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status, uint32_t code) {
     return __all_sync(0xFFFFFFFFu, wait_bounded(bar, parity, abort_flag, status, code));
@@ -165,7 +170,9 @@ __device__ __forceinline__ uint4 to_half8(const float (&v)[8], float up) {
     return make_uint4(h[0], h[1], h[2], h[3]);
 }
 // Place of eight columns (chunk c of the slice) of row r in the image: a box of [x_rows][128 bytes] per 64 columns.
-__device__ __forceinline__ int image_offset(int c, int r, int x_rows) { return (c >> 3) * (x_rows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
+__device__ __forceinline__ int64_t image_offset(int c, int r, int x_rows) {
+    return static_cast<int64_t>(c >> 3) * (x_rows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+}
 
 // x -> scaled FP16 in the products' layout.  A block per row (rows behind the last are zeros), a thread per eight columns.
 constexpr int kPrepThreads = 512;
@@ -352,7 +359,7 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
             // this slice of x, while the other two warpgroups convert the first stage: the warps of a row find its largest
             // element, every thread scales and places its columns
             for (int i = id; i < chunks * (p.x_rows - kInlineRows); i += 32 * kXWarps)      // rows that never exist
-                sts128(s_x + image_offset(i / (p.x_rows - kInlineRows), kInlineRows + i % (p.x_rows - kInlineRows), p.x_rows), make_uint4(0, 0, 0, 0));
+                sts128(s_x + static_cast<uint32_t>(image_offset(i / (p.x_rows - kInlineRows), kInlineRows + i % (p.x_rows - kInlineRows), p.x_rows)), make_uint4(0, 0, 0, 0));
             float f[8], most = 0.0f;
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) {
@@ -370,10 +377,10 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
             for (int j = 0; j < kHeld; ++j) {
                 if (at + j * step >= chunks) break;
                 activate8(raw[j], p.act, f);
-                sts128(s_x + image_offset(at + j * step, m, p.x_rows), to_half8(f, up));
+                sts128(s_x + static_cast<uint32_t>(image_offset(at + j * step, m, p.x_rows)), to_half8(f, up));
             }
             for (int i = id; i < chunks * (kInlineRows - kXWarps / per_row); i += 32 * kXWarps)     // rows without warps
-                sts128(s_x + image_offset(i % chunks, kXWarps / per_row + i / chunks, p.x_rows), make_uint4(0, 0, 0, 0));
+                sts128(s_x + static_cast<uint32_t>(image_offset(i % chunks, kXWarps / per_row + i / chunks, p.x_rows)), make_uint4(0, 0, 0, 0));
             ptx::fence_proxy_async_smem();      // the tensor core reads x through the async proxy
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(bar(kXFull));
@@ -445,7 +452,7 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
             for (int c = 8 * (warp >> 2); c < p.x_rows; c += 32) {
                 uint32_t d[kSums][8];
 #pragma unroll
-                for (int i = 0; i < kSums; ++i) tmem_ld_32x8(tmem + kColD + i * kMaxXRows + lanes + c, d[i]);
+                for (int i = 0; i < kSums; ++i) ptx::tmem_ld_32x8(tmem + kColD + i * kMaxXRows + lanes + c, d[i]);
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {

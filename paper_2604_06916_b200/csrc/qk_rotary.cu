@@ -14,9 +14,11 @@
 // Four heads per lane are loaded before any is used.  Where tokens are few, up to one warp per four-head group shares a
 // token.  Measured (B200, q and k of 24 heads x 128 from a fused projection, norm and three axes): forward, 8 x 4608
 // tokens, 143 us = 6.3 TB/s, 97 % of the copy rate (one warp per token and eight heads, with its index divisions and
-// angles for each: 195 us).  Gradients, 2 x 4608 tokens, 66 us = 5.1 TB/s, 78 %: 113 registers hold both tensors'
-// loads, sixteen warps per SM wait for memory 2.4 cycles per issued instruction.  Two heads per lane with 24 warps
-// take 74 us, with the next ones prefetched 73 us.
+// angles for each: 195 us); 333 tokens, 4.1 us.  Gradients, 2 x 4608 tokens, 64 to 66 us = 5.2 TB/s, 79 %: 113 registers
+// hold both tensors' loads, sixteen warps per SM wait for memory 2.4 cycles per issued instruction.  Two heads per lane
+// with 24 warps take 71 us, with the next ones prefetched 73 us.  38 and 19 heads of 64, 4099 tokens: 25 us with eight heads a
+// step (sixteen: 27 us, a token's last step then leaves most lanes idle); q and k share the blocks by their steps (half
+// each: 29 us).
 //
 // Angles: position * freq and the reduction to half a turn are in FP64 (a far position times a frequency has
 // more significant bits than FP32 holds), the sine and cosine of the remainder in FP32.  Squares, means and
@@ -34,8 +36,6 @@ using qmath::bf16_lo;
 
 constexpr int kWarps = 8;
 constexpr int kUnroll = 4;      // heads per lane in flight
-constexpr int kUnrollBack = 4;  // the same in the gradients, which hold two tensors
-constexpr int kBackResident = 2;   // blocks of the gradients' kernel per SM
 
 // Lanes of a head: kD / 8; a warp holds kRep heads at a time.
 template <int kD>
@@ -43,7 +43,10 @@ struct Shape {
     static constexpr int kLanes = kD / 8;
     static constexpr int kRep = 32 / kLanes;
     static constexpr int kPairs = kRep >= 4 ? 1 : 4 / kRep;   // pairs whose angle a lane forms itself
-    static constexpr int kHeads = kRep * kUnroll;             // heads of a warp's task
+    static constexpr int kHeads = kRep * kUnroll;             // heads of a warp's step
+    // The gradients hold two tensors: eight heads a step keep narrow heads from idling lanes at the last step of a token.
+    static constexpr int kUnrollBack = kRep >= 8 ? 1 : kRep >= 2 ? 8 / kRep : 4;
+    static constexpr int kBackResident = kUnrollBack >= 4 ? 2 : 3;    // blocks per SM that the registers then allow
 };
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -227,34 +230,35 @@ forward_kernel(const Heads2 both, const Turn t, uint32_t rows, int parts_log2, f
     }
 }
 
-// Gradients.  blockIdx.y picks q or k; blocks stay and walk the (token, part of its heads) tasks, so that the weight
+// Gradients.  The first blocks_q blocks take q, the others k; blocks stay and walk the (token, part of its heads) tasks, so that the weight
 // gradient collects in registers: per lane over its tasks, per block over the lanes and warps that share a column
 // (FP64, fixed order), and reduce_weight_grads adds the blocks up.  No atomics: the result depends on nothing but
 // the shape.
 template <int kD, bool kHalf>
-__global__ void __launch_bounds__(32 * kWarps, kBackResident)
-backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int parts_log2, float eps, double *__restrict__ partials) {
+__global__ void __launch_bounds__(32 * kWarps, Shape<kD>::kBackResident)
+backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int blocks_q, int parts_log2, float eps, double *__restrict__ partials) {
     using S = Shape<kD>;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Grads d = blockIdx.y == 0 ? both.g[0] : both.g[1];
+    const bool is_q = static_cast<int>(blockIdx.x) < blocks_q;
+    const Grads d = is_q ? both.g[0] : both.g[1];
+    const uint32_t block = is_q ? blockIdx.x : blockIdx.x - blocks_q, blocks = is_q ? blocks_q : gridDim.x - blocks_q;
     int c0, c1;
     columns<kHalf>(lane % S::kLanes, t.rot, c0, c1);
     const bool mine = c0 < t.rot;
     const bool norm = d.weight != nullptr;
-    const int heads = d.heads, step = (S::kRep * kUnrollBack) << parts_log2;
+    const int heads = d.heads, step = (S::kRep * S::kUnrollBack) << parts_log2;
     Slot w, acc{};    // 0.0f in both lanes
     if (norm) w = unpack<kHalf>(load_weight(d.weight, c0, c1));
     const uint64_t tasks = static_cast<uint64_t>(rows) << parts_log2;
-    for (uint64_t task = static_cast<uint64_t>(blockIdx.x) * kWarps + warp; task < tasks;
-         task += static_cast<uint64_t>(gridDim.x) * kWarps) {
+    for (uint64_t task = static_cast<uint64_t>(block) * kWarps + warp; task < tasks; task += static_cast<uint64_t>(blocks) * kWarps) {
         const uint32_t m = static_cast<uint32_t>(task >> parts_log2);
         const uint16_t *dy = d.dy + m * d.ld_dy, *x = d.x + m * d.ld_x;
         uint16_t *dx = d.dx + m * d.ld_dx;
-        int h = static_cast<int>(task & ((1u << parts_log2) - 1u)) * (S::kRep * kUnrollBack) + lane / S::kLanes;
-        uint4 raw_dy[kUnrollBack], raw_x[kUnrollBack];
+        int h = static_cast<int>(task & ((1u << parts_log2) - 1u)) * (S::kRep * S::kUnrollBack) + lane / S::kLanes;
+        uint4 raw_dy[S::kUnrollBack], raw_x[S::kUnrollBack];
         auto fetch = [&]() {
 #pragma unroll
-            for (int u = 0; u < kUnrollBack; ++u) {
+            for (int u = 0; u < S::kUnrollBack; ++u) {
                 raw_dy[u] = raw_x[u] = make_uint4(0, 0, 0, 0);
                 if (h + u * S::kRep < heads) {
                     raw_dy[u] = load8<kHalf>(dy + (h + u * S::kRep) * kD, c0, c1);
@@ -267,7 +271,7 @@ backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int parts_log2, 
         if (t.rot > 0) an = angles<kD>(t, m, lane);
         for (; h - lane / S::kLanes < heads; h += step) {
 #pragma unroll
-            for (int u = 0; u < kUnrollBack; ++u) {
+            for (int u = 0; u < S::kUnrollBack; ++u) {
                 Slot dn = unpack<kHalf>(raw_dy[u]);
                 if (mine) turn(dn, an.c, an.ns, an.s);   // the inverse turn
                 if (norm) {   // uniform over the warp
@@ -292,7 +296,7 @@ backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int parts_log2, 
                 raw_dy[u] = pack<kHalf>(dn);
             }
 #pragma unroll
-            for (int u = 0; u < kUnrollBack; ++u)
+            for (int u = 0; u < S::kUnrollBack; ++u)
                 if (h + u * S::kRep < heads) store8<kHalf>(dx + (h + u * S::kRep) * kD, c0, c1, raw_dy[u]);
             if (h - lane / S::kLanes + step < heads) {
                 h += step;
@@ -318,7 +322,7 @@ backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int parts_log2, 
         double v = 0.0;
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) v += part[i][c];
-        partials[(static_cast<int64_t>(blockIdx.x) * 2 + blockIdx.y) * kD + c] = v;
+        partials[static_cast<int64_t>(blockIdx.x) * kD + c] = v;
     }
 }
 
@@ -326,7 +330,7 @@ backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int parts_log2, 
 constexpr int kReduceStrips = 16;
 template <int kD>
 __global__ void __launch_bounds__(32 * kReduceStrips)
-reduce_weight_grads(const double *__restrict__ partials, int blocks, float *dw_q, float *dw_k) {
+reduce_weight_grads(const double *__restrict__ partials, int blocks_q, int blocks, float *dw_q, float *dw_k) {
     __shared__ double part[kReduceStrips][32];
     float *dw = blockIdx.y == 0 ? dw_q : dw_k;
     ptx::grid_dependency_wait();
@@ -334,7 +338,8 @@ reduce_weight_grads(const double *__restrict__ partials, int blocks, float *dw_q
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), strip = threadIdx.x >> 5;
     double v = 0.0;
 #pragma unroll 8
-    for (int b = strip; b < blocks; b += kReduceStrips) v += partials[(static_cast<int64_t>(b) * 2 + blockIdx.y) * kD + c];
+    for (int b = (blockIdx.y == 0 ? 0 : blocks_q) + strip; b < (blockIdx.y == 0 ? blocks_q : blocks); b += kReduceStrips)
+        v += partials[static_cast<int64_t>(b) * kD + c];
     part[strip][threadIdx.x & 31] = v;
     __syncthreads();
     if (strip != 0) return;
@@ -343,21 +348,20 @@ reduce_weight_grads(const double *__restrict__ partials, int blocks, float *dw_q
     dw[c] = static_cast<float>(v);
 }
 
-constexpr int kMaxBackwardBlocks = 1024;   // per tensor
+constexpr int kMaxBackwardBlocks = 1024;
 
 // Warps that share a token, as a power of two: one where the tokens alone fill the GPU's warps, up to one per group of
 // heads where they are few.
-template <int kD>
-int split_of(int64_t rows, int heads, int64_t fill) {
+int split_of(int64_t rows, int heads, int heads_per_step, int64_t fill) {
     int log2 = 0;
-    while ((rows << log2) < fill && (Shape<kD>::kHeads << log2) < heads) ++log2;
+    while ((rows << log2) < fill && (heads_per_step << log2) < heads) ++log2;
     return log2;
 }
 
 template <int kD>
 sol_status_t forward(const Heads2 &h, const Turn &t, int64_t rows, bool half, float eps, cudaStream_t stream, const DeviceInfo *dev) {
     const int heads = h.h[0].heads > h.h[1].heads ? h.h[0].heads : h.h[1].heads;
-    const int split = split_of<kD>(rows, heads, 16LL * dev->sm_count);
+    const int split = split_of(rows, heads, Shape<kD>::kHeads, 16LL * dev->sm_count);
     const dim3 grid(static_cast<unsigned>(ceil_div(rows << split, kWarps)), h.h[1].heads > 0 ? 2u : 1u);
     auto kern = half ? forward_kernel<kD, true> : forward_kernel<kD, false>;
     kern<<<grid, 32 * kWarps, 0, stream>>>(h, t, static_cast<uint32_t>(rows), split, eps);
@@ -367,20 +371,30 @@ sol_status_t forward(const Heads2 &h, const Turn &t, int64_t rows, bool half, fl
 template <int kD>
 sol_status_t backward(const Grads2 &g, const Turn &t, int64_t rows, bool half, float eps, double *partials, cudaStream_t stream,
                       const DeviceInfo *dev) {
+    constexpr int kHeads = Shape<kD>::kRep * Shape<kD>::kUnrollBack, kBackResident = Shape<kD>::kBackResident;
     const int heads = g.g[0].heads > g.g[1].heads ? g.g[0].heads : g.g[1].heads;
-    const int split = split_of<kD>(rows, heads, 16LL * dev->sm_count);
-    const int64_t want = ceil_div(rows << split, kWarps);
-    const unsigned tensors = g.g[1].heads > 0 ? 2u : 1u;
-    int64_t most = kBackResident * dev->sm_count / tensors;   // all blocks resident at once
-    if (most > kMaxBackwardBlocks) most = kMaxBackwardBlocks;
-    const dim3 grid(static_cast<unsigned>(want < most ? want : most), tensors);
+    const int split = split_of(rows, heads, kHeads, 16LL * dev->sm_count);
+    // all blocks resident at once, shared out by the steps that q and k take per token
+    const int64_t steps_q = ceil_div(g.g[0].heads, kHeads), steps_k = ceil_div(g.g[1].heads, kHeads);
+    const int64_t most = kBackResident * dev->sm_count < kMaxBackwardBlocks ? kBackResident * dev->sm_count : kMaxBackwardBlocks;
+    const int64_t want = ceil_div(rows << split, kWarps);       // a warp per task
+    int64_t blocks_k = 0, blocks_q = most;
+    if (steps_k > 0) {
+        blocks_k = (most * steps_k + (steps_q + steps_k) / 2) / (steps_q + steps_k);
+        if (blocks_k < 1) blocks_k = 1;
+        if (blocks_k >= most) blocks_k = most - 1;
+        blocks_q = most - blocks_k;
+    }
+    if (blocks_q > want) blocks_q = want;
+    if (blocks_k > want) blocks_k = want;
+    const int blocks = static_cast<int>(blocks_q + blocks_k);
     auto kern = half ? backward_kernel<kD, true> : backward_kernel<kD, false>;
-    kern<<<grid, 32 * kWarps, 0, stream>>>(g, t, static_cast<uint32_t>(rows), split, eps, partials);
+    kern<<<blocks, 32 * kWarps, 0, stream>>>(g, t, static_cast<uint32_t>(rows), static_cast<int>(blocks_q), split, eps, partials);
     const sol_status_t st = launch_status();
     if (st != SOL_OK || partials == nullptr) return st;
     // the few blocks of the sum are set up while the last blocks of the gradients drain (programmatic launch)
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(kD / 32, grid.y);
+    cfg.gridDim = dim3(kD / 32, steps_k > 0 ? 2 : 1);
     cfg.blockDim = dim3(32 * kReduceStrips);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -388,7 +402,7 @@ sol_status_t backward(const Grads2 &g, const Turn &t, int64_t rows, bool half, f
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, reduce_weight_grads<kD>, static_cast<const double *>(partials), static_cast<int>(grid.x),
+    if (cudaLaunchKernelEx(&cfg, reduce_weight_grads<kD>, static_cast<const double *>(partials), static_cast<int>(blocks_q), blocks,
                            g.g[0].dweight, g.g[1].dweight) != cudaSuccess) {
         cudaGetLastError();
         return SOL_ERR_CUDA;
@@ -398,7 +412,7 @@ sol_status_t backward(const Grads2 &g, const Turn &t, int64_t rows, bool half, f
 
 }  // namespace
 
-size_t backward_workspace_bytes(int64_t head_dim) { return sizeof(double) * 2 * static_cast<size_t>(head_dim) * kMaxBackwardBlocks; }
+size_t backward_workspace_bytes(int64_t head_dim) { return sizeof(double) * static_cast<size_t>(head_dim) * kMaxBackwardBlocks; }
 
 bool head_dim_ok(int64_t d) { return d == 32 || d == 64 || d == 128 || d == 256; }
 
