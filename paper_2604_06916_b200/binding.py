@@ -161,7 +161,10 @@ _guarding = False        # inside a guarded call
 
 
 def guard_mode() -> bool:
-    return "SOL_NVFP4_GUARD" in os.environ and os.environ["SOL_NVFP4_GUARD"] not in ("", "0")
+    if "SOL_NVFP4_GUARD" not in os.environ or os.environ["SOL_NVFP4_GUARD"] in ("", "0"):
+        return False
+    # a capture records the bands' fills without running them, and must not be synchronised: nothing to check there
+    return not (torch.cuda.is_available() and torch.cuda.is_current_stream_capturing())
 
 
 def _empty(shape, dtype, device) -> torch.Tensor:
