@@ -316,6 +316,20 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         if (c * 32 + e >= valid) s[c][e] = 0xFF800000u;
+                if (kListed && t == 0 && kv_len < p.seq_kv) {
+                    // Value rows behind the length may hold anything, and 0 times NaN is NaN: they are cleared before P is handed
+                    // over, which the issuer waits for before it uses V for either query tile.  (Rows behind seq_kv arrive as zeros.)
+                    const int st = j & 1;
+                    if (!wait_bounded(bar(kVFull + st), static_cast<uint32_t>(j >> 1) & 1u, abort_flag, p.status, 0xB90u | st)) {
+                        ok = false;
+                        break;
+                    }
+                    for (int i = valid * 8 + (warp - 2) * 32 + lane; i < kBKV * 8; i += 4 * 32) {
+#pragma unroll
+                        for (int bx = 0; bx < kBoxes; ++bx) sts128(sV + st * kTile + bx * kBox + i * 16, 0, 0, 0, 0);
+                    }
+                    ptx::fence_proxy_async_smem();
+                }
             }
             float mx8[8];
 #pragma unroll

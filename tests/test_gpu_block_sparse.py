@@ -190,6 +190,26 @@ def test_bad_entries_counts_and_lengths(B):
     assert torch.equal(B.sol_attention_blocks(q, k2, v2, blocks, counts, lens), got)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("junk", [float("nan"), float("inf"), -3.0e38])
+def test_anything_may_stand_behind_the_lengths(B, D, junk):
+    q, k, v = make(3, 520, 900, 2, 1, D, 37)
+    lens = torch.tensor([899, 1, 390], dtype=torch.int32, device="cuda")
+    blocks, counts = random_lists(3, 2, 3, 9, 8, 5)
+    blocks[..., 0] = 7 - 4 * torch.tensor([0, 1, 1], device="cuda", dtype=torch.int32)[:, None, None]    # the ragged block: 7, 3, 3
+    blocks[..., 4] = blocks[..., 0]                                                                     # twice
+    counts.fill_(9)
+    want = check_attend(B, q, k, v, blocks, counts, lens)
+    for b, n in enumerate(lens.tolist()):
+        k[b, n:], v[b, n:] = junk, junk
+    assert torch.equal(B.sol_attention_blocks(q, k, v, blocks, counts, lens), want)
+    a = B.sol_select_blocks(q, k, 3, 1, lens)
+    for b, n in enumerate(lens.tolist()):
+        k[b, n:] = 0
+    c = B.sol_select_blocks(q, k, 3, 1, lens)
+    assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+
+
 def test_sharp_scores_and_output_view(B):
     q, k, v = make(1, 400, 1400, 2, 2, 128, 19)
     q = (q.float() * 6).to(torch.bfloat16)
