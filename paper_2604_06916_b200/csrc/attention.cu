@@ -52,6 +52,7 @@ constexpr int list_bytes(int64_t max_blocks) { return static_cast<int>((2 * max_
 static_assert(smem_bytes(128) + list_bytes(blocks::kMaxKeyBlocks) <= 232448, "shared memory budget with a list");
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 128, kColTile = 256;   // per query tile; P overwrites columns [0, 64) of S
+constexpr uint32_t kColO3 = 384;                             // outputs behind three score tiles (head dimension 64)
 static_assert(smem_bytes(128) <= 232448, "shared memory budget");
 
 #ifdef SOL_TUNING
@@ -109,6 +110,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                  const __grid_constant__ CUtensorMap tm_qb, const __grid_constant__ CUtensorMap tm_kb,
                  const __grid_constant__ CUtensorMap tm_vb, const __grid_constant__ CUtensorMap tm_ob, const Params p) {
     constexpr int kBoxes = kD / 64;
+    // Heads of 64 leave tensor memory for a third score tile.  Over lists it is used: step n = 2 j + t (key tile j, query tile
+    // t) has its scores and P in tile n % 3, so the scores of a query tile's next step are there before its softmax asks.
+    constexpr bool kThree = kListed && kD == 64;
     constexpr int kTile = kBoxes * kBox;    // bytes of a [128][kD] BF16 tile
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem_base = ptx::smem_u32(smem_raw);
@@ -124,7 +128,8 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     auto bar = [&](int i) { return bar_base + 8u * i; };
     // K / V rings: [stage]; S, P, PV-done: [query tile]
     constexpr int kQFull = 0, kKFull = 1, kKEmpty = 3, kVFull = 5, kVEmpty = 7, kSFull = 9, kPFull = 11, kPvDone = 13,
-                  kNumBars = 15;
+                  kNumBars = kThree ? 27 : 15;
+    constexpr int kSOf = 15, kPOf = 19, kPvOf = 23;    // kThree: scores, P and products of [query tile][odd key tile]
     uint32_t *tmem_ptr_smem = reinterpret_cast<uint32_t *>(bar_gen + 8 * kNumBars);
     volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(bar_gen + 8 * kNumBars + 4);
 
@@ -150,7 +155,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         }
     };
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kNumBars; ++i) ptx::mbar_init(bar(i), (i == kPFull || i == kPFull + 1) ? 4 : 1);
+        for (int i = 0; i < kNumBars; ++i) ptx::mbar_init(bar(i), (i == kPFull || i == kPFull + 1 || (kThree && i >= kPOf && i < kPvOf)) ? 4 : 1);
         *abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tmap(tm_q);
@@ -244,6 +249,42 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
             };
             bool ok = wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xB30u) && (!kListed || n_tiles > 0) &&
                       wait_bounded(bar(kKFull), 0, abort_flag, p.status, 0xB31u);
+            if constexpr (kThree) {
+                // Tensor work runs in the order of issue: the scores of step n + 3, written over P of step n, follow its product.
+                // Barriers alternate with j: scores of step n mean that the products up to step n - 3 are done, so of any two phases
+                // of one barrier the earlier one is over before the later one is waited for.
+                const int steps = 2 * n_tiles;
+                auto scores = [&](int n) {
+                    const int t = n & 1, j = n >> 1, st = j & 1;
+                    if (t == 0 && !wait_bounded(bar(kKFull + st), static_cast<uint32_t>(j >> 1) & 1u, abort_flag, p.status, 0xB40u | st)) return false;
+                    ptx::tc_fence_after_sync();
+#pragma unroll
+                    for (int i = 0; i < kD / 16; ++i) {
+                        const uint64_t a = ptx::smem_desc_sw128(sQ + t * kTile) + 2u * i, b = ptx::smem_desc_sw128(sK + st * kTile) + 2u * i;
+                        ptx::mma_bf16(tmem_base + 128 * (n % 3), a, b, idesc_qk, i > 0);
+                    }
+                    ptx::tc_commit(bar(kSOf + 2 * t + st));
+                    if (t == 1) ptx::tc_commit(bar(kKEmpty + st));
+                    return true;
+                };
+                for (int n = 0; ok && n < 3 && n < steps; ++n) ok = scores(n);
+                for (int n = 0; ok && n < steps; ++n) {
+                    const int t = n & 1, j = n >> 1, st = j & 1;
+                    const uint32_t par = static_cast<uint32_t>(j >> 1) & 1u;
+                    if (!wait_bounded(bar(kPOf + 2 * t + st), par, abort_flag, p.status, 0xB60u | t)) break;
+                    if (t == 0 && !wait_bounded(bar(kVFull + st), par, abort_flag, p.status, 0xB70u | st)) break;
+                    ptx::tc_fence_after_sync();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint64_t b = ptx::smem_desc_sw128_mn(sV + st * kTile + i * 2048, kBox, 1024);
+                        ptx::mma_bf16_a_tmem(tmem_base + kColO3 + kD * t, tmem_base + 128 * (n % 3) + 8 * i, b, idesc_pv, j > 0 || i > 0);
+                    }
+                    ptx::tc_commit(bar(kPvOf + 2 * t + st));
+                    if (t == 1) ptx::tc_commit(bar(kVEmpty + st));
+                    if (n + 3 < steps) ok = scores(n + 3);
+                }
+                ok = false;      // the two-tile form below is not for this one
+            }
             if (ok) {
                 ptx::tc_fence_after_sync();
                 issue_qk(0, 0);
@@ -291,22 +332,26 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         const int t = (warp - 2) >> 2;                        // query tile of this warpgroup
         const int quad = warp & 3;
         const int r = quad * 32 + lane;                       // row of the tile = TMEM lane
-        const uint32_t t_lane = tmem_base + t * kColTile + (static_cast<uint32_t>(quad * 32) << 16);
+        const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
+        const uint32_t t_out = (kThree ? tmem_base + kColO3 + kD * t : tmem_base + t * kColTile + kColO) + lanes;
         const uint32_t sw = static_cast<uint32_t>(r & 7);
         const bool tracer = warp == 2;
         float m = -INFINITY, l = 0.0f;
         bool ok = true;
         for (int j = 0; j < n_tiles; ++j) {
             // S_j is complete, and with it every earlier MMA of this tile: O holds the sum over tiles 0..j-1
-            if (!wait_bounded(bar(kSFull + t), static_cast<uint32_t>(j) & 1u, abort_flag, p.status, 0xB80u | t)) {
+            // (three score tiles: the product of step j - 1 may still run)
+            if (!wait_bounded(bar(kThree ? kSOf + 2 * t + (j & 1) : kSFull + t), static_cast<uint32_t>(kThree ? j >> 1 : j) & 1u, abort_flag,
+                              p.status, 0xB80u | t)) {
                 ok = false;
                 break;
             }
             ptx::tc_fence_after_sync();
+            const uint32_t t_s = (kThree ? tmem_base + 128 * ((2 * j + t) % 3) : tmem_base + t * kColTile + kColS) + lanes;
             if (tracer) ATTN_TRACE(4, j);
             uint32_t s[4][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_lane + kColS + 32 * c, s[c]);
+            for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_s + 32 * c, s[c]);
             ptx::tmem_ld_wait();
             if (tracer) ATTN_TRACE(5, j);
             const int valid = kv_len - first_key(j);            // keys of this tile that exist (>= 1)
@@ -368,29 +413,37 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
             m = m_new;
             if (tracer) ATTN_TRACE(7, j);
             if (j > 0 && __any_sync(0xFFFFFFFFu, move)) {
+                if (kThree) {
+                    if (!wait_bounded(bar(kPvOf + 2 * t + ((j - 1) & 1)), static_cast<uint32_t>((j - 1) >> 1) & 1u, abort_flag, p.status, 0xBA8u | t)) {
+                        ok = false;
+                        break;
+                    }
+                    ptx::tc_fence_after_sync();
+                }
 #pragma unroll
                 for (int c = 0; c < kD / 32; ++c) {
                     uint32_t o[32];
-                    ptx::tmem_ld_32x32(t_lane + kColO + 32 * c, o);
+                    ptx::tmem_ld_32x32(t_out + 32 * c, o);
                     ptx::tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                    ptx::tmem_st_32x32(t_lane + kColO + 32 * c, o);
+                    ptx::tmem_st_32x32(t_out + 32 * c, o);
                 }
             }
             if (tracer) ATTN_TRACE(8, j);
             // P row: keys 2c and 2c+1 in column c, over the row's own scores (all of them are in registers)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ptx::tmem_st_32x16(t_lane + kColS + 16 * c, s[c]);
+            for (int c = 0; c < 4; ++c) ptx::tmem_st_32x16(t_s + 16 * c, s[c]);
             ptx::tc_wait_st();
             ptx::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar(kPFull + t));
+            if (lane == 0) ptx::mbar_arrive(bar(kThree ? kPOf + 2 * t + (j & 1) : kPFull + t));
             if (tracer) ATTN_TRACE(9, j);
         }
         const bool empty = kListed && n_tiles == 0;            // no products: Q's place is free once Q has arrived
         if (ok && (empty ? wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xBB0u | t)
-                         : wait_bounded(bar(kPvDone + t), 0, abort_flag, p.status, 0xBA0u | t))) {
+                         : wait_bounded(bar(kThree ? kPvOf + 2 * t + ((n_tiles - 1) & 1) : kPvDone + t),
+                                        kThree ? static_cast<uint32_t>((n_tiles - 1) >> 1) & 1u : 0u, abort_flag, p.status, 0xBA0u | t))) {
             ptx::tc_fence_after_sync();
             const float inv = 1.0f / l;
             if constexpr (kQuantOut) {
@@ -407,7 +460,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 #pragma unroll
                 for (int c = 0; c < kD / 32; ++c) {
                     uint32_t o[32];
-                    ptx::tmem_ld_32x32(t_lane + kColO + 32 * c, o);
+                    ptx::tmem_ld_32x32(t_out + 32 * c, o);
                     ptx::tmem_ld_wait();
                     uint32_t w[16];
                     uint32_t *code = codes + 4 * c;
@@ -452,7 +505,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 #pragma unroll
             for (int c = 0; c < kD / 32; ++c) {
                 uint32_t o[32];
-                ptx::tmem_ld_32x32(t_lane + kColO + 32 * c, o);
+                ptx::tmem_ld_32x32(t_out + 32 * c, o);
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
