@@ -48,11 +48,12 @@ constexpr int kStages = 2;              // K ring and V ring
 constexpr int kThreads = 32 * (2 + 4 * kQTiles);
 constexpr float kLazyLog2 = 8.0f;       // slack of the softmax reference maximum, in powers of two
 constexpr int smem_bytes(int head_dim) { return (kQTiles + 2 * kStages) * (head_dim / 64) * kBox + 256; }
-constexpr int list_bytes(int64_t max_blocks) { return static_cast<int>((2 * max_blocks + 15) / 16 * 16); }   // 16-bit block numbers
+constexpr int list_bytes(int64_t max_blocks) { return 16 + static_cast<int>((2 * max_blocks + 15) / 16 * 16); }   // the list's length, then 16-bit block numbers
 static_assert(smem_bytes(128) + list_bytes(blocks::kMaxKeyBlocks) <= 232448, "shared memory budget with a list");
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 128, kColTile = 256;   // per query tile; P overwrites columns [0, 64) of S
-constexpr uint32_t kColO3 = 384;                             // outputs behind three score tiles (head dimension 64)
+constexpr uint32_t kColO3 = 384;                             // over lists: outputs behind three score tiles (head dimension 64)
+constexpr uint32_t kColAhead = 256;                          // over lists: P, scores, P behind the outputs (head dimension 128)
 static_assert(smem_bytes(128) <= 232448, "shared memory budget");
 
 #ifdef SOL_TUNING
@@ -110,9 +111,15 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                  const __grid_constant__ CUtensorMap tm_qb, const __grid_constant__ CUtensorMap tm_kb,
                  const __grid_constant__ CUtensorMap tm_vb, const __grid_constant__ CUtensorMap tm_ob, const Params p) {
     constexpr int kBoxes = kD / 64;
-    // Heads of 64 leave tensor memory for a third score tile.  Over lists it is used: step n = 2 j + t (key tile j, query tile
-    // t) has its scores and P in tile n % 3, so the scores of a query tile's next step are there before its softmax asks.
+    // Over lists the scores run ahead of the softmax.  Step n = 2 j + t (key tile j, query tile t) needs 128 columns for its
+    // scores and, once these are in registers, 64 for P.  Heads of 64 leave tensor memory for three whole score tiles, taken
+    // in turn; P of step n lies over its scores, and the scores of step n + 3 follow its product.  Heads of 128 leave 256
+    // columns: each query tile has a place of its own for P, and one score tile between them serves every step, free again
+    // as soon as the softmax has loaded it, that is most of a step before its P is there.
     constexpr bool kThree = kListed && kD == 64;
+    auto score_column = [](int n) -> uint32_t { return static_cast<uint32_t>(kThree ? 128 * (n % 3) : kColAhead + 64); };
+    auto p_column = [](int n) -> uint32_t { return static_cast<uint32_t>(kThree ? 128 * (n % 3) : kColAhead + 192 * (n & 1)); };
+    auto output_column = [](int t) -> uint32_t { return static_cast<uint32_t>(kThree ? kColO3 + 64 * t : 128 * t); };
     constexpr int kTile = kBoxes * kBox;    // bytes of a [128][kD] BF16 tile
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem_base = ptx::smem_u32(smem_raw);
@@ -128,15 +135,16 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     auto bar = [&](int i) { return bar_base + 8u * i; };
     // K / V rings: [stage]; S, P, PV-done: [query tile]
     constexpr int kQFull = 0, kKFull = 1, kKEmpty = 3, kVFull = 5, kVEmpty = 7, kSFull = 9, kPFull = 11, kPvDone = 13,
-                  kNumBars = kThree ? 27 : 15;
-    constexpr int kSOf = 15, kPOf = 19, kPvOf = 23;    // kThree: scores, P and products of [query tile][odd key tile]
+                  kNumBars = !kListed ? 15 : kThree ? 27 : 31;
+    constexpr int kSOf = 15, kPOf = 19, kPvOf = 23, kLoadOf = 27;    // kListed: scores, P, products, loads of [query tile][odd key tile]
+    static_assert(8 * kNumBars + 8 <= 256, "barriers, the tensor memory address and the abort flag");
     uint32_t *tmem_ptr_smem = reinterpret_cast<uint32_t *>(bar_gen + 8 * kNumBars);
     volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(bar_gen + 8 * kNumBars + 4);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int q0_joint = blockIdx.x * (kQTiles * kBQ), head = blockIdx.y, batch = blockIdx.z;
-    uint16_t *list = reinterpret_cast<uint16_t *>(smem_raw + (sV + kStages * kTile - smem_base) + 256);
-    uint32_t *list_len = tmem_ptr_smem + 2;
+    uint16_t *list = reinterpret_cast<uint16_t *>(smem_raw + (bar_base - smem_base) + 272);
+    uint32_t *list_len = reinterpret_cast<uint32_t *>(smem_raw + (bar_base - smem_base) + 256);
     const int kv_len = !kListed || p.kv_lens == nullptr ? p.seq_kv : min(max(__ldg(p.kv_lens + batch), 0), p.seq_kv);
     // the CTA's queries come from one stream (the split is a multiple of the CTA's 256 rows)
     const bool q_in_a = q0_joint < p.q_split;
@@ -155,7 +163,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         }
     };
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kNumBars; ++i) ptx::mbar_init(bar(i), (i == kPFull || i == kPFull + 1 || (kThree && i >= kPOf && i < kPvOf)) ? 4 : 1);
+        for (int i = 0; i < kNumBars; ++i) ptx::mbar_init(bar(i), (i == kPFull || i == kPFull + 1 || (i >= kPOf && i < kPvOf) || i >= kLoadOf) ? 4 : 1);
         *abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tmap(tm_q);
@@ -249,10 +257,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
             };
             bool ok = wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xB30u) && (!kListed || n_tiles > 0) &&
                       wait_bounded(bar(kKFull), 0, abort_flag, p.status, 0xB31u);
-            if constexpr (kThree) {
-                // Tensor work runs in the order of issue: the scores of step n + 3, written over P of step n, follow its product.
-                // Barriers alternate with j: scores of step n mean that the products up to step n - 3 are done, so of any two phases
-                // of one barrier the earlier one is over before the later one is waited for.
+            if constexpr (kListed) {
+                // Tensor work runs in the order of issue, so what overwrites P of a step only has to be issued after its product.
+                // Barriers alternate with j: whoever waits for a phase has come by way of the phase before.
                 const int steps = 2 * n_tiles;
                 auto scores = [&](int n) {
                     const int t = n & 1, j = n >> 1, st = j & 1;
@@ -260,30 +267,41 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                     ptx::tc_fence_after_sync();
 #pragma unroll
                     for (int i = 0; i < kD / 16; ++i) {
-                        const uint64_t a = ptx::smem_desc_sw128(sQ + t * kTile) + 2u * i, b = ptx::smem_desc_sw128(sK + st * kTile) + 2u * i;
-                        ptx::mma_bf16(tmem_base + 128 * (n % 3), a, b, idesc_qk, i > 0);
+                        const uint64_t a = ptx::smem_desc_sw128(sQ + t * kTile + (i >> 2) * kBox) + 2u * (i & 3);
+                        const uint64_t b = ptx::smem_desc_sw128(sK + st * kTile + (i >> 2) * kBox) + 2u * (i & 3);
+                        ptx::mma_bf16(tmem_base + score_column(n), a, b, idesc_qk, i > 0);
                     }
                     ptx::tc_commit(bar(kSOf + 2 * t + st));
                     if (t == 1) ptx::tc_commit(bar(kKEmpty + st));
                     return true;
                 };
-                for (int n = 0; ok && n < 3 && n < steps; ++n) ok = scores(n);
-                for (int n = 0; ok && n < steps; ++n) {
+                auto product = [&](int n) {
                     const int t = n & 1, j = n >> 1, st = j & 1;
                     const uint32_t par = static_cast<uint32_t>(j >> 1) & 1u;
-                    if (!wait_bounded(bar(kPOf + 2 * t + st), par, abort_flag, p.status, 0xB60u | t)) break;
-                    if (t == 0 && !wait_bounded(bar(kVFull + st), par, abort_flag, p.status, 0xB70u | st)) break;
+                    if (!wait_bounded(bar(kPOf + 2 * t + st), par, abort_flag, p.status, 0xB60u | t)) return false;
+                    if (t == 0 && !wait_bounded(bar(kVFull + st), par, abort_flag, p.status, 0xB70u | st)) return false;
                     ptx::tc_fence_after_sync();
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const uint64_t b = ptx::smem_desc_sw128_mn(sV + st * kTile + i * 2048, kBox, 1024);
-                        ptx::mma_bf16_a_tmem(tmem_base + kColO3 + kD * t, tmem_base + 128 * (n % 3) + 8 * i, b, idesc_pv, j > 0 || i > 0);
+                        ptx::mma_bf16_a_tmem(tmem_base + output_column(t), tmem_base + p_column(n) + 8 * i, b, idesc_pv, j > 0 || i > 0);
                     }
                     ptx::tc_commit(bar(kPvOf + 2 * t + st));
                     if (t == 1) ptx::tc_commit(bar(kVEmpty + st));
-                    if (n + 3 < steps) ok = scores(n + 3);
+                    return true;
+                };
+                if constexpr (kThree) {
+                    for (int n = 0; ok && n < 3 && n < steps; ++n) ok = scores(n);
+                    for (int n = 0; ok && n < steps; ++n) ok = product(n) && (n + 3 >= steps || scores(n + 3));
+                } else {
+                    auto loaded = [&](int n) {   // the scores of step n are in the softmax's registers
+                        return wait_bounded(bar(kLoadOf + 2 * (n & 1) + ((n >> 1) & 1)), static_cast<uint32_t>(n >> 2) & 1u, abort_flag, p.status, 0xB50u | (n & 1));
+                    };
+                    ok = ok && scores(0);
+                    for (int n = 1; ok && n < steps; ++n) ok = loaded(n - 1) && scores(n) && (n < 2 || product(n - 2));
+                    ok = ok && product(steps - 2) && product(steps - 1);
                 }
-                ok = false;      // the two-tile form below is not for this one
+                ok = false;      // the form below is the dense one
             }
             if (ok) {
                 ptx::tc_fence_after_sync();
@@ -333,26 +351,32 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         const int quad = warp & 3;
         const int r = quad * 32 + lane;                       // row of the tile = TMEM lane
         const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
-        const uint32_t t_out = (kThree ? tmem_base + kColO3 + kD * t : tmem_base + t * kColTile + kColO) + lanes;
+        const uint32_t t_out = tmem_base + (kListed ? output_column(t) : t * kColTile + kColO) + lanes;
         const uint32_t sw = static_cast<uint32_t>(r & 7);
         const bool tracer = warp == 2;
         float m = -INFINITY, l = 0.0f;
         bool ok = true;
         for (int j = 0; j < n_tiles; ++j) {
             // S_j is complete, and with it every earlier MMA of this tile: O holds the sum over tiles 0..j-1
-            // (three score tiles: the product of step j - 1 may still run)
-            if (!wait_bounded(bar(kThree ? kSOf + 2 * t + (j & 1) : kSFull + t), static_cast<uint32_t>(kThree ? j >> 1 : j) & 1u, abort_flag,
+            // (over lists the product of step j - 1 may still run)
+            if (!wait_bounded(bar(kListed ? kSOf + 2 * t + (j & 1) : kSFull + t), static_cast<uint32_t>(kListed ? j >> 1 : j) & 1u, abort_flag,
                               p.status, 0xB80u | t)) {
                 ok = false;
                 break;
             }
             ptx::tc_fence_after_sync();
-            const uint32_t t_s = (kThree ? tmem_base + 128 * ((2 * j + t) % 3) : tmem_base + t * kColTile + kColS) + lanes;
+            const uint32_t t_s = tmem_base + (kListed ? score_column(2 * j + t) : t * kColTile + kColS) + lanes;
+            const uint32_t t_p = tmem_base + (kListed ? p_column(2 * j + t) : t * kColTile + kColS) + lanes;
             if (tracer) ATTN_TRACE(4, j);
             uint32_t s[4][32];
 #pragma unroll
             for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_s + 32 * c, s[c]);
             ptx::tmem_ld_wait();
+            if constexpr (kListed && !kThree) {
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar(kLoadOf + 2 * t + (j & 1)));
+            }
             if (tracer) ATTN_TRACE(5, j);
             const int valid = kv_len - first_key(j);            // keys of this tile that exist (>= 1)
             if (valid < kBKV) {  // the last tile of a ragged sequence: keys that do not exist score -inf
@@ -412,14 +436,14 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
             l = fmaf(l, alpha, sum);
             m = m_new;
             if (tracer) ATTN_TRACE(7, j);
-            if (j > 0 && __any_sync(0xFFFFFFFFu, move)) {
-                if (kThree) {
-                    if (!wait_bounded(bar(kPvOf + 2 * t + ((j - 1) & 1)), static_cast<uint32_t>((j - 1) >> 1) & 1u, abort_flag, p.status, 0xBA8u | t)) {
-                        ok = false;
-                        break;
-                    }
-                    ptx::tc_fence_after_sync();
+            if (kListed && j > 0) {      // the output may be rescaled, and P's place written, once the product before is done
+                if (!wait_bounded(bar(kPvOf + 2 * t + ((j - 1) & 1)), static_cast<uint32_t>((j - 1) >> 1) & 1u, abort_flag, p.status, 0xBA8u | t)) {
+                    ok = false;
+                    break;
                 }
+                ptx::tc_fence_after_sync();
+            }
+            if (j > 0 && __any_sync(0xFFFFFFFFu, move)) {
 #pragma unroll
                 for (int c = 0; c < kD / 32; ++c) {
                     uint32_t o[32];
@@ -433,17 +457,17 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
             if (tracer) ATTN_TRACE(8, j);
             // P row: keys 2c and 2c+1 in column c, over the row's own scores (all of them are in registers)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ptx::tmem_st_32x16(t_s + 16 * c, s[c]);
+            for (int c = 0; c < 4; ++c) ptx::tmem_st_32x16(t_p + 16 * c, s[c]);
             ptx::tc_wait_st();
             ptx::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar(kThree ? kPOf + 2 * t + (j & 1) : kPFull + t));
+            if (lane == 0) ptx::mbar_arrive(bar(kListed ? kPOf + 2 * t + (j & 1) : kPFull + t));
             if (tracer) ATTN_TRACE(9, j);
         }
         const bool empty = kListed && n_tiles == 0;            // no products: Q's place is free once Q has arrived
         if (ok && (empty ? wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xBB0u | t)
-                         : wait_bounded(bar(kThree ? kPvOf + 2 * t + ((n_tiles - 1) & 1) : kPvDone + t),
-                                        kThree ? static_cast<uint32_t>((n_tiles - 1) >> 1) & 1u : 0u, abort_flag, p.status, 0xBA0u | t))) {
+                         : wait_bounded(bar(kListed ? kPvOf + 2 * t + ((n_tiles - 1) & 1) : kPvDone + t),
+                                        kListed ? static_cast<uint32_t>((n_tiles - 1) >> 1) & 1u : 0u, abort_flag, p.status, 0xBA0u | t))) {
             ptx::tc_fence_after_sync();
             const float inv = 1.0f / l;
             if constexpr (kQuantOut) {
