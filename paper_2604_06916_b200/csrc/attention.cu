@@ -52,8 +52,6 @@ constexpr int list_bytes(int64_t max_blocks) { return 16 + static_cast<int>((2 *
 static_assert(smem_bytes(128) + list_bytes(blocks::kMaxKeyBlocks) <= 232448, "shared memory budget with a list");
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 128, kColTile = 256;   // per query tile; P overwrites columns [0, 64) of S
-constexpr uint32_t kColO3 = 384;                             // over lists: outputs behind three score tiles (head dimension 64)
-constexpr uint32_t kColAhead = 256;                          // over lists: P, scores, P behind the outputs (head dimension 128)
 static_assert(smem_bytes(128) <= 232448, "shared memory budget");
 
 #ifdef SOL_TUNING
@@ -112,14 +110,15 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                  const __grid_constant__ CUtensorMap tm_vb, const __grid_constant__ CUtensorMap tm_ob, const Params p) {
     constexpr int kBoxes = kD / 64;
     // Over lists the scores run ahead of the softmax.  Step n = 2 j + t (key tile j, query tile t) needs 128 columns for its
-    // scores and, once these are in registers, 64 for P.  Heads of 64 leave tensor memory for three whole score tiles, taken
-    // in turn; P of step n lies over its scores, and the scores of step n + 3 follow its product.  Heads of 128 leave 256
-    // columns: each query tile has a place of its own for P, and one score tile between them serves every step, free again
-    // as soon as the softmax has loaded it, that is most of a step before its P is there.
-    constexpr bool kThree = kListed && kD == 64;
-    auto score_column = [](int n) -> uint32_t { return static_cast<uint32_t>(kThree ? 128 * (n % 3) : kColAhead + 64); };
-    auto p_column = [](int n) -> uint32_t { return static_cast<uint32_t>(kThree ? 128 * (n % 3) : kColAhead + 192 * (n & 1)); };
-    auto output_column = [](int t) -> uint32_t { return static_cast<uint32_t>(kThree ? kColO3 + 64 * t : 128 * t); };
+    // scores, free again as soon as the softmax has loaded them, and 64 for P.  Each query tile has a place of its own for
+    // P.  Heads of 64 leave room for a score tile for each query tile as well: the scores of its next step are computed
+    // under its softmax.  Heads of 128 leave room for one, which serves both query tiles in turn.
+    constexpr int kScoreTiles = 1;
+    constexpr uint32_t kColP = 2 * kD, kColScores = kTmemCols - 128 * kScoreTiles;     // behind the outputs; at the end
+    auto output_column = [](int t) -> uint32_t { return static_cast<uint32_t>(kD * t); };
+    auto p_column = [](int n) -> uint32_t { return kColP + 64u * (n & 1); };
+    auto score_column = [](int n) -> uint32_t { return kColScores + 128u * (n % kScoreTiles); };
+    static_assert(kColP + 128 <= kColScores, "tensor memory over lists");
     constexpr int kTile = kBoxes * kBox;    // bytes of a [128][kD] BF16 tile
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem_base = ptx::smem_u32(smem_raw);
@@ -135,7 +134,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     auto bar = [&](int i) { return bar_base + 8u * i; };
     // K / V rings: [stage]; S, P, PV-done: [query tile]
     constexpr int kQFull = 0, kKFull = 1, kKEmpty = 3, kVFull = 5, kVEmpty = 7, kSFull = 9, kPFull = 11, kPvDone = 13,
-                  kNumBars = !kListed ? 15 : kThree ? 27 : 31;
+                  kNumBars = kListed ? 31 : 15;
     constexpr int kSOf = 15, kPOf = 19, kPvOf = 23, kLoadOf = 27;    // kListed: scores, P, products, loads of [query tile][odd key tile]
     static_assert(8 * kNumBars + 8 <= 256, "barriers, the tensor memory address and the abort flag");
     uint32_t *tmem_ptr_smem = reinterpret_cast<uint32_t *>(bar_gen + 8 * kNumBars);
@@ -290,17 +289,14 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                     if (t == 1) ptx::tc_commit(bar(kVEmpty + st));
                     return true;
                 };
-                if constexpr (kThree) {
-                    for (int n = 0; ok && n < 3 && n < steps; ++n) ok = scores(n);
-                    for (int n = 0; ok && n < steps; ++n) ok = product(n) && (n + 3 >= steps || scores(n + 3));
-                } else {
-                    auto loaded = [&](int n) {   // the scores of step n are in the softmax's registers
-                        return wait_bounded(bar(kLoadOf + 2 * (n & 1) + ((n >> 1) & 1)), static_cast<uint32_t>(n >> 2) & 1u, abort_flag, p.status, 0xB50u | (n & 1));
-                    };
-                    ok = ok && scores(0);
-                    for (int n = 1; ok && n < steps; ++n) ok = loaded(n - 1) && scores(n) && (n < 2 || product(n - 2));
-                    ok = ok && product(steps - 2) && product(steps - 1);
-                }
+                auto loaded = [&](int n) {   // the scores of step n are in the softmax's registers
+                    return wait_bounded(bar(kLoadOf + 2 * (n & 1) + ((n >> 1) & 1)), static_cast<uint32_t>(n >> 2) & 1u, abort_flag, p.status, 0xB50u | (n & 1));
+                };
+                for (int n = 0; ok && n < kScoreTiles; ++n) ok = scores(n);
+                // a score tile is refilled when it is free; then comes the product whose P is the next to arrive
+                constexpr int kLag = kScoreTiles + 1;
+                for (int n = kScoreTiles; ok && n < steps; ++n) ok = loaded(n - kScoreTiles) && scores(n) && (n < kLag || product(n - kLag));
+                for (int n = max(steps - kLag, 0); ok && n < steps; ++n) ok = product(n);
                 ok = false;      // the form below is the dense one
             }
             if (ok) {
@@ -372,7 +368,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 #pragma unroll
             for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_s + 32 * c, s[c]);
             ptx::tmem_ld_wait();
-            if constexpr (kListed && !kThree) {
+            if constexpr (kListed) {
                 ptx::tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar(kLoadOf + 2 * t + (j & 1)));
