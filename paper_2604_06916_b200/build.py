@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["api.cu", "quantize.cu", "gemm.cu", "gemm_pair.cu", "gemm_pair_fp4.cu", "static_scratch.cu",
-           "lora_merge.cu", "selection.cu", "layernorm_quantize.cu", "attention.cu", "qk_rotary.cu", "matvec.cu", "select_blocks.cu"]
+           "lora_merge.cu", "selection.cu", "layernorm_quantize.cu", "attention.cu", "attention_blocks.cu", "qk_rotary.cu", "matvec.cu", "select_blocks.cu"]
 LIB = os.path.join(HERE, "libsol_nvfp4.so")
 
 

@@ -585,7 +585,7 @@ sol_status_t sol_attention_bf16(const void *q, const void *k, const void *v, voi
     sol_status_t st = check_arch(&dev);
     if (st != SOL_OK) return st;
     const attn::Stream b{q, k, v, out, seq_q, seq_kv, ld_q, ld_k, ld_v, ld_out};
-    return attn::launch_attention(nullptr, b, batch, heads, head_dim, nullptr, nullptr, static_cast<cudaStream_t>(stream));
+    return attn::launch_attention(nullptr, b, batch, heads, head_dim, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 sol_status_t sol_attention_nvfp4_out(const void *q, const void *k, const void *v, int64_t batch, int64_t seq_q,
@@ -610,7 +610,7 @@ sol_status_t sol_attention_nvfp4_out(const void *q, const void *k, const void *v
     if (st != SOL_OK) return st;
     const attn::Stream b{q, k, v, nullptr, seq_q, seq_kv, ld_q, ld_k, ld_v, cols};
     const attn::QuantDest qd{q_dest, sf_dest, out_tscale, reinterpret_cast<uint32_t *>(amax_out), dest_K, dest_col0};
-    return attn::launch_attention(nullptr, b, batch, heads, head_dim, &qd, nullptr, static_cast<cudaStream_t>(stream));
+    return attn::launch_attention(nullptr, b, batch, heads, head_dim, &qd, static_cast<cudaStream_t>(stream));
 }
 
 sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const sol_attention_stream_t *second,
@@ -636,7 +636,7 @@ sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const
                          first->ld_q, first->ld_k, first->ld_v, first->ld_out};
     const attn::Stream b{second->q, second->k, second->v, second->out, second->seq, second->seq,
                          second->ld_q, second->ld_k, second->ld_v, second->ld_out};
-    return attn::launch_attention(&a, b, batch, heads, head_dim, nullptr, nullptr, static_cast<cudaStream_t>(stream));
+    return attn::launch_attention(&a, b, batch, heads, head_dim, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 namespace {
@@ -690,7 +690,7 @@ sol_status_t sol_attention_blocks(const void *q, const void *k, const void *v, v
     if (st != SOL_OK) return st;
     const attn::Stream b{q, k, v, out, seq_q, seq_kv, ld_q, ld_k, ld_v, ld_out};
     const attn::BlockLists lists{block_lists, counts, kv_lens, max_blocks, heads_kv};
-    return attn::launch_attention(nullptr, b, batch, heads, head_dim, nullptr, &lists, static_cast<cudaStream_t>(stream));
+    return attn::launch_attention_blocks(b, lists, batch, heads, head_dim, static_cast<cudaStream_t>(stream), dev);
 }
 
 namespace {

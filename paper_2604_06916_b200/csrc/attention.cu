@@ -18,16 +18,6 @@
 // tensor pipe works for one tile while the other is in its softmax.  TMEM: S_t/P_t and O_t, 128
 // columns each.  The epilogue divides by l and leaves through TMA stores (staged where Q_t was).
 //
-// Over listed key blocks (kListed) the tiles are the entries of a list per query block: a warp copies the entries that
-// name existing keys into shared memory while Q loads, and tile j is the j-th of them; a list without any leaves
-// zeros.  A key / value head may serve several query heads.  Measured: 4 x 4608 tokens, 24 heads x 128, 9 of 36 blocks,
-// 267 us = 980 TFLOP/s (the dense form reaches 1.05 to 1.1 PFLOP/s on 36 tiles; a CTA's way in and out costs 2.5 us, over
-// nine tiles of 2.3 us); 2 x 4429, 38 heads x 64, 8 blocks, 184 us.  Per tile of 3600 cycles a query tile's chain
-// is 1430 of exponentials, 500 of loads, maximum and stores, 400 until the issuer sees P, 1000 of P V and the next scores.
-// Built and not kept: two threads per row and sixteen softmax warps (345 us: 96 registers, and the two halves have to agree
-// on the maximum every tile); P handed over in two halves so that P V starts under the second half's
-// exponentials (277 us); three-input maxima and two-lane sums (no change).
-//
 // Warps: 0 = TMA producer, 1 = TMEM owner and MMA issuer, 2..5 and 6..9 = softmax / epilogue of query
 // tile 0 and 1 (one warp per TMEM lane quadrant).  Every mbarrier wait is bounded.
 #include "gemm_common.cuh"
@@ -48,8 +38,6 @@ constexpr int kStages = 2;              // K ring and V ring
 constexpr int kThreads = 32 * (2 + 4 * kQTiles);
 constexpr float kLazyLog2 = 8.0f;       // slack of the softmax reference maximum, in powers of two
 constexpr int smem_bytes(int head_dim) { return (kQTiles + 2 * kStages) * (head_dim / 64) * kBox + 256; }
-constexpr int list_bytes(int64_t max_blocks) { return 16 + static_cast<int>((2 * max_blocks + 15) / 16 * 16); }   // the list's length, then 16-bit block numbers
-static_assert(smem_bytes(128) + list_bytes(blocks::kMaxKeyBlocks) <= 232448, "shared memory budget with a list");
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 128, kColTile = 256;   // per query tile; P overwrites columns [0, 64) of S
 static_assert(smem_bytes(128) <= 232448, "shared memory budget");
@@ -76,12 +64,6 @@ struct Params {
     int dest_pitch;        // dest_K / 2
     int dest_col0;         // first destination column of head 0
     int dest_chunks_k;     // dest_K / 64
-    // listed key blocks (kListed)
-    const int32_t *blocks;
-    const int32_t *counts;
-    const int32_t *kv_lens;   // null: every batch element has seq_kv keys
-    int max_blocks;
-    int group;             // query heads per key / value head
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -101,24 +83,13 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, ui
 // kD: head dimension, 64 or 128 (a tile of kD columns is kD / 64 boxes of [128 rows][64 BF16]).
 // kQuantOut: the output leaves as the next linear's NVFP4 activations (h = bf16(O / l), then the
 // quantizer's FP32 sequence per 16 columns) instead of BF16 -- one stream only.
-// kListed: over the listed key blocks -- one stream, BF16 output.
-template <int kD, bool kQuantOut, bool kListed>
+template <int kD, bool kQuantOut>
 __global__ void __launch_bounds__(kThreads, 1)
 attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constant__ CUtensorMap tm_ka,
                  const __grid_constant__ CUtensorMap tm_va, const __grid_constant__ CUtensorMap tm_oa,
                  const __grid_constant__ CUtensorMap tm_qb, const __grid_constant__ CUtensorMap tm_kb,
                  const __grid_constant__ CUtensorMap tm_vb, const __grid_constant__ CUtensorMap tm_ob, const Params p) {
     constexpr int kBoxes = kD / 64;
-    // Over lists the scores run ahead of the softmax.  Step n = 2 j + t (key tile j, query tile t) needs 128 columns for its
-    // scores, free again as soon as the softmax has loaded them, and 64 for P.  Each query tile has a place of its own for
-    // P.  Heads of 64 leave room for a score tile for each query tile as well: the scores of its next step are computed
-    // under its softmax.  Heads of 128 leave room for one, which serves both query tiles in turn.
-    constexpr int kScoreTiles = 1;
-    constexpr uint32_t kColP = 2 * kD, kColScores = kTmemCols - 128 * kScoreTiles;     // behind the outputs; at the end
-    auto output_column = [](int t) -> uint32_t { return static_cast<uint32_t>(kD * t); };
-    auto p_column = [](int n) -> uint32_t { return kColP + 64u * (n & 1); };
-    auto score_column = [](int n) -> uint32_t { return kColScores + 128u * (n % kScoreTiles); };
-    static_assert(kColP + 128 <= kColScores, "tensor memory over lists");
     constexpr int kTile = kBoxes * kBox;    // bytes of a [128][kD] BF16 tile
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem_base = ptx::smem_u32(smem_raw);
@@ -134,17 +105,13 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     auto bar = [&](int i) { return bar_base + 8u * i; };
     // K / V rings: [stage]; S, P, PV-done: [query tile]
     constexpr int kQFull = 0, kKFull = 1, kKEmpty = 3, kVFull = 5, kVEmpty = 7, kSFull = 9, kPFull = 11, kPvDone = 13,
-                  kNumBars = kListed ? 31 : 15;
-    constexpr int kSOf = 15, kPOf = 19, kPvOf = 23, kLoadOf = 27;    // kListed: scores, P, products, loads of [query tile][odd key tile]
-    static_assert(8 * kNumBars + 8 <= 256, "barriers, the tensor memory address and the abort flag");
+                  kNumBars = 15;
     uint32_t *tmem_ptr_smem = reinterpret_cast<uint32_t *>(bar_gen + 8 * kNumBars);
     volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(bar_gen + 8 * kNumBars + 4);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int q0_joint = blockIdx.x * (kQTiles * kBQ), head = blockIdx.y, batch = blockIdx.z;
-    uint16_t *list = reinterpret_cast<uint16_t *>(smem_raw + (bar_base - smem_base) + 272);
-    uint32_t *list_len = reinterpret_cast<uint32_t *>(smem_raw + (bar_base - smem_base) + 256);
-    const int kv_len = !kListed || p.kv_lens == nullptr ? p.seq_kv : min(max(__ldg(p.kv_lens + batch), 0), p.seq_kv);
+    const int n_tiles = (p.seq_kv + kBKV - 1) / kBKV;
     // the CTA's queries come from one stream (the split is a multiple of the CTA's 256 rows)
     const bool q_in_a = q0_joint < p.q_split;
     const CUtensorMap *tm_q = q_in_a ? &tm_qa : &tm_qb;
@@ -152,44 +119,14 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     const int q0 = q_in_a ? q0_joint : q0_joint - p.q_split;                 // row within its stream
     const int q_rows = q_in_a ? p.q_split : p.seq_q - p.q_split;             // rows of that stream
 
-    auto load_q = [&]() {
-        ptx::mbar_arrive_expect_tx(bar(kQFull), kQTiles * kTile);
-#pragma unroll
-        for (int t = 0; t < kQTiles; ++t) {
-#pragma unroll
-            for (int bx = 0; bx < kBoxes; ++bx)
-                ptx::tma_load_3d(sQ + t * kTile + bx * kBox, tm_q, head * kD + 64 * bx, q0 + t * kBQ, batch, bar(kQFull));
-        }
-    };
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kNumBars; ++i) ptx::mbar_init(bar(i), (i == kPFull || i == kPFull + 1 || (i >= kPOf && i < kPvOf) || i >= kLoadOf) ? 4 : 1);
+        for (int i = 0; i < kNumBars; ++i) ptx::mbar_init(bar(i), (i == kPFull || i == kPFull + 1) ? 4 : 1);
         *abort_flag = 0;
         ptx::fence_mbar_init();
         ptx::prefetch_tmap(tm_q);
         ptx::prefetch_tmap(tm_o);
         ptx::prefetch_tmap(&tm_kb);
         ptx::prefetch_tmap(&tm_vb);
-        if (kListed) {                // the list takes a while: Q need not wait for it
-            ptx::fence_proxy_async_smem();
-            load_q();
-        }
-    }
-    if (kListed && warp == 2) {   // the entries that name existing keys, in their order
-        const int64_t row = (static_cast<int64_t>(batch) * gridDim.y + head) * gridDim.x + blockIdx.x;
-        const int32_t *from = p.blocks + row * p.max_blocks;
-        int next = lane < p.max_blocks ? __ldg(from + lane) : -1;       // not after the count: one latency, not two
-        const int named = min(max(__ldg(p.counts + row), 0), p.max_blocks);
-        const int existing = (kv_len + kBKV - 1) / kBKV;
-        int kept = 0;
-        for (int i0 = 0; i0 < named; i0 += 32) {
-            const int e = i0 + lane < named ? next : -1;
-            if (i0 + 32 + lane < named) next = __ldg(from + i0 + 32 + lane);
-            const bool keep = e >= 0 && e < existing;
-            const uint32_t mask = __ballot_sync(0xFFFFFFFFu, keep);
-            if (keep) list[kept + __popc(mask & ((1u << lane) - 1u))] = static_cast<uint16_t>(e);
-            kept += __popc(mask);
-        }
-        if (lane == 0) *list_len = static_cast<uint32_t>(kept);
     }
     if (warp == 1) {
         ptx::tmem_alloc(ptx::smem_u32(tmem_ptr_smem), kTmemCols);
@@ -199,14 +136,18 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     __syncthreads();
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_ptr_smem;
-    const int n_tiles = kListed ? static_cast<int>(*list_len) : (p.seq_kv + kBKV - 1) / kBKV;
-    auto first_key = [&](int j) { return kListed ? list[j] * kBKV : j * kBKV; };   // of tile j
 
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer
         if (ptx::elect_one()) {
-            const int x0 = head * kD, x0_kv = kListed ? head / p.group * kD : x0;
-            if (!kListed) load_q();
+            const int x0 = head * kD;
+            ptx::mbar_arrive_expect_tx(bar(kQFull), kQTiles * kTile);
+#pragma unroll
+            for (int t = 0; t < kQTiles; ++t) {
+#pragma unroll
+                for (int bx = 0; bx < kBoxes; ++bx)
+                    ptx::tma_load_3d(sQ + t * kTile + bx * kBox, tm_q, x0 + 64 * bx, q0 + t * kBQ, batch, bar(kQFull));
+            }
             for (int j = 0; j < n_tiles; ++j) {
                 const int st = j & 1;
                 const uint32_t par = static_cast<uint32_t>(j >> 1) & 1u;
@@ -215,18 +156,18 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                 ptx::mbar_arrive_expect_tx(bar(kKFull + st), kTile);
                 // key tile j of the joint sequence: stream a up to the split (a multiple of the tile), then stream b
                 const bool kv_in_a = j * kBKV < p.kv_split;
-                const int kv0 = kListed || kv_in_a ? first_key(j) : j * kBKV - p.kv_split;
+                const int kv0 = kv_in_a ? j * kBKV : j * kBKV - p.kv_split;
                 const CUtensorMap *tm_k = kv_in_a ? &tm_ka : &tm_kb;
                 const CUtensorMap *tm_v = kv_in_a ? &tm_va : &tm_vb;
 #pragma unroll
                 for (int bx = 0; bx < kBoxes; ++bx)
-                    ptx::tma_load_3d(sK + st * kTile + bx * kBox, tm_k, x0_kv + 64 * bx, kv0, batch, bar(kKFull + st));
+                    ptx::tma_load_3d(sK + st * kTile + bx * kBox, tm_k, x0 + 64 * bx, kv0, batch, bar(kKFull + st));
                 if (!wait_bounded(bar(kVEmpty + st), par ^ 1u, abort_flag, p.status, 0xB20u | st)) break;
                 ATTN_TRACE(11, j);
                 ptx::mbar_arrive_expect_tx(bar(kVFull + st), kTile);
 #pragma unroll
                 for (int bx = 0; bx < kBoxes; ++bx)
-                    ptx::tma_load_3d(sV + st * kTile + bx * kBox, tm_v, x0_kv + 64 * bx, kv0, batch, bar(kVFull + st));
+                    ptx::tma_load_3d(sV + st * kTile + bx * kBox, tm_v, x0 + 64 * bx, kv0, batch, bar(kVFull + st));
             }
         }
         __syncwarp();
@@ -254,51 +195,8 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
                                          idesc_pv, acc || i > 0);
                 }
             };
-            bool ok = wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xB30u) && (!kListed || n_tiles > 0) &&
+            bool ok = wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xB30u) &&
                       wait_bounded(bar(kKFull), 0, abort_flag, p.status, 0xB31u);
-            if constexpr (kListed) {
-                // Tensor work runs in the order of issue, so what overwrites P of a step only has to be issued after its product.
-                // Barriers alternate with j: whoever waits for a phase has come by way of the phase before.
-                const int steps = 2 * n_tiles;
-                auto scores = [&](int n) {
-                    const int t = n & 1, j = n >> 1, st = j & 1;
-                    if (t == 0 && !wait_bounded(bar(kKFull + st), static_cast<uint32_t>(j >> 1) & 1u, abort_flag, p.status, 0xB40u | st)) return false;
-                    ptx::tc_fence_after_sync();
-#pragma unroll
-                    for (int i = 0; i < kD / 16; ++i) {
-                        const uint64_t a = ptx::smem_desc_sw128(sQ + t * kTile + (i >> 2) * kBox) + 2u * (i & 3);
-                        const uint64_t b = ptx::smem_desc_sw128(sK + st * kTile + (i >> 2) * kBox) + 2u * (i & 3);
-                        ptx::mma_bf16(tmem_base + score_column(n), a, b, idesc_qk, i > 0);
-                    }
-                    ptx::tc_commit(bar(kSOf + 2 * t + st));
-                    if (t == 1) ptx::tc_commit(bar(kKEmpty + st));
-                    return true;
-                };
-                auto product = [&](int n) {
-                    const int t = n & 1, j = n >> 1, st = j & 1;
-                    const uint32_t par = static_cast<uint32_t>(j >> 1) & 1u;
-                    if (!wait_bounded(bar(kPOf + 2 * t + st), par, abort_flag, p.status, 0xB60u | t)) return false;
-                    if (t == 0 && !wait_bounded(bar(kVFull + st), par, abort_flag, p.status, 0xB70u | st)) return false;
-                    ptx::tc_fence_after_sync();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const uint64_t b = ptx::smem_desc_sw128_mn(sV + st * kTile + i * 2048, kBox, 1024);
-                        ptx::mma_bf16_a_tmem(tmem_base + output_column(t), tmem_base + p_column(n) + 8 * i, b, idesc_pv, j > 0 || i > 0);
-                    }
-                    ptx::tc_commit(bar(kPvOf + 2 * t + st));
-                    if (t == 1) ptx::tc_commit(bar(kVEmpty + st));
-                    return true;
-                };
-                auto loaded = [&](int n) {   // the scores of step n are in the softmax's registers
-                    return wait_bounded(bar(kLoadOf + 2 * (n & 1) + ((n >> 1) & 1)), static_cast<uint32_t>(n >> 2) & 1u, abort_flag, p.status, 0xB50u | (n & 1));
-                };
-                for (int n = 0; ok && n < kScoreTiles; ++n) ok = scores(n);
-                // a score tile is refilled when it is free; then comes the product whose P is the next to arrive
-                constexpr int kLag = kScoreTiles + 1;
-                for (int n = kScoreTiles; ok && n < steps; ++n) ok = loaded(n - kScoreTiles) && scores(n) && (n < kLag || product(n - kLag));
-                for (int n = max(steps - kLag, 0); ok && n < steps; ++n) ok = product(n);
-                ok = false;      // the form below is the dense one
-            }
             if (ok) {
                 ptx::tc_fence_after_sync();
                 issue_qk(0, 0);
@@ -346,55 +244,31 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
         const int t = (warp - 2) >> 2;                        // query tile of this warpgroup
         const int quad = warp & 3;
         const int r = quad * 32 + lane;                       // row of the tile = TMEM lane
-        const uint32_t lanes = static_cast<uint32_t>(quad * 32) << 16;
-        const uint32_t t_out = tmem_base + (kListed ? output_column(t) : t * kColTile + kColO) + lanes;
+        const uint32_t t_lane = tmem_base + t * kColTile + (static_cast<uint32_t>(quad * 32) << 16);
         const uint32_t sw = static_cast<uint32_t>(r & 7);
         const bool tracer = warp == 2;
         float m = -INFINITY, l = 0.0f;
         bool ok = true;
         for (int j = 0; j < n_tiles; ++j) {
             // S_j is complete, and with it every earlier MMA of this tile: O holds the sum over tiles 0..j-1
-            // (over lists the product of step j - 1 may still run)
-            if (!wait_bounded(bar(kListed ? kSOf + 2 * t + (j & 1) : kSFull + t), static_cast<uint32_t>(kListed ? j >> 1 : j) & 1u, abort_flag,
-                              p.status, 0xB80u | t)) {
+            if (!wait_bounded(bar(kSFull + t), static_cast<uint32_t>(j) & 1u, abort_flag, p.status, 0xB80u | t)) {
                 ok = false;
                 break;
             }
             ptx::tc_fence_after_sync();
-            const uint32_t t_s = tmem_base + (kListed ? score_column(2 * j + t) : t * kColTile + kColS) + lanes;
-            const uint32_t t_p = tmem_base + (kListed ? p_column(2 * j + t) : t * kColTile + kColS) + lanes;
             if (tracer) ATTN_TRACE(4, j);
             uint32_t s[4][32];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_s + 32 * c, s[c]);
+            for (int c = 0; c < 4; ++c) ptx::tmem_ld_32x32(t_lane + kColS + 32 * c, s[c]);
             ptx::tmem_ld_wait();
-            if constexpr (kListed) {
-                ptx::tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(bar(kLoadOf + 2 * t + (j & 1)));
-            }
             if (tracer) ATTN_TRACE(5, j);
-            const int valid = kv_len - first_key(j);            // keys of this tile that exist (>= 1)
+            const int valid = p.seq_kv - j * kBKV;              // keys of this tile that exist (>= 1)
             if (valid < kBKV) {  // the last tile of a ragged sequence: keys that do not exist score -inf
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int e = 0; e < 32; ++e)
                         if (c * 32 + e >= valid) s[c][e] = 0xFF800000u;
-                if (kListed && t == 0 && kv_len < p.seq_kv) {
-                    // Value rows behind the length may hold anything, and 0 times NaN is NaN: they are cleared before P is handed
-                    // over, which the issuer waits for before it uses V for either query tile.  (Rows behind seq_kv arrive as zeros.)
-                    const int st = j & 1;
-                    if (!wait_bounded(bar(kVFull + st), static_cast<uint32_t>(j >> 1) & 1u, abort_flag, p.status, 0xB90u | st)) {
-                        ok = false;
-                        break;
-                    }
-                    for (int i = valid * 8 + (warp - 2) * 32 + lane; i < kBKV * 8; i += 4 * 32) {
-#pragma unroll
-                        for (int bx = 0; bx < kBoxes; ++bx) sts128(sV + st * kTile + bx * kBox + i * 16, 0, 0, 0, 0);
-                    }
-                    ptx::fence_proxy_async_smem();
-                }
             }
             float mx8[8];
 #pragma unroll
@@ -432,38 +306,28 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
             l = fmaf(l, alpha, sum);
             m = m_new;
             if (tracer) ATTN_TRACE(7, j);
-            if (kListed && j > 0) {      // the output may be rescaled, and P's place written, once the product before is done
-                if (!wait_bounded(bar(kPvOf + 2 * t + ((j - 1) & 1)), static_cast<uint32_t>((j - 1) >> 1) & 1u, abort_flag, p.status, 0xBA8u | t)) {
-                    ok = false;
-                    break;
-                }
-                ptx::tc_fence_after_sync();
-            }
             if (j > 0 && __any_sync(0xFFFFFFFFu, move)) {
 #pragma unroll
                 for (int c = 0; c < kD / 32; ++c) {
                     uint32_t o[32];
-                    ptx::tmem_ld_32x32(t_out + 32 * c, o);
+                    ptx::tmem_ld_32x32(t_lane + kColO + 32 * c, o);
                     ptx::tmem_ld_wait();
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
-                    ptx::tmem_st_32x32(t_out + 32 * c, o);
+                    ptx::tmem_st_32x32(t_lane + kColO + 32 * c, o);
                 }
             }
             if (tracer) ATTN_TRACE(8, j);
             // P row: keys 2c and 2c+1 in column c, over the row's own scores (all of them are in registers)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ptx::tmem_st_32x16(t_p + 16 * c, s[c]);
+            for (int c = 0; c < 4; ++c) ptx::tmem_st_32x16(t_lane + kColS + 16 * c, s[c]);
             ptx::tc_wait_st();
             ptx::tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar(kListed ? kPOf + 2 * t + (j & 1) : kPFull + t));
+            if (lane == 0) ptx::mbar_arrive(bar(kPFull + t));
             if (tracer) ATTN_TRACE(9, j);
         }
-        const bool empty = kListed && n_tiles == 0;            // no products: Q's place is free once Q has arrived
-        if (ok && (empty ? wait_bounded(bar(kQFull), 0, abort_flag, p.status, 0xBB0u | t)
-                         : wait_bounded(bar(kListed ? kPvOf + 2 * t + ((n_tiles - 1) & 1) : kPvDone + t),
-                                        kListed ? static_cast<uint32_t>((n_tiles - 1) >> 1) & 1u : 0u, abort_flag, p.status, 0xBA0u | t))) {
+        if (ok && wait_bounded(bar(kPvDone + t), 0, abort_flag, p.status, 0xBA0u | t)) {
             ptx::tc_fence_after_sync();
             const float inv = 1.0f / l;
             if constexpr (kQuantOut) {
@@ -480,7 +344,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 #pragma unroll
                 for (int c = 0; c < kD / 32; ++c) {
                     uint32_t o[32];
-                    ptx::tmem_ld_32x32(t_out + 32 * c, o);
+                    ptx::tmem_ld_32x32(t_lane + kColO + 32 * c, o);
                     ptx::tmem_ld_wait();
                     uint32_t w[16];
                     uint32_t *code = codes + 4 * c;
@@ -525,16 +389,14 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 #pragma unroll
             for (int c = 0; c < kD / 32; ++c) {
                 uint32_t o[32];
-                ptx::tmem_ld_32x32(t_out + 32 * c, o);
+                ptx::tmem_ld_32x32(t_lane + kColO + 32 * c, o);
                 ptx::tmem_ld_wait();
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     uint32_t w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                    for (int e = 0; e < 4; ++e)
                         w[e] = pack_bf16(__uint_as_float(o[8 * q + 2 * e]) * inv, __uint_as_float(o[8 * q + 2 * e + 1]) * inv);
-                        if (kListed && empty) w[e] = 0;        // O was never written
-                    }
                     const int ch = c * 4 + q;
                     sts128(o_row + (ch >> 3) * kBox + ((static_cast<uint32_t>(ch & 7) ^ sw) << 4), w[0], w[1], w[2], w[3]);
                 }
@@ -565,26 +427,20 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
 }  // namespace
 
 sol_status_t launch_attention(const Stream *a, const Stream &b, int64_t batch, int64_t heads, int64_t head_dim,
-                              const QuantDest *qd, const BlockLists *lists, cudaStream_t stream) {
+                              const QuantDest *qd, cudaStream_t stream) {
     CUtensorMap tm[8];
     const uint64_t cols = static_cast<uint64_t>(heads) * static_cast<uint64_t>(head_dim);
-    const uint64_t cols_kv = lists != nullptr ? static_cast<uint64_t>(lists->heads_kv) * static_cast<uint64_t>(head_dim) : cols;
-    auto make = [&](CUtensorMap *t, const void *base, int64_t seq, int64_t ld, uint32_t box_rows, uint64_t columns) {
-        return make_tmap_3d_bf16(t, base, columns, static_cast<uint64_t>(seq), static_cast<uint64_t>(batch),
+    auto make = [&](CUtensorMap *t, const void *base, int64_t seq, int64_t ld, uint32_t box_rows) {
+        return make_tmap_3d_bf16(t, base, cols, static_cast<uint64_t>(seq), static_cast<uint64_t>(batch),
                                  static_cast<uint64_t>(ld) * 2, static_cast<uint64_t>(seq) * ld * 2, 64, box_rows);
     };
     auto make4 = [&](CUtensorMap *t, const Stream &s) {
         // a quantized destination has no BF16 output tensor: the (unused) output map is a copy of the query map
-        return make(t, s.q, s.seq_q, s.ld_q, kBQ, cols) && make(t + 1, s.k, s.seq_kv, s.ld_k, kBKV, cols_kv) &&
-               make(t + 2, s.v, s.seq_kv, s.ld_v, kBKV, cols_kv) &&
-               (qd != nullptr ? make(t + 3, s.q, s.seq_q, s.ld_q, 32, cols) : make(t + 3, s.out, s.seq_q, s.ld_out, 32, cols));
+        return make(t, s.q, s.seq_q, s.ld_q, kBQ) && make(t + 1, s.k, s.seq_kv, s.ld_k, kBKV) &&
+               make(t + 2, s.v, s.seq_kv, s.ld_v, kBKV) &&
+               (qd != nullptr ? make(t + 3, s.q, s.seq_q, s.ld_q, 32) : make(t + 3, s.out, s.seq_q, s.ld_out, 32));
     };
-    if (!make4(tm + 4, b)) return SOL_ERR_CUDA;
-    if (a == nullptr) {  // one stream: the a maps are never used
-        for (int i = 0; i < 4; ++i) tm[i] = tm[4 + i];
-    } else if (!make4(tm, *a)) {
-        return SOL_ERR_CUDA;
-    }
+    if (!make4(tm + 4, b) || !make4(tm, a != nullptr ? *a : b)) return SOL_ERR_CUDA;  // one stream: the a maps are never used
     Params p{};
     p.q_split = a != nullptr ? static_cast<int>(a->seq_q) : 0;
     p.kv_split = a != nullptr ? static_cast<int>(a->seq_kv) : 0;
@@ -601,25 +457,16 @@ sol_status_t launch_attention(const Stream *a, const Stream &b, int64_t batch, i
         p.dest_col0 = static_cast<int>(qd->dest_col0);
         p.dest_chunks_k = static_cast<int>(qd->dest_K / 64);
     }
-    if (lists != nullptr) {
-        p.blocks = lists->blocks;
-        p.counts = lists->counts;
-        p.kv_lens = lists->kv_lens;
-        p.max_blocks = static_cast<int>(lists->max_blocks);
-        p.group = static_cast<int>(heads / lists->heads_kv);
-    }
-    const bool quant = qd != nullptr, wide = head_dim == 128, listed = lists != nullptr;
-    auto kern = wide ? (listed ? attention_kernel<128, false, true> : quant ? attention_kernel<128, true, false> : attention_kernel<128, false, false>)
-                     : (listed ? attention_kernel<64, false, true> : quant ? attention_kernel<64, true, false> : attention_kernel<64, false, false>);
-    const int fixed = smem_bytes(static_cast<int>(head_dim));
-    const int smem = fixed + (listed ? list_bytes(lists->max_blocks) : 0);
-    const int smem_most = fixed + (listed ? list_bytes(blocks::kMaxKeyBlocks) : 0);
-    static bool configured[6][64] = {};
+    const bool quant = qd != nullptr, wide = head_dim == 128;
+    auto kern = wide ? (quant ? attention_kernel<128, true> : attention_kernel<128, false>)
+                     : (quant ? attention_kernel<64, true> : attention_kernel<64, false>);
+    const int smem = smem_bytes(static_cast<int>(head_dim));
+    static bool configured[4][64] = {};
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return SOL_ERR_CUDA;
-    const int slot = (wide ? 3 : 0) + (listed ? 2 : quant ? 1 : 0);
+    const int slot = (wide ? 2 : 0) + (quant ? 1 : 0);
     if (!configured[slot][dev]) {
-        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_most) != cudaSuccess)
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
             return SOL_ERR_CUDA;
         configured[slot][dev] = true;
     }

@@ -148,10 +148,12 @@ struct QuantDest {   // NVFP4 destination of the output: columns [dest_col0, des
     int64_t dest_K, dest_col0;
 };
 // Attention over the concatenation (a, then b) of two token streams, or over b alone when a is null;
-// with `qd` (one stream only) the output is quantized into `qd` instead of written as BF16; with `lists` (one stream
-// only, BF16 output) over the listed key blocks.
+// with `qd` (one stream only) the output is quantized into `qd` instead of written as BF16.
 sol_status_t launch_attention(const Stream *a, const Stream &b, int64_t batch, int64_t heads, int64_t head_dim,
-                              const QuantDest *qd, const BlockLists *lists, cudaStream_t stream);
+                              const QuantDest *qd, cudaStream_t stream);
+// Attention of one stream over the listed key blocks.
+sol_status_t launch_attention_blocks(const Stream &s, const BlockLists &lists, int64_t batch, int64_t heads, int64_t head_dim,
+                                     cudaStream_t stream, const DeviceInfo *dev);
 }
 
 // Selection of key blocks for block-sparse attention.
