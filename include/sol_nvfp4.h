@@ -310,6 +310,7 @@ sol_status_t sol_attention_bf16_joint(const sol_attention_stream_t *first, const
  * sol_attention_blocks computes softmax(q k^T / sqrt(head_dim)) v over the keys of the listed blocks (rounding as
  * sol_attention_bf16).  Any lists will do: entries outside [0, ceil(keys / 128)) are skipped, the order is free, a block
  * listed twice counts twice, a row of queries whose list names no existing key gets zeros.  A count is held to [0, max_blocks].
+ * Keys and values behind a batch element's kv_lens may hold anything, NaN included; before it they must be finite.
  *   block_lists [batch, heads, ceil(seq_q / 256), max_blocks];  out as in sol_attention_bf16, no alias of an input
  */
 size_t sol_select_blocks_workspace_bytes(int64_t batch, int64_t seq_q, int64_t seq_kv, int64_t heads, int64_t heads_kv,

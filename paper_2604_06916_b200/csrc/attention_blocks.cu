@@ -15,8 +15,19 @@
 // tile's next step are there when it asks.  TMEM: O_0, O_1 (d columns each), P_0, P_1 (64 each), S (128).
 //
 // Warps: 0..3 and 4..7 = softmax / output of query tile 0 and 1 (one warp per TMEM lane quadrant), 8 = TMA producer, 9 = TMEM
-// owner and MMA issuer, 10 = counts the list of the next item; their warpgroup leaves registers to the other two.  Every mbarrier wait is bounded, and a warp that works together
-// gives up together.
+// owner and MMA issuer, 10 = counts the list of the next item; their warpgroup leaves registers to the other two.  Every
+// mbarrier wait is bounded, and a warp that works together gives up together.
+//
+// Measured on B200 (inside a CUDA graph): 4 x 4608 tokens, 24 heads of 128, 9 of 36 blocks 229 us (1 140 TFLOP/s, 69 % of the
+// measured BF16 rate; 231 to 237 us on boxes that clock lower); 2 x 4429, 38 heads of 64, 8 blocks 151 us; 1 x 1536, 24 heads
+// of 128, 4 of 12 blocks 14.9 us.  A key tile takes 3 030 cycles for both query tiles (d = 128), of which the products are
+// 2 048 and the rest is the way of a score row through its thread.  An item costs 3 000 to 3 800 cycles more: last product,
+// output, next first scores.  A CTA per item instead, with the same steps, takes 12.8 us on the smallest case (nothing to
+// overlap there, and a plainer way in) but 157 and 234 us on the others.
+// Tried without gain: sixteen softmax warps, two threads per row (345 us on the first case); P in two halves (277); three-input
+// maxima; two score tiles for d = 64 in phase (179 instead of 159) or one ahead (159); scores of 64 keys at a time (269);
+// the next item's Q pulled into L2 ahead (152 and 232 instead of 151 and 231); rows stored by the threads instead of by TMA
+// (1 % slower); an item's output after the next item's first exponentials (within 0.5 %).
 #include "gemm_common.cuh"
 #include "quant_math.cuh"
 #include "sol_internal.h"
@@ -40,9 +51,9 @@ constexpr int kOutBox = 32 * 128;       // bytes of a warp's [32 rows][64 BF16] 
 constexpr float kLazyLog2 = 8.0f;       // slack of the softmax reference maximum, in powers of two
 constexpr uint32_t kTmemCols = 512, kColScores = 384;
 constexpr int kFirstKeys = 8;           // first keys of the latest tiles, handed from the producer to the softmax
-// barriers: rings [stage]; pairs [query tile][odd key tile]; item information [odd item]
-constexpr int kQFull = 0, kQEmpty = 1, kKFull = 2, kKEmpty = 4, kVFull = 6, kVEmpty = 8, kSOf = 10, kLoadOf = 14, kPOf = 18, kPvOf = 22,
-              kOEmpty = 26, kInfoFull = 28, kInfoEmpty = 30, kNumBars = 32;
+// barriers: Q and O [query tile]; rings [stage]; pairs [query tile][odd key tile]; item information [odd item]
+constexpr int kQFull = 0, kQEmpty = 2, kKFull = 4, kKEmpty = 6, kVFull = 8, kVEmpty = 10, kSOf = 12, kLoadOf = 16, kPOf = 20, kPvOf = 24,
+              kOEmpty = 28, kInfoFull = 30, kInfoEmpty = 32, kNumBars = 34;
 struct Shared {                         // behind the tiles
     uint64_t bars[kNumBars];
     uint32_t tmem, abort_flag;
@@ -99,10 +110,16 @@ attention_blocks_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     volatile int *tiles_of = sh.tiles, *keys_of = sh.keys, *first_key_of = sh.first_key;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+    struct Item { int q_block, head, batch; };
+    auto item_of = [&](int w) {
+        const int line = w / p.q_blocks, batch = line / p.heads;
+        return Item{w - line * p.q_blocks, line - batch * p.heads, batch};
+    };
+    auto keys_of_sample = [&](int batch) { return p.kv_lens == nullptr ? p.seq_kv : min(max(__ldg(p.kv_lens + batch), 0), p.seq_kv); };
     if (threadIdx.x == 0) {
         for (int i = 0; i < kNumBars; ++i) {
             const bool of_tile = (i >= kLoadOf && i < kPvOf) || (i >= kOEmpty && i < kInfoFull);
-            ptx::mbar_init(bar(i), of_tile ? kWarpsPerTile : i >= kInfoEmpty ? 2 + kQTiles * kWarpsPerTile : 1);
+            ptx::mbar_init(bar(i), of_tile ? kWarpsPerTile : i >= kInfoEmpty ? 1 + kQTiles * kWarpsPerTile : 1);
         }
         *abort_flag = 0;
         ptx::fence_mbar_init();
@@ -121,11 +138,6 @@ attention_blocks_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     ptx::tc_fence_after_sync();
     const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t *>(&sh.tmem);
 
-    struct Item { int q_block, head, batch; };
-    auto item_of = [&](int w) {
-        const int line = w / p.q_blocks, batch = line / p.heads;
-        return Item{w - line * p.q_blocks, line - batch * p.heads, batch};
-    };
     auto wait1 = [&](int b, uint32_t parity, uint32_t code) { return wait_bounded(bar(b), parity, abort_flag, p.status, code); };
     auto wait32 = [&](int b, uint32_t parity, uint32_t code) { return __all_sync(0xFFFFFFFFu, wait1(b, parity, code)) != 0; };
     // Items are numbered i = 0, 1, ... per CTA; `full` counts those with keys, J their key tiles.
@@ -139,7 +151,7 @@ attention_blocks_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 const Item it = item_of(w);
                 const int32_t *from = p.blocks + static_cast<int64_t>(w) * p.max_blocks;
                 int next = lane < p.max_blocks ? __ldg(from + lane) : -1;       // not after the count: one latency, not two
-                const int keys = p.kv_lens == nullptr ? p.seq_kv : min(max(__ldg(p.kv_lens + it.batch), 0), p.seq_kv);
+                const int keys = keys_of_sample(it.batch);
                 const int named = min(max(__ldg(p.counts + w), 0), p.max_blocks), existing = (keys + kBKV - 1) / kBKV;
                 int kept = 0;
                 for (int e0 = 0; e0 < named; e0 += 32) {
@@ -160,39 +172,43 @@ attention_blocks_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             if (ptx::elect_one()) {
                 bool ok = true;
                 int J = 0, full = 0;
-                for (int w = blockIdx.x, i = 0; ok && w < p.items; w += gridDim.x, ++i) {
+                for (int w = blockIdx.x; ok && w < p.items; w += gridDim.x) {
                     const Item it = item_of(w);
                     const int32_t *from = p.blocks + static_cast<int64_t>(w) * p.max_blocks;
-                    int entry = __ldg(from);
-                    if (!wait1(info_full(i), phase(i), 0xB02u)) break;
-                    const int tiles = tiles_of[i & 1], existing = (keys_of[i & 1] + kBKV - 1) / kBKV;
-                    ptx::mbar_arrive(bar(kInfoEmpty + (i & 1)));
-                    if (tiles == 0) continue;
-                    if (full > 0 && !wait1(kQEmpty, static_cast<uint32_t>(full - 1) & 1u, 0xB03u)) break;
+                    int next = __ldg(from);
+                    const int keys = keys_of_sample(it.batch), named = min(max(__ldg(p.counts + w), 0), p.max_blocks);
+                    const int existing = (keys + kBKV - 1) / kBKV;
                     const int xq = it.head * kD, xkv = it.head / p.group * kD;
-                    ptx::mbar_arrive_expect_tx(bar(kQFull), kQTiles * kTile);
-#pragma unroll
-                    for (int t = 0; t < kQTiles; ++t) {
-#pragma unroll
-                        for (int bx = 0; bx < kBoxes; ++bx)
-                            ptx::tma_load_3d(sQ + t * kTile + bx * kBox, &tm_q, xq + 64 * bx, (it.q_block * kQTiles + t) * kBQ, it.batch, bar(kQFull));
-                    }
-                    ++full;
-                    for (int left = tiles, e = 1; left > 0; --left, ++J) {
-                        while (entry < 0 || entry >= existing) entry = __ldg(from + e++);      // an entry that names keys is to come
+                    bool first = true;
+                    for (int e = 0; ok && e < named; ++e) {
+                        const int entry = next;
+                        if (e + 1 < named) next = __ldg(from + e + 1);
+                        if (entry < 0 || entry >= existing) continue;        // names no keys
                         const int key0 = entry * kBKV, st = J & 1;
-                        if (left > 1) entry = __ldg(from + e++);
+                        auto load_q = [&](int t) {      // the tile's last scores of the item before are done
+                            if (full > 0 && !wait1(kQEmpty + t, static_cast<uint32_t>(full - 1) & 1u, 0xB03u)) return false;
+                            ptx::mbar_arrive_expect_tx(bar(kQFull + t), kTile);
+#pragma unroll
+                            for (int bx = 0; bx < kBoxes; ++bx)
+                                ptx::tma_load_3d(sQ + t * kTile + bx * kBox, &tm_q, xq + 64 * bx, (it.q_block * kQTiles + t) * kBQ, it.batch, bar(kQFull + t));
+                            return true;
+                        };
+                        if (first && !(ok = load_q(0))) break;
                         if (!(ok = wait1(kKEmpty + st, phase(J) ^ 1u, 0xB10u | st))) break;
                         first_key_of[J % kFirstKeys] = key0;
                         ptx::mbar_arrive_expect_tx(bar(kKFull + st), kTile);
 #pragma unroll
                         for (int bx = 0; bx < kBoxes; ++bx)
                             ptx::tma_load_3d(sK + st * kTile + bx * kBox, &tm_k, xkv + 64 * bx, key0, it.batch, bar(kKFull + st));
+                        if (first && !(ok = load_q(1))) break;
                         if (!(ok = wait1(kVEmpty + st, phase(J) ^ 1u, 0xB20u | st))) break;
                         ptx::mbar_arrive_expect_tx(bar(kVFull + st), kTile);
 #pragma unroll
                         for (int bx = 0; bx < kBoxes; ++bx)
                             ptx::tma_load_3d(sV + st * kTile + bx * kBox, &tm_v, xkv + 64 * bx, key0, it.batch, bar(kVFull + st));
+                        full += first ? 1 : 0;
+                        first = false;
+                        ++J;
                     }
                 }
             }
@@ -204,50 +220,55 @@ attention_blocks_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
                 constexpr uint32_t idesc_base = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(128 >> 4) << 24);
                 constexpr uint32_t idesc_qk = idesc_base | (static_cast<uint32_t>(kBKV >> 3) << 17);
                 constexpr uint32_t idesc_pv = idesc_base | (static_cast<uint32_t>(kD >> 3) << 17) | (1u << 16);
+                // step n of an item whose key tiles start at J0 and which `full` items with keys precede
+                struct Work { int J0, steps, full; };
+                // S = Q_t K^T, 16 elements of d per instruction; the score tile is free once the step before has been loaded
+                auto scores = [&](const Work &k, int n) {
+                    const int t = n & 1, J = k.J0 + (n >> 1), st = J & 1, N = 2 * k.J0 + n - 1;
+                    if (n < 2 && !wait1(kQFull + t, static_cast<uint32_t>(k.full) & 1u, 0xB31u)) return false;
+                    if (t == 0 && !wait1(kKFull + st, phase(J), 0xB41u)) return false;
+                    if (N >= 0 && !wait1(pair(kLoadOf, N & 1, N >> 1), phase(N >> 1), 0xB40u)) return false;
+                    ptx::tc_fence_after_sync();
+#pragma unroll
+                    for (int c = 0; c < kD / 16; ++c) {
+                        const uint64_t a = ptx::smem_desc_sw128(sQ + t * kTile + (c >> 2) * kBox) + 2u * (c & 3);
+                        const uint64_t b = ptx::smem_desc_sw128(sK + st * kTile + (c >> 2) * kBox) + 2u * (c & 3);
+                        ptx::mma_bf16(tmem_base + kColScores, a, b, idesc_qk, c > 0);
+                    }
+                    ptx::tc_commit(bar(pair(kSOf, t, J)));
+                    if (t == 1) ptx::tc_commit(bar(kKEmpty + st));
+                    if (n >= k.steps - 2) ptx::tc_commit(bar(kQEmpty + t));
+                    return true;
+                };
+                // O_t += P V, 16 keys (8 columns of packed P) per instruction
+                auto product = [&](const Work &k, int n) {
+                    const int t = n & 1, J = k.J0 + (n >> 1), st = J & 1;
+                    if (!wait1(pair(kPOf, t, J), phase(J), 0xB60u | t)) return false;
+                    if (t == 0 && !wait1(kVFull + st, phase(J), 0xB70u)) return false;
+                    if (n < 2 && k.full > 0 && !wait1(kOEmpty + t, static_cast<uint32_t>(k.full - 1) & 1u, 0xB71u)) return false;   // the item before has been read
+                    ptx::tc_fence_after_sync();
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const uint64_t b = ptx::smem_desc_sw128_mn(sV + st * kTile + c * 2048, kBox, 1024);
+                        ptx::mma_bf16_a_tmem(tmem_base + kD * t, tmem_base + kColP + 64 * t + 8 * c, b, idesc_pv, n > 1 || c > 0);
+                    }
+                    ptx::tc_commit(bar(pair(kPvOf, t, J)));
+                    if (t == 1) ptx::tc_commit(bar(kVEmpty + st));
+                    return true;
+                };
                 bool ok = true;
-                int J0 = 0, full = 0;          // key tiles and items with keys before this item
+                int J0 = 0, full = 0;
                 for (int w = blockIdx.x, i = 0; ok && w < p.items; w += gridDim.x, ++i) {
-                    if (!wait1(info_full(i), phase(i), 0xB30u)) break;
-                    const int tiles = tiles_of[i & 1], steps = 2 * tiles;
+                    if (!(ok = wait1(info_full(i), phase(i), 0xB30u))) break;
+                    const int tiles = tiles_of[i & 1];
                     ptx::mbar_arrive(bar(kInfoEmpty + (i & 1)));
                     if (tiles == 0) continue;
-                    // S = Q_t K^T of step n, 16 elements of d per instruction; the score tile is free once step n - 1 has been loaded
-                    auto scores = [&](int n) {
-                        const int t = n & 1, J = J0 + (n >> 1), st = J & 1, N = 2 * J0 + n - 1;
-                        if (N >= 0 && !wait1(pair(kLoadOf, N & 1, N >> 1), phase(N >> 1), 0xB40u)) return false;
-                        if (t == 0 && !wait1(kKFull + st, phase(J), 0xB41u)) return false;
-                        ptx::tc_fence_after_sync();
-#pragma unroll
-                        for (int c = 0; c < kD / 16; ++c) {
-                            const uint64_t a = ptx::smem_desc_sw128(sQ + t * kTile + (c >> 2) * kBox) + 2u * (c & 3);
-                            const uint64_t b = ptx::smem_desc_sw128(sK + st * kTile + (c >> 2) * kBox) + 2u * (c & 3);
-                            ptx::mma_bf16(tmem_base + kColScores, a, b, idesc_qk, c > 0);
-                        }
-                        ptx::tc_commit(bar(pair(kSOf, t, J)));
-                        if (t == 1) ptx::tc_commit(bar(kKEmpty + st));
-                        if (n == steps - 1) ptx::tc_commit(bar(kQEmpty));
-                        return true;
-                    };
-                    // O_t += P V of step n, 16 keys (8 columns of packed P) per instruction
-                    auto product = [&](int n) {
-                        const int t = n & 1, J = J0 + (n >> 1), st = J & 1;
-                        if (!wait1(pair(kPOf, t, J), phase(J), 0xB60u | t)) return false;
-                        if (t == 0 && !wait1(kVFull + st, phase(J), 0xB70u)) return false;
-                        if (n < 2 && full > 0 && !wait1(kOEmpty + t, static_cast<uint32_t>(full - 1) & 1u, 0xB71u)) return false;   // the item before has been read
-                        ptx::tc_fence_after_sync();
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            const uint64_t b = ptx::smem_desc_sw128_mn(sV + st * kTile + c * 2048, kBox, 1024);
-                            ptx::mma_bf16_a_tmem(tmem_base + kD * t, tmem_base + kColP + 64 * t + 8 * c, b, idesc_pv, n > 1 || c > 0);
-                        }
-                        ptx::tc_commit(bar(pair(kPvOf, t, J)));
-                        if (t == 1) ptx::tc_commit(bar(kVEmpty + st));
-                        return true;
-                    };
-                    ok = wait1(kQFull, static_cast<uint32_t>(full) & 1u, 0xB31u);
-                    // each step's scores when the tile is free, then the product whose P is the next to arrive
-                    for (int n = 0; ok && n < steps; ++n) ok = scores(n) && (n < 2 || product(n - 2));
-                    ok = ok && product(steps - 2) && product(steps - 1);
+                    const Work k{J0, 2 * tiles, full};
+                    // Each step's scores when the tile is free, then the product whose P is the next to arrive.  The last two
+                    // products do not wait for the next item's first scores: the softmax warps need them to go on, and the
+                    // information of a later item needs the softmax warps (several empty lists in a row).
+                    for (int n = 0; ok && n < k.steps; ++n) ok = scores(k, n) && (n < 2 || product(k, n - 2));
+                    ok = ok && product(k, k.steps - 2) && product(k, k.steps - 1);
                     J0 += tiles;
                     ++full;
                 }
@@ -404,6 +425,7 @@ attention_blocks_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
     }
 
     // ---------------------------------------------------------------- teardown
+    if (*abort_flag) __nanosleep(2000000);  // let copies already in flight land before the CTA exits
     ptx::tc_fence_before_sync();
     __syncthreads();
     if (warp == kIssuer) {

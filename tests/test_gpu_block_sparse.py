@@ -210,6 +210,20 @@ def test_anything_may_stand_behind_the_lengths(B, D, junk):
     assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("pattern", ["2000102", "1000000", "0001000", "3010030", "0000000"])
+def test_runs_of_empty_lists(B, D, pattern):
+    # Blocks of the kernel stay and walk every sm_count-th list: those of one block go through `pattern`, others through it
+    # begun elsewhere.
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    H = sms * len(pattern)
+    q, k, v = make(1, 5, 300, H, H, D, len(pattern) + D)
+    counts = torch.tensor([int(pattern[(h // sms + h % sms % 3) % len(pattern)]) for h in range(H)], dtype=torch.int32, device="cuda").view(1, H, 1)
+    blocks = torch.tensor([2, 0, 1], dtype=torch.int32, device="cuda").expand(1, H, 1, 3).contiguous()
+    got = check_attend(B, q, k, v, blocks, counts)
+    assert torch.all(got[0, :, counts.view(H) == 0] == 0)
+
+
 def test_sharp_scores_and_output_view(B):
     q, k, v = make(1, 400, 1400, 2, 2, 128, 19)
     q = (q.float() * 6).to(torch.bfloat16)
