@@ -362,7 +362,8 @@ sol_status_t mxfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const
  *             of row m % position_rows, so samples of one geometry share a table.
  *             Pairs are neighbours (2i, 2i+1) or halves (i, i + R/2); pair i takes freqs[i]; the first axis_dims[0] / 2
  *             pairs belong to axis 0 and so on.  axis_dims are positive and even, 1 <= axes <= 4, R % 8 == 0, R <= head_dim
- *   head_dim  32, 64, 128 or 256;  eps >= 0
+ *   head_dim  32, 64, 128 or 256;  eps >= 0 (with eps = 0 a head of zeros has no norm: NaN, in its gradients as well)
+ * The mean of squares is FP32 too: values beyond 2^60, or with eps = 0 a head all below 2^-60, may leave its range.
  */
 typedef enum { SOL_ROTARY_INTERLEAVED = 0, SOL_ROTARY_HALF = 1 } sol_rotary_layout_t;
 typedef enum {

@@ -259,7 +259,9 @@ backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int blocks_q, in
         auto fetch = [&]() {
 #pragma unroll
             for (int u = 0; u < S::kUnrollBack; ++u) {
-                raw_dy[u] = raw_x[u] = make_uint4(0, 0, 0, 0);
+                // a head that does not exist: dy = 0 and x = 1, whose root mean square is not 0 (with eps = 0 as well)
+                raw_dy[u] = make_uint4(0, 0, 0, 0);
+                raw_x[u] = make_uint4(0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u);
                 if (h + u * S::kRep < heads) {
                     raw_dy[u] = load8<kHalf>(dy + (h + u * S::kRep) * kD, c0, c1);
                     if (norm) raw_x[u] = load8<kHalf>(x + (h + u * S::kRep) * kD, c0, c1);
@@ -288,7 +290,7 @@ backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int blocks_q, in
                     const float mean = head_sum<S::kLanes>(sum_lanes(dot)) * r * (1.0f / kD);       // mean of w dn xhat
                     const uint64_t r2 = twice(r), back = twice(-(r * r * mean));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {   // heads that do not exist were read as zeros: they add nothing
+                    for (int e = 0; e < 4; ++e) {   // heads that do not exist have dn = 0 and a finite r: they add nothing
                         acc.v[e] = qmath::fma2(prod.v[e], r2, acc.v[e]);
                         dn.v[e] = qmath::fma2(qmath::mul2(dn.v[e], w.v[e]), r2, qmath::mul2(x8.v[e], back));
                     }
