@@ -336,7 +336,9 @@ sol_status_t sol_attention_blocks(const void *q, const void *k, const void *v, v
  *               NULL will do, for up to four rows of up to 3072 columns, which every block prepares for itself
  *   M >= 1 (the weight is read once per 64 rows), N % 8 == 0, K % 32 == 0
  * Two launches, one where no workspace is needed.  Sums are FP32 and in a fixed order.  Before the product act(x) is
- * scaled by a power of two per row (and slice of K) and held in FP16: BF16 values down to 2^-29 of the row's largest are kept exactly (an activation's result to 11 bits).
+ * scaled by a power of two per row (and slice of K) and held in FP16: BF16 values down to 2^-29 of the row's largest are kept
+ * exactly where that is at least 2^-100 (an activation's result to 11 bits).  The operands' scales may lie anywhere: only a sum
+ * over a slice of K that FP32 does not hold is lost.
  */
 size_t sol_matvec_workspace_bytes(int64_t M, int64_t K);
 sol_status_t nvfp4_matvec(const void *x_bf16, int64_t ldx, const void *wq, const void *wsf, const float *w_tscale,

@@ -29,8 +29,9 @@
 // scales are powers of two of any size: they are taken relative to the largest one of the row's slice, 2^13 for that
 // one, so every block within 2^36 of it is exact; what lies below is off by at most 2^-25 of 2^-13 of it.  x (after the
 // activation) is scaled by a power of two per row and slice so that its largest element is in [2^14, 2^15): BF16 values
-// within 2^-29 of the largest stay exact, smaller ones are off by 2^-40 of the largest; an activation's FP32 result is
-// rounded to FP16's 11 bits.  Sums are FP32.
+// within 2^-29 of the largest stay exact, smaller ones are off by 2^-40 of the largest (a largest one below 2^-100 is
+// scaled by 2^114 all the same); an activation's FP32 result is rounded to FP16's 11 bits.  Sums are FP32; the powers of two
+// of x, of the MXFP4 scales and of T are undone together, which stays in FP32's range wherever the slice's sum does.
 #include <cuda_fp16.h>
 
 #include "gemm_common.cuh"
@@ -67,7 +68,7 @@ struct Params {
     int64_t ldx;
     int K, act;
     const uint8_t *ximage;   // FP16 x: [row chunk][64 columns of K][x_rows][128 bytes, 128-byte swizzle], K padded to stages
-    const float *x_back;     // per row: what undoes its scaling
+    const int *x_exp;        // per row: the exponent that undoes its scaling
     const uint8_t *wsf;
     const float *wts;        // null: MXFP4
     const uint16_t *bias;    // null: none
@@ -148,13 +149,26 @@ __device__ __forceinline__ void activate8(uint4 r, int act, float (&f)[8]) {
     }
 }
 
-// 2^(kXExp - e) with e the exponent of the largest element (FP32 bits), held to what FP32 can scale by; and its inverse.
-__device__ __forceinline__ float scale_up(uint32_t bits) {
-    return __uint_as_float(static_cast<uint32_t>(127 + kXExp - min(max(static_cast<int>(bits >> 23) - 127, -100), 127)) << 23);
+// e - kXExp with e the exponent of the largest element (FP32 bits), held to what FP32 can scale by; and 2^(kXExp - e).
+__device__ __forceinline__ int exponent_back(uint32_t bits) { return min(max(static_cast<int>(bits >> 23) - 127, -100), 127) - kXExp; }
+__device__ __forceinline__ float scale_up(uint32_t bits) { return __uint_as_float(static_cast<uint32_t>(127 - exponent_back(bits)) << 23); }
+// T = t 2^exp with t in [1, 2) (zero, infinities and NaN keep their value).
+__device__ __forceinline__ float split_scale(float T, int &exp) {
+    const uint32_t bits = __float_as_uint(T), field = bits >> 23 & 255u;
+    exp = field == 0 ? -100 : field == 255u ? 0 : static_cast<int>(field) - 127;
+    return field == 0 ? T * 0x1p100f : field == 255u ? T : __uint_as_float((bits & 0x807FFFFFu) | 0x3F800000u);
 }
-__device__ __forceinline__ float scale_back(uint32_t bits) {
-    return bits ? __uint_as_float(static_cast<uint32_t>(127 - kXExp + min(max(static_cast<int>(bits >> 23) - 127, -100), 127)) << 23) : 0.0f;
-}
+// v 2^n in two exact steps, for |v| < 2^55 and n from -263 to 241: where the first step overflows or loses bits, the result is
+// infinite or zero anyway.
+struct PowerOfTwo {
+    float a, b;
+    __device__ __forceinline__ explicit PowerOfTwo(int n) {
+        n = max(n, -252);
+        a = __uint_as_float(static_cast<uint32_t>(127 + (n >> 1)) << 23);
+        b = __uint_as_float(static_cast<uint32_t>(127 + n - (n >> 1)) << 23);
+    }
+    __device__ __forceinline__ float times(float v) const { return v * a * b; }
+};
 __device__ __forceinline__ float largest8(const float (&v)[8], float most) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(v[e]));
@@ -178,7 +192,7 @@ __device__ __forceinline__ int64_t image_offset(int c, int r, int x_rows) {
 constexpr int kPrepThreads = 512;
 __global__ void __launch_bounds__(kPrepThreads)
 prepare_x(const uint16_t *__restrict__ x, int64_t ldx, int M, int K, int x_rows, int stages, int act, uint8_t *__restrict__ image,
-          float *__restrict__ x_back) {
+          int *__restrict__ x_exp) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // the products' CTAs may start loading weights
     __shared__ uint32_t warp_max[kPrepThreads / 32];
     const int m = blockIdx.x, chunks = stages * (kStageK / 8), live = K / 8;
@@ -202,7 +216,7 @@ prepare_x(const uint16_t *__restrict__ x, int64_t ldx, int M, int K, int x_rows,
     __syncthreads();
     bits = __reduce_max_sync(0xFFFFFFFFu, warp_max[threadIdx.x & (kPrepThreads / 32 - 1)]);
     const float up = scale_up(bits);
-    if (threadIdx.x == 0) x_back[m] = scale_back(bits);
+    if (threadIdx.x == 0) x_exp[m] = exponent_back(bits);
     uint8_t *to = image + static_cast<int64_t>(m / x_rows) * (4 * stages) * (x_rows * 128);
     auto put = [&](int c, const float (&v)[8]) { *reinterpret_cast<uint4 *>(to + image_offset(c, m % x_rows, x_rows)) = to_half8(v, up); };
 #pragma unroll
@@ -221,7 +235,6 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     constexpr int kChunksPerStage = kMx ? 2 : 4;      // 512-byte scale chunks of a stage
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ uint8_t row_most[kMx ? 4 : 1][kRows];
-    __shared__ float back[kMaxXRows];
     __shared__ uint32_t warp_most[kXWarps];
     const uint32_t base = ptx::smem_u32(smem_raw);
     const uint32_t x_bytes = static_cast<uint32_t>(stage_x_bytes(p.x_rows));
@@ -432,36 +445,55 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
             if (lane == 0) ptx::mbar_arrive(bar(kAFull + odd));
         }
         // ------------------------------------------------------------ this slice's sums, to the rank that owns the column
-        float x_back[kInlineRows];
+        // The scalings of x, of the MXFP4 scales and T's exponent are undone as one power of two: one after the other they
+        // may leave FP32's range on the way to a finite sum.
+        constexpr int kSteps = kInline ? 1 : kMaxXRows / 32, kStepRows = kInline ? kInlineRows : 8;      // rows of x in each of the four warpgroups
+        int undo[kSteps][kStepRows];
+        if (!kInline && ok) {
+            ptx::grid_dependency_wait();        // returns at once: x_exp was written with the x that is being multiplied
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int c = 8 * (warp >> 2) + 32 * i;
+                if (c < p.x_rows) {
+                    const int4 *from = reinterpret_cast<const int4 *>(p.x_exp + m0 + c);
+                    const int4 a = __ldcg(from), b = __ldcg(from + 1);
+                    const int all[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int e = 0; e < kStepRows; ++e) undo[i][e] = all[e];
+                }
+            }
+        }
+        int base_exp = ref - 127 - kMxExp;
+        if (!kMx) split_scale(__ldg(p.wts), base_exp);
         ok = ok && warp_wait(bar(kDone), 0, abort_flag, p.status, 0xC60u);
         if (kInline) ok = ok && warp_wait(bar(kXFull), 0, abort_flag, p.status, 0xC61u);    // long complete: warp_most is in view
         if (ranks > 1) ptx::cluster_wait();
         if (ok) {
-            if (!kInline && threadIdx.x < p.x_rows) back[threadIdx.x] = __ldcg(p.x_back + m0 + threadIdx.x);   // written before x was loaded
-            if (kInline) {     // what undoes the slice's own scaling of each row
+            if (kInline) {     // the slice's own scaling of each row
 #pragma unroll
                 for (int r = 0; r < kInlineRows; ++r) {
                     uint32_t bits = 0;
                     for (int i = r * per_row; i < (r + 1) * per_row && i < kXWarps; ++i) bits = max(bits, warp_most[i]);
-                    x_back[r] = scale_back(bits);
+                    undo[0][r] = exponent_back(bits);
                 }
             }
             ptx::tc_fence_after_sync();
             const int own = kRows / ranks;
             const uint32_t to = ptx::map_to_cta(s_part + (rank * p.x_rows * own + row % own) * 4, row / own);
-            for (int c = 8 * (warp >> 2); c < p.x_rows; c += 32) {
+#pragma unroll
+            for (int j = 0; j < kSteps; ++j) {
+                const int c = 8 * (warp >> 2) + 32 * j;
+                if (c >= (kInline ? kInlineRows : p.x_rows)) break;
                 uint32_t d[kSums][8];
 #pragma unroll
                 for (int i = 0; i < kSums; ++i) ptx::tmem_ld_32x8(tmem + kColD + i * kMaxXRows + lanes + c, d[i]);
                 ptx::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < kStepRows; ++e) {
                     float v = __uint_as_float(d[0][e]);
 #pragma unroll
                     for (int i = 1; i < kSums; ++i) v += __uint_as_float(d[i][e]);
-                    if (kMx) v = scalbnf(v, ref - 127 - kMxExp);
-                    if (kInline) v *= c == 0 && e < kInlineRows ? x_back[e % kInlineRows] : 0.0f;    // every slice has its own scale
-                    st_cluster(to + (c + e) * own * 4, v);
+                    st_cluster(to + (c + e) * own * 4, PowerOfTwo(base_exp + undo[j][e]).times(v));
                 }
             }
         }
@@ -472,7 +504,8 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     // ---------------------------------------------------------------- own columns: sum over the ranks, scale, bias, store
     const int own = kRows / ranks, pairs = own / 2, rows = min(p.x_rows, p.M - m0);
     const int r = 2 * (threadIdx.x % pairs), n = group * kRows + rank * own + r;
-    const float T = kMx ? 1.0f : __ldg(p.wts);
+    int t_exp;                          // (already in the sums)
+    const float T = kMx ? 1.0f : split_scale(__ldg(p.wts), t_exp);
     uint32_t b2 = 0;
     if (p.bias != nullptr && n < p.N) b2 = __ldg(reinterpret_cast<const uint32_t *>(p.bias + n));
     if (ranks > 1) ptx::cluster_sync();
@@ -484,8 +517,7 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
             v0 += v.x;
             v1 += v.y;
         }
-        const float scale = kInline ? 1.0f : back[i];
-        const float y0 = fmaf(v0 * scale, T, qmath::bf16_lo(b2)), y1 = fmaf(v1 * scale, T, qmath::bf16_hi(b2));
+        const float y0 = fmaf(v0, T, qmath::bf16_lo(b2)), y1 = fmaf(v1, T, qmath::bf16_hi(b2));
         uint32_t o;
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o) : "f"(y1), "f"(y0));
         *reinterpret_cast<uint32_t *>(p.y + (m0 + i) * p.ldy + n) = o;
@@ -584,11 +616,11 @@ sol_status_t launch(const void *x, int64_t ldx, bool silu, void *workspace, cons
     if (!share_k<kMx, false>(p, ranks)) return SOL_ERR_CUDA;
     const int64_t row_chunks = ceil_div(p.M, p.x_rows);
     uint8_t *image = static_cast<uint8_t *>(workspace);
-    float *x_back = reinterpret_cast<float *>(image + row_chunks * p.stages * stage_x_bytes(p.x_rows));
+    int *x_exp = reinterpret_cast<int *>(image + row_chunks * p.stages * stage_x_bytes(p.x_rows));
     p.ximage = image;
-    p.x_back = x_back;
+    p.x_exp = x_exp;
     prepare_x<<<static_cast<unsigned>(row_chunks * p.x_rows), kPrepThreads, 0, stream>>>(
-        static_cast<const uint16_t *>(x), ldx, p.M, static_cast<int>(K), p.x_rows, p.stages, silu ? 1 : 0, image, x_back);
+        static_cast<const uint16_t *>(x), ldx, p.M, static_cast<int>(K), p.x_rows, p.stages, silu ? 1 : 0, image, x_exp);
     const sol_status_t st = launch_status();
     return st != SOL_OK ? st : launch_products<kMx, false>(tm_w, p, ranks, stream);
 }
