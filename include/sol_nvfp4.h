@@ -600,7 +600,8 @@ sol_status_t sol_set_wait_limit_cycles(int64_t cycles);
  * device, the load-issuing warps of the CTA-pair GEMM kernels (M > 128: nvfp4_linear, mxfp4_linear,
  * bf16_linear and the entries built on them) issue no loads, so every consumer wait of such a launch
  * runs into the wait limit: nothing traps, faults or spins without bound, the kernel returns with Y
- * unwritten and the status word set.  Use it with a short limit (about 1e6 cycles) and switch it off
+ * unwritten and the status word set.  The few-row linears (nvfp4_matvec, mxfp4_matvec) then load their first codes, but x is
+ * never handed to the products, with the same outcome.  Use it with a short limit (about 1e6 cycles) and switch it off
  * again; it is not meant for anything but exercising the time-out path.
  */
 sol_status_t sol_test_hold_loads(int on);

@@ -42,6 +42,7 @@ namespace sol {
 namespace matvec {
 namespace {
 
+using gemm::loads_held;
 using gemm::wait_bounded;
 
 constexpr int kConvWarps = 16;       // four warpgroups
@@ -125,6 +126,9 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
 }
 __device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t cluster_addr, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(cluster_addr), "r"(v) : "memory");
 }
 __device__ __forceinline__ void st_cluster(uint32_t cluster_addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
@@ -244,6 +248,8 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     const float *part = reinterpret_cast<const float *>(smem_raw + (s_part - base));
     uint32_t *tmem_ptr = reinterpret_cast<uint32_t *>(bar_gen + 8 * kBars);
     volatile uint32_t *abort_flag = reinterpret_cast<volatile uint32_t *>(bar_gen + 8 * kBars + 4);
+    // sums are missing, this CTA's own or those of another of its cluster: a wait ran out, y is left alone
+    volatile uint32_t *failed = abort_flag + 1;
     auto bar = [&](int i) { return bar_base + 8u * i; };
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -273,7 +279,9 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     const int chunks = stages * (kStageK / 8), live = min(chunks, (p.K - stage0 * kStageK) / 8), step = 32 * per_row;
     const int at = (me % per_row) * 32 + lane, id = me * 32 + lane;
     uint4 raw[kInline ? kHeld : 1];
+    bool held = false;
     if (kInline && me >= 0 && me < kXWarps) {
+        held = loads_held(p.status);
         const uint16_t *xrow = p.x + m * p.ldx + stage0 * kStageK;
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
@@ -293,6 +301,7 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
             }
             ptx::mbar_init(bar(kDone), 1);
             *abort_flag = 0;
+            *failed = 0;
             ptx::fence_mbar_init();
             ptx::fence_proxy_async_smem();
             for (int s = 0; s < first; ++s) load_codes(s);
@@ -329,10 +338,11 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
         // ------------------------------------------------------------ loads
         if (ptx::elect_one()) {
             if (!kInline) {
+                held = loads_held(p.status);
                 ptx::grid_dependency_wait();       // x is prepared
-                for (int s = 0; s < first; ++s) load_x(s);
+                for (int s = 0; !held && s < first; ++s) load_x(s);
             }
-            for (int s = first; s < stages; ++s) {
+            for (int s = first; !held && s < stages; ++s) {
                 if (!wait_bounded(bar(kEmpty + s % p.ring), static_cast<uint32_t>(s / p.ring - 1) & 1u, abort_flag, p.status, 0xC10u)) break;
                 load_codes(s);
                 if (!kInline) load_x(s);
@@ -396,7 +406,7 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
                 sts128(s_x + static_cast<uint32_t>(image_offset(i % chunks, kXWarps / per_row + i / chunks, p.x_rows)), make_uint4(0, 0, 0, 0));
             ptx::fence_proxy_async_smem();      // the tensor core reads x through the async proxy
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar(kXFull));
+            if (lane == 0 && !held) ptx::mbar_arrive(bar(kXFull));
         }
         for (int s = odd; s < stages; s += 2) {
             const int st = s % p.ring;
@@ -468,6 +478,7 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
         ok = ok && warp_wait(bar(kDone), 0, abort_flag, p.status, 0xC60u);
         if (kInline) ok = ok && warp_wait(bar(kXFull), 0, abort_flag, p.status, 0xC61u);    // long complete: warp_most is in view
         if (ranks > 1) ptx::cluster_wait();
+        if (!ok && lane < ranks) st_cluster(ptx::map_to_cta(bar_base + 8 * kBars + 8, lane), 1u);
         if (ok) {
             if (kInline) {     // the slice's own scaling of each row
 #pragma unroll
@@ -507,10 +518,12 @@ matvec_kernel(const __grid_constant__ CUtensorMap tm_w, const Params p) {
     int t_exp;                          // (already in the sums)
     const float T = kMx ? 1.0f : split_scale(__ldg(p.wts), t_exp);
     uint32_t b2 = 0;
+    if (aligned && *abort_flag) __nanosleep(2000000);  // let copies already in flight land before the CTA exits
     if (p.bias != nullptr && n < p.N) b2 = __ldg(reinterpret_cast<const uint32_t *>(p.bias + n));
     if (ranks > 1) ptx::cluster_sync();
     else __syncthreads();
-    for (int i = threadIdx.x / pairs; i < rows && warp < kConvWarps && n < p.N; i += 32 * kConvWarps / pairs) {
+    const bool store = aligned && *failed == 0 && warp < kConvWarps && n < p.N;
+    for (int i = threadIdx.x / pairs; store && i < rows; i += 32 * kConvWarps / pairs) {
         float v0 = 0.0f, v1 = 0.0f;
         for (int c = 0; c < ranks; ++c) {
             const float2 v = *reinterpret_cast<const float2 *>(part + (c * p.x_rows + i) * own + r);
