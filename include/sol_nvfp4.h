@@ -598,9 +598,9 @@ sol_status_t sol_set_wait_limit_cycles(int64_t cycles);
 /*
  * Test hook for that path (no counterpart in the paper).  While `on` is non-zero on the current
  * device, the load-issuing warps of the CTA-pair GEMM kernels (M > 128: nvfp4_linear, mxfp4_linear,
- * bf16_linear and the entries built on them) issue no loads, so every consumer wait of such a launch
+ * bf16_linear and the entries built on them) and of sol_attention_blocks issue no loads, so every consumer wait of such a launch
  * runs into the wait limit: nothing traps, faults or spins without bound, the kernel returns with Y
- * unwritten and the status word set.  The few-row linears (nvfp4_matvec, mxfp4_matvec) then load their first codes, but x is
+ * unwritten (queries with empty lists aside) and the status word set.  The few-row linears (nvfp4_matvec, mxfp4_matvec) then load their first codes, but x is
  * never handed to the products, with the same outcome.  Use it with a short limit (about 1e6 cycles) and switch it off
  * again; it is not meant for anything but exercising the time-out path.
  */

@@ -36,6 +36,7 @@ namespace sol {
 namespace attn {
 namespace {
 
+using gemm::loads_held;
 using gemm::wait_bounded;
 
 constexpr int kBQ = 128, kQTiles = 2, kBKV = 128;
@@ -170,13 +171,14 @@ attention_blocks_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         } else if (warp == kProducer) {
             // ------------------------------------------------------------ TMA producer
             if (ptx::elect_one()) {
+                const bool held = loads_held(p.status);     // looked at with the first list: one latency, not two
                 bool ok = true;
                 int J = 0, full = 0;
                 for (int w = blockIdx.x; ok && w < p.items; w += gridDim.x) {
                     const Item it = item_of(w);
                     const int32_t *from = p.blocks + static_cast<int64_t>(w) * p.max_blocks;
                     int next = __ldg(from);
-                    const int keys = keys_of_sample(it.batch), named = min(max(__ldg(p.counts + w), 0), p.max_blocks);
+                    const int keys = keys_of_sample(it.batch), named = held ? 0 : min(max(__ldg(p.counts + w), 0), p.max_blocks);
                     const int existing = (keys + kBKV - 1) / kBKV;
                     const int xq = it.head * kD, xkv = it.head / p.group * kD;
                     bool first = true;
