@@ -416,6 +416,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_qa, const __grid_constan
     }
 
     // ---------------------------------------------------------------- teardown
+    if (*abort_flag) __nanosleep(2000000);  // let copies already in flight land before the CTA exits
     ptx::tc_fence_before_sync();
     __syncthreads();
     if (warp == 1) {
