@@ -221,17 +221,24 @@ def _on_device_of_first(fn):
     current one of that device) are then that device's, whichever device the caller has current.  The guard bands are
     checked here as well, in one wrapper: these calls are a few microseconds of GPU work at their smallest."""
     guarded = _guarded(fn)
+    name = fn.__code__.co_varnames[0]
 
     @functools.wraps(fn)
-    def call(first, *args, **kwargs):
-        index = first.get_device()
+    def call(*args, **kwargs):
+        if args:
+            first = args[0]
+        elif name in kwargs:
+            first = kwargs[name]
+        else:
+            return fn(**kwargs)                   # raises: the message names what is missing
+        index = first.get_device() if isinstance(first, torch.Tensor) else -1
         if index < 0:
             raise TypeError(f"{fn.__name__}: expected CUDA tensors")
         run = guarded if guard_mode() else fn
         if index == torch._C._cuda_getDevice():
-            return run(first, *args, **kwargs)
+            return run(*args, **kwargs)
         with torch.cuda.device(first.device):
-            return run(first, *args, **kwargs)
+            return run(*args, **kwargs)
     call._guards_itself = True
     return call
 
