@@ -334,7 +334,7 @@ sol_status_t sol_attention_blocks(const void *q, const void *k, const void *v, v
  *   workspace   device scratch of at least sol_matvec_workspace_bytes(M, K) bytes, 256-byte aligned; holds x in the
  *               products' layout; contents undefined after.  Two calls that may overlap need one each.  The size is 0, and
  *               NULL will do, for up to four rows of up to 3072 columns, which every block prepares for itself
- *   M >= 1 (the weight is read once per 64 rows), N % 8 == 0, K % 32 == 0
+ *   M >= 1 (the weight is read once per 64 rows), N % 8 == 0, K % 32 == 0;  y shares no element with an input
  * Two launches, one where no workspace is needed.  Sums are FP32 and in a fixed order.  Before the product act(x) is
  * scaled by a power of two per row (and slice of K) and held in FP16: BF16 values down to 2^-29 of the row's largest are kept
  * exactly where that is at least 2^-100 (an activation's result to 11 bits).  The operands' scales may lie anywhere: only a sum
@@ -396,7 +396,8 @@ sol_status_t sol_qk_rotary(const sol_head_tensor_t *q, const sol_head_tensor_t *
  *   dweight    [head_dim] FP32, overwritten; needed when there is a weight (NULL without one)
  *   workspace  device scratch of sol_qk_rotary_backward_workspace_bytes(head_dim) bytes, 256-byte aligned; needed when
  *              there is a weight.  Two calls that may overlap need one each.
- * The weight gradients are summed in a fixed order: equal inputs give equal bits.
+ * The weight gradients are summed in a fixed order: equal inputs give equal bits.  The terms that one GPU thread meets on its
+ * walk over the tokens are added in FP32, the sums of different warps in FP64.
  */
 typedef struct {
     const void *dy, *x;

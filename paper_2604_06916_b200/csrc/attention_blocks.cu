@@ -18,10 +18,11 @@
 // owner and MMA issuer, 10 = counts the list of the next item; their warpgroup leaves registers to the other two.  Every
 // mbarrier wait is bounded, and a warp that works together gives up together.
 //
-// Measured on B200 (inside a CUDA graph): 4 x 4608 tokens, 24 heads of 128, 9 of 36 blocks 229 us (1 140 TFLOP/s, 69 % of the
-// measured BF16 rate; 231 to 237 us on boxes that clock lower); 2 x 4429, 38 heads of 64, 8 blocks 151 us; 1 x 1536, 24 heads
-// of 128, 4 of 12 blocks 14.9 us.  A key tile takes 3 030 cycles for both query tiles (d = 128), of which the products are
-// 2 048 and the rest is the way of a score row through its thread.  An item costs 3 000 to 3 800 cycles more: last product,
+// Measured on B200: 4 x 4608 tokens, 24 heads of 128, 9 of 36 blocks 271 us in a loop of calls (960 TFLOP/s, 58 % of the measured
+// BF16 rate) and 229 to 256 us inside a graph, by the clock that the board holds; 2 x 4429, 38 heads of 64, 8 blocks 153 and
+// 151 us; 1 x 1536, 24 heads of 128, 4 of 12 blocks 16.4 and 13.8 us.  A key tile takes 3 030 cycles for both query tiles (d =
+// 128; clock readings of a tracing copy), of which the products are 2 048 and the rest is the way of a score row through its
+// thread; the tensor pipe is busy 59 % of a block's time (d = 64: 30 %).  An item costs 3 000 to 3 800 cycles more: last product,
 // output, next first scores.  A CTA per item instead, with the same steps, takes 12.8 us on the smallest case (nothing to
 // overlap there, and a plainer way in) but 157 and 234 us on the others.
 // Tried without gain: sixteen softmax warps, two threads per row (345 us on the first case); P in two halves (277); three-input

@@ -7,9 +7,13 @@
 // Two launches.  prepare_x turns x (after the activation) into FP16 once, in the shared-memory image of the products'
 // operand; the products' kernel is launched along with it (programmatic launch) and waits for it only where x enters.
 // Up to four rows of K <= 3072 are prepared by every CTA for its own slice instead (two of its warpgroups, while the other
-// two convert the first stage): one launch and no workspace, which is what a caller without graphs waits for (1 x 9216 x
-// 3072: 13 us a call against 17; 9.7 against 9.2 us inside a graph).  With eight rows the exponentials alone would
-// take a CTA longer than its weights.
+// two convert the first stage): one launch and no workspace, 2.1 to 2.7 us less for a caller without graphs.  Inside a graph
+// it is the slower form, by more the more x a CTA prepares (one / two launches, us, 9216 columns; in brackets with weights from HBM):
+//     K = 1536: 1 row 7.4 / 7.4 (8.2 / 8.3), 4 rows 7.9 / 7.5 (8.9 / 8.3);   K = 3072: 9.6 / 9.1 (11.4 / 10.3), 10.3 / 9.2 (11.8 / 10.3)
+//     K = 4608: 11.5 / 11.0 (13.4 / 12.1), 12.4 / 11.0 (14.4 / 12.1);   2304 columns, K = 8192: 10.4 / 9.6, 11.3 / 9.7
+// The bound on K is that of a CTA's slice (the registers that hold x), for a grid without a cluster, whose slice is all of K;
+// beyond it the graph would lose up to 2.2 us where the call gains 2.4.  With eight rows the exponentials alone would take a CTA longer
+// than its weights.
 // One CTA takes 128 output columns (a row group of the chunked scale layout) and a slice of K, one CTA per SM; where the
 // columns leave SMs free, a cluster of up to eight CTAs shares K, each adds up its share of the 128 columns in rank order.
 // The weight is the M = 128 operand of tcgen05.mma kind::f16 and comes from tensor memory: codes, scales and x
@@ -17,10 +21,12 @@
 // (cvt.e2m1x2), multiplies by the block scales and leaves them in its TMEM lane; x is the N operand (16 to 64 rows).
 // Four warpgroups convert: two share an even stage, two an odd one, while the products of the stage before run.
 //
-// Measured (B200, inside a graph): NVFP4 1 x 9216 x 3072 9.7 us, 8 x 18432 x 3072 12.0 us (floor 4.9 us), MXFP4 24 x 14592 x
-// 2432 12.9 us (floor 3.0 us).  While stages run they run at the weights' HBM rate (800 cycles per 18 KB stage and SM; leaving
-// out three quarters of the products or of the conversions changes nothing at up to sixteen rows); the rest is the way
-// in (2 to 2.5 us until the first codes arrive) and out (1.5 us from the last product to the stores).  Four stages: with eight
+// Measured (B200, inside a graph, one weight again and again, which L2 then holds): NVFP4 1 x 9216 x 3072 9.4 us, 8 x 18432 x
+// 3072 11.4 us, MXFP4 24 x 14592 x 2432 12.1 us; 400 MB of weights in turn, so that each comes from HBM: 10.9, 13.1 and 14.5 us
+// (floors 2.4, 4.9 and 3.0 us).  A stage takes 800 cycles per SM while stages run; leaving out three quarters of the products
+// or of the conversions changes nothing at up to sixteen rows, nor does L2 in place of HBM make up more than 2.4 us of the
+// whole.  The rest is the way in (2 to 2.5 us until the first codes arrive, prepare_x beside it) and out (1.5 us from the last
+// product to the stores).  Four stages: with eight
 // in flight the first one arrives with the last (13.5 us), with two the ring runs dry (16.8 us).  Register tiles and
 // mma.sync m16n8k16 in place of tensor memory: 11.5, 23.7 and 28 us; converting for mma.sync costs 2 codes per cycle and
 // scheduler and every eight rows of x as much again, tcgen05 takes 64 rows for the price of one.

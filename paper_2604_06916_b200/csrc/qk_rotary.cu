@@ -12,11 +12,11 @@
 // same eight columns of every head (in the half layout four and their four partners), so the angles are formed once
 // per token and tensor, each by one lane, and handed round by shuffles while the first heads' loads are under way.
 // Four heads per lane are loaded before any is used.  Where tokens are few, up to one warp per four-head group shares a
-// token.  Measured (B200, q and k of 24 heads x 128 from a fused projection, norm and three axes): forward, 8 x 4608
-// tokens, 143 us = 6.3 TB/s, 97 % of the copy rate (one warp per token and eight heads, with its index divisions and
-// angles for each: 195 us); 333 tokens, 4.1 us.  Gradients, 2 x 4608 tokens, 64 to 66 us = 5.2 TB/s, 79 %: 113 registers
-// hold both tensors' loads, sixteen warps per SM wait for memory 2.4 cycles per issued instruction.  Two heads per lane
-// with 24 warps take 71 us, with the next ones prefetched 73 us.  38 and 19 heads of 64, 4099 tokens: 25 us with eight heads a
+// token.  Measured (B200, inside a graph, q and k of 24 heads x 128 from a fused projection, norm and three axes): forward,
+// 8 x 4608 tokens, 143 us = 6.3 TB/s, 97 % of the copy rate (one warp per token and eight heads, with its index divisions and
+// angles for each: 195 us); 333 tokens, 4.0 us.  Gradients, 2 x 4608 tokens, 63 to 65 us = 5.3 TB/s, 81 %: 116 registers
+// hold both tensors' loads, sixteen warps per SM wait for memory 2.3 cycles per issued instruction.  Two heads per lane
+// with 24 warps take 71 us, with the next ones prefetched 73 us.  38 and 19 heads of 64, 4099 tokens: 24 us with eight heads a
 // step (sixteen: 27 us, a token's last step then leaves most lanes idle); q and k share the blocks by their steps (half
 // each: 29 us).
 //
@@ -231,8 +231,9 @@ forward_kernel(const Heads2 both, const Turn t, uint32_t rows, int parts_log2, f
 }
 
 // Gradients.  The first blocks_q blocks take q, the others k; blocks stay and walk the (token, part of its heads) tasks, so that the weight
-// gradient collects in registers: per lane over its tasks, per block over the lanes and warps that share a column
-// (FP64, fixed order), and reduce_weight_grads adds the blocks up.  No atomics: the result depends on nothing but
+// gradient collects in registers: per lane over its tasks and then over the lanes that share a column in FP32 (the FP32
+// chain: one term per head that the lane holds in each of its tasks, 384 for 8 x 4608 tokens of 24 heads x 128), over the block's warps
+// and, in reduce_weight_grads, over the blocks in FP64, all in a fixed order.  No atomics: the result depends on nothing but
 // the shape.
 template <int kD, bool kHalf>
 __global__ void __launch_bounds__(32 * kWarps, Shape<kD>::kBackResident)
@@ -308,7 +309,7 @@ backward_kernel(const Grads2 both, const Turn t, uint32_t rows, int blocks_q, in
         }
     }
     if (partials == nullptr) return;
-    // lanes that hold the same columns, then the warps, then one FP64 value per column and block
+    // lanes that hold the same columns (FP32), then the warps: one FP64 value per column and block
     __shared__ float part[kWarps][kD];
     float sums[8];
 #pragma unroll

@@ -10,9 +10,11 @@
 // 2^-896, undone once per mean): two or three integer operations in place of a conversion instruction, which issues
 // at a quarter of the rate of the additions.
 //
-// Measured (B200): 2 x 4608 tokens, 24 heads x 128, 9 of 36 blocks: 35 us, of which pooling 25 us (4.5 TB/s; floor of both
-// 17 us); 16421 tokens, 38 heads x 64, 24 of 129 blocks: 49 us (pooling 35 us, floor 24 us).  What pooling spends beside
-// its loads is 6.5 instructions per element.  One block per unit with sixteen rows in flight per warp, whose warps all load
+// Measured (B200, inside a graph): 2 x 4608 tokens, 24 heads x 128, 9 of 36 blocks: 35 us, of which pooling 25 us (4.5 TB/s; floor of both
+// 17 us); 16421 tokens, 38 heads x 64, 24 of 129 blocks: 48 us (pooling 35 us, floor 24 us).  Pooling issues 6.5 instructions
+// per element, which is half of its blocks' time and goes on under the loads; the other loss is uneven work: a query unit
+// has twice a key unit's rows, and the fullest block gets 7 half-units of 128 rows against a mean of 5.84 (16421 tokens: 10
+// against 8.75, the last of ten column chunks half empty besides).  One block per unit with sixteen rows in flight per warp, whose warps all load
 // at once and then add at once: 34 us and 69 us; eight rows: 46 and 96 us.  A warp per query block for the scores, the
 // key means read again for each: 84 us and 145 us.
 #include "ptx.cuh"
