@@ -162,13 +162,13 @@ __device__ __forceinline__ void activate8(uint4 r, int act, float (&f)[8]) {
 // e - kXExp with e the exponent of the largest element (FP32 bits), held to what FP32 can scale by; and 2^(kXExp - e).
 __device__ __forceinline__ int exponent_back(uint32_t bits) { return min(max(static_cast<int>(bits >> 23) - 127, -100), 127) - kXExp; }
 __device__ __forceinline__ float scale_up(uint32_t bits) { return __uint_as_float(static_cast<uint32_t>(127 - exponent_back(bits)) << 23); }
-// T = t 2^exp with t in [1, 2) (zero, infinities and NaN keep their value).
+// T = t 2^exp with t in [1, 2); a subnormal T: t = T 2^100; zero, infinities and NaN keep their value.
 __device__ __forceinline__ float split_scale(float T, int &exp) {
     const uint32_t bits = __float_as_uint(T), field = bits >> 23 & 255u;
     exp = field == 0 ? -100 : field == 255u ? 0 : static_cast<int>(field) - 127;
     return field == 0 ? T * 0x1p100f : field == 255u ? T : __uint_as_float((bits & 0x807FFFFFu) | 0x3F800000u);
 }
-// v 2^n in two exact steps, for |v| < 2^55 and n from -263 to 241: where the first step overflows or loses bits, the result is
+// v 2^n in two exact steps, for |v| < 2^55 and n from -254 to 240: where the first step overflows or loses bits, the result is
 // infinite or zero anyway.
 struct PowerOfTwo {
     float a, b;
