@@ -33,6 +33,7 @@ EXPORTS = [
     "mxfp4_linear_split_out", "mxfp4_quantize_into", "sol_qk_rotary", "sol_qk_rotary_backward",
     "sol_qk_rotary_backward_workspace_bytes", "sol_rotary_frequencies", "nvfp4_matvec", "mxfp4_matvec",
     "sol_matvec_workspace_bytes", "sol_select_blocks", "sol_select_blocks_workspace_bytes", "sol_attention_blocks",
+    "sol_layernorm", "sol_layernorm_backward", "sol_layernorm_backward_workspace_bytes",
 ]
 
 _lib = None
@@ -129,6 +130,12 @@ def lib() -> ctypes.CDLL:
     L.sol_qk_rotary_backward_workspace_bytes.restype, L.sol_qk_rotary_backward_workspace_bytes.argtypes = sz, [i64]
     L.sol_rotary_frequencies.restype = i32
     L.sol_rotary_frequencies.argtypes = [i64, f64, i32, f64, f64, f64, f64, vp, vp]
+    L.sol_layernorm.restype = i32
+    L.sol_layernorm.argtypes = [vp, i64, i64, i64, vp, vp, i64, f32, f32, vp, i64, vp, vp]
+    L.sol_layernorm_backward.restype = i32
+    L.sol_layernorm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, f32, vp, i64, vp, vp, vp, sz, vp]
+    L.sol_layernorm_backward_workspace_bytes.restype = sz
+    L.sol_layernorm_backward_workspace_bytes.argtypes = [i64, i64, i64]
     L.sol_set_wait_limit_cycles.restype, L.sol_set_wait_limit_cycles.argtypes = i32, [i64]
     L.sol_test_hold_loads.restype, L.sol_test_hold_loads.argtypes = i32, [i32]
     L.sol_last_device_status.restype = i32
@@ -786,6 +793,97 @@ def sol_qk_rotary_backward(dq, dk, q, k, positions, freqs, axis_dims=None, layou
     if code:
         raise SolError(code, "sol_qk_rotary_backward")
     return dxs[0], dxs[1], dws[0], dws[1]
+
+
+def _rows_view(name: str, t: torch.Tensor, index: int, shape=None) -> int:
+    """Checks a BF16 matrix [M, K] with contiguous rows on CUDA device `index` and returns its row pitch."""
+    if t.dtype is not torch.bfloat16 or t.dim() != 2:
+        raise TypeError(f"{name}: expected a 2-D bf16 tensor")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, the call's first tensor on cuda:{index}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return t.stride(0) if rows > 1 else cols
+
+
+def _dense(name: str, t: torch.Tensor, dtype, shape, index: int) -> int:
+    """Checks a dense tensor of the given type and shape on CUDA device `index` and returns its address."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
+        raise TypeError(f"{name}: expected a dense {dtype} tensor of shape {tuple(shape)} on cuda:{index}")
+    return t.data_ptr()
+
+
+def _scratch(workspace, need: int, like: torch.Tensor, index: int):
+    """A call's workspace: the caller's, or a new one of `need` bytes; (tensor or None, address, bytes)."""
+    if workspace is None:
+        if need == 0:
+            return None, None, 0
+        workspace = _new(like, need, torch.uint8)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise TypeError("workspace: expected a dense tensor on the first tensor's device")
+    return workspace, workspace.data_ptr(), workspace.nbytes
+
+
+@_on_device_of_first
+def sol_layernorm(x, scale=None, shift=None, rows_per_sample: int | None = None, eps: float = 1e-6, scale_offset: float = 1.0,
+                  out: torch.Tensor | None = None, with_stats: bool = False):
+    """LN(x) * (scale_offset + scale[sample]) + shift[sample] in BF16; scale_offset 1: modulation, 0: a weight and a bias.
+
+    x [M, K] (a view with a row pitch will do); scale and shift [samples, K] or None, a sample being `rows_per_sample` rows (default:
+    all).  Returns y, or (y, stats) `with_stats`: FP32 [M, 2] mean and 1 / sqrt(var + eps) for sol_layernorm_backward.
+    """
+    index = x.get_device()
+    ldx = _rows_view("x", x, index)
+    M, K = x.shape
+    rows = M if rows_per_sample is None else rows_per_sample
+    samples = -(-M // rows) if rows > 0 else 0
+    scale_ptr = None if scale is None else _dense("scale", scale, torch.bfloat16, (samples, K), index)
+    shift_ptr = None if shift is None else _dense("shift", shift, torch.bfloat16, (samples, K), index)
+    if out is None:
+        out, ldy = _new(x, (M, K)), K
+    else:
+        ldy = _rows_view("out", out, index, x.shape)
+    stats = _new(x, (M, 2), torch.float32) if with_stats else None
+    code = lib().sol_layernorm(x.data_ptr(), M, K, ldx, scale_ptr, shift_ptr, rows, scale_offset, eps, out.data_ptr(), ldy,
+                               None if stats is None else stats.data_ptr(), _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_layernorm")
+    return (out, stats) if with_stats else out
+
+
+@_on_device_of_first
+def sol_layernorm_backward(dy, x, stats, scale=None, rows_per_sample: int | None = None, scale_offset: float = 1.0,
+                           out: torch.Tensor | None = None, with_scale: bool = True, with_shift: bool = True,
+                           workspace: torch.Tensor | None = None):
+    """Gradients of sol_layernorm from that of its output: (grad x, grad scale, grad shift).
+
+    x, stats and scale are the forward call's.  The gradients of scale and shift are FP32 [samples, K], summed over each
+    sample's rows, None where not asked for.  `out` = grad x may be dy or x itself.
+    """
+    index = dy.get_device()
+    ld_dy = _rows_view("dy", dy, index)
+    M, K = dy.shape
+    ldx = _rows_view("x", x, index, dy.shape)
+    rows = M if rows_per_sample is None else rows_per_sample
+    samples = -(-M // rows) if rows > 0 else 0
+    stats_ptr = _dense("stats", stats, torch.float32, (M, 2), index)
+    scale_ptr = None if scale is None else _dense("scale", scale, torch.bfloat16, (samples, K), index)
+    if out is None:
+        out, ld_dx = _new(dy, (M, K)), K
+    else:
+        ld_dx = _rows_view("out", out, index, dy.shape)
+    dscale = _new(dy, (samples, K), torch.float32) if with_scale else None
+    dshift = _new(dy, (samples, K), torch.float32) if with_shift else None
+    need = lib().sol_layernorm_backward_workspace_bytes(M, K, rows) if with_scale or with_shift else 0
+    workspace, ws_ptr, ws_bytes = _scratch(workspace, need, dy, index)
+    code = lib().sol_layernorm_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ldx, stats_ptr, scale_ptr, M, K, rows, scale_offset,
+                                        out.data_ptr(), ld_dx, _ptr(dscale), _ptr(dshift), ws_ptr, ws_bytes, _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_layernorm_backward")
+    return out, dscale, dshift
 
 
 QUERY_BLOCK, KEY_BLOCK = 256, 128
