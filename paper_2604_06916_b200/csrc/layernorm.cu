@@ -6,16 +6,25 @@
 //     dx = rstd (w - mean(w) - xhat mean(w xhat)),   dscale[s] = sum over the sample's rows of dy xhat,   dshift[s] = sum of dy.
 // HBM bound: 4 bytes per element forward, 6 backward.
 //
-// Forward: a warp (wide rows: four warps) holds a row in registers, so mean, variance (of the centred values) and output
-// take one read of x; scale and shift come from the caches.
+// Forward: a group of warps (one to sixteen, so that a lane holds up to three pieces of eight columns) walks neighbouring rows with
+// the row in registers, so mean, variance (of the centred values) and output take one read of x; scale and shift stay in
+// registers while the sample lasts and the next row is under way while this one is summed.  Measured (B200, inside a graph): 36864 x 3072,
+// eight samples, 75.6 us = 6.0 TB/s, 91 % of the copy rate (a warp per row of its own 113 us: 16 warps per SM, each waiting for its
+// one row; two warps 97 us, four 87 us); 333 x 2432 2.8 us.
 //
 // Gradients: a thread owns the same eight columns of every row that its block walks, so that the sums over rows stay in its
-// registers; the two row means go over the block (a group of warps per row, as many groups as fit the block) once per kRows
-// rows.  A block's sums leave as FP32 partials, which a second launch adds up in FP64 in a fixed order: equal inputs give
-// equal bits.
+// registers; the two row means go over the block (a group of warps per row, as many groups as fit the block) once per four
+// rows, whose successors are under way meanwhile.  A block's sums leave as FP32 partials, which a second launch adds up in FP64 in
+// a fixed order: equal inputs give equal bits.  Measured: 9216 x 3072, two samples, 33.3 us = 5.1 TB/s, 78 %; 13287 x 2432 43.2 us.
+// Bound by issuing: some 560 instructions a warp and four rows, half of them taking BF16 apart and putting it together; twelve warps a
+// block with 168 registers issue every second cycle.  The sum over the blocks is 4 us of it.  Rows through a ring in shared
+// memory (24 warps, bulk copies) took 43.6 us: the same instructions and the second reads; without loads ahead 41 us, two
+// sets of registers in turn spill (51 us), two blocks an SM with fewer rows a step 43 us.
 #include "ptx.cuh"
 #include "quant_math.cuh"
 #include "sol_internal.h"
+
+#include <type_traits>
 
 namespace sol {
 namespace norm {
@@ -68,72 +77,92 @@ struct Forward {
 
 constexpr int kForwardWarps = 8;
 
-// kWarps warps share a row; a lane holds kChunks pieces of eight columns.
+// kWarps warps (a group) share a row and walk neighbouring rows, a lane holds the same kChunks pieces of eight columns of each:
+// scale and shift stay in registers while the sample lasts, and the next row is under way while this one is summed.
 template <int kWarps, int kChunks>
-__global__ void __launch_bounds__(32 * kForwardWarps)
+__global__ void __launch_bounds__(kWarps > kForwardWarps ? 32 * kWarps : 32 * kForwardWarps)
 forward_kernel(const Forward p) {
-    constexpr int kRows = kForwardWarps / kWarps, kLanes = 32 * kWarps;
-    __shared__ float part[2][kForwardWarps];
-    const int lane = threadIdx.x % kLanes, warp = threadIdx.x >> 5;
-    const uint32_t m = blockIdx.x * kRows + threadIdx.x / kLanes;
-    const bool there = m < p.rows;
-    if (kWarps == 1 && !there) return;
-    const int pieces = there ? p.K >> 3 : 0;
-    const uint16_t *x = p.x + m * p.ldx;
-    uint4 raw[kChunks];
+    constexpr int kBlockWarps = kWarps > kForwardWarps ? kWarps : kForwardWarps;
+    constexpr int kGroups = kBlockWarps / kWarps, kLanes = 32 * kWarps;
+    __shared__ float part[2][kBlockWarps];
+    const int lane = threadIdx.x % kLanes, warp = threadIdx.x >> 5, group = threadIdx.x / kLanes;
+    const uint64_t groups = static_cast<uint64_t>(gridDim.x) * kGroups, mine = static_cast<uint64_t>(blockIdx.x) * kGroups + group;
+    const uint32_t r0 = static_cast<uint32_t>(p.rows * mine / groups), r1 = static_cast<uint32_t>(p.rows * (mine + 1) / groups);
+    if (r0 >= r1) return;               // the whole group: its barrier is its own
+    const int pieces = p.K >> 3;
+    auto load_row = [&](uint4 (&raw)[kChunks], uint32_t m) {
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) raw[i] = lane + i * kLanes < pieces ? load8(x + 8 * (lane + i * kLanes)) : make_uint4(0, 0, 0, 0);
-    // the sum over the row's lanes, in a fixed order; buffer b is written once
+        for (int i = 0; i < kChunks; ++i)
+            raw[i] = lane + i * kLanes < pieces ? load8(p.x + m * p.ldx + 8 * (lane + i * kLanes)) : make_uint4(0, 0, 0, 0);
+    };
+    // the sum over the row's lanes in a fixed order; the two buffers take turns, so one barrier a sum is enough
     auto row_sum = [&](float v, int b) {
         v = warp_sum(v);
         if (kWarps == 1) return v;
         if ((threadIdx.x & 31) == 0) part[b][warp] = v;
-        __syncthreads();
+        asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(kLanes) : "memory");
         float s = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) s += part[b][warp / kWarps * kWarps + w];
+        for (int w = 0; w < kWarps; ++w) s += part[b][group * kWarps + w];
         return s;
     };
-    uint64_t s2 = 0;
+    const uint64_t o2 = twice(p.offset);
+    uint4 gain[kChunks], shift[kChunks], raw[kChunks];
+    uint32_t left = 0;                  // rows of the sample whose scale and shift are held
+    load_row(raw, r0);
+    for (uint32_t m = r0; m < r1; ++m, --left) {
+        if (left == 0) {
+            const uint32_t sample = m / p.rows_per_sample;
+            left = p.rows_per_sample - (m - sample * p.rows_per_sample);
+            const int64_t s = static_cast<int64_t>(sample) * p.K;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        s2 = add2(s2, add2(add2(f32x2_of_bf16x2(raw[i].x), f32x2_of_bf16x2(raw[i].y)), add2(f32x2_of_bf16x2(raw[i].z), f32x2_of_bf16x2(raw[i].w))));
-    }
-    const float mean = row_sum(sum_lanes(s2), 0) * p.inv_k;
-    const uint64_t nm = twice(-mean);
-    uint64_t q2 = 0;
-#pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        if (lane + i * kLanes < pieces) {
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint64_t d = add2(f32x2_of_bf16x2(w[e]), nm);
-                q2 = fma2(d, d, q2);
+            for (int i = 0; i < kChunks; ++i) {
+                const int c = 8 * (lane + i * kLanes);
+                gain[i] = p.scale != nullptr && c < p.K ? cached8(p.scale + s + c) : make_uint4(0, 0, 0, 0);
+                shift[i] = p.shift != nullptr && c < p.K ? cached8(p.shift + s + c) : make_uint4(0, 0, 0, 0);
             }
         }
-    }
-    const float rstd = 1.0f / sqrtf(fmaf(row_sum(sum_lanes(q2), 1), p.inv_k, p.eps));
-    if (!there) return;
-    if (p.stats != nullptr && lane == 0) p.stats[m] = make_float2(mean, rstd);
-    const int64_t s = static_cast<int64_t>(m / p.rows_per_sample) * p.K;
-    uint16_t *y = p.y + m * p.ldy;
-    const uint64_t r2 = twice(rstd), o2 = twice(p.offset);
+        uint4 next[kChunks];
+        if (m + 1 < r1) load_row(next, m + 1);
+        uint64_t s2 = 0;
 #pragma unroll
-    for (int i = 0; i < kChunks; ++i) {
-        const int c = 8 * (lane + i * kLanes);
-        if (lane + i * kLanes < pieces) {
-            const uint4 g = p.scale != nullptr ? cached8(p.scale + s + c) : make_uint4(0, 0, 0, 0);
-            const uint4 b = p.shift != nullptr ? cached8(p.shift + s + c) : make_uint4(0, 0, 0, 0);
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w}, gw[4] = {g.x, g.y, g.z, g.w}, bw[4] = {b.x, b.y, b.z, b.w};
-            uint32_t out[4];
+        for (int i = 0; i < kChunks; ++i)
+            s2 = add2(s2, add2(add2(f32x2_of_bf16x2(raw[i].x), f32x2_of_bf16x2(raw[i].y)), add2(f32x2_of_bf16x2(raw[i].z), f32x2_of_bf16x2(raw[i].w))));
+        const float mean = row_sum(sum_lanes(s2), 0) * p.inv_k;
+        const uint64_t nm = twice(-mean);
+        uint64_t q2 = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint64_t xhat = mul2(add2(f32x2_of_bf16x2(w[e]), nm), r2);
-                out[e] = pack2(fma2(xhat, add2(f32x2_of_bf16x2(gw[e]), o2), f32x2_of_bf16x2(bw[e])));
+        for (int i = 0; i < kChunks; ++i) {
+            if (lane + i * kLanes < pieces) {
+                const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t d = add2(f32x2_of_bf16x2(w[e]), nm);
+                    q2 = fma2(d, d, q2);
+                }
             }
-            *reinterpret_cast<uint4 *>(y + c) = make_uint4(out[0], out[1], out[2], out[3]);
         }
+        const float rstd = 1.0f / sqrtf(fmaf(row_sum(sum_lanes(q2), 1), p.inv_k, p.eps));
+        if (p.stats != nullptr && lane == 0) p.stats[m] = make_float2(mean, rstd);
+        uint16_t *y = p.y + m * p.ldy;
+        const uint64_t r2 = twice(rstd);
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = 8 * (lane + i * kLanes);
+            if (lane + i * kLanes < pieces) {
+                const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                const uint32_t gw[4] = {gain[i].x, gain[i].y, gain[i].z, gain[i].w}, bw[4] = {shift[i].x, shift[i].y, shift[i].z, shift[i].w};
+                uint32_t out[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t xhat = mul2(add2(f32x2_of_bf16x2(w[e]), nm), r2);
+                    out[e] = pack2(fma2(xhat, add2(f32x2_of_bf16x2(gw[e]), o2), f32x2_of_bf16x2(bw[e])));
+                }
+                *reinterpret_cast<uint4 *>(y + c) = make_uint4(out[0], out[1], out[2], out[3]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) raw[i] = next[i];
     }
 }
 
@@ -147,12 +176,13 @@ struct Backward {
     int64_t ld_dy, ld_x, ld_dx;
     uint32_t rows, rows_per_sample;
     int K, samples, pieces;     // pieces of a sample
+    int warps_per_row;
     float offset, inv_k;
 };
 
-constexpr int kMaxWarps = 16;           // of a block
+constexpr int kMaxWarps = 16;           // of a block, at most (twelve where 168 registers a thread are wanted: up to 12288 columns)
 constexpr int kGroupColumns = 256;      // columns of a warp and piece
-
+__host__ __device__ constexpr int rows_of(int chunks) { return chunks == 1 ? 4 : chunks == 2 ? 2 : 1; }   // rows of a group's step
 // Sums of kValues (a power of two up to 32) values over the warp: lane l ends up with that of value l >> (5 - log2 kValues).
 template <int kValues>
 __device__ __forceinline__ float transpose_sum(float (&v)[kValues], int lane) {
@@ -175,108 +205,131 @@ __device__ __forceinline__ float transpose_sum(float (&v)[kValues], int lane) {
     return v[0];
 }
 
-template <int kChunks, int kRows>
-__global__ void __launch_bounds__(32 * kMaxWarps, 1)
-backward_kernel(const Backward p, int warps_per_row) {
-    constexpr int kValues = 2 * kRows;
+template <int kChunks, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps, 1)
+backward_kernel(const Backward p) {
+    constexpr int kRows = rows_of(kChunks), kValues = 2 * kRows;
     constexpr int kLanesPer = 32 / kValues;                   // lanes that hold one value after the warp's sum
     __shared__ float part[2][kMaxWarps][kValues];             // [buffer][warp]
-    __shared__ __align__(16) float across[kChunks == 1 ? kMaxWarps * kGroupColumns : 4];   // the groups' sums: eight columns a thread
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int groups = (blockDim.x >> 5) / warps_per_row, group = warp / warps_per_row, first_warp = group * warps_per_row;
-    const int lanes = 32 * warps_per_row, at = threadIdx.x - 32 * first_warp;
+    __shared__ __align__(16) float across[kMaxWarps * kGroupColumns];   // the groups' sums: eight columns a thread
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per_row = p.warps_per_row;
+    const int groups = (blockDim.x >> 5) / per_row, group = warp / per_row, first_warp = group * per_row;
+    const int lanes = 32 * per_row, at = threadIdx.x - 32 * first_warp;
     const int columns8 = p.K >> 3;
+    const uint32_t stride = groups * kRows;
+    struct Step {
+        uint4 x[kRows][kChunks], dy[kRows][kChunks];
+        float2 stats[kRows];
+    };
     const uint64_t o2 = twice(p.offset);
     int buffer = 0;
+    int place[kChunks];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) place[i] = at + i * lanes < columns8 ? 8 * (at + i * lanes) : 0;
     for (int item = blockIdx.x; item < p.samples * p.pieces; item += gridDim.x) {
         const int sample = item / p.pieces, piece = item - sample * p.pieces;
-        const uint32_t s0 = static_cast<uint32_t>(sample) * p.rows_per_sample;
-        const uint32_t len = min(p.rows_per_sample, p.rows - s0);
-        const uint32_t r0 = s0 + static_cast<uint32_t>(static_cast<uint64_t>(len) * piece / p.pieces);
-        const uint32_t r1 = s0 + static_cast<uint32_t>(static_cast<uint64_t>(len) * (piece + 1) / p.pieces);
-        uint4 gain[kChunks];
-        uint64_t acc_scale[kChunks][4], acc_shift[kChunks][4];
+        const uint32_t s0 = static_cast<uint32_t>(sample) * p.rows_per_sample, len = min(p.rows_per_sample, p.rows - s0);
+        // the piece's steps, `stride` rows each: all whole but the sample's last one
+        const uint64_t steps = (len + stride - 1) / stride;
+        const uint32_t t0 = static_cast<uint32_t>(steps * piece / p.pieces), t1 = static_cast<uint32_t>(steps * (piece + 1) / p.pieces);
+        const uint32_t end = s0 + len;
+        uint64_t gain[kChunks][4], acc_scale[kChunks][4], acc_shift[kChunks][4];
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
-            gain[i] = make_uint4(0, 0, 0, 0);
-            if (p.scale != nullptr && at + i * lanes < columns8) gain[i] = cached8(p.scale + static_cast<int64_t>(sample) * p.K + 8 * (at + i * lanes));
+            uint4 g = make_uint4(0, 0, 0, 0);
+            const bool there = at + i * lanes < columns8;
+            if (p.scale != nullptr && there) g = cached8(p.scale + static_cast<int64_t>(sample) * p.K + 8 * (at + i * lanes));
+            const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc_scale[i][e] = acc_shift[i][e] = 0;
+            for (int e = 0; e < 4; ++e) {
+                gain[i][e] = there ? add2(f32x2_of_bf16x2(gw[e]), o2) : 0;
+                acc_scale[i][e] = acc_shift[i][e] = 0;
+            }
         }
-        // every group takes as many steps: the barrier below is its own, the block's only at the end
-        for (uint32_t base = r0 + group * kRows; base < r1; base += groups * kRows) {
-            uint4 raw_x[kRows][kChunks], raw_d[kRows][kChunks];
-            float2 st[kRows];
+        // rows that do not exist read as 0; a lane without columns reads the first ones, which its gain of 0 takes out of the sums
+        auto fetch = [&](Step &s, uint32_t base, auto whole) {
+            const uint16_t *x = p.x + base * p.ld_x, *dy = p.dy + base * p.ld_dy;
 #pragma unroll
             for (int j = 0; j < kRows; ++j) {
-                const bool there = base + j < r1;
-                st[j] = there ? __ldg(p.stats + base + j) : make_float2(0.0f, 0.0f);
+                const bool there = decltype(whole)::value || base + j < end;
+                s.stats[j] = there ? __ldg(p.stats + base + j) : make_float2(0.0f, 0.0f);
 #pragma unroll
                 for (int i = 0; i < kChunks; ++i) {
-                    raw_x[j][i] = raw_d[j][i] = make_uint4(0, 0, 0, 0);
-                    if (there && at + i * lanes < columns8) {
-                        raw_x[j][i] = load8(p.x + (base + j) * p.ld_x + 8 * (at + i * lanes));
-                        raw_d[j][i] = load8(p.dy + (base + j) * p.ld_dy + 8 * (at + i * lanes));
-                    }
+                    s.x[j][i] = there ? load8(x + j * p.ld_x + place[i]) : make_uint4(0, 0, 0, 0);
+                    s.dy[j][i] = there ? load8(dy + j * p.ld_dy + place[i]) : make_uint4(0, 0, 0, 0);
                 }
             }
+        };
+        auto work = [&](const Step &s, uint32_t base, auto whole) {
             float sums[kValues];
 #pragma unroll
             for (int j = 0; j < kRows; ++j) {
-                const uint64_t r2 = twice(st[j].y), back = twice(-st[j].x * st[j].y);
                 uint64_t s1 = 0, s2 = 0;
+                const uint64_t r2 = twice(s.stats[j].y), back = twice(-s.stats[j].x * s.stats[j].y);
 #pragma unroll
                 for (int i = 0; i < kChunks; ++i) {
-                    const uint32_t xw[4] = {raw_x[j][i].x, raw_x[j][i].y, raw_x[j][i].z, raw_x[j][i].w};
-                    const uint32_t dw[4] = {raw_d[j][i].x, raw_d[j][i].y, raw_d[j][i].z, raw_d[j][i].w};
-                    const uint32_t gw[4] = {gain[i].x, gain[i].y, gain[i].z, gain[i].w};
+                    const uint32_t xw[4] = {s.x[j][i].x, s.x[j][i].y, s.x[j][i].z, s.x[j][i].w};
+                    const uint32_t dw[4] = {s.dy[j][i].x, s.dy[j][i].y, s.dy[j][i].z, s.dy[j][i].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const uint64_t xhat = fma2(f32x2_of_bf16x2(xw[e]), r2, back), d = f32x2_of_bf16x2(dw[e]);
-                        const uint64_t w = mul2(d, add2(f32x2_of_bf16x2(gw[e]), o2));
-                        s1 = add2(s1, w);
-                        s2 = fma2(w, xhat, s2);
+                        const uint64_t d = f32x2_of_bf16x2(dw[e]), dxhat = mul2(d, fma2(f32x2_of_bf16x2(xw[e]), r2, back));
+                        s1 = fma2(d, gain[i][e], s1);
+                        s2 = fma2(dxhat, gain[i][e], s2);
                         acc_shift[i][e] = add2(acc_shift[i][e], d);
-                        acc_scale[i][e] = fma2(d, xhat, acc_scale[i][e]);
+                        acc_scale[i][e] = add2(acc_scale[i][e], dxhat);
                     }
                 }
                 sums[2 * j] = sum_lanes(s1);
                 sums[2 * j + 1] = sum_lanes(s2);
             }
             float total = transpose_sum<kValues>(sums, lane);
-            if (warps_per_row > 1) {
+            if (per_row > 1) {
+                // the two buffers take turns, so one barrier a step is enough
                 if (lane % kLanesPer == 0) part[buffer][warp][lane / kLanesPer] = total;
                 asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(lanes) : "memory");
                 total = 0.0f;
-                for (int w = lane % kLanesPer; w < warps_per_row; w += kLanesPer) total += part[buffer][first_warp + w][lane / kLanesPer];
+                for (int w = lane % kLanesPer; w < per_row; w += kLanesPer) total += part[buffer][first_warp + w][lane / kLanesPer];
 #pragma unroll
                 for (int o = 1; o < kLanesPer; o <<= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
                 buffer ^= 1;
             }
+            total *= p.inv_k;
+            uint16_t *out = p.dx + base * p.ld_dx;
 #pragma unroll
             for (int j = 0; j < kRows; ++j) {
-                const float mean_w = __shfl_sync(0xFFFFFFFFu, total, 2 * j * kLanesPer) * p.inv_k;
-                const float mean_wx = __shfl_sync(0xFFFFFFFFu, total, (2 * j + 1) * kLanesPer) * p.inv_k;
-                if (base + j < r1) {
-                    const uint64_t r2 = twice(st[j].y), back = twice(-st[j].x * st[j].y);
-                    const uint64_t n1 = twice(-mean_w), n2 = twice(-mean_wx);
+                const float mean_w = __shfl_sync(0xFFFFFFFFu, total, 2 * j * kLanesPer);
+                const float mean_wx = __shfl_sync(0xFFFFFFFFu, total, (2 * j + 1) * kLanesPer);
+                // rstd (w - mean_w - xhat mean_wx), with xhat = x rstd - mean rstd, as d (gain rstd) + x a + b
+                const float rstd = s.stats[j].y, a = -rstd * rstd * mean_wx;
+                const uint64_t r2 = twice(rstd), a2 = twice(a), b2 = twice(-fmaf(a, s.stats[j].x, rstd * mean_w));
 #pragma unroll
-                    for (int i = 0; i < kChunks; ++i) {
-                        const uint32_t xw[4] = {raw_x[j][i].x, raw_x[j][i].y, raw_x[j][i].z, raw_x[j][i].w};
-                        const uint32_t dw[4] = {raw_d[j][i].x, raw_d[j][i].y, raw_d[j][i].z, raw_d[j][i].w};
-                        const uint32_t gw[4] = {gain[i].x, gain[i].y, gain[i].z, gain[i].w};
-                        uint32_t out[4];
+                for (int i = 0; i < kChunks; ++i) {
+                    const uint32_t xw[4] = {s.x[j][i].x, s.x[j][i].y, s.x[j][i].z, s.x[j][i].w};
+                    const uint32_t dw[4] = {s.dy[j][i].x, s.dy[j][i].y, s.dy[j][i].z, s.dy[j][i].w};
+                    uint32_t o[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const uint64_t xhat = fma2(f32x2_of_bf16x2(xw[e]), r2, back);
-                            const uint64_t w = mul2(f32x2_of_bf16x2(dw[e]), add2(f32x2_of_bf16x2(gw[e]), o2));
-                            out[e] = pack2(mul2(r2, add2(w, fma2(xhat, n2, n1))));
-                        }
-                        if (at + i * lanes < columns8)
-                            *reinterpret_cast<uint4 *>(p.dx + (base + j) * p.ld_dx + 8 * (at + i * lanes)) = make_uint4(out[0], out[1], out[2], out[3]);
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        o[e] = pack2(fma2(f32x2_of_bf16x2(xw[e]), a2, fma2(f32x2_of_bf16x2(dw[e]), mul2(gain[i][e], r2), b2)));
+                    if ((decltype(whole)::value || base + j < end) && at + i * lanes < columns8)
+                        *reinterpret_cast<uint4 *>(out + j * p.ld_dx + place[i]) = make_uint4(o[0], o[1], o[2], o[3]);
                 }
             }
+        };
+        // whole steps, each one's rows asked for while the one before is worked on
+        uint32_t base = s0 + t0 * stride + group * kRows, left = t1 - t0;
+        const bool tail = left > 0 && base + (left - 1) * stride + kRows > end;     // this group's last step
+        if (tail) --left;
+        Step next;
+        if (left > 0) fetch(next, base, std::true_type{});
+#pragma unroll 1
+        for (; left > 0; --left, base += stride) {
+            const Step now = next;
+            if (left > 1) fetch(next, base + stride, std::true_type{});
+            work(now, base, std::true_type{});
+        }
+        if (tail) {
+            fetch(next, base, std::false_type{});
+            work(next, base, std::false_type{});
         }
         // the groups' sums in order of the groups, one of the two gradients at a time
         const bool whole = p.pieces == 1;
@@ -290,20 +343,20 @@ backward_kernel(const Backward p, int warps_per_row) {
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) f32x2_split(which == 0 ? acc_scale[i][e] : acc_shift[i][e], v[2 * e], v[2 * e + 1]);
-                const int c = at + i * lanes;
-                if (groups > 1) {      // one chunk only: c < lanes
-                    float4 *mine = reinterpret_cast<float4 *>(across) + (group * lanes + c) * 2;
+                if (groups > 1) {
+                    float4 *mine = reinterpret_cast<float4 *>(across) + (group * lanes + at) * 2;
                     mine[0] = make_float4(v[0], v[1], v[2], v[3]);
                     mine[1] = make_float4(v[4], v[5], v[6], v[7]);
                     __syncthreads();
                     if (group == 0) {
                         for (int g = 1; g < groups; ++g) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] += across[(g * lanes + c) * 8 + e];
+                            for (int e = 0; e < 8; ++e) v[e] += across[(g * lanes + at) * 8 + e];
                         }
                     }
                     __syncthreads();
                 }
+                const int c = at + i * lanes;
                 if (group == 0 && c < columns8) {
                     reinterpret_cast<float4 *>(to + 8 * c)[0] = make_float4(v[0], v[1], v[2], v[3]);
                     reinterpret_cast<float4 *>(to + 8 * c)[1] = make_float4(v[4], v[5], v[6], v[7]);
@@ -314,7 +367,7 @@ backward_kernel(const Backward p, int warps_per_row) {
 }
 
 // Sum of a sample's pieces, in FP64 and in order within each of the strips that the threads take.
-constexpr int kStrips = 8;
+constexpr int kStrips = 16;
 __global__ void __launch_bounds__(32 * kStrips)
 reduce_kernel(const float *__restrict__ partials, int K, int pieces, float *dscale, float *dshift) {
     __shared__ double part[kStrips][32];
@@ -325,7 +378,7 @@ reduce_kernel(const float *__restrict__ partials, int K, int pieces, float *dsca
     if (to == nullptr) return;
     double v = 0.0;
     if (c < K) {
-#pragma unroll 4
+#pragma unroll 8
         for (int i = strip; i < pieces; i += kStrips) v += partials[(2 * (static_cast<int64_t>(sample) * pieces + i) + which) * K + c];
     }
     part[strip][threadIdx.x & 31] = v;
@@ -339,18 +392,17 @@ reduce_kernel(const float *__restrict__ partials, int K, int pieces, float *dsca
 constexpr int kMaxItems = 512;      // pieces in all, where a sample has more than one
 
 struct Shape {
-    int chunks, warps_per_row, groups, blocks_per_sm;
+    int chunks, warps_per_row, groups;
 };
-// A thread holds one piece of eight columns of a row up to 4096 columns, two up to 8192, four beyond; blocks of up to sixteen warps.
+// A thread holds one piece of eight columns of a row up to 3072 columns, two up to 6144, four beyond; as many groups of warps as twelve
+// warps make.
 Shape shape_of(int64_t K) {
     Shape s;
-    s.chunks = K <= 4096 ? 1 : K <= 8192 ? 2 : 4;
+    s.chunks = K <= 3072 ? 1 : K <= 6144 ? 2 : 4;
     s.warps_per_row = static_cast<int>(ceil_div(K, kGroupColumns * s.chunks));
-    s.groups = s.chunks > 1 ? 1 : 12 / s.warps_per_row > 0 ? 12 / s.warps_per_row : 1;
-    s.blocks_per_sm = 1;
+    s.groups = s.warps_per_row > 12 ? 1 : 12 / s.warps_per_row;
     return s;
 }
-int rows_of(int chunks) { return chunks == 1 ? 4 : chunks == 2 ? 2 : 1; }
 // Pieces of a sample: so many that the blocks all have one, none of fewer rows than the groups take in a step.
 int pieces_of(int64_t M, int64_t rows_per_sample, const Shape &s, int blocks) {
     const int64_t samples = ceil_div(M, rows_per_sample);
@@ -360,20 +412,27 @@ int pieces_of(int64_t M, int64_t rows_per_sample, const Shape &s, int blocks) {
     return pieces < 1 ? 1 : static_cast<int>(pieces);
 }
 
-template <int kWarps>
-sol_status_t forward_of(const Forward &p, cudaStream_t stream) {
-    const unsigned grid = static_cast<unsigned>(ceil_div(p.rows, kForwardWarps / kWarps));
-    const int chunks = static_cast<int>(ceil_div(p.K, 256 * kWarps));
-    auto launch = [&](auto kern) { kern<<<grid, 32 * kForwardWarps, 0, stream>>>(p); };
-    if (chunks <= 1) launch(forward_kernel<kWarps, 1>);
-    else if (chunks <= 2) launch(forward_kernel<kWarps, 2>);
-    else if (chunks <= 4) launch(forward_kernel<kWarps, 4>);
-    else if (chunks <= 6) launch(forward_kernel<kWarps, 6>);
-    else if (chunks <= 8) launch(forward_kernel<kWarps, 8>);
-    else if (chunks <= 10) launch(forward_kernel<kWarps, 10>);
-    else if (chunks <= 12) launch(forward_kernel<kWarps, 12>);
-    else launch(forward_kernel<kWarps, 16>);
+template <int kWarps, int kChunks>
+sol_status_t forward_of(const Forward &p, cudaStream_t stream, const DeviceInfo *dev) {
+    constexpr int kBlockWarps = kWarps > kForwardWarps ? kWarps : kForwardWarps;
+    static int resident = 0;            // blocks per SM that the kernel's registers allow
+    if (resident == 0 && cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, forward_kernel<kWarps, kChunks>, 32 * kBlockWarps, 0) != cudaSuccess) {
+        cudaGetLastError();
+        return SOL_ERR_CUDA;
+    }
+    const int64_t most = static_cast<int64_t>(resident) * dev->sm_count, want = ceil_div(p.rows, kBlockWarps / kWarps);
+    forward_kernel<kWarps, kChunks><<<static_cast<unsigned>(want < most ? want : most), 32 * kBlockWarps, 0, stream>>>(p);
     return launch_status();
+}
+template <int kWarps>
+sol_status_t forward_by_chunks(const Forward &p, cudaStream_t stream, const DeviceInfo *dev) {
+    switch (ceil_div(p.K, 256 * kWarps)) {
+        case 1: return forward_of<kWarps, 1>(p, stream, dev);
+        case 2: return forward_of<kWarps, 2>(p, stream, dev);
+        case 3: return forward_of<kWarps, 3>(p, stream, dev);
+    }
+    if constexpr (kWarps == 16) return forward_of<kWarps, 4>(p, stream, dev);
+    return SOL_ERR_BAD_SHAPE;
 }
 
 }  // namespace
@@ -387,8 +446,11 @@ sol_status_t launch_forward(const void *x, int64_t M, int64_t K, int64_t ldx, co
                     static_cast<uint16_t *>(y), reinterpret_cast<float2 *>(stats), ldx, ldy, static_cast<uint32_t>(M),
                     static_cast<uint32_t>(rows_per_sample), static_cast<int>(K), scale != nullptr ? offset : 1.0f, eps,
                     1.0f / static_cast<float>(K)};
-    (void)dev;
-    return K <= 4096 ? forward_of<1>(p, stream) : forward_of<4>(p, stream);
+    if (K <= 768) return forward_by_chunks<1>(p, stream, dev);
+    if (K <= 1536) return forward_by_chunks<2>(p, stream, dev);
+    if (K <= 3072) return forward_by_chunks<4>(p, stream, dev);
+    if (K <= 6144) return forward_by_chunks<8>(p, stream, dev);
+    return forward_by_chunks<16>(p, stream, dev);
 }
 
 size_t backward_workspace_bytes(int64_t M, int64_t K, int64_t rows_per_sample) {
@@ -401,17 +463,19 @@ sol_status_t launch_backward(const void *dy, int64_t ld_dy, const void *x, int64
                              float *partials, cudaStream_t stream, const DeviceInfo *dev) {
     const Shape s = shape_of(K);
     const int64_t samples = ceil_div(M, rows_per_sample);
-    int blocks = s.blocks_per_sm * dev->sm_count;
-    if (blocks > kMaxItems) blocks = kMaxItems;
-    Backward p{static_cast<const uint16_t *>(dy), static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(scale),
-               reinterpret_cast<const float2 *>(stats), static_cast<uint16_t *>(dx), dscale, dshift, partials, ld_dy, ld_x, ld_dx,
-               static_cast<uint32_t>(M), static_cast<uint32_t>(rows_per_sample), static_cast<int>(K), static_cast<int>(samples),
-               pieces_of(M, rows_per_sample, s, blocks), scale != nullptr ? offset : 1.0f, 1.0f / static_cast<float>(K)};
+    const int blocks = dev->sm_count < kMaxItems ? dev->sm_count : kMaxItems;
+    const Backward p{static_cast<const uint16_t *>(dy), static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(scale),
+                     reinterpret_cast<const float2 *>(stats), static_cast<uint16_t *>(dx), dscale, dshift, partials,
+                     ld_dy, ld_x, ld_dx, static_cast<uint32_t>(M), static_cast<uint32_t>(rows_per_sample),
+                     static_cast<int>(K), static_cast<int>(samples), pieces_of(M, rows_per_sample, s, blocks), s.warps_per_row,
+                     scale != nullptr ? offset : 1.0f, 1.0f / static_cast<float>(K)};
     const int64_t items = samples * p.pieces;
     const unsigned grid = static_cast<unsigned>(items < blocks ? items : blocks), threads = 32u * s.warps_per_row * s.groups;
-    if (s.chunks == 1) backward_kernel<1, 4><<<grid, threads, 0, stream>>>(p, s.warps_per_row);
-    else if (s.chunks == 2) backward_kernel<2, 2><<<grid, threads, 0, stream>>>(p, s.warps_per_row);
-    else backward_kernel<4, 1><<<grid, threads, 0, stream>>>(p, s.warps_per_row);
+    auto launch = [&](auto kern) { kern<<<grid, threads, 0, stream>>>(p); };
+    if (s.chunks == 1) launch(backward_kernel<1, 12>);
+    else if (s.chunks == 2) launch(backward_kernel<2, 12>);
+    else if (s.warps_per_row <= 12) launch(backward_kernel<4, 12>);
+    else launch(backward_kernel<4, 16>);
     const sol_status_t st = launch_status();
     if (st != SOL_OK || p.pieces == 1 || (dscale == nullptr && dshift == nullptr)) return st;
     cudaLaunchConfig_t cfg{};
