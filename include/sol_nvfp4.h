@@ -150,6 +150,39 @@ sol_status_t nvfp4_requantize_lora_batch(int64_t count, const void *const *w_lis
                                          void *stream);
 
 /*
+ * One AdamW step over many tensors (the policy update in front of that refresh), in place.  Per element, FP32, with t the step:
+ *     g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2       (every operation rounded)
+ *     param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *   tensors     HOST array of `count` descriptions (read during the call only) of device tensors of n >= 0 dense elements, 16-byte
+ *               aligned, no two of them overlapping:  param FP32 or BF16;  copy BF16 or NULL, receives bf16_rne(param) beside an FP32
+ *               param;  grad FP32 or BF16, of the same types for all;  m, v the states
+ *   state_bits  32: m and v are FP32 [n], the scales NULL.   8: blocks of 32 elements under a power of two, one byte 2^(b-127)
+ *               each in m_scale and v_scale [ceil(n/32)], m as E4M3 and v as E5M2 codes [n] (all zero at the start); the
+ *               power of two takes a block's largest finite |m| to [2^7, 2^8), its largest v to [2^14, 2^15) (b >= 1)
+ *   stochastic  8-bit states and BF16 params are rounded up or down by chance, in proportion, from a hash of seed, t, the tensor's
+ *               place in the list and the element's in the tensor; 0: to nearest, ties to even
+ *   step_state  two 64-bit words (device, 8-byte aligned): [0] steps done so far, read and advanced by this call (t is one more),
+ *               [1] scratch, 0 between calls.  The same for all tensors of a call
+ *   lr_scale, grad_scale  one float each (device) or NULL (1): factors that change between the replays of a captured call
+ * lr and weight_decay >= 0, 0 <= beta < 1, eps >= 0.  An element whose gradient is not finite becomes NaN, with its states; its
+ * block's other elements do not.  One launch for up to 448 tensors.
+ */
+typedef struct {
+    void *param, *copy;
+    const void *grad;
+    void *m, *v, *m_scale, *v_scale;
+    int64_t n;
+} sol_adamw_tensor_t;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    const float *lr_scale, *grad_scale;
+    uint64_t seed;
+    int32_t stochastic, param_bf16, grad_bf16, state_bits;
+} sol_adamw_options_t;
+sol_status_t sol_adamw_step(const sol_adamw_tensor_t *tensors, int64_t count, const sol_adamw_options_t *options, int64_t *step_state,
+                            void *stream);
+
+/*
  * Block-scaled FP4 GEMM with BF16 output (the NVFP4 linear the rollout runs, Section 3.4):
  *     acc[m,n] = sum_b sx[m,b] * sw[n,b] * sum_{k in b} qx[m,k] * qw[n,k]      (FP32 accumulate)
  *     Y[m,n]   = bf16_rne( fma(acc, Tx*Tw, bias[n]) )

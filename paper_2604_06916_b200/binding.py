@@ -33,7 +33,7 @@ EXPORTS = [
     "mxfp4_linear_split_out", "mxfp4_quantize_into", "sol_qk_rotary", "sol_qk_rotary_backward",
     "sol_qk_rotary_backward_workspace_bytes", "sol_rotary_frequencies", "nvfp4_matvec", "mxfp4_matvec",
     "sol_matvec_workspace_bytes", "sol_select_blocks", "sol_select_blocks_workspace_bytes", "sol_attention_blocks",
-    "sol_layernorm", "sol_layernorm_backward", "sol_layernorm_backward_workspace_bytes",
+    "sol_layernorm", "sol_layernorm_backward", "sol_layernorm_backward_workspace_bytes", "sol_adamw_step",
 ]
 
 _lib = None
@@ -136,6 +136,7 @@ def lib() -> ctypes.CDLL:
     L.sol_layernorm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, f32, vp, i64, vp, vp, vp, sz, vp]
     L.sol_layernorm_backward_workspace_bytes.restype = sz
     L.sol_layernorm_backward_workspace_bytes.argtypes = [i64, i64, i64]
+    L.sol_adamw_step.restype, L.sol_adamw_step.argtypes = i32, [vp, i64, vp, vp, vp]
     L.sol_set_wait_limit_cycles.restype, L.sol_set_wait_limit_cycles.argtypes = i32, [i64]
     L.sol_test_hold_loads.restype, L.sol_test_hold_loads.argtypes = i32, [i32]
     L.sol_last_device_status.restype = i32
@@ -884,6 +885,124 @@ def sol_layernorm_backward(dy, x, stats, scale=None, rows_per_sample: int | None
     if code:
         raise SolError(code, "sol_layernorm_backward")
     return out, dscale, dshift
+
+
+# sol_adamw_tensor_t and sol_adamw_options_t of the C header, packed by the native rules.
+_ADAMW_TENSOR = struct.Struct("@PPPPPPPq")
+_ADAMW_OPTIONS = struct.Struct("@dddddPPQiiii")
+_ADAMW_STATES = {32: (("m", torch.float32, 1), ("v", torch.float32, 1)),
+                 8: (("m", torch.uint8, 1), ("v", torch.uint8, 1), ("m_scale", torch.uint8, 32), ("v_scale", torch.uint8, 32))}
+
+
+class AdamWPlan:
+    """Tensors of an AdamW step laid out once: parameters, gradients, states and the step counter (see sol_adamw_plan)."""
+
+    def __init__(self, params, grads, copies, state_bits: int, states, step: int):
+        params = list(params)
+        if not params:
+            raise ValueError("no parameters")
+        if state_bits not in _ADAMW_STATES:
+            raise ValueError("state_bits must be 32 or 8")
+        self.index, self.state_bits, self.params = params[0].get_device(), state_bits, params
+        if self.index < 0:
+            raise TypeError("sol_adamw_plan: expected CUDA tensors")
+        self.device = params[0].device
+        self.param_dtype = params[0].dtype
+        if self.param_dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("params: expected float32 or bfloat16")
+        for p in params:
+            self._check("params", p, self.param_dtype, p.numel())
+        if len({p.data_ptr() for p in params if p.numel()}) != sum(p.numel() > 0 for p in params):
+            raise ValueError("params: the same tensor twice")
+        if copies is not None:
+            if self.param_dtype is not torch.float32:
+                raise ValueError("copies: only beside float32 parameters")
+            copies = list(copies)
+            self._check_all("copies", copies, torch.bfloat16, 1)
+        self.copies = copies
+        for name, dtype, unit in _ADAMW_STATES[state_bits]:
+            if states is None:
+                # one buffer for all, every tensor's part on a 128-byte boundary
+                sizes = [-(-p.numel() // unit) for p in params]
+                each = [-(-n // 128) * 128 for n in sizes]
+                flat = torch.zeros(sum(each), dtype=dtype, device=self.device)
+                parts, at = [], 0
+                for n, e in zip(sizes, each):
+                    parts.append(flat[at:at + n])
+                    at += e
+            else:
+                parts = list(states[name])
+                self._check_all(name, parts, dtype, unit)
+            setattr(self, name, parts)
+        self.step = torch.tensor([step, 0], dtype=torch.int64, device=self.device)
+        self.set_grads(grads)
+
+    def _check(self, name, t, dtype, numel):
+        if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != self.index:
+            raise TypeError(f"{name}: expected a dense {dtype} tensor of {numel} elements on cuda:{self.index}")
+
+    def _check_all(self, name, tensors, dtype, unit):
+        if len(tensors) != len(self.params):
+            raise ValueError(f"{name}: one for each parameter")
+        for t, p in zip(tensors, self.params):
+            self._check(name, t, dtype, -(-p.numel() // unit))
+
+    def set_grads(self, grads) -> None:
+        """Other gradient tensors for the following steps (None for a parameter that takes no step)."""
+        grads = list(grads)
+        if len(grads) != len(self.params):
+            raise ValueError("grads: one for each parameter")
+        dtypes = {g.dtype for g in grads if g is not None}
+        if len(dtypes) > 1 or not dtypes <= {torch.float32, torch.bfloat16}:
+            raise TypeError("grads: expected float32 or bfloat16, the same for all")
+        for g, p in zip(grads, self.params):
+            if g is not None:
+                self._check("grads", g, g.dtype, p.numel())
+        self.grads = grads
+        self.grad_bf16 = torch.bfloat16 in dtypes
+        scales = self.state_bits == 8
+        self._packed = b"".join(
+            _ADAMW_TENSOR.pack(p.data_ptr(), 0 if self.copies is None else self.copies[i].data_ptr(), 0 if g is None else g.data_ptr(),
+                               self.m[i].data_ptr(), self.v[i].data_ptr(), self.m_scale[i].data_ptr() if scales else 0,
+                               self.v_scale[i].data_ptr() if scales else 0, 0 if g is None else p.numel())
+            for i, (p, g) in enumerate(zip(self.params, grads)))
+
+
+def sol_adamw_plan(params, grads, copies=None, state_bits: int = 32, states=None, step: int = 0) -> AdamWPlan:
+    """Lays out tensors for sol_adamw_step: dense FP32 or BF16 parameters and their FP32 or BF16 gradients.
+
+    `copies`: BF16 tensors that receive the rounded FP32 parameters (what the linears read).  `state_bits` 32: FP32 moments;
+    8: E4M3 and E5M2 codes under one power of two per 32 values.  The states are new and zero, or `states`' lists ("m", "v" and, in
+    8 bits, "m_scale", "v_scale"); `step` is the number of steps that they have behind them.  The plan keeps the tensors and
+    offers them as attributes: params, grads, copies, m, v, m_scale, v_scale, step ([0] on the device).
+    """
+    return AdamWPlan(params, grads, copies, state_bits, states, step)
+
+
+def sol_adamw_step(plan: AdamWPlan, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.01,
+                   seed: int | None = None, lr_scale: torch.Tensor | None = None, grad_scale: torch.Tensor | None = None) -> None:
+    """One AdamW step of the plan's parameters, in place, from the gradients that its tensors hold now.
+
+    With a `seed`, 8-bit states and BF16 parameters are rounded up or down by chance in proportion (other bits every step), without
+    one to nearest.  `lr_scale` and `grad_scale` are one-element FP32 device tensors or None: factors read when the step runs.
+    """
+    if not isinstance(plan, AdamWPlan):
+        raise TypeError("sol_adamw_step: expected a plan of sol_adamw_plan")
+    index = plan.index
+    scales = [0, 0]
+    for i, (name, t) in enumerate((("lr_scale", lr_scale), ("grad_scale", grad_scale))):
+        if t is not None:
+            scales[i] = _dense(name, t.reshape(-1), torch.float32, (1,), index)
+    options = _ADAMW_OPTIONS.pack(lr, beta1, beta2, eps, weight_decay, *scales, 0 if seed is None else seed & (2 ** 64 - 1), seed is not None,
+                                  plan.param_dtype is torch.bfloat16, plan.grad_bf16, plan.state_bits)
+    packed, count = plan._packed, len(plan.params)
+    if index == torch._C._cuda_getDevice():
+        code = lib().sol_adamw_step(packed, count, options, plan.step.data_ptr(), _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            code = lib().sol_adamw_step(packed, count, options, plan.step.data_ptr(), _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_adamw_step")
 
 
 QUERY_BLOCK, KEY_BLOCK = 256, 128

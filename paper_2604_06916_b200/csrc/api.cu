@@ -844,6 +844,32 @@ sol_status_t sol_layernorm_backward(const void *dy, int64_t ld_dy, const void *x
                                  static_cast<float *>(workspace), static_cast<cudaStream_t>(stream), dev);
 }
 
+sol_status_t sol_adamw_step(const sol_adamw_tensor_t *tensors, int64_t count, const sol_adamw_options_t *o, int64_t *step_state,
+                            void *stream) {
+    if (o == nullptr || step_state == nullptr || (tensors == nullptr && count > 0)) return SOL_ERR_NULL_POINTER;
+    if (count < 0 || count > 0x7FFFFFFFLL) return SOL_ERR_BAD_SHAPE;
+    if (o->state_bits != 32 && o->state_bits != 8) return SOL_ERR_BAD_LAYOUT;
+    auto from = [](double v, double lo) { return v >= lo && std::isfinite(v); };
+    if (!from(o->lr, 0.0) || !from(o->weight_decay, 0.0) || !from(o->eps, 0.0) || !from(o->beta1, 0.0) || !from(o->beta2, 0.0) ||
+        o->beta1 >= 1.0 || o->beta2 >= 1.0)
+        return SOL_ERR_BAD_SHAPE;
+    for (int64_t i = 0; i < count; ++i) {
+        const sol_adamw_tensor_t &t = tensors[i];
+        if (t.n < 0 || t.n > (1LL << 40)) return SOL_ERR_BAD_SHAPE;
+        if (t.n == 0) continue;
+        if (t.param == nullptr || t.grad == nullptr || t.m == nullptr || t.v == nullptr) return SOL_ERR_NULL_POINTER;
+        if (o->state_bits == 8 && (t.m_scale == nullptr || t.v_scale == nullptr)) return SOL_ERR_NULL_POINTER;
+        if (o->param_bf16 && t.copy != nullptr) return SOL_ERR_BAD_LAYOUT;
+        if (!aligned16(t.param) || !aligned16(t.copy) || !aligned16(t.grad) || !aligned16(t.m) || !aligned16(t.v)) return SOL_ERR_ALIGNMENT;
+    }
+    if (!aligned8(step_state) || (reinterpret_cast<uintptr_t>(o->lr_scale) & 3u) || (reinterpret_cast<uintptr_t>(o->grad_scale) & 3u))
+        return SOL_ERR_ALIGNMENT;
+    const DeviceInfo *dev = nullptr;
+    const sol_status_t st = check_arch(&dev);
+    if (st != SOL_OK) return st;
+    return adamw::launch_step(tensors, count, *o, step_state, static_cast<cudaStream_t>(stream), dev);
+}
+
 sol_status_t sol_rotary_frequencies(int64_t dim, double theta, sol_rotary_scaling_t scaling, double factor,
                                     double original_length, double beta_fast, double beta_slow, double *freqs_out,
                                     double *scale_out) {

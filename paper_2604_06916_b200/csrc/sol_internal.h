@@ -214,6 +214,13 @@ sol_status_t launch_backward(const void *dy, int64_t ld_dy, const void *x, int64
                              float *partials, cudaStream_t stream, const DeviceInfo *dev);
 }
 
+// AdamW over many tensors (arguments as the header's entry).
+namespace adamw {
+using Tensor = sol_adamw_tensor_t;
+sol_status_t launch_step(const Tensor *tensors, int64_t count, const sol_adamw_options_t &options, int64_t *state, cudaStream_t stream,
+                         const DeviceInfo *dev);
+}
+
 // Few BF16 rows against a 4-bit weight (wts null: MXFP4).
 namespace matvec {
 size_t workspace_bytes(int64_t M, int64_t K);
