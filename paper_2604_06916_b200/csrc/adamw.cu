@@ -12,8 +12,13 @@
 // at [2^7, 2^8) of E4M3, [2^14, 2^15) of E5M2, so rounding up never leaves the format.
 // The new parameter comes from m and v before they are rounded.
 //
-// HBM bound: 28 bytes per element in FP32 (30 with the BF16 copy), 16.1 with 8-bit states, 10.1 with BF16 parameters as well.  A thread
-// takes eight neighbouring values (16-byte accesses, a block of 32 is four lanes).
+// HBM bound in FP32: 28 bytes per element (30 with the BF16 copy); 18.1 with 8-bit states and a copy; 10.1 with BF16 parameters and
+// gradients as well, where issuing is the bound (67 instructions a value).  A thread takes eight neighbouring values (a block of 32 is
+// four lanes); FP32 goes in 32-byte accesses where the addresses allow it (304 tensors of 60 M values 304 us, with 16-byte ones 324).
+// Measured (B200, inside a graph): 60 M FP32 values in 304 tensors with the BF16 copy 306 us = 5.9 TB/s, 90 % of the copy
+// rate; 8-bit states 197 us = 5.5 TB/s; 71 M BF16 values with 8-bit states 187 us = 3.9 TB/s.  Neighbouring chunks for a block in place
+// of every gridDim-th one: 226 and 180 us; loads a chunk ahead: 194 and 200 us (fewer blocks fit); every operation and conversion by
+// itself, without the hardware's 8-bit conversions and byte permutes: 259 and 310 us.
 #include "ptx.cuh"
 #include "quant_math.cuh"
 #include "sol_internal.h"
@@ -23,6 +28,10 @@
 namespace sol {
 namespace adamw {
 namespace {
+
+using qmath::f32x2;
+using qmath::f32x2_split;
+using qmath::mul2;
 
 constexpr int kThreads = 256;
 constexpr int kVec = 8;                        // values of a thread
@@ -36,7 +45,7 @@ struct Hyper {
     long long *state;                          // [0] steps done, [1] tickets
     uint64_t seed;
     uint32_t first_tensor, chunks;
-    int count, stochastic, advance;
+    int count, stochastic, advance, tiny_eps;
 };
 template <int kN>
 struct Table {
@@ -44,94 +53,167 @@ struct Table {
     uint32_t first[kN + 1];                    // chunk that each tensor begins with
 };
 
-__device__ __forceinline__ uint32_t mix(uint32_t x) {
-    x ^= x >> 16;
+__device__ __forceinline__ uint32_t mix_rest(uint32_t x) {
     x *= 0x7FEB352Du;
     x ^= x >> 15;
     x *= 0x846CA68Bu;
     return x ^ x >> 16;
 }
+__device__ __forceinline__ uint32_t mix(uint32_t x) { return mix_rest(x ^ x >> 16); }
 __device__ __forceinline__ uint32_t mix_word(uint32_t h, uint32_t w) { return mix(h ^ (w + 0x9E3779B9u)); }
 
-__device__ __forceinline__ void load(float (&f)[kVec], const float *p) {
-    const float4 a = __ldcs(reinterpret_cast<const float4 *>(p)), b = __ldcs(reinterpret_cast<const float4 *>(p) + 1);
-    f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+// FP32 in one 32-byte access where the tensor's addresses allow it (`wide`): half an access a sector costs 7 % of the rate.
+__device__ __forceinline__ void load(uint32_t (&w)[8], const float *p, bool wide) {
+    if (!wide) {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p)), b = __ldcs(reinterpret_cast<const uint4 *>(p) + 1);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+        return;
+    }
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p)
+                 : "memory");
 }
-__device__ __forceinline__ void load(float (&f)[kVec], const uint16_t *p) {
-    const uint4 r = __ldcs(reinterpret_cast<const uint4 *>(p));
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+__device__ __forceinline__ void load(uint32_t (&w)[4], const uint16_t *p, bool) {
+    const uint4 a = __ldcs(reinterpret_cast<const uint4 *>(p));
+    w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+}
+__device__ __forceinline__ void load(uint32_t (&w)[2], const uint8_t *p, bool) {
+    const uint2 a = __ldcs(reinterpret_cast<const uint2 *>(p));
+    w[0] = a.x, w[1] = a.y;
+}
+// The same from a tensor's last values, 0 behind them.
+template <int kWords, class T>
+__device__ __forceinline__ void load_some(uint32_t (&w)[kWords], const T *p, int64_t left) {
+    constexpr int kPer = 4 / sizeof(T);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) f[2 * i] = qmath::bf16_lo(w[i]), f[2 * i + 1] = qmath::bf16_hi(w[i]);
+    for (int i = 0; i < kWords; ++i) {
+        w[i] = 0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            if (i * kPer + e >= left) continue;
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
+            else w[i] |= static_cast<uint32_t>(p[i * kPer + e]) << (8 * sizeof(T) * e);
+        }
+    }
 }
-__device__ __forceinline__ float one(const float *p) { return *p; }
-__device__ __forceinline__ float one(const uint16_t *p) { return __uint_as_float(static_cast<uint32_t>(*p) << 16); }
-__device__ __forceinline__ void store(float *p, const float (&f)[kVec]) {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+template <bool k16, int kWords>
+__device__ __forceinline__ void unpack(float (&f)[kVec], const uint32_t (&w)[kWords]) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+        if constexpr (k16) f[i] = i & 1 ? qmath::bf16_hi(w[i / 2]) : qmath::bf16_lo(w[i / 2]);
+        else f[i] = __uint_as_float(w[i]);
+    }
 }
-__device__ __forceinline__ uint32_t bf16_rn(float f) {
-    uint16_t r;
-    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(f));
-    return r;
+__device__ __forceinline__ void store(float *p, const float (&f)[kVec], bool wide) {
+    if (!wide) {
+        reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+        reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+        return;
+    }
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]),
+                 "f"(f[5]), "f"(f[6]), "f"(f[7])
+                 : "memory");
 }
-
 // kMantissa 3: E4M3, values 2^120 times those of the FP32 number with the code's bits on top; 2: E5M2, 2^112 times.
 template <int kMantissa>
 struct Format {
     static constexpr int kDrop = 23 - kMantissa;
     static constexpr uint32_t kTop = kMantissa == 3 ? 7 : 14;          // exponent of a block's largest value
-    static constexpr float kUp = kMantissa == 3 ? 0x1p120f : 0x1p112f, kDown = kMantissa == 3 ? 0x1p-120f : 0x1p-112f;
+    static constexpr float kDown = kMantissa == 3 ? 0x1p-120f : 0x1p-112f;
 };
-// The 7-bit code of y in [0, 2^kTop+1): to nearest, or up or down by chance.  By chance: scaled down so that its bits are the
-// code's, further down (exact but for subnormal codes, where what lies below a 2^-kDrop of a step is rounded), plus the noise's 16
-// bits below the code's, in the middle of what they stand for.
-template <int kMantissa>
-__device__ __forceinline__ uint32_t round_code(float y, uint32_t noise16, bool stochastic) {
-    using F = Format<kMantissa>;
-    if (stochastic) return (__float_as_uint(__fmul_rn(y, F::kDown)) + (noise16 << (F::kDrop - 16)) + (1u << (F::kDrop - 17))) >> F::kDrop;
-    uint16_t r;
-    if constexpr (kMantissa == 3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(y));
-    else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(y));
-    return r;
+// A block's eight codes of a thread and its exponent byte -> FP32.  The codes go through FP16, which holds both formats exactly (E5M2 is its
+// upper byte), NaN and sign included.
+__device__ __forceinline__ void halves_to_float(uint32_t pair, float scale, float *f) {
+    float lo, hi;
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(pair));
+    f[0] = __fmul_rn(lo, scale);
+    f[1] = __fmul_rn(hi, scale);
 }
 template <int kMantissa>
 __device__ __forceinline__ void decode(float (&f)[kVec], uint2 codes, uint32_t e) {
-    using F = Format<kMantissa>;
     const float scale = __uint_as_float(e << 23);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        const uint32_t c = (i < 4 ? codes.x : codes.y) >> (8 * (i & 3));
-        const float size = __fmul_rn(__fmul_rn(__uint_as_float((c & 127u) << F::kDrop), F::kUp), scale);
-        f[i] = __uint_as_float(((c & 127u) == 127u ? 0x7FC00000u : __float_as_uint(size)) | (c & 128u) << 24);
+    for (int i = 0; i < kVec; i += 2) {
+        const uint32_t word = i < 4 ? codes.x : codes.y;
+        uint32_t pair;
+        if constexpr (kMantissa == 3) {
+            const uint16_t two = static_cast<uint16_t>(word >> (8 * (i & 2)));
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(pair) : "h"(two));
+        } else {
+            pair = __byte_perm(word, 0, (i & 2) ? 0x3424 : 0x1404);     // codes into the upper bytes
+        }
+        halves_to_float(pair, scale, f + i);
     }
 }
-// The codes of a thread's eight values and the exponent byte of its block (lanes 4i .. 4i+3); values that are not finite become
-// NaN and do not count for the block.
+__device__ __forceinline__ bool finite_bits(uint32_t b) { return (b & 0x7F800000u) != 0x7F800000u; }
+
+// The codes of a thread's eight values and the exponent byte of its block (lanes 4i .. 4i+3).  To nearest by the hardware's conversion.
+// By chance: y scaled down so that its FP32 bits are the code's, further down (exact but for subnormal codes, where what lies below
+// 2^-kDrop of a step is rounded), plus the noise's 16 bits below the code's, in the middle of what they leave open.  `odd`: some value
+// of the warp is not finite; such values become NaN and do not count for the block.
 template <int kMantissa>
-__device__ __forceinline__ uint2 encode(const float (&f)[kVec], uint32_t &e, const uint32_t (&noise)[kVec], int noise_shift, bool stochastic) {
+__device__ __forceinline__ uint2 encode(const float (&f)[kVec], uint32_t &e, const uint32_t (&noise)[kVec], bool stochastic, bool odd) {
     using F = Format<kMantissa>;
-    uint32_t most = 0;
+    float most = 0.0f;
+    if (!odd) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        const uint32_t b = __float_as_uint(f[i]) & 0x7FFFFFFFu;
-        most = max(most, b < 0x7F800000u ? b : 0u);
-    }
-    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-    most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-    e = max(most >> 23, F::kTop + 1u) - F::kTop;
-    const float inv = __uint_as_float((254u - e) << 23);
-    uint32_t w[2] = {0, 0};
+        for (int i = 0; i < kVec; ++i) most = fmaxf(most, fabsf(f[i]));
+    } else {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        const uint32_t b = __float_as_uint(f[i]), size = b & 0x7FFFFFFFu;
-        const uint32_t c = round_code<kMantissa>(__fmul_rn(__uint_as_float(size), inv), (noise[i] >> noise_shift) & 0xFFFFu, stochastic) & 127u;
-        w[i >> 2] |= ((size < 0x7F800000u ? c : 127u) | b >> 31 << 7) << (8 * (i & 3));
+        for (int i = 0; i < kVec; ++i) most = fmaxf(most, finite_bits(__float_as_uint(f[i])) ? fabsf(f[i]) : 0.0f);
     }
+    most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+    most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+    e = max(__float_as_uint(most) >> 23, F::kTop + 1u) - F::kTop;
+    uint32_t c[kVec];                      // the code in the uppermost byte
+    if (stochastic) {
+        // 2^(127 - e) and the format's 2^-120 (2^-112) in one factor where FP32 has it
+        constexpr uint32_t kOne = kMantissa == 3 ? 134u : 142u;
+        if (__all_sync(0xFFFFFFFFu, e < kOne)) {
+            const float down = __uint_as_float((kOne - e) << 23);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) c[i] = __float_as_uint(__fmul_rn(fabsf(f[i]), down));
+        } else {
+            const float inv = __uint_as_float((254u - e) << 23);
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) c[i] = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(f[i]), inv), F::kDown));
+        }
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            // everything shifted so that the code is the uppermost byte: the noise is the two bytes below, a half of its last bit the third
+            const uint32_t r = __byte_perm(noise[i], 0x80u, kMantissa == 3 ? 0x5104 : 0x5324);
+            c[i] = (c[i] << (24 - F::kDrop)) + r;
+        }
+    } else {
+        const float inv = __uint_as_float((254u - e) << 23);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            const float y = __fmul_rn(fabsf(f[i]), inv);
+            uint16_t r;
+            if constexpr (kMantissa == 3) asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(y));
+            else asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(0.0f), "f"(y));
+            c[i] = static_cast<uint32_t>(r) << 24;
+        }
+    }
+    if (odd) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+            if (!finite_bits(__float_as_uint(f[i]))) c[i] = 0x7F000000u;
+    }
+    if constexpr (kMantissa == 3) {        // squares have no sign
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) c[i] = (c[i] & 0x7FFFFFFFu) | (__float_as_uint(f[i]) & 0x80000000u);
+    }
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x73), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x73), 0x5410);
     return make_uint2(w[0], w[1]);
 }
 
 template <int kN, bool kP16, bool kG16, bool k8>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyper h) {
     using P = typename std::conditional<kP16, uint16_t, float>::type;
     using G = typename std::conditional<kG16, uint16_t, float>::type;
@@ -139,6 +221,7 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
     constexpr bool kNoise = kP16 || k8;
     __shared__ float coefficients[3];      // 1 - lr decay, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
     __shared__ uint32_t hash;              // of seed and step
+    __shared__ uint16_t of_chunk[kThreads];
     if (threadIdx.x == 0) {
         const long long t = *reinterpret_cast<volatile long long *>(h.state) + 1;
         // b^t by squaring, in FP64
@@ -165,125 +248,189 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
     __syncthreads();
     const float keep = coefficients[0], size = coefficients[1], root = coefficients[2];
     const float grad_scale = h.grad_scale != nullptr ? __ldg(h.grad_scale) : 1.0f;
-    for (uint32_t chunk = blockIdx.x; chunk < h.chunks; chunk += gridDim.x) {
-        int lo = 0, hi = h.count;          // the last tensor that begins at or before this chunk
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (table.first[mid] <= chunk) lo = mid;
-            else hi = mid;
-        }
-        const Tensor &t = table.t[lo];
-        const int64_t i0 = static_cast<int64_t>(chunk - table.first[lo]) * kChunk + threadIdx.x * kVec;
-        const int64_t left = t.n - i0;     // a thread without values still takes part in its block's maximum
-        float p[kVec], g[kVec], m[kVec], v[kVec];
-        uint2 cm = make_uint2(0, 0), cv = make_uint2(0, 0);
-        uint32_t em = 0, ev = 0;
-        P *pp = static_cast<P *>(t.param) + i0;
-        const G *gp = static_cast<const G *>(t.grad) + i0;
-        S *mp = static_cast<S *>(t.m) + i0, *vp = static_cast<S *>(t.v) + i0;
-        if (left >= kVec) {
-            load(p, pp);
-            load(g, gp);
-            if constexpr (k8) {
-                cm = __ldcs(reinterpret_cast<const uint2 *>(mp));
-                cv = __ldcs(reinterpret_cast<const uint2 *>(vp));
-            } else {
-                load(m, mp);
-                load(v, vp);
+    const uint64_t gs2 = f32x2(grad_scale, grad_scale), b1 = f32x2(h.b1, h.b1), c1 = f32x2(h.c1, h.c1), b2 = f32x2(h.b2, h.b2), c2 = f32x2(h.c2, h.c2);
+    for (uint64_t first = blockIdx.x; first < h.chunks; first += static_cast<uint64_t>(kThreads) * gridDim.x) {
+        // the tensors of this block's next chunks, one looked for by each thread: the last tensor that begins at or before the chunk
+        if (first != blockIdx.x) __syncthreads();
+        const uint64_t mine = first + static_cast<uint64_t>(threadIdx.x) * gridDim.x;
+        if (mine < h.chunks) {
+            int lo = 0, hi = h.count;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (table.first[mid] <= mine) lo = mid;
+                else hi = mid;
             }
-        } else {
+            of_chunk[threadIdx.x] = static_cast<uint16_t>(lo);
+        }
+        __syncthreads();
+        // a thread's values of the block's k-th chunk, as they lie in memory; 0 behind the tensor's end
+        struct Raw {
+            uint32_t p[kVec * sizeof(P) / 4], g[kVec * sizeof(G) / 4], m[kVec * sizeof(S) / 4], v[kVec * sizeof(S) / 4];
+            uint32_t em, ev;
+        };
+        auto place = [&](int k, int &lo) {
+            lo = of_chunk[k];
+            return static_cast<int64_t>(first + static_cast<uint64_t>(k) * gridDim.x - table.first[lo]) * kChunk + threadIdx.x * kVec;
+        };
+        auto aligned32 = [](const Tensor &t) {
+            uintptr_t all = 0;
+            if (!kP16) all |= reinterpret_cast<uintptr_t>(t.param);
+            if (!kG16) all |= reinterpret_cast<uintptr_t>(t.grad);
+            if (!k8) all |= reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v);
+            return (all & 31u) == 0;
+        };
+        auto fetch = [&](Raw &r, int k) {
+            int lo;
+            const int64_t i0 = place(k, lo);
+            const Tensor &t = table.t[lo];
+            const int64_t left = t.n - i0;
+            const P *pp = static_cast<const P *>(t.param) + i0;
+            const G *gp = static_cast<const G *>(t.grad) + i0;
+            const S *mp = static_cast<const S *>(t.m) + i0, *vp = static_cast<const S *>(t.v) + i0;
+            if (left >= kVec) {
+                const bool wide = aligned32(t);
+                load(r.p, pp, wide);
+                load(r.g, gp, wide);
+                load(r.m, mp, wide);
+                load(r.v, vp, wide);
+            } else {
+                load_some(r.p, pp, left);
+                load_some(r.g, gp, left);
+                load_some(r.m, mp, left);
+                load_some(r.v, vp, left);
+            }
+            r.em = r.ev = 0;
+            if (k8 && left > 0) {
+                r.em = static_cast<const uint8_t *>(t.m_scale)[i0 >> 5];
+                r.ev = static_cast<const uint8_t *>(t.v_scale)[i0 >> 5];
+            }
+        };
+        const int chunks = static_cast<int>(min(static_cast<uint64_t>(kThreads), (h.chunks - first + gridDim.x - 1) / gridDim.x));
+        for (int k = 0; k < chunks; ++k) {
+            Raw raw;
+            fetch(raw, k);
+            int lo;
+            const int64_t i0 = place(k, lo);
+            const Tensor &t = table.t[lo];
+            const int64_t left = t.n - i0;     // a thread without values still takes part in its block's maximum
+            P *pp = static_cast<P *>(t.param) + i0;
+            S *mp = static_cast<S *>(t.m) + i0, *vp = static_cast<S *>(t.v) + i0;
+            float p[kVec], g[kVec], m[kVec], v[kVec];
+            unpack<kP16>(p, raw.p);
+            unpack<kG16>(g, raw.g);
+            uint2 cm = make_uint2(raw.m[0], raw.m[1]), cv = make_uint2(raw.v[0], raw.v[1]);
+            uint32_t em = raw.em, ev = raw.ev;
+            if constexpr (k8) {
+                decode<3>(m, cm, em);
+                decode<2>(v, cv, ev);
+            } else {
+                unpack<false>(m, raw.m);
+                unpack<false>(v, raw.v);
+            }
+            uint32_t noise[kVec] = {};
+            if (kNoise && h.stochastic) {
+                uint32_t base = mix_word(hash, h.first_tensor + lo);
+                if (i0 >> 32) base = mix(base ^ static_cast<uint32_t>(i0 >> 32));
+                base ^= static_cast<uint32_t>(i0);
+                base ^= base >> 16;            // mix's first step: i0 is a multiple of eight, so i changes none of the bits that it moves
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                p[i] = g[i] = m[i] = v[i] = 0.0f;
-                if (i < left) {
-                    p[i] = one(pp + i);
-                    g[i] = one(gp + i);
-                    if constexpr (k8) {
-                        (i < 4 ? cm.x : cm.y) |= static_cast<uint32_t>(mp[i]) << (8 * (i & 3));
-                        (i < 4 ? cv.x : cv.y) |= static_cast<uint32_t>(vp[i]) << (8 * (i & 3));
-                    } else {
-                        m[i] = mp[i];
-                        v[i] = vp[i];
-                    }
+                for (int i = 0; i < kVec; ++i) noise[i] = mix_rest(base ^ i);
+            }
+            // products two an instruction, sums one by one: a two-lane sum behind two-lane products would be made one operation with one
+            // rounding, and the definition has two
+#pragma unroll
+            for (int i = 0; i < kVec; i += 2) {
+                const uint64_t gi = mul2(f32x2(g[i], g[i + 1]), gs2);
+                float a0, a1, g0, g1;
+                f32x2_split(mul2(f32x2(m[i], m[i + 1]), b1), a0, a1);
+                f32x2_split(mul2(gi, c1), g0, g1);
+                m[i] = __fadd_rn(a0, g0), m[i + 1] = __fadd_rn(a1, g1);
+                f32x2_split(mul2(f32x2(v[i], v[i + 1]), b2), a0, a1);
+                f32x2_split(mul2(mul2(gi, gi), c2), g0, g1);
+                v[i] = __fadd_rn(a0, g0), v[i + 1] = __fadd_rn(a1, g1);
+            }
+            if (h.tiny_eps) {                  // squares below FP32's normal range count
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    float r;
+                    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v[i]));
+                    p[i] = fmaf(p[i], keep, -__fdividef(m[i] * size, fmaf(r, root, h.eps)));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    float r, q;
+                    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v[i]));
+                    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(q) : "f"(fmaf(r, root, h.eps)));
+                    p[i] = fmaf(p[i], keep, -(m[i] * size) * q);
                 }
             }
-        }
-        if constexpr (k8) {
-            if (left > 0) {
-                em = static_cast<const uint8_t *>(t.m_scale)[i0 >> 5];
-                ev = static_cast<const uint8_t *>(t.v_scale)[i0 >> 5];
-            }
-            decode<3>(m, cm, em);
-            decode<2>(v, cv, ev);
-        }
-        uint32_t noise[kVec] = {};
-        if (kNoise && h.stochastic) {
-            uint32_t base = mix_word(hash, h.first_tensor + lo);
-            if (i0 >> 32) base = mix(base ^ static_cast<uint32_t>(i0 >> 32));
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) noise[i] = mix(base ^ (static_cast<uint32_t>(i0) + i));
-        }
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            const float gi = __fmul_rn(g[i], grad_scale);
-            m[i] = __fadd_rn(__fmul_rn(m[i], h.b1), __fmul_rn(gi, h.c1));
-            v[i] = __fadd_rn(__fmul_rn(v[i], h.b2), __fmul_rn(__fmul_rn(gi, gi), h.c2));
-            float r;
-            asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v[i]));
-            p[i] = fmaf(p[i], keep, -__fdividef(m[i] * size, fmaf(r, root, h.eps)));
-        }
-        uint32_t short_p[kVec];
-        if constexpr (kP16) {
+            // is a value not finite?  Then v is not (m is only with it), or p is not
+            uint32_t largest = 0;
 #pragma unroll
             for (int i = 0; i < kVec; ++i) {
-                const uint32_t b = __float_as_uint(p[i]);
-                const bool by_chance = h.stochastic && (b & 0x7F800000u) != 0x7F800000u;
-                short_p[i] = by_chance ? (b + (noise[i] * 0x9E3779B1u >> 16)) >> 16 : bf16_rn(p[i]);
+                if (k8) largest = max(largest, __float_as_uint(v[i]));         // a square's bits, or a NaN's of either sign
+                if (kP16) largest = max(largest, __float_as_uint(p[i]) & 0x7FFFFFFFu);
             }
-        } else {
+            const bool odd = kNoise && __any_sync(0xFFFFFFFFu, largest >= 0x7F800000u);
+            uint32_t packed_p[kVec / 2];
+            if (kP16 && h.stochastic) {
+                uint32_t b[kVec];
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) short_p[i] = bf16_rn(p[i]);
-        }
-        if constexpr (k8) {
-            if (left < kVec) {
+                for (int i = 0; i < kVec; ++i) b[i] = __float_as_uint(p[i]) + (noise[i] * 0x9E3779B1u >> 16);
+                if (odd) {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i)
-                    if (i >= left) m[i] = v[i] = 0.0f;        // behind the end: nothing that counts for the block
-            }
-            cm = encode<3>(m, em, noise, 0, h.stochastic);
-            cv = encode<2>(v, ev, noise, 16, h.stochastic);
-            if (left > 0 && (threadIdx.x & 3) == 0) {
-                static_cast<uint8_t *>(t.m_scale)[i0 >> 5] = static_cast<uint8_t>(em);
-                static_cast<uint8_t *>(t.v_scale)[i0 >> 5] = static_cast<uint8_t>(ev);
-            }
-        }
-        uint16_t *copy = kP16 ? nullptr : static_cast<uint16_t *>(t.copy);
-        if (left >= kVec) {
-            const uint4 packed = make_uint4(short_p[0] | short_p[1] << 16, short_p[2] | short_p[3] << 16, short_p[4] | short_p[5] << 16,
-                                            short_p[6] | short_p[7] << 16);
-            if constexpr (kP16) *reinterpret_cast<uint4 *>(pp) = packed;
-            else store(pp, p);
-            if (copy != nullptr) *reinterpret_cast<uint4 *>(copy + i0) = packed;
-            if constexpr (k8) {
-                *reinterpret_cast<uint2 *>(mp) = cm;
-                *reinterpret_cast<uint2 *>(vp) = cv;
+                    for (int i = 0; i < kVec; ++i)
+                        if (!finite_bits(__float_as_uint(p[i]))) b[i] = __float_as_uint(p[i]) | (__float_as_uint(p[i]) << 9 ? 0x400000u : 0u);
+                }
+#pragma unroll
+                for (int i = 0; i < kVec; i += 2) packed_p[i / 2] = __byte_perm(b[i], b[i + 1], 0x7632);
             } else {
-                store(mp, m);
-                store(vp, v);
-            }
-        } else {
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                if (i >= left) continue;
-                if constexpr (kP16) pp[i] = static_cast<uint16_t>(short_p[i]);
-                else pp[i] = p[i];
-                if (copy != nullptr) copy[i0 + i] = static_cast<uint16_t>(short_p[i]);
+                for (int i = 0; i < kVec; i += 2) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed_p[i / 2]) : "f"(p[i + 1]), "f"(p[i]));
+            }
+            if constexpr (k8) {
+                if (left < kVec) {
+#pragma unroll
+                    for (int i = 0; i < kVec; ++i)
+                        if (i >= left) m[i] = v[i] = 0.0f;        // behind the end: nothing that counts for the block
+                }
+                cm = encode<3>(m, em, noise, h.stochastic, odd);
+                cv = encode<2>(v, ev, noise, h.stochastic, odd);
+                if (left > 0 && (threadIdx.x & 3) == 0) {
+                    static_cast<uint8_t *>(t.m_scale)[i0 >> 5] = static_cast<uint8_t>(em);
+                    static_cast<uint8_t *>(t.v_scale)[i0 >> 5] = static_cast<uint8_t>(ev);
+                }
+            }
+            uint16_t *copy = kP16 ? nullptr : static_cast<uint16_t *>(t.copy);
+            if (left >= kVec) {
+                const bool wide = aligned32(t);
+                const uint4 packed = make_uint4(packed_p[0], packed_p[1], packed_p[2], packed_p[3]);
+                if constexpr (kP16) *reinterpret_cast<uint4 *>(pp) = packed;
+                else store(pp, p, wide);
+                if (copy != nullptr) *reinterpret_cast<uint4 *>(copy + i0) = packed;
                 if constexpr (k8) {
-                    mp[i] = static_cast<uint8_t>((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
-                    vp[i] = static_cast<uint8_t>((i < 4 ? cv.x : cv.y) >> (8 * (i & 3)));
+                    *reinterpret_cast<uint2 *>(mp) = cm;
+                    *reinterpret_cast<uint2 *>(vp) = cv;
                 } else {
-                    mp[i] = m[i];
-                    vp[i] = v[i];
+                    store(mp, m, wide);
+                    store(vp, v, wide);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kVec; ++i) {
+                    if (i >= left) continue;
+                    const uint16_t short_p = static_cast<uint16_t>(packed_p[i / 2] >> (16 * (i & 1)));
+                    if constexpr (kP16) pp[i] = short_p;
+                    else pp[i] = p[i];
+                    if (copy != nullptr) copy[i0 + i] = short_p;
+                    if constexpr (k8) {
+                        mp[i] = static_cast<uint8_t>((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
+                        vp[i] = static_cast<uint8_t>((i < 4 ? cv.x : cv.y) >> (8 * (i & 3)));
+                    } else {
+                        mp[i] = m[i];
+                        vp[i] = v[i];
+                    }
                 }
             }
         }
@@ -338,6 +485,7 @@ sol_status_t launch_step(const Tensor *tensors, int64_t count, const sol_adamw_o
     h.b1 = static_cast<float>(o.beta1), h.c1 = static_cast<float>(1.0 - o.beta1);
     h.b2 = static_cast<float>(o.beta2), h.c2 = static_cast<float>(1.0 - o.beta2);
     h.eps = static_cast<float>(o.eps);
+    h.tiny_eps = o.eps < 1e-12;              // the root of what FP32 flushes to 0 is below 2^-63
     h.lr_scale = o.lr_scale, h.grad_scale = o.grad_scale;
     h.state = reinterpret_cast<long long *>(state);
     h.seed = o.seed, h.stochastic = o.stochastic != 0;

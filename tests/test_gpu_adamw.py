@@ -185,6 +185,19 @@ def test_other_gradients_and_parameters_without_one(B):
     assert plan.step.tolist() == [2, 0]
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tensors_on_16_byte_boundaries(B, bits):
+    g = torch.Generator(device="cuda").manual_seed(13)
+    ps, gs = ([torch.randn(n, generator=g, device="cuda")[4:] for n in (3004, 68)] for _ in range(2))
+    other = [torch.cat((torch.zeros(4, device="cuda"), p)) for p in ps]
+    plan = B.sol_adamw_plan(ps, gs, state_bits=bits)
+    same = B.sol_adamw_plan([p[4:].clone() for p in other], [x.clone() for x in gs], state_bits=bits)
+    for _ in range(2):
+        B.sol_adamw_step(plan, 1e-3, seed=4)
+        B.sol_adamw_step(same, 1e-3, seed=4)
+    assert all(torch.equal(a, b) for n in ("params", "m", "v") for a, b in zip(getattr(plan, n), getattr(same, n)))
+
+
 def test_a_tensor_past_32_bits(B):
     n, tail = 2 ** 32 + 100, 100 + 4096
     p, g = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
