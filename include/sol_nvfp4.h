@@ -150,6 +150,41 @@ sol_status_t nvfp4_requantize_lora_batch(int64_t count, const void *const *w_lis
                                          void *stream);
 
 /*
+ * Low-rank adapters of many requests at once beside a shared projection whose output is y (in any precision): request i is the
+ * rows [offsets[i], offsets[i+1]) and has the adapter a = ids[i], or none (an index outside [0, adapters)):
+ *     t = x A_a^T;     y = bf16_rne( y + scaling[a] t B_a^T )                       (in place)
+ *   x_bf16   [M, K], pitch ldx;   y_bf16  [M, N], pitch ldy
+ *   lora_a   [adapters, r, K] BF16, dense;   lora_b  [adapters, N, r] BF16, dense;   scaling  [adapters] FP32
+ *   offsets  [requests + 1] int32, ascending, held to [0, M];   ids  [requests] int32   (device, as everything here).  Rows in
+ *            front of the first offset and behind the last stay as they are, requests without rows are fine
+ *   t_out    [M, 2 r] BF16 or NULL: t in two parts (columns [0, r): rounded; [r, 2 r): what that left), for the gradients;
+ *            rows without an adapter are not written
+ *   K, N multiples of 8 up to 1048576;  r a multiple of 8, 8 <= r <= 64;  adapters, requests <= 1024
+ *   workspace  sol_lora_workspace_bytes(M, K, N, r, adapters, requests, 0) bytes of device scratch, 256-byte aligned; two calls
+ *              that may overlap need one each
+ * Sums are FP32 in a fixed order; t enters the second product with 16 bits.  Two launches.  A wait that runs out (sol_last_device_status)
+ * leaves y incomplete or NaN.
+ */
+size_t sol_lora_workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, int backward);
+sol_status_t sol_lora_apply(const void *x_bf16, int64_t ldx, const void *lora_a, const void *lora_b, const float *scaling,
+                            const int32_t *offsets, const int32_t *ids, int64_t requests, int64_t adapters, void *y_bf16, int64_t ldy,
+                            void *t_out, int64_t M, int64_t K, int64_t N, int64_t r, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/*
+ * Gradients of sol_lora_apply from dy = d loss / d y; with dt = scaling[a] dy B_a:
+ *     dx = bf16_rne( dx + dt A_a ),   dlora_a = sum over the adapter's rows of dt^T x,   dlora_b = scaling[a] sum of dy^T t
+ *   t        [M, 2 r] as sol_lora_apply left it;  dx_bf16  [M, K], pitch ld_dx, in place: the gradient that x has from the shared
+ *            projection, or NULL
+ *   dlora_a, dlora_b  FP32, shaped as the factors, 16-byte aligned, overwritten (zeros for an adapter without rows)
+ *   workspace  sol_lora_workspace_bytes(..., 1) bytes.  Everything else as there.  Three or four launches.
+ */
+sol_status_t sol_lora_backward(const void *dy_bf16, int64_t ld_dy, const void *x_bf16, int64_t ldx, const void *t, const void *lora_a,
+                               const void *lora_b, const float *scaling, const int32_t *offsets, const int32_t *ids, int64_t requests,
+                               int64_t adapters, void *dx_bf16, int64_t ld_dx, float *dlora_a, float *dlora_b, int64_t M, int64_t K,
+                               int64_t N, int64_t r, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * One AdamW step over many tensors (the policy update in front of that refresh), in place.  Per element, FP32, with t the step:
  *     g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2       (every operation rounded)
  *     param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)

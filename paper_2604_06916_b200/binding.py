@@ -34,6 +34,7 @@ EXPORTS = [
     "sol_qk_rotary_backward_workspace_bytes", "sol_rotary_frequencies", "nvfp4_matvec", "mxfp4_matvec",
     "sol_matvec_workspace_bytes", "sol_select_blocks", "sol_select_blocks_workspace_bytes", "sol_attention_blocks",
     "sol_layernorm", "sol_layernorm_backward", "sol_layernorm_backward_workspace_bytes", "sol_adamw_step",
+    "sol_lora_apply", "sol_lora_backward", "sol_lora_workspace_bytes",
 ]
 
 _lib = None
@@ -137,6 +138,11 @@ def lib() -> ctypes.CDLL:
     L.sol_layernorm_backward_workspace_bytes.restype = sz
     L.sol_layernorm_backward_workspace_bytes.argtypes = [i64, i64, i64]
     L.sol_adamw_step.restype, L.sol_adamw_step.argtypes = i32, [vp, i64, vp, vp, vp]
+    L.sol_lora_workspace_bytes.restype, L.sol_lora_workspace_bytes.argtypes = sz, [i64] * 6 + [i32]
+    L.sol_lora_apply.restype = i32
+    L.sol_lora_apply.argtypes = [vp, i64, vp, vp, vp, vp, vp, i64, i64, vp, i64, vp, i64, i64, i64, i64, vp, sz, vp]
+    L.sol_lora_backward.restype = i32
+    L.sol_lora_backward.argtypes = [vp, i64, vp, i64, vp, vp, vp, vp, vp, vp, i64, i64, vp, i64, vp, vp, i64, i64, i64, i64, vp, sz, vp]
     L.sol_set_wait_limit_cycles.restype, L.sol_set_wait_limit_cycles.argtypes = i32, [i64]
     L.sol_test_hold_loads.restype, L.sol_test_hold_loads.argtypes = i32, [i32]
     L.sol_last_device_status.restype = i32
@@ -885,6 +891,67 @@ def sol_layernorm_backward(dy, x, stats, scale=None, rows_per_sample: int | None
     if code:
         raise SolError(code, "sol_layernorm_backward")
     return out, dscale, dshift
+
+
+def _lora_stacks(lora_a, lora_b, scaling, offsets, ids, K: int, N: int, index: int):
+    """Checks the adapters' stacks and the requests; returns (adapters, rank, requests) and the five addresses."""
+    if lora_a.dim() != 3 or lora_b.dim() != 3:
+        raise TypeError("lora_a, lora_b: expected [adapters, r, K] and [adapters, N, r] tensors")
+    adapters, r = lora_a.shape[:2]
+    requests = ids.shape[0] if ids.dim() == 1 else -1
+    return (adapters, r, requests, _dense("lora_a", lora_a, torch.bfloat16, (adapters, r, K), index),
+            _dense("lora_b", lora_b, torch.bfloat16, (adapters, N, r), index), _dense("scaling", scaling, torch.float32, (adapters,), index),
+            _dense("offsets", offsets, torch.int32, (requests + 1,), index), _dense("ids", ids, torch.int32, (requests,), index))
+
+
+@_on_device_of_first
+def sol_lora_apply(x, lora_a, lora_b, scaling, offsets, ids, y, with_t: bool = False, workspace: torch.Tensor | None = None):
+    """y += scaling[a] (x A_a^T) B_a^T in place for every request's rows, a being the request's adapter (or none); returns y.
+
+    x [M, K], y [M, N] BF16 (views with a row pitch will do); lora_a [n, r, K], lora_b [n, N, r] BF16, scaling [n] FP32; request i is
+    the rows offsets[i] .. offsets[i + 1] (int32, ascending) and has adapter ids[i] (int32), none outside 0 .. n - 1.  `with_t`
+    returns (y, t) with t [M, 2 r], x A^T in two BF16 parts, for sol_lora_backward.
+    """
+    index = x.get_device()
+    ldx, ldy = _rows_view("x", x, index), _rows_view("y", y, index)
+    M, K = x.shape
+    N = y.shape[1]
+    if y.shape[0] != M:
+        raise ValueError("x and y must have the same rows")
+    n, r, requests, a_ptr, b_ptr, s_ptr, o_ptr, i_ptr = _lora_stacks(lora_a, lora_b, scaling, offsets, ids, K, N, index)
+    t = _new(x, (M, 2 * r)) if with_t else None
+    workspace, ws_ptr, ws_bytes = _scratch(workspace, lib().sol_lora_workspace_bytes(M, K, N, r, n, requests, 0), x, index)
+    code = lib().sol_lora_apply(x.data_ptr(), ldx, a_ptr, b_ptr, s_ptr, o_ptr, i_ptr, requests, n, y.data_ptr(), ldy, _ptr(t), M, K, N, r,
+                                ws_ptr, ws_bytes, _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_lora_apply")
+    return (y, t) if with_t else y
+
+
+@_on_device_of_first
+def sol_lora_backward(dy, x, t, lora_a, lora_b, scaling, offsets, ids, dx: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None):
+    """Gradients of sol_lora_apply: (grad lora_a, grad lora_b) in FP32, zeros for an adapter without rows.
+
+    x, t and the stacks are the forward call's.  `dx` [M, K] BF16, the gradient that x has from the shared projection, gets the
+    adapters' part added in place.
+    """
+    index = dy.get_device()
+    ld_dy, ldx = _rows_view("dy", dy, index), _rows_view("x", x, index)
+    M, N = dy.shape
+    K = x.shape[1]
+    if x.shape[0] != M:
+        raise ValueError("dy and x must have the same rows")
+    n, r, requests, a_ptr, b_ptr, s_ptr, o_ptr, i_ptr = _lora_stacks(lora_a, lora_b, scaling, offsets, ids, K, N, index)
+    t_ptr = _dense("t", t, torch.bfloat16, (M, 2 * r), index)
+    ld_dx = K if dx is None else _rows_view("dx", dx, index, x.shape)
+    da, db = _new(dy, (n, r, K), torch.float32), _new(dy, (n, N, r), torch.float32)
+    workspace, ws_ptr, ws_bytes = _scratch(workspace, lib().sol_lora_workspace_bytes(M, K, N, r, n, requests, 1), dy, index)
+    code = lib().sol_lora_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ldx, t_ptr, a_ptr, b_ptr, s_ptr, o_ptr, i_ptr, requests, n, _ptr(dx), ld_dx,
+                                   da.data_ptr(), db.data_ptr(), M, K, N, r, ws_ptr, ws_bytes, _raw_stream(index))
+    if code:
+        raise SolError(code, "sol_lora_backward")
+    return da, db
 
 
 # sol_adamw_tensor_t and sol_adamw_options_t of the C header, packed by the native rules.

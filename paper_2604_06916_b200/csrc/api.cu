@@ -870,6 +870,58 @@ sol_status_t sol_adamw_step(const sol_adamw_tensor_t *tensors, int64_t count, co
     return adamw::launch_step(tensors, count, *o, step_state, static_cast<cudaStream_t>(stream), dev);
 }
 
+static bool lora_shape_ok(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests) {
+    auto width = [](int64_t c) { return c > 0 && c % 8 == 0 && c <= 1048576; };
+    return M > 0 && M <= 0x7FFFFF00LL && width(K) && width(N) && r > 0 && r % 8 == 0 && r <= lora::max_rank() && adapters > 0 && adapters <= 1024 &&
+           requests > 0 && requests <= lora::max_requests();
+}
+static sol_status_t lora_check(const lora::Call &c, const void *a_rows, int64_t lda, const void *b_rows, int64_t ldb, const void *ws, size_t ws_bytes, bool backward) {
+    if (a_rows == nullptr || b_rows == nullptr || c.a == nullptr || c.b == nullptr || c.scaling == nullptr || c.offsets == nullptr || c.ids == nullptr)
+        return SOL_ERR_NULL_POINTER;
+    if (!lora_shape_ok(c.M, c.K, c.N, c.r, c.adapters, c.requests) || lda < c.K || ldb < c.N) return SOL_ERR_BAD_SHAPE;
+    auto aligned4 = [](const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; };
+    if (!aligned16(a_rows) || !aligned16(b_rows) || !aligned16(c.a) || !aligned16(c.b) || lda % 8 != 0 || ldb % 8 != 0 || !aligned4(c.scaling) ||
+        !aligned4(c.offsets) || !aligned4(c.ids))
+        return SOL_ERR_ALIGNMENT;
+    if (ws == nullptr) return SOL_ERR_NULL_POINTER;
+    if (ws_bytes < lora::workspace_bytes(c.M, c.K, c.N, c.r, c.adapters, c.requests, backward)) return SOL_ERR_WORKSPACE_TOO_SMALL;
+    if (reinterpret_cast<uintptr_t>(ws) & 255u) return SOL_ERR_ALIGNMENT;
+    return SOL_OK;
+}
+
+size_t sol_lora_workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, int backward) {
+    return lora_shape_ok(M, K, N, r, adapters, requests) ? lora::workspace_bytes(M, K, N, r, adapters, requests, backward != 0) : 0;
+}
+
+sol_status_t sol_lora_apply(const void *x, int64_t ldx, const void *a, const void *b, const float *scaling, const int32_t *offsets,
+                            const int32_t *ids, int64_t requests, int64_t adapters, void *y, int64_t ldy, void *t_out, int64_t M, int64_t K,
+                            int64_t N, int64_t r, void *workspace, size_t workspace_bytes, void *stream) {
+    const lora::Call c{a, b, scaling, offsets, ids, requests, adapters, M, K, N, r};
+    sol_status_t st = lora_check(c, x, ldx, y, ldy, workspace, workspace_bytes, false);
+    if (st != SOL_OK) return st;
+    if (!aligned16(t_out)) return SOL_ERR_ALIGNMENT;
+    const DeviceInfo *dev = nullptr;
+    st = check_arch(&dev);
+    if (st != SOL_OK) return st;
+    return lora::launch_apply(c, x, ldx, y, ldy, t_out, workspace, static_cast<cudaStream_t>(stream));
+}
+
+sol_status_t sol_lora_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ldx, const void *t, const void *a, const void *b,
+                               const float *scaling, const int32_t *offsets, const int32_t *ids, int64_t requests, int64_t adapters,
+                               void *dx, int64_t ld_dx, float *da, float *db, int64_t M, int64_t K, int64_t N, int64_t r, void *workspace,
+                               size_t workspace_bytes, void *stream) {
+    const lora::Call c{a, b, scaling, offsets, ids, requests, adapters, M, K, N, r};
+    sol_status_t st = lora_check(c, x, ldx, dy, ld_dy, workspace, workspace_bytes, true);
+    if (st != SOL_OK) return st;
+    if (t == nullptr || da == nullptr || db == nullptr) return SOL_ERR_NULL_POINTER;
+    if (dx != nullptr && ld_dx < K) return SOL_ERR_BAD_SHAPE;
+    if (!aligned16(t) || !aligned16(da) || !aligned16(db) || !aligned16(dx) || (dx != nullptr && ld_dx % 8 != 0)) return SOL_ERR_ALIGNMENT;
+    const DeviceInfo *dev = nullptr;
+    st = check_arch(&dev);
+    if (st != SOL_OK) return st;
+    return lora::launch_backward(c, dy, ld_dy, x, ldx, t, dx, ld_dx, da, db, workspace, static_cast<cudaStream_t>(stream));
+}
+
 sol_status_t sol_rotary_frequencies(int64_t dim, double theta, sol_rotary_scaling_t scaling, double factor,
                                     double original_length, double beta_fast, double beta_slow, double *freqs_out,
                                     double *scale_out) {

@@ -1,0 +1,706 @@
+// Low-rank adapters of many requests beside a shared projection, forward and gradients, in BF16 (sm_100a).
+//
+// A request is a run of rows with an adapter of its own (or none).  With t = x A^T (rank r <= 64 columns):
+//     y += s t B^T;     from dy:  dt = s dy B,  dx += dt A,  dA = dt^T x,  dB = s dy^T t
+// All products run on tcgen05 with FP32 sums.  t and dt are held in two BF16 parts, high and low (16 bits), side by side as one
+// operand of twice the width against the factor taken twice: what is lost is 2^-17 of a value and not 2^-9, at no more memory traffic.
+//
+// HBM bound: the adapters' products are r / 2 operations a byte of x, y, dy, far below the tensor cores' rate.  Three kernels, each
+// of which streams one large operand through a ring of TMA stages once:
+//   shrink  t = x A^T (or dy B): 128 rows a block and a slice of the columns; FP32 partial sums to the workspace, one per slice
+//   expand  sums the slices, splits t into its parts, then walks 64 columns at a time: a stage brings the columns of y and the
+//           factor's rows, the product is added to y in the stage's own memory, and a TMA store takes it back
+//   outer   dA and dB: 128 columns of x or dy by the 2r columns of dt or t, summed over an adapter's rows (both operands have the
+//           row as their second index: MN-major); row slices of one adapter are added up in order by a last small launch
+// Which rows and adapter a block has follows from the requests' offsets on the device: the host knows neither, the grid covers the most
+// that there can be (a tile of 128 rows for each 128 rows and one more per request) and blocks without a tile leave.
+// Everything is summed in a fixed order: equal inputs give equal bits.
+#include "gemm_common.cuh"
+#include "quant_math.cuh"
+#include "sol_internal.h"
+
+namespace sol {
+namespace lora {
+namespace {
+
+using gemm::loads_held;
+using gemm::wait_bounded;
+
+constexpr int kRows = 128;               // rows of a tile
+constexpr int kBox = 64;                 // 16-bit columns of a 128-byte swizzled row
+constexpr int kMaxRank = 64, kMaxRequests = 1024;
+constexpr int kRowBox = kRows * 128;     // bytes of a [128][64] box
+constexpr int kFactorBox = 64 * 128;     // bytes of a [64][64] box
+constexpr int kStage = kRowBox + kFactorBox;
+constexpr int kMaxStages = 8;
+constexpr int kSlots = 296;              // blocks that are resident at once: two on each of 148 SMs
+
+struct Requests {
+    const int32_t *offsets;    // [requests + 1]
+    const int32_t *ids;        // [requests]
+    int requests, adapters, rows;
+};
+struct Item {
+    int row0, end, adapter;    // first row of the tile, row behind the request's last
+};
+
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag, uint32_t *status, uint32_t code) {
+    return __all_sync(0xFFFFFFFFu, wait_bounded(bar, parity, abort_flag, status, code));
+}
+// Rows of request `s`, held to the rows that exist; the adapter, -1 for none.
+__device__ __forceinline__ void request(const Requests &q, int s, int &begin, int &end, int &adapter) {
+    begin = min(max(__ldg(q.offsets + s), 0), q.rows);
+    end = min(max(__ldg(q.offsets + s + 1), begin), q.rows);
+    adapter = __ldg(q.ids + s);
+    if (adapter < 0 || adapter >= q.adapters) adapter = -1;
+}
+// The index-th tile of all requests in order; called by a whole warp.  False: there are not so many.
+__device__ __forceinline__ bool find_item(const Requests &q, int index, int lane, Item &item) {
+    int before = 0;
+    for (int s0 = 0; s0 < q.requests; s0 += 32) {
+        int begin = 0, end = 0, adapter = -1;
+        if (s0 + lane < q.requests) request(q, s0 + lane, begin, end, adapter);
+        const int tiles = adapter >= 0 ? (end - begin + kRows - 1) / kRows : 0;
+        int upto = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            if (lane >= o) upto += v;
+        }
+        const int total = __shfl_sync(0xFFFFFFFFu, upto, 31);
+        if (index < before + total) {
+            const int src = __ffs(__ballot_sync(0xFFFFFFFFu, before + upto > index)) - 1;
+            const int tile = index - before - __shfl_sync(0xFFFFFFFFu, upto - tiles, src);
+            item.row0 = __shfl_sync(0xFFFFFFFFu, begin, src) + tile * kRows;
+            item.end = __shfl_sync(0xFFFFFFFFu, end, src);
+            item.adapter = __shfl_sync(0xFFFFFFFFu, adapter, src);
+            return true;
+        }
+        before += total;
+    }
+    return false;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint32_t idesc_of(int n, bool a_mn, bool b_mn) {   // BF16 x BF16 -> FP32, M = 128
+    return (1u << 4) | (1u << 7) | (1u << 10) | (a_mn ? 1u << 15 : 0u) | (b_mn ? 1u << 16 : 0u) | (static_cast<uint32_t>(n >> 3) << 17) |
+           (static_cast<uint32_t>(kRows >> 4) << 24);
+}
+
+// The first 1024 bytes of a block's shared memory (all of it dynamic, so that what follows lies on 1024-byte boundaries as the
+// swizzled operands want it): barriers, the tensor memory's address, the flag of waits that ran out, the item.
+constexpr int kControl = 1024;
+struct Control {
+    uint64_t bars[32];
+    uint32_t tmem, abort;
+    int found;
+    Item item;
+    int n_runs;
+};
+static_assert(sizeof(Control) <= kControl, "control block");
+
+// False: the shared memory is not where it has to be (never seen; recorded, nothing is done).
+__device__ __forceinline__ bool aligned_block(const uint8_t *smem, uint32_t *status) {
+    if ((ptx::smem_u32(smem) & 1023u) == 0) return true;
+    if (threadIdx.x == 0) atomicExch(status, 0xDF0u);
+    return false;
+}
+// `count(i)`: arrivals that barrier i waits for.
+template <uint32_t kColumns, class Count>
+__device__ __forceinline__ void begin_block(Control &c, int n_bars, Count count, int warp) {
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < n_bars; ++i) ptx::mbar_init(ptx::smem_u32(c.bars + i), count(i));
+        c.abort = 0;
+        ptx::fence_mbar_init();
+    }
+    if (warp == 1) {
+        ptx::tmem_alloc(ptx::smem_u32(&c.tmem), kColumns);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+}
+template <uint32_t kColumns>
+__device__ __forceinline__ void end_block(volatile uint32_t *abort_flag, int warp, uint32_t tmem) {
+    if (*abort_flag) __nanosleep(2000000);   // let copies already in flight land before the block exits
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, kColumns);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ shrink
+struct Shrink {
+    Requests q;
+    float *partials;          // [splits][rows][r]
+    uint32_t *status;
+    int r, r16;               // rank, and the next multiple of 16
+    int tiles, per_split;     // 64-column tiles of the long side, and those of a block
+    int splits, stages;
+};
+
+// kFlip: the factor is [long side][r] (dy B: B is [N][r]) and not [r][long side].
+template <bool kFlip>
+__global__ void __launch_bounds__(192, 2)
+shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_f, const Shrink p) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    if (!aligned_block(smem, p.status)) return;
+    Control &control = *reinterpret_cast<Control *>(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = blockIdx.x % p.splits;
+    if (warp == 0) {
+        Item it{};
+        const bool there = find_item(p.q, blockIdx.x / p.splits, lane, it);
+        if (lane == 0) control.item = it, control.found = there;
+    }
+    __syncthreads();
+    if (!control.found) return;
+    const Item item = control.item;
+    // full, empty: [stage]; done
+    begin_block<64>(control, 2 * kMaxStages + 1, [](int) { return 1; }, warp);
+    const uint32_t bars = ptx::smem_u32(control.bars), tmem = control.tmem, ring = ptx::smem_u32(smem) + kControl;
+    volatile uint32_t *abort_flag = &control.abort;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (kMaxStages + s); };
+    const uint32_t done = bars + 8u * (2 * kMaxStages);
+    const int t0 = split * p.per_split, t1 = min(p.tiles, t0 + p.per_split);
+    if (warp == 0) {
+        if (ptx::elect_one() && !loads_held(p.status)) {
+            const uint32_t factor_bytes = kFlip ? kFactorBox : p.r16 * 128;
+            for (int t = t0, s = 0, n = 0; t < t1; ++t, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
+                if (n >= p.stages && !wait_bounded(empty(s), ((n / p.stages) - 1) & 1u, abort_flag, p.status, 0xD00u | s)) break;
+                const uint32_t to = ring + s * kStage;
+                ptx::mbar_arrive_expect_tx(full(s), kRowBox + factor_bytes);
+                ptx::tma_load_2d(to, &tm_x, t * kBox, item.row0, full(s));
+                if (kFlip) ptx::tma_load_3d(to + kRowBox, &tm_f, 0, t * kBox, item.adapter, full(s));
+                else ptx::tma_load_3d(to + kRowBox, &tm_f, t * kBox, 0, item.adapter, full(s));
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (ptx::elect_one()) {
+            const uint32_t idesc = idesc_of(p.r16, false, kFlip);
+            bool ok = true;
+            for (int t = t0, s = 0, n = 0; t < t1; ++t, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
+                if (!(ok = wait_bounded(full(s), (n / p.stages) & 1u, abort_flag, p.status, 0xD10u | s))) break;
+                ptx::tc_fence_after_sync();
+                const uint32_t from = ring + s * kStage;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint64_t a = ptx::smem_desc_sw128(from) + 2u * i;
+                    const uint64_t b = kFlip ? ptx::smem_desc_sw128_mn(from + kRowBox + i * 2048, kFactorBox, 1024)
+                                             : ptx::smem_desc_sw128(from + kRowBox) + 2u * i;
+                    ptx::mma_bf16(tmem, a, b, idesc, n > 0 || i > 0);
+                }
+                ptx::tc_commit(empty(s));
+            }
+            if (ok) ptx::tc_commit(done);
+        }
+        __syncwarp();
+    } else {
+        const int quad = warp & 3, row = item.row0 + quad * 32 + lane;
+        const bool ok = warp_wait(done, 0, abort_flag, p.status, 0xD20u);
+        ptx::tc_fence_after_sync();
+        float *out = p.partials + (static_cast<int64_t>(split) * p.q.rows + row) * p.r;
+        for (int c = 0; c < p.r; c += 8) {
+            uint32_t v[8];
+            if (ok) {
+                ptx::tmem_ld_32x8(tmem + (static_cast<uint32_t>(quad * 32) << 16) + c, v);
+                ptx::tmem_ld_wait();
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = 0x7FC00000u;     // what reads this shall not take it for a result
+            }
+            if (row < item.end) {
+                *reinterpret_cast<uint4 *>(out + c) = make_uint4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<uint4 *>(out + c + 4) = make_uint4(v[4], v[5], v[6], v[7]);
+            }
+        }
+    }
+    end_block<64>(abort_flag, warp, tmem);
+}
+
+// ------------------------------------------------------------------------------------------------ expand
+struct Expand {
+    Requests q;
+    const float *partials;    // [splits][rows][r]
+    const float *scaling;     // [adapters]
+    uint16_t *parts;          // [rows][2 r]: t's high and low parts, or null
+    uint16_t *y;
+    uint32_t *status;
+    int64_t ldy;
+    int r, r16, splits, stages;
+    int scale_t;              // the adapter's factor goes on t (gradients) and not on the product
+    int columns, chunks, per_slice, slices;    // 64-column chunks of y, and those of a block
+};
+
+// kFlip: the factor is [r][columns] (dt A) and not [columns][r].
+template <bool kFlip>
+__global__ void __launch_bounds__(320, 2)
+expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ CUtensorMap tm_f,
+              const Expand p) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    if (!aligned_block(smem, p.status)) return;
+    Control &control = *reinterpret_cast<Control *>(smem);
+    constexpr int kSums = 4;              // accumulators of 64 columns
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int slice = blockIdx.x % p.slices;
+    if (warp == 0) {
+        Item it{};
+        const bool there = find_item(p.q, blockIdx.x / p.slices, lane, it);
+        if (lane == 0) control.item = it, control.found = there;
+    }
+    __syncthreads();
+    if (!control.found) return;
+    const Item item = control.item;
+    // full, empty: [stage]; sum full, sum empty: [accumulator]; t ready
+    constexpr int kSumFull = 2 * kMaxStages, kSumEmpty = kSumFull + kSums, kReady = kSumEmpty + kSums, kBars = kReady + 1;
+    begin_block<64 * kSums>(control, kBars,
+                            [](int i) { return i == kReady ? 8 : (i >= kMaxStages && i < kSumFull) || i >= kSumEmpty ? 4 : 1; }, warp);
+    const uint32_t bars = ptx::smem_u32(control.bars), tmem = control.tmem;
+    volatile uint32_t *abort_flag = &control.abort;
+    auto bar = [&](int i) { return bars + 8u * i; };
+    const uint32_t sT = ptx::smem_u32(smem) + kControl;           // t as [128][2 r16], boxes of 64 columns
+    const int t_boxes = (2 * p.r16 + kBox - 1) / kBox;
+    const uint32_t ring = sT + t_boxes * kRowBox;
+    const int c0 = slice * p.per_slice, c1 = min(p.chunks, c0 + p.per_slice);
+    if (warp == 0) {
+        if (ptx::elect_one() && !loads_held(p.status)) {
+            const uint32_t factor_bytes = kFlip ? p.r16 * 128 : kFactorBox;
+            for (int c = c0, s = 0, n = 0; c < c1; ++c, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
+                if (n >= p.stages && !wait_bounded(bar(kMaxStages + s), ((n / p.stages) - 1) & 1u, abort_flag, p.status, 0xD30u | s)) break;
+                const uint32_t to = ring + s * kStage;
+                ptx::mbar_arrive_expect_tx(bar(s), kRowBox + factor_bytes);
+                ptx::tma_load_2d(to, &tm_y, c * kBox, item.row0, bar(s));
+                if (kFlip) ptx::tma_load_3d(to + kRowBox, &tm_f, c * kBox, 0, item.adapter, bar(s));
+                else ptx::tma_load_3d(to + kRowBox, &tm_f, 0, c * kBox, item.adapter, bar(s));
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (ptx::elect_one() && c0 < c1) {
+            const uint32_t idesc = idesc_of(kBox, false, kFlip);
+            const int half = p.r16 >> 4;          // products for each of t's parts
+            bool ok = wait_bounded(bar(kReady), 0, abort_flag, p.status, 0xD40u);
+            for (int c = c0, s = 0, n = 0; ok && c < c1; ++c, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
+                const int d = n % kSums;
+                if (n >= kSums && !wait_bounded(bar(kSumEmpty + d), ((n / kSums) - 1) & 1u, abort_flag, p.status, 0xD50u | d)) break;
+                if (!wait_bounded(bar(s), (n / p.stages) & 1u, abort_flag, p.status, 0xD60u | s)) break;
+                ptx::tc_fence_after_sync();
+                const uint32_t from = ring + s * kStage + kRowBox;
+                for (int i = 0; i < 2 * half; ++i) {
+                    const int j = i < half ? i : i - half;
+                    const uint64_t a = ptx::smem_desc_sw128(sT + (i >> 2) * kRowBox) + 2u * (i & 3);
+                    const uint64_t b = kFlip ? ptx::smem_desc_sw128_mn(from + j * 2048, kFactorBox, 1024) : ptx::smem_desc_sw128(from) + 2u * j;
+                    ptx::mma_bf16(tmem + d * kBox, a, b, idesc, i > 0);
+                }
+                ptx::tc_commit(bar(kSumFull + d));
+            }
+        }
+        __syncwarp();
+    } else {
+        const int group = (warp - 2) >> 2, quad = warp & 3;
+        const int tile_row = quad * 32 + lane, row = item.row0 + tile_row;
+        const bool there = row < item.end;
+        const float factor = __ldg(p.scaling + item.adapter);
+        const uint32_t sw = static_cast<uint32_t>(tile_row & 7);
+        ptx::grid_dependency_wait();
+        // t: the slices in order, eight columns at a time (the two groups take turns), both parts into the operand
+        for (int c = 8 * group; c < p.r16; c += 16) {
+            float t[8] = {};
+            if (there && c < p.r) {
+                for (int s = 0; s < p.splits; ++s) {
+                    const float4 *from = reinterpret_cast<const float4 *>(p.partials + (static_cast<int64_t>(s) * p.q.rows + row) * p.r + c);
+                    const float4 a = __ldcg(from), b = __ldcg(from + 1);
+                    t[0] += a.x, t[1] += a.y, t[2] += a.z, t[3] += a.w, t[4] += b.x, t[5] += b.y, t[6] += b.z, t[7] += b.w;
+                }
+            }
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float a = t[2 * e], b = t[2 * e + 1];
+                if (p.scale_t) a *= factor, b *= factor;
+                hi[e] = pack_bf16(a, b);
+                lo[e] = pack_bf16(a - qmath::bf16_lo(hi[e]), b - qmath::bf16_hi(hi[e]));
+            }
+            const uint4 h = make_uint4(hi[0], hi[1], hi[2], hi[3]), l = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            const int ch = c >> 3, cl = (c + p.r16) >> 3;       // 16-byte pieces of the operand's row
+            sts128(sT + (ch >> 3) * kRowBox + tile_row * 128 + ((static_cast<uint32_t>(ch & 7) ^ sw) << 4), h);
+            sts128(sT + (cl >> 3) * kRowBox + tile_row * 128 + ((static_cast<uint32_t>(cl & 7) ^ sw) << 4), l);
+            if (p.parts != nullptr && slice == 0 && there && c < p.r) {
+                uint16_t *out = p.parts + static_cast<int64_t>(row) * 2 * p.r + c;
+                *reinterpret_cast<uint4 *>(out) = h;
+                *reinterpret_cast<uint4 *>(out + p.r) = l;
+            }
+        }
+        ptx::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(bar(kReady));
+        // chunks of 64 columns, the two groups in turn
+        const float scale = p.scale_t ? 1.0f : factor;
+        const bool whole = item.row0 + quad * 32 + 32 <= item.end;         // all of this warp's rows are the request's
+        int held = -1;
+        bool ok = true;
+        for (int c = c0 + group, n = group; c < c1; c += 2, n += 2) {
+            const int d = n % kSums, s = n % p.stages;
+            ok = warp_wait(bar(kSumFull + d), (n / kSums) & 1u, abort_flag, p.status, 0xD70u | d) &&
+                 warp_wait(bar(s), (n / p.stages) & 1u, abort_flag, p.status, 0xD80u | s);
+            if (!ok) break;
+            ptx::tc_fence_after_sync();
+            uint32_t v[2][32];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) ptx::tmem_ld_32x32(tmem + (static_cast<uint32_t>(quad * 32) << 16) + d * kBox + 32 * h, v[h]);
+            ptx::tmem_ld_wait();
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(kSumEmpty + d));
+            const uint32_t at = ring + s * kStage + tile_row * 128;
+            uint16_t *out = p.y + row * p.ldy + c * kBox;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const uint32_t place = at + ((static_cast<uint32_t>(q) ^ sw) << 4);
+                const uint4 old = ptx::lds128(place);
+                const uint32_t w[4] = {old.x, old.y, old.z, old.w};
+                uint32_t o[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float a = __uint_as_float(v[q >> 2][(q & 3) * 8 + 2 * e]), b = __uint_as_float(v[q >> 2][(q & 3) * 8 + 2 * e + 1]);
+                    o[e] = pack_bf16(fmaf(a, scale, qmath::bf16_lo(w[e])), fmaf(b, scale, qmath::bf16_hi(w[e])));
+                }
+                const uint4 now = make_uint4(o[0], o[1], o[2], o[3]);
+                if (whole) sts128(place, now);
+                else if (there && c * kBox + 8 * q < p.columns) *reinterpret_cast<uint4 *>(out + 8 * q) = now;
+            }
+            if (whole) {
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    ptx::tma_store_2d(&tm_out, c * kBox, item.row0 + quad * 32, ring + s * kStage + quad * 32 * 128);
+                    ptx::tma_store_commit();
+                    if (held >= 0) {       // the store before this one has left its stage
+                        ptx::tma_store_wait_read<1>();
+                        ptx::mbar_arrive(bar(kMaxStages + held));
+                    }
+                }
+                held = s;
+            } else {
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(bar(kMaxStages + s));
+            }
+        }
+        if (lane == 0) ptx::tma_store_wait_all<0>();
+    }
+    end_block<64 * kSums>(abort_flag, warp, tmem);
+}
+
+// ------------------------------------------------------------------------------------------------ outer
+struct Outer {
+    Requests q;
+    const float *scaling;
+    float *da, *db;           // [adapters][r][K], [adapters][N][r]; with several row slices those of the workspace's first
+    int64_t slice_floats;     // from one row slice's sums to the next's
+    uint32_t *status;
+    int r, K, N, tiles_x, tiles;    // 128-column tiles of x, and of x and dy
+    int slices, stages;       // row slices of an adapter
+};
+constexpr int kStepRows = 64;
+constexpr int kRunBytes = kMaxRequests * 8;
+constexpr int outer_stage(int u_boxes) { return (2 + u_boxes) * kFactorBox; }     // 128 columns of x or dy, 64 or 128 of t's parts
+
+__global__ void __launch_bounds__(192, 2)
+outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_dt,
+             const __grid_constant__ CUtensorMap tm_t, const Outer p) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    if (!aligned_block(smem, p.status)) return;
+    Control &control = *reinterpret_cast<Control *>(smem);
+    int2 *runs = reinterpret_cast<int2 *>(smem + kControl);       // this block's rows: [begin, end) of each request of its adapter, cut to the slice
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tile = blockIdx.x % p.tiles, slice = blockIdx.x / p.tiles % p.slices, adapter = blockIdx.x / p.tiles / p.slices;
+    const bool of_x = tile < p.tiles_x;
+    const int column = (of_x ? tile : tile - p.tiles_x) * 128;
+    if (warp == 0) {
+        const int lo = static_cast<int>(static_cast<int64_t>(p.q.rows) * slice / p.slices);
+        const int hi = static_cast<int>(static_cast<int64_t>(p.q.rows) * (slice + 1) / p.slices);
+        int n = 0;
+        for (int s0 = 0; s0 < p.q.requests; s0 += 32) {
+            int begin = 0, end = 0, a = -1;
+            if (s0 + lane < p.q.requests) request(p.q, s0 + lane, begin, end, a);
+            begin = max(begin, lo), end = min(end, hi);
+            const uint32_t mine = __ballot_sync(0xFFFFFFFFu, a == adapter && begin < end);
+            if (mine >> lane & 1u) runs[n + __popc(mine & ((1u << lane) - 1u))] = make_int2(begin, end);
+            n += __popc(mine);
+        }
+        if (lane == 0) control.n_runs = n;
+    }
+    begin_block<128>(control, 2 * kMaxStages + 1, [](int) { return 1; }, warp);
+    const uint32_t bars = ptx::smem_u32(control.bars), tmem = control.tmem, ring = ptx::smem_u32(smem) + kControl + kRunBytes;
+    volatile uint32_t *abort_flag = &control.abort;
+    const int n_runs = control.n_runs;
+    auto full = [&](int s) { return bars + 8u * s; };
+    auto empty = [&](int s) { return bars + 8u * (kMaxStages + s); };
+    const uint32_t done = bars + 8u * (2 * kMaxStages);
+    const int u_boxes = (2 * p.r + kBox - 1) / kBox, stage_bytes = (2 + u_boxes) * kFactorBox;
+    if (warp == 0) {
+        ptx::grid_dependency_wait();
+        if (ptx::elect_one() && !loads_held(p.status)) {
+            const CUtensorMap *tm_z = of_x ? &tm_x : &tm_dy, *tm_u = of_x ? &tm_dt : &tm_t;
+            int s = 0, n = 0;
+            bool ok = true;
+            for (int run = 0; ok && run < n_runs; ++run) {
+                for (int row = runs[run].x; row < runs[run].y; row += kStepRows, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
+                    if (n >= p.stages && !(ok = wait_bounded(empty(s), ((n / p.stages) - 1) & 1u, abort_flag, p.status, 0xD90u | s))) break;
+                    const uint32_t to = ring + s * stage_bytes;
+                    ptx::mbar_arrive_expect_tx(full(s), (2 + u_boxes) * kFactorBox);
+                    ptx::tma_load_2d(to, tm_z, column, row, full(s));
+                    ptx::tma_load_2d(to + kFactorBox, tm_z, column + kBox, row, full(s));
+                    for (int b = 0; b < u_boxes; ++b) ptx::tma_load_2d(to + (2 + b) * kFactorBox, tm_u, b * kBox, row, full(s));
+                }
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        const uint32_t idesc = idesc_of(2 * p.r, true, true);
+        int s = 0, n = 0;
+        bool ok = true;
+        for (int run = 0; ok && run < n_runs; ++run) {
+            for (int row = runs[run].x; row < runs[run].y; row += kStepRows, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
+                if (!(ok = warp_wait(full(s), (n / p.stages) & 1u, abort_flag, p.status, 0xDA0u | s))) break;
+                const uint32_t from = ring + s * stage_bytes;
+                const int rows = runs[run].y - row;
+                if (rows < kStepRows) {       // rows that belong to somebody else may hold anything: zeros in their place
+                    for (int i = rows * 8 + lane; i < kStepRows * 8; i += 32)
+                        for (int b = 0; b < 2 + u_boxes; ++b) sts128(from + b * kFactorBox + i * 16, make_uint4(0, 0, 0, 0));
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                if (ptx::elect_one()) {
+                    ptx::tc_fence_after_sync();
+#pragma unroll
+                    for (int i = 0; i < kStepRows / 16; ++i)
+                        ptx::mma_bf16(tmem, ptx::smem_desc_sw128_mn(from + i * 2048, kFactorBox, 1024),
+                                      ptx::smem_desc_sw128_mn(from + 2 * kFactorBox + i * 2048, kFactorBox, 1024), idesc, n > 0 || i > 0);
+                    ptx::tc_commit(empty(s));
+                }
+                __syncwarp();
+            }
+        }
+        if (ok && n > 0 && ptx::elect_one()) ptx::tc_commit(done);
+        __syncwarp();
+    } else {
+        const int quad = warp & 3, c = column + quad * 32 + lane;
+        const bool any = n_runs > 0;
+        const bool ok = !any || warp_wait(done, 0, abort_flag, p.status, 0xDB0u);
+        ptx::tc_fence_after_sync();
+        const float scale = of_x ? 1.0f : __ldg(p.scaling + adapter);
+        float *out = (of_x ? p.da : p.db) + slice * p.slice_floats;
+        if (ok) {
+            for (int j = 0; j < p.r; j += 8) {
+                uint32_t hi[8], lo[8];
+                float v[8];
+                if (any) {
+                    ptx::tmem_ld_32x8(tmem + (static_cast<uint32_t>(quad * 32) << 16) + j, hi);
+                    ptx::tmem_ld_32x8(tmem + (static_cast<uint32_t>(quad * 32) << 16) + p.r + j, lo);
+                    ptx::tmem_ld_wait();
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = any ? (__uint_as_float(hi[e]) + __uint_as_float(lo[e])) * scale : 0.0f;
+                if (of_x) {
+                    if (c < p.K) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) out[(static_cast<int64_t>(adapter) * p.r + j + e) * p.K + c] = v[e];
+                    }
+                } else if (c < p.N) {
+                    float4 *to = reinterpret_cast<float4 *>(out + (static_cast<int64_t>(adapter) * p.N + c) * p.r + j);
+                    to[0] = make_float4(v[0], v[1], v[2], v[3]);
+                    to[1] = make_float4(v[4], v[5], v[6], v[7]);
+                }
+            }
+        }
+    }
+    end_block<128>(abort_flag, warp, tmem);
+}
+
+// The row slices' sums, in order: dA's values, then dB's.
+__global__ void __launch_bounds__(256)
+add_slices(const float4 *__restrict__ from, int64_t slice4, int slices, int64_t da4, float4 *da, float4 *db) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    ptx::grid_dependency_wait();
+    if (i >= slice4) return;
+    float4 v = __ldcg(from + i);
+    for (int s = 1; s < slices; ++s) {
+        const float4 w = __ldcg(from + s * slice4 + i);
+        v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    }
+    if (i < da4) da[i] = v;
+    else db[i - da4] = v;
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+// How a call's work is shared out: from its sizes alone, so that the workspace's size follows from them too.
+struct Plan {
+    int64_t items;                         // tiles of rows, at most
+    int shrink_tiles, shrink_splits, shrink_per;
+    int chunks, slices, per_slice;         // of expand
+    int outer_tiles, outer_tiles_x, outer_slices;
+};
+Plan plan_of(int64_t M, int64_t from, int64_t to, int64_t requests, int64_t adapters) {     // shrink over `from` columns, expand to `to`
+    Plan p;
+    p.items = ceil_div(M, kRows) + requests;
+    // one wave of blocks where the tiles alone do not fill it, none with fewer than four stages
+    p.shrink_tiles = static_cast<int>(ceil_div(from, kBox));
+    int64_t splits = p.items < kSlots ? kSlots / p.items : 1;
+    if (splits > p.shrink_tiles / 4) splits = p.shrink_tiles / 4;
+    if (splits < 1) splits = 1;
+    p.shrink_per = static_cast<int>(ceil_div(p.shrink_tiles, splits));
+    p.shrink_splits = static_cast<int>(ceil_div(p.shrink_tiles, p.shrink_per));
+    // the same, or four waves whose last one is short
+    p.chunks = static_cast<int>(ceil_div(to, kBox));
+    int64_t slices = p.items <= kSlots / 2 ? kSlots / p.items : ceil_div(4 * kSlots, p.items);
+    if (slices > p.chunks) slices = p.chunks;
+    p.per_slice = static_cast<int>(ceil_div(p.chunks, slices));
+    p.slices = static_cast<int>(ceil_div(p.chunks, p.per_slice));
+    // gradients of the factors: `from` is dy's width, `to` that of x
+    p.outer_tiles_x = static_cast<int>(ceil_div(to, 128));
+    p.outer_tiles = p.outer_tiles_x + static_cast<int>(ceil_div(from, 128));
+    int64_t rows = kSlots / (p.outer_tiles * adapters);
+    if (rows > ceil_div(M, 512)) rows = ceil_div(M, 512);
+    p.outer_slices = rows < 1 ? 1 : static_cast<int>(rows);
+    return p;
+}
+int64_t pad256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
+int64_t partial_bytes(const Plan &p, int64_t M, int64_t r) { return pad256(4 * p.shrink_splits * M * r); }
+int64_t parts_bytes(int64_t M, int64_t r) { return pad256(4 * M * r); }
+
+sol_status_t configure(const void *kern, int smem) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+        cudaGetLastError();
+        return SOL_ERR_CUDA;
+    }
+    return SOL_OK;
+}
+template <class... P, class... A>
+sol_status_t launch_after(void (*kern)(P...), int64_t grid, int threads, int smem, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) {
+        cudaGetLastError();
+        return SOL_ERR_CUDA;
+    }
+    return launch_status();
+}
+bool rows_map(CUtensorMap *out, const void *base, int64_t cols, int64_t rows, int64_t ld, int box_rows) {
+    return make_tmap_2d(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, cols, rows, 2 * ld, kBox, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// A stack of factors [adapters][rows][cols]; boxes of 64 columns.
+bool factor_map(CUtensorMap *out, const void *base, int64_t cols, int64_t rows, int64_t adapters, int box_rows) {
+    return make_tmap_3d_bf16(out, base, cols, rows, adapters, 2 * cols, 2 * cols * rows, kBox, box_rows);
+}
+
+constexpr int kHalfSmem = 115712, kFullSmem = 232448;     // two blocks an SM, or one
+
+template <bool kFlip>
+sol_status_t launch_shrink(const Requests &q, const void *x, int64_t ldx, const void *factor, int64_t cols, int64_t r, const Plan &plan, float *partials,
+                           cudaStream_t stream) {
+    const int r16 = static_cast<int>(ceil_div(r, 16) * 16);
+    CUtensorMap tm_x, tm_f;
+    if (!rows_map(&tm_x, x, cols, q.rows, ldx, kRows)) return SOL_ERR_CUDA;
+    if (!(kFlip ? factor_map(&tm_f, factor, r, cols, q.adapters, kBox) : factor_map(&tm_f, factor, cols, r, q.adapters, r16))) return SOL_ERR_CUDA;
+    Shrink p{q, partials, device_status_word(), static_cast<int>(r), r16, plan.shrink_tiles, plan.shrink_per, plan.shrink_splits, (kHalfSmem - kControl) / kStage};
+    const sol_status_t st = configure(reinterpret_cast<const void *>(shrink_kernel<kFlip>), kControl + p.stages * kStage);
+    if (st != SOL_OK) return st;
+    shrink_kernel<kFlip><<<static_cast<unsigned>(plan.items * plan.shrink_splits), 192, kControl + p.stages * kStage, stream>>>(tm_x, tm_f, p);
+    return launch_status();
+}
+// y null: t's parts only
+template <bool kFlip>
+sol_status_t launch_expand(const Requests &q, const float *partials, const float *scaling, bool scale_t, void *parts, void *y, int64_t ldy,
+                           const void *factor, int64_t cols, int64_t r, const Plan &plan, cudaStream_t stream) {
+    const int r16 = static_cast<int>(ceil_div(r, 16) * 16);
+    CUtensorMap tm_y{}, tm_out{}, tm_f{};
+    if (y != nullptr) {
+        if (!rows_map(&tm_y, y, cols, q.rows, ldy, kRows) || !rows_map(&tm_out, y, cols, q.rows, ldy, 32)) return SOL_ERR_CUDA;
+        if (!(kFlip ? factor_map(&tm_f, factor, cols, r, q.adapters, r16) : factor_map(&tm_f, factor, r, cols, q.adapters, kBox))) return SOL_ERR_CUDA;
+    }
+    const int t_bytes = static_cast<int>(ceil_div(2 * r16, kBox)) * kRowBox;
+    Expand p{q, partials, scaling, static_cast<uint16_t *>(parts), static_cast<uint16_t *>(y), device_status_word(), ldy, static_cast<int>(r), r16,
+             plan.shrink_splits, 0, scale_t, static_cast<int>(cols), y != nullptr ? plan.chunks : 0, plan.per_slice, y != nullptr ? plan.slices : 1};
+    // two blocks an SM with four stages up to rank 32, one with seven beyond
+    p.stages = ((t_bytes == kRowBox ? kHalfSmem : kFullSmem) - kControl - t_bytes) / kStage;
+    if (p.stages > kMaxStages) p.stages = kMaxStages;
+    const int smem = kControl + t_bytes + p.stages * kStage;
+    const sol_status_t st = configure(reinterpret_cast<const void *>(expand_kernel<kFlip>), smem);
+    if (st != SOL_OK) return st;
+    return launch_after(expand_kernel<kFlip>, plan.items * p.slices, 320, smem, stream, tm_y, tm_out, tm_f, p);
+}
+
+}  // namespace
+
+int max_rank() { return kMaxRank; }
+int max_requests() { return kMaxRequests; }
+
+size_t workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, bool backward) {
+    if (!backward) return static_cast<size_t>(partial_bytes(plan_of(M, K, N, requests, adapters), M, r));
+    const Plan p = plan_of(M, N, K, requests, adapters);
+    return static_cast<size_t>(partial_bytes(p, M, r) + parts_bytes(M, r) + (p.outer_slices > 1 ? 4 * p.outer_slices * adapters * r * (K + N) : 0));
+}
+
+sol_status_t launch_apply(const Call &c, const void *x, int64_t ldx, void *y, int64_t ldy, void *t_out, void *workspace, cudaStream_t stream) {
+    const Requests q{c.offsets, c.ids, static_cast<int>(c.requests), static_cast<int>(c.adapters), static_cast<int>(c.M)};
+    const Plan plan = plan_of(c.M, c.K, c.N, c.requests, c.adapters);
+    float *partials = static_cast<float *>(workspace);
+    const sol_status_t st = launch_shrink<false>(q, x, ldx, c.a, c.K, c.r, plan, partials, stream);
+    if (st != SOL_OK) return st;
+    return launch_expand<false>(q, partials, c.scaling, false, t_out, y, ldy, c.b, c.N, c.r, plan, stream);
+}
+
+sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, const void *t, void *dx, int64_t ld_dx,
+                             float *da, float *db, void *workspace, cudaStream_t stream) {
+    const Requests q{c.offsets, c.ids, static_cast<int>(c.requests), static_cast<int>(c.adapters), static_cast<int>(c.M)};
+    const Plan plan = plan_of(c.M, c.N, c.K, c.requests, c.adapters);
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    float *partials = reinterpret_cast<float *>(ws);
+    void *dt = ws + partial_bytes(plan, c.M, c.r);
+    float *sums = reinterpret_cast<float *>(ws + partial_bytes(plan, c.M, c.r) + parts_bytes(c.M, c.r));
+    sol_status_t st = launch_shrink<true>(q, dy, ld_dy, c.b, c.N, c.r, plan, partials, stream);
+    if (st != SOL_OK) return st;
+    st = launch_expand<true>(q, partials, c.scaling, true, dt, dx, ld_dx, c.a, c.K, c.r, plan, stream);
+    if (st != SOL_OK) return st;
+    CUtensorMap tm_x, tm_dy, tm_dt, tm_t;
+    if (!rows_map(&tm_x, x, c.K, c.M, ldx, kStepRows) || !rows_map(&tm_dy, dy, c.N, c.M, ld_dy, kStepRows) ||
+        !rows_map(&tm_dt, dt, 2 * c.r, c.M, 2 * c.r, kStepRows) || !rows_map(&tm_t, t, 2 * c.r, c.M, 2 * c.r, kStepRows))
+        return SOL_ERR_CUDA;
+    const int64_t da_floats = c.adapters * c.r * c.K, db_floats = c.adapters * c.r * c.N;
+    const bool sliced = plan.outer_slices > 1;
+    Outer p{q, c.scaling, sliced ? sums : da, sliced ? sums + da_floats : db, da_floats + db_floats, device_status_word(), static_cast<int>(c.r),
+            static_cast<int>(c.K), static_cast<int>(c.N), plan.outer_tiles_x, plan.outer_tiles, plan.outer_slices, 0};
+    const int stage = outer_stage(static_cast<int>(ceil_div(2 * c.r, kBox)));
+    p.stages = (kHalfSmem - kControl - kRunBytes) / stage;
+    const int smem = kControl + kRunBytes + p.stages * stage;
+    st = configure(reinterpret_cast<const void *>(outer_kernel), smem);
+    if (st != SOL_OK) return st;
+    st = launch_after(outer_kernel, static_cast<int64_t>(plan.outer_tiles) * plan.outer_slices * c.adapters, 192, smem, stream, tm_x, tm_dy, tm_dt, tm_t, p);
+    if (st != SOL_OK || !sliced) return st;
+    const int64_t slice4 = (da_floats + db_floats) / 4;
+    return launch_after(add_slices, ceil_div(slice4, 256), 256, 0, stream, reinterpret_cast<const float4 *>(sums), slice4, plan.outer_slices,
+                        da_floats / 4, reinterpret_cast<float4 *>(da), reinterpret_cast<float4 *>(db));
+}
+
+}  // namespace lora
+}  // namespace sol

@@ -221,6 +221,22 @@ sol_status_t launch_step(const Tensor *tensors, int64_t count, const sol_adamw_o
                          const DeviceInfo *dev);
 }
 
+// Low-rank adapters of many requests beside a shared projection (arguments as the header's entries).
+namespace lora {
+struct Call {
+    const void *a, *b;          // [adapters][r][K], [adapters][N][r]
+    const float *scaling;
+    const int32_t *offsets, *ids;
+    int64_t requests, adapters, M, K, N, r;
+};
+int max_rank();
+int max_requests();
+size_t workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, bool backward);
+sol_status_t launch_apply(const Call &c, const void *x, int64_t ldx, void *y, int64_t ldy, void *t_out, void *workspace, cudaStream_t stream);
+sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, const void *t, void *dx, int64_t ld_dx,
+                             float *da, float *db, void *workspace, cudaStream_t stream);
+}
+
 // Few BF16 rows against a 4-bit weight (wts null: MXFP4).
 namespace matvec {
 size_t workspace_bytes(int64_t M, int64_t K);
