@@ -138,6 +138,10 @@ __device__ __forceinline__ void end_block(volatile uint32_t *abort_flag, int war
     }
 }
 
+// The tensor core adds to an FP32 sum with truncation, 2^-25 of it a step on average and always towards zero: a sum is taken out after so
+// many stages of 64 (32 steps, 2^-20) and goes on in a register, where additions are rounded.
+constexpr int kWindow = 8;
+
 // ------------------------------------------------------------------------------------------------ shrink
 struct Shrink {
     Requests q;
@@ -165,13 +169,15 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     __syncthreads();
     if (!control.found) return;
     const Item item = control.item;
-    // full, empty: [stage]; done
-    begin_block<64>(control, 2 * kMaxStages + 1, [](int) { return 1; }, warp);
+    // full, empty: [stage]; sum full, sum empty: [accumulator]
+    constexpr int kSumFull = 2 * kMaxStages, kSumEmpty = kSumFull + 2;
+    begin_block<128>(control, kSumEmpty + 2, [](int i) { return i >= kSumEmpty ? 4 : 1; }, warp);
+    ptx::grid_launch_dependents();
     const uint32_t bars = ptx::smem_u32(control.bars), tmem = control.tmem, ring = ptx::smem_u32(smem) + kControl;
     volatile uint32_t *abort_flag = &control.abort;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (kMaxStages + s); };
-    const uint32_t done = bars + 8u * (2 * kMaxStages);
+    auto bar = [&](int i) { return bars + 8u * i; };
     const int t0 = split * p.per_split, t1 = min(p.tiles, t0 + p.per_split);
     if (warp == 0) {
         if (ptx::elect_one() && !loads_held(p.status)) {
@@ -189,9 +195,10 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
     } else if (warp == 1) {
         if (ptx::elect_one()) {
             const uint32_t idesc = idesc_of(p.r16, false, kFlip);
-            bool ok = true;
             for (int t = t0, s = 0, n = 0; t < t1; ++t, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
-                if (!(ok = wait_bounded(full(s), (n / p.stages) & 1u, abort_flag, p.status, 0xD10u | s))) break;
+                const int w = n / kWindow, d = w & 1;
+                if (n % kWindow == 0 && w >= 2 && !wait_bounded(bar(kSumEmpty + d), ((w >> 1) - 1) & 1u, abort_flag, p.status, 0xD18u | d)) break;
+                if (!wait_bounded(full(s), (n / p.stages) & 1u, abort_flag, p.status, 0xD10u | s)) break;
                 ptx::tc_fence_after_sync();
                 const uint32_t from = ring + s * kStage;
 #pragma unroll
@@ -199,34 +206,44 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
                     const uint64_t a = ptx::smem_desc_sw128(from) + 2u * i;
                     const uint64_t b = kFlip ? ptx::smem_desc_sw128_mn(from + kRowBox + i * 2048, kFactorBox, 1024)
                                              : ptx::smem_desc_sw128(from + kRowBox) + 2u * i;
-                    ptx::mma_bf16(tmem, a, b, idesc, n > 0 || i > 0);
+                    ptx::mma_bf16(tmem + d * kBox, a, b, idesc, n % kWindow > 0 || i > 0);
                 }
                 ptx::tc_commit(empty(s));
+                if (n % kWindow == kWindow - 1 || t + 1 == t1) ptx::tc_commit(bar(kSumFull + d));
             }
-            if (ok) ptx::tc_commit(done);
         }
         __syncwarp();
     } else {
         const int quad = warp & 3, row = item.row0 + quad * 32 + lane;
-        const bool ok = warp_wait(done, 0, abort_flag, p.status, 0xD20u);
-        ptx::tc_fence_after_sync();
-        float *out = p.partials + (static_cast<int64_t>(split) * p.q.rows + row) * p.r;
-        for (int c = 0; c < p.r; c += 8) {
-            uint32_t v[8];
-            if (ok) {
-                ptx::tmem_ld_32x8(tmem + (static_cast<uint32_t>(quad * 32) << 16) + c, v);
-                ptx::tmem_ld_wait();
-            } else {
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        float sum[kMaxRank] = {};
+        bool ok = true;
+        for (int w = 0; w * kWindow < t1 - t0; ++w) {
+            const int d = w & 1;
+            if (!(ok = warp_wait(bar(kSumFull + d), (w >> 1) & 1u, abort_flag, p.status, 0xD20u | d))) break;
+            ptx::tc_fence_after_sync();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = 0x7FC00000u;     // what reads this shall not take it for a result
+            for (int c = 0; c < kMaxRank; c += 8) {
+                if (c >= p.r) continue;
+                uint32_t v[8];
+                ptx::tmem_ld_32x8(lanes + d * kBox + c, v);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[c + e] += __uint_as_float(v[e]);
             }
-            if (row < item.end) {
-                *reinterpret_cast<uint4 *>(out + c) = make_uint4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<uint4 *>(out + c + 4) = make_uint4(v[4], v[5], v[6], v[7]);
-            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(kSumEmpty + d));
+        }
+        float *out = p.partials + (static_cast<int64_t>(split) * p.q.rows + row) * p.r;
+        const float nan = __uint_as_float(0x7FC00000u);       // what reads a sum that is not whole shall not take it for a result
+#pragma unroll
+        for (int c = 0; c < kMaxRank; c += 4) {
+            if (c < p.r && row < item.end)
+                *reinterpret_cast<float4 *>(out + c) = ok ? make_float4(sum[c], sum[c + 1], sum[c + 2], sum[c + 3]) : make_float4(nan, nan, nan, nan);
         }
     }
-    end_block<64>(abort_flag, warp, tmem);
+    end_block<128>(abort_flag, warp, tmem);
 }
 
 // ------------------------------------------------------------------------------------------------ expand
@@ -264,8 +281,11 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
     const Item item = control.item;
     // full, empty: [stage]; sum full, sum empty: [accumulator]; t ready
     constexpr int kSumFull = 2 * kMaxStages, kSumEmpty = kSumFull + kSums, kReady = kSumEmpty + kSums, kBars = kReady + 1;
+    // a request's last tile may leave warps without rows: they do not take part
+    const int quads = min(4, (item.end - item.row0 + 31) / 32);
     begin_block<64 * kSums>(control, kBars,
-                            [](int i) { return i == kReady ? 8 : (i >= kMaxStages && i < kSumFull) || i >= kSumEmpty ? 4 : 1; }, warp);
+                            [quads](int i) { return i == kReady ? 8 : (i >= kMaxStages && i < kSumFull) || i >= kSumEmpty ? quads : 1; }, warp);
+    ptx::grid_launch_dependents();
     const uint32_t bars = ptx::smem_u32(control.bars), tmem = control.tmem;
     volatile uint32_t *abort_flag = &control.abort;
     auto bar = [&](int i) { return bars + 8u * i; };
@@ -318,6 +338,7 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
         for (int c = 8 * group; c < p.r16; c += 16) {
             float t[8] = {};
             if (there && c < p.r) {
+#pragma unroll 4
                 for (int s = 0; s < p.splits; ++s) {
                     const float4 *from = reinterpret_cast<const float4 *>(p.partials + (static_cast<int64_t>(s) * p.q.rows + row) * p.r + c);
                     const float4 a = __ldcg(from), b = __ldcg(from + 1);
@@ -348,37 +369,40 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
         // chunks of 64 columns, the two groups in turn
         const float scale = p.scale_t ? 1.0f : factor;
         const bool whole = item.row0 + quad * 32 + 32 <= item.end;         // all of this warp's rows are the request's
-        int held = -1;
         bool ok = true;
-        for (int c = c0 + group, n = group; c < c1; c += 2, n += 2) {
+        for (int c = c0 + group, n = group; c < c1 && quad < quads; c += 2, n += 2) {
             const int d = n % kSums, s = n % p.stages;
             ok = warp_wait(bar(kSumFull + d), (n / kSums) & 1u, abort_flag, p.status, 0xD70u | d) &&
                  warp_wait(bar(s), (n / p.stages) & 1u, abort_flag, p.status, 0xD80u | s);
             if (!ok) break;
             ptx::tc_fence_after_sync();
-            uint32_t v[2][32];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) ptx::tmem_ld_32x32(tmem + (static_cast<uint32_t>(quad * 32) << 16) + d * kBox + 32 * h, v[h]);
-            ptx::tmem_ld_wait();
-            ptx::tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(bar(kSumEmpty + d));
             const uint32_t at = ring + s * kStage + tile_row * 128;
             uint16_t *out = p.y + row * p.ldy + c * kBox;
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                const uint32_t place = at + ((static_cast<uint32_t>(q) ^ sw) << 4);
-                const uint4 old = ptx::lds128(place);
-                const uint32_t w[4] = {old.x, old.y, old.z, old.w};
-                uint32_t o[4];
+            for (int h = 0; h < 2; ++h) {
+                uint32_t v[32];
+                ptx::tmem_ld_32x32(tmem + (static_cast<uint32_t>(quad * 32) << 16) + d * kBox + 32 * h, v);
+                uint4 old[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float a = __uint_as_float(v[q >> 2][(q & 3) * 8 + 2 * e]), b = __uint_as_float(v[q >> 2][(q & 3) * 8 + 2 * e + 1]);
-                    o[e] = pack_bf16(fmaf(a, scale, qmath::bf16_lo(w[e])), fmaf(b, scale, qmath::bf16_hi(w[e])));
+                for (int q = 0; q < 4; ++q) old[q] = ptx::lds128(at + ((static_cast<uint32_t>(4 * h + q) ^ sw) << 4));
+                ptx::tmem_ld_wait();
+                if (h == 1) {
+                    ptx::tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(bar(kSumEmpty + d));
                 }
-                const uint4 now = make_uint4(o[0], o[1], o[2], o[3]);
-                if (whole) sts128(place, now);
-                else if (there && c * kBox + 8 * q < p.columns) *reinterpret_cast<uint4 *>(out + 8 * q) = now;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t w[4] = {old[q].x, old[q].y, old[q].z, old[q].w};
+                    uint32_t o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        o[e] = pack_bf16(fmaf(__uint_as_float(v[q * 8 + 2 * e]), scale, qmath::bf16_lo(w[e])),
+                                         fmaf(__uint_as_float(v[q * 8 + 2 * e + 1]), scale, qmath::bf16_hi(w[e])));
+                    const uint4 now = make_uint4(o[0], o[1], o[2], o[3]);
+                    if (whole) sts128(at + ((static_cast<uint32_t>(4 * h + q) ^ sw) << 4), now);
+                    else if (there && c * kBox + 32 * h + 8 * q < p.columns) *reinterpret_cast<uint4 *>(out + 32 * h + 8 * q) = now;
+                }
             }
             if (whole) {
                 ptx::fence_proxy_async_smem();
@@ -386,12 +410,9 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
                 if (lane == 0) {
                     ptx::tma_store_2d(&tm_out, c * kBox, item.row0 + quad * 32, ring + s * kStage + quad * 32 * 128);
                     ptx::tma_store_commit();
-                    if (held >= 0) {       // the store before this one has left its stage
-                        ptx::tma_store_wait_read<1>();
-                        ptx::mbar_arrive(bar(kMaxStages + held));
-                    }
+                    ptx::tma_store_wait_read<0>();
+                    ptx::mbar_arrive(bar(kMaxStages + s));
                 }
-                held = s;
             } else {
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(bar(kMaxStages + s));
@@ -441,13 +462,18 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
         }
         if (lane == 0) control.n_runs = n;
     }
-    begin_block<128>(control, 2 * kMaxStages + 1, [](int) { return 1; }, warp);
+    // full, empty: [stage]; sum full, sum empty: [accumulator]
+    constexpr int kSumFull = 2 * kMaxStages, kSumEmpty = kSumFull + 2, kSumColumns = 2 * kMaxRank;
+    begin_block<2 * kSumColumns>(control, kSumEmpty + 2, [](int i) { return i >= kSumEmpty ? 4 : 1; }, warp);
+    ptx::grid_launch_dependents();
     const uint32_t bars = ptx::smem_u32(control.bars), tmem = control.tmem, ring = ptx::smem_u32(smem) + kControl + kRunBytes;
     volatile uint32_t *abort_flag = &control.abort;
     const int n_runs = control.n_runs;
     auto full = [&](int s) { return bars + 8u * s; };
     auto empty = [&](int s) { return bars + 8u * (kMaxStages + s); };
-    const uint32_t done = bars + 8u * (2 * kMaxStages);
+    auto bar = [&](int i) { return bars + 8u * i; };
+    int steps = 0;                        // of 64 rows
+    for (int run = 0; run < n_runs; ++run) steps += (runs[run].y - runs[run].x + kStepRows - 1) / kStepRows;
     const int u_boxes = (2 * p.r + kBox - 1) / kBox, stage_bytes = (2 + u_boxes) * kFactorBox;
     if (warp == 0) {
         ptx::grid_dependency_wait();
@@ -473,6 +499,8 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
         bool ok = true;
         for (int run = 0; ok && run < n_runs; ++run) {
             for (int row = runs[run].x; row < runs[run].y; row += kStepRows, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
+                const int w = n / kWindow, d = w & 1;
+                if (n % kWindow == 0 && w >= 2 && !(ok = warp_wait(bar(kSumEmpty + d), ((w >> 1) - 1) & 1u, abort_flag, p.status, 0xDA8u | d))) break;
                 if (!(ok = warp_wait(full(s), (n / p.stages) & 1u, abort_flag, p.status, 0xDA0u | s))) break;
                 const uint32_t from = ring + s * stage_bytes;
                 const int rows = runs[run].y - row;
@@ -486,47 +514,54 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
                     ptx::tc_fence_after_sync();
 #pragma unroll
                     for (int i = 0; i < kStepRows / 16; ++i)
-                        ptx::mma_bf16(tmem, ptx::smem_desc_sw128_mn(from + i * 2048, kFactorBox, 1024),
-                                      ptx::smem_desc_sw128_mn(from + 2 * kFactorBox + i * 2048, kFactorBox, 1024), idesc, n > 0 || i > 0);
+                        ptx::mma_bf16(tmem + d * kSumColumns, ptx::smem_desc_sw128_mn(from + i * 2048, kFactorBox, 1024),
+                                      ptx::smem_desc_sw128_mn(from + 2 * kFactorBox + i * 2048, kFactorBox, 1024), idesc, n % kWindow > 0 || i > 0);
                     ptx::tc_commit(empty(s));
+                    if (n % kWindow == kWindow - 1 || n + 1 == steps) ptx::tc_commit(bar(kSumFull + d));
                 }
                 __syncwarp();
             }
         }
-        if (ok && n > 0 && ptx::elect_one()) ptx::tc_commit(done);
-        __syncwarp();
     } else {
         const int quad = warp & 3, c = column + quad * 32 + lane;
-        const bool any = n_runs > 0;
-        const bool ok = !any || warp_wait(done, 0, abort_flag, p.status, 0xDB0u);
-        ptx::tc_fence_after_sync();
+        const uint32_t lanes_at = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        float v[kMaxRank] = {};
+        bool ok = true;
+        for (int w = 0; w * kWindow < steps; ++w) {
+            const int d = w & 1;
+            if (!(ok = warp_wait(bar(kSumFull + d), (w >> 1) & 1u, abort_flag, p.status, 0xDB0u | d))) break;
+            ptx::tc_fence_after_sync();
+#pragma unroll
+            for (int j = 0; j < kMaxRank; j += 8) {
+                if (j >= p.r) continue;
+                uint32_t hi[8], lo[8];
+                ptx::tmem_ld_32x8(lanes_at + d * kSumColumns + j, hi);
+                ptx::tmem_ld_32x8(lanes_at + d * kSumColumns + p.r + j, lo);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[j + e] += __uint_as_float(hi[e]) + __uint_as_float(lo[e]);
+            }
+            ptx::tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(bar(kSumEmpty + d));
+        }
         const float scale = of_x ? 1.0f : __ldg(p.scaling + adapter);
         float *out = (of_x ? p.da : p.db) + slice * p.slice_floats;
-        if (ok) {
-            for (int j = 0; j < p.r; j += 8) {
-                uint32_t hi[8], lo[8];
-                float v[8];
-                if (any) {
-                    ptx::tmem_ld_32x8(tmem + (static_cast<uint32_t>(quad * 32) << 16) + j, hi);
-                    ptx::tmem_ld_32x8(tmem + (static_cast<uint32_t>(quad * 32) << 16) + p.r + j, lo);
-                    ptx::tmem_ld_wait();
-                }
+        if (ok && c < (of_x ? p.K : p.N)) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = any ? (__uint_as_float(hi[e]) + __uint_as_float(lo[e])) * scale : 0.0f;
+            for (int j = 0; j < kMaxRank; j += 4) {
+                if (j >= p.r) continue;
                 if (of_x) {
-                    if (c < p.K) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) out[(static_cast<int64_t>(adapter) * p.r + j + e) * p.K + c] = v[e];
-                    }
-                } else if (c < p.N) {
-                    float4 *to = reinterpret_cast<float4 *>(out + (static_cast<int64_t>(adapter) * p.N + c) * p.r + j);
-                    to[0] = make_float4(v[0], v[1], v[2], v[3]);
-                    to[1] = make_float4(v[4], v[5], v[6], v[7]);
+                    for (int e = 0; e < 4; ++e) out[(static_cast<int64_t>(adapter) * p.r + j + e) * p.K + c] = v[j + e];
+                } else {
+                    *reinterpret_cast<float4 *>(out + (static_cast<int64_t>(adapter) * p.N + c) * p.r + j) =
+                        make_float4(v[j] * scale, v[j + 1] * scale, v[j + 2] * scale, v[j + 3] * scale);
                 }
             }
         }
     }
-    end_block<128>(abort_flag, warp, tmem);
+    end_block<2 * kSumColumns>(abort_flag, warp, tmem);
 }
 
 // The row slices' sums, in order: dA's values, then dB's.
@@ -562,10 +597,16 @@ Plan plan_of(int64_t M, int64_t from, int64_t to, int64_t requests, int64_t adap
     if (splits < 1) splits = 1;
     p.shrink_per = static_cast<int>(ceil_div(p.shrink_tiles, splits));
     p.shrink_splits = static_cast<int>(ceil_div(p.shrink_tiles, p.shrink_per));
-    // the same, or four waves whose last one is short
+    // the number of slices with the least (waves + 1/2) (chunks of a block + 4): a block's way in and out is worth some four chunks, and half
+    // a wave stands for slots that stay empty at the end and behind short requests
     p.chunks = static_cast<int>(ceil_div(to, kBox));
-    int64_t slices = p.items <= kSlots / 2 ? kSlots / p.items : ceil_div(4 * kSlots, p.items);
-    if (slices > p.chunks) slices = p.chunks;
+    int64_t slices = 1;
+    double least = 0.0;
+    for (int64_t per = p.chunks; per >= 1; --per) {
+        const int64_t n = ceil_div(p.chunks, per);
+        const double waves = static_cast<double>(p.items * n) / kSlots, cost = ((waves < 1.0 ? 1.0 : waves) + 0.5) * static_cast<double>(per + 4);
+        if (per == p.chunks || cost < least) least = cost, slices = n;
+    }
     p.per_slice = static_cast<int>(ceil_div(p.chunks, slices));
     p.slices = static_cast<int>(ceil_div(p.chunks, p.per_slice));
     // gradients of the factors: `from` is dy's width, `to` that of x
