@@ -7,9 +7,10 @@
 //
 // HBM bound: the adapters' products are r / 2 operations a byte of x, y, dy, far below the tensor cores' rate.  Three kernels, each
 // of which streams one large operand through a ring of TMA stages once:
-//   shrink  t = x A^T (or dy B): 128 rows a block and a slice of the columns; FP32 partial sums to the workspace, one per slice
-//   expand  sums the slices, splits t into its parts, then walks 64 columns at a time: a stage brings the columns of y and the
-//           factor's rows, the product is added to y in the stage's own memory, and a TMA store takes it back
+//   shrink  t = x A^T (or dy B): 128 rows a cluster, whose blocks share the columns and add up their sums over one another's shared
+//           memory; leaves t's two parts
+//   expand  takes t as an operand and walks 64 columns at a time: a stage brings the columns of y and the factor's rows, the
+//           product is added to y in the stage's own memory, and a TMA store takes it back
 //   outer   dA and dB: 128 columns of x or dy by the 2r columns of dt or t, summed over an adapter's rows (both operands have the
 //           row as their second index: MN-major); row slices of one adapter are added up in order by a last small launch
 // Which rows and adapter a block has follows from the requests' offsets on the device: the host knows neither, the grid covers the most
@@ -33,6 +34,7 @@ constexpr int kRowBox = kRows * 128;     // bytes of a [128][64] box
 constexpr int kFactorBox = 64 * 128;     // bytes of a [64][64] box
 constexpr int kStage = kRowBox + kFactorBox;
 constexpr int kMaxStages = 8;
+constexpr int kMaxCluster = 8;
 constexpr int kSlots = 296;              // blocks that are resident at once: two on each of 148 SMs
 
 struct Requests {
@@ -145,12 +147,18 @@ constexpr int kWindow = 8;
 // ------------------------------------------------------------------------------------------------ shrink
 struct Shrink {
     Requests q;
-    float *partials;          // [splits][rows][r]
+    const float *scaling;     // [adapters]; null: t as it is
+    uint16_t *parts;          // [rows][2 r]: t's high and low parts
     uint32_t *status;
     int r, r16;               // rank, and the next multiple of 16
     int tiles, per_split;     // 64-column tiles of the long side, and those of a block
-    int splits, stages;
+    int splits, stages;       // blocks of a cluster, which share the long side
 };
+__device__ __forceinline__ float4 ld_cluster(uint32_t cluster_addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+    return v;
+}
 
 // kFlip: the factor is [long side][r] (dy B: B is [N][r]) and not [r][long side].
 template <bool kFlip>
@@ -214,7 +222,7 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         }
         __syncwarp();
     } else {
-        const int quad = warp & 3, row = item.row0 + quad * 32 + lane;
+        const int quad = warp & 3;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         float sum[kMaxRank] = {};
         bool ok = true;
@@ -235,28 +243,52 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(bar(kSumEmpty + d));
         }
-        float *out = p.partials + (static_cast<int64_t>(split) * p.q.rows + row) * p.r;
+        // this slice's sums, for the cluster: rows of r floats and four that keep them off one another's banks, where the ring was
         const float nan = __uint_as_float(0x7FC00000u);       // what reads a sum that is not whole shall not take it for a result
+        float *mine = reinterpret_cast<float *>(smem + kControl) + (quad * 32 + lane) * (p.r + 4);
 #pragma unroll
         for (int c = 0; c < kMaxRank; c += 4) {
-            if (c < p.r && row < item.end)
-                *reinterpret_cast<float4 *>(out + c) = ok ? make_float4(sum[c], sum[c + 1], sum[c + 2], sum[c + 3]) : make_float4(nan, nan, nan, nan);
+            if (c < p.r)
+                *reinterpret_cast<float4 *>(mine + c) = ok ? make_float4(sum[c], sum[c + 1], sum[c + 2], sum[c + 3]) : make_float4(nan, nan, nan, nan);
         }
     }
+    __syncwarp();
+    ptx::cluster_sync();
+    // every block adds up its share of the rows' pieces of eight columns, slice after slice, and writes both parts
+    const float factor = p.scaling != nullptr ? __ldg(p.scaling + item.adapter) : 1.0f;
+    const int pieces = p.r >> 3, rows_here = min(kRows, item.end - item.row0);
+    for (int i = split + p.splits * threadIdx.x; i < rows_here * pieces; i += p.splits * blockDim.x) {
+        const int r = i / pieces, c = 8 * (i - r * pieces);
+        float t[8] = {};
+        for (int s = 0; s < p.splits; ++s) {
+            const uint32_t from = ptx::map_to_cta(ring + 4 * (r * (p.r + 4) + c), s);
+            const float4 a = ld_cluster(from), b = ld_cluster(from + 16);
+            t[0] += a.x, t[1] += a.y, t[2] += a.z, t[3] += a.w, t[4] += b.x, t[5] += b.y, t[6] += b.z, t[7] += b.w;
+        }
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = t[2 * e] * factor, b = t[2 * e + 1] * factor;
+            hi[e] = pack_bf16(a, b);
+            lo[e] = pack_bf16(a - qmath::bf16_lo(hi[e]), b - qmath::bf16_hi(hi[e]));
+        }
+        uint16_t *out = p.parts + static_cast<int64_t>(item.row0 + r) * 2 * p.r + c;
+        *reinterpret_cast<uint4 *>(out) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4 *>(out + p.r) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    ptx::cluster_sync();                   // nobody leaves while others read its memory
     end_block<128>(abort_flag, warp, tmem);
 }
 
 // ------------------------------------------------------------------------------------------------ expand
 struct Expand {
     Requests q;
-    const float *partials;    // [splits][rows][r]
-    const float *scaling;     // [adapters]
-    uint16_t *parts;          // [rows][2 r]: t's high and low parts, or null
+    const uint16_t *parts;    // [rows][2 r]: t's high and low parts
+    const float *scaling;     // [adapters]; null: it is on t already
     uint16_t *y;
     uint32_t *status;
     int64_t ldy;
-    int r, r16, splits, stages;
-    int scale_t;              // the adapter's factor goes on t (gradients) and not on the product
+    int r, r16, stages;
     int columns, chunks, per_slice, slices;    // 64-column chunks of y, and those of a block
 };
 
@@ -307,7 +339,7 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (ptx::elect_one() && c0 < c1) {
+        if (ptx::elect_one()) {
             const uint32_t idesc = idesc_of(kBox, false, kFlip);
             const int half = p.r16 >> 4;          // products for each of t's parts
             bool ok = wait_bounded(bar(kReady), 0, abort_flag, p.status, 0xD40u);
@@ -331,43 +363,28 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
         const int group = (warp - 2) >> 2, quad = warp & 3;
         const int tile_row = quad * 32 + lane, row = item.row0 + tile_row;
         const bool there = row < item.end;
-        const float factor = __ldg(p.scaling + item.adapter);
+        const float scale = p.scaling != nullptr ? __ldg(p.scaling + item.adapter) : 1.0f;
         const uint32_t sw = static_cast<uint32_t>(tile_row & 7);
         ptx::grid_dependency_wait();
-        // t: the slices in order, eight columns at a time (the two groups take turns), both parts into the operand
-        for (int c = 8 * group; c < p.r16; c += 16) {
-            float t[8] = {};
-            if (there && c < p.r) {
-#pragma unroll 4
-                for (int s = 0; s < p.splits; ++s) {
-                    const float4 *from = reinterpret_cast<const float4 *>(p.partials + (static_cast<int64_t>(s) * p.q.rows + row) * p.r + c);
-                    const float4 a = __ldcg(from), b = __ldcg(from + 1);
-                    t[0] += a.x, t[1] += a.y, t[2] += a.z, t[3] += a.w, t[4] += b.x, t[5] += b.y, t[6] += b.z, t[7] += b.w;
-                }
-            }
-            uint32_t hi[4], lo[4];
+        // t's parts into the operand, each on a multiple of 16 columns, zeros where there is nothing; the two groups take turns
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float a = t[2 * e], b = t[2 * e + 1];
-                if (p.scale_t) a *= factor, b *= factor;
-                hi[e] = pack_bf16(a, b);
-                lo[e] = pack_bf16(a - qmath::bf16_lo(hi[e]), b - qmath::bf16_hi(hi[e]));
+        for (int k = 0; k < kMaxRank / 16; ++k) {
+            const int c = 8 * group + 16 * k;
+            if (c >= p.r16) continue;
+            uint4 h = make_uint4(0, 0, 0, 0), l = h;
+            if (there && c < p.r) {
+                const uint16_t *from = p.parts + static_cast<int64_t>(row) * 2 * p.r + c;
+                h = __ldcg(reinterpret_cast<const uint4 *>(from));
+                l = __ldcg(reinterpret_cast<const uint4 *>(from + p.r));
             }
-            const uint4 h = make_uint4(hi[0], hi[1], hi[2], hi[3]), l = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             const int ch = c >> 3, cl = (c + p.r16) >> 3;       // 16-byte pieces of the operand's row
             sts128(sT + (ch >> 3) * kRowBox + tile_row * 128 + ((static_cast<uint32_t>(ch & 7) ^ sw) << 4), h);
             sts128(sT + (cl >> 3) * kRowBox + tile_row * 128 + ((static_cast<uint32_t>(cl & 7) ^ sw) << 4), l);
-            if (p.parts != nullptr && slice == 0 && there && c < p.r) {
-                uint16_t *out = p.parts + static_cast<int64_t>(row) * 2 * p.r + c;
-                *reinterpret_cast<uint4 *>(out) = h;
-                *reinterpret_cast<uint4 *>(out + p.r) = l;
-            }
         }
         ptx::fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(bar(kReady));
         // chunks of 64 columns, the two groups in turn
-        const float scale = p.scale_t ? 1.0f : factor;
         const bool whole = item.row0 + quad * 32 + 32 <= item.end;         // all of this warp's rows are the request's
         bool ok = true;
         for (int c = c0 + group, n = group; c < c1 && quad < quads; c += 2, n += 2) {
@@ -568,6 +585,7 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
 __global__ void __launch_bounds__(256)
 add_slices(const float4 *__restrict__ from, int64_t slice4, int slices, int64_t da4, float4 *da, float4 *db) {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    ptx::grid_launch_dependents();
     ptx::grid_dependency_wait();
     if (i >= slice4) return;
     float4 v = __ldcg(from + i);
@@ -583,20 +601,12 @@ add_slices(const float4 *__restrict__ from, int64_t slice4, int slices, int64_t 
 // How a call's work is shared out: from its sizes alone, so that the workspace's size follows from them too.
 struct Plan {
     int64_t items;                         // tiles of rows, at most
-    int shrink_tiles, shrink_splits, shrink_per;
     int chunks, slices, per_slice;         // of expand
     int outer_tiles, outer_tiles_x, outer_slices;
 };
 Plan plan_of(int64_t M, int64_t from, int64_t to, int64_t requests, int64_t adapters) {     // shrink over `from` columns, expand to `to`
     Plan p;
     p.items = ceil_div(M, kRows) + requests;
-    // one wave of blocks where the tiles alone do not fill it, none with fewer than four stages
-    p.shrink_tiles = static_cast<int>(ceil_div(from, kBox));
-    int64_t splits = p.items < kSlots ? kSlots / p.items : 1;
-    if (splits > p.shrink_tiles / 4) splits = p.shrink_tiles / 4;
-    if (splits < 1) splits = 1;
-    p.shrink_per = static_cast<int>(ceil_div(p.shrink_tiles, splits));
-    p.shrink_splits = static_cast<int>(ceil_div(p.shrink_tiles, p.shrink_per));
     // the number of slices with the least (waves + 1/2) (chunks of a block + 4): a block's way in and out is worth some four chunks, and half
     // a wave stands for slots that stay empty at the end and behind short requests
     p.chunks = static_cast<int>(ceil_div(to, kBox));
@@ -618,28 +628,38 @@ Plan plan_of(int64_t M, int64_t from, int64_t to, int64_t requests, int64_t adap
     return p;
 }
 int64_t pad256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-int64_t partial_bytes(const Plan &p, int64_t M, int64_t r) { return pad256(4 * p.shrink_splits * M * r); }
 int64_t parts_bytes(int64_t M, int64_t r) { return pad256(4 * M * r); }
 
-sol_status_t configure(const void *kern, int smem) {
+// Allows kernel `kern` `smem` bytes of dynamic shared memory on the current device (asked for once).
+template <auto kern>
+bool allow_smem(int smem) {
+    static bool done[64] = {};
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+    if (done[dev]) return true;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
         cudaGetLastError();
-        return SOL_ERR_CUDA;
+        return false;
     }
-    return SOL_OK;
+    return done[dev] = true;
 }
-template <class... P, class... A>
-sol_status_t launch_after(void (*kern)(P...), int64_t grid, int threads, int smem, cudaStream_t stream, A... args) {
+// kAfter: the kernel may come into the SMs while the one in front of it drains, and waits itself for what that one writes.
+template <bool kAfter, class... P, class... A>
+sol_status_t launch(void (*kern)(P...), int64_t grid, int threads, int smem, int cluster, cudaStream_t stream, A... args) {
+    if (grid > 0x7FFFFFFFLL) return SOL_ERR_BAD_SHAPE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = kAfter ? 2 : 1;
     if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) {
         cudaGetLastError();
         return SOL_ERR_CUDA;
@@ -654,41 +674,64 @@ bool factor_map(CUtensorMap *out, const void *base, int64_t cols, int64_t rows, 
     return make_tmap_3d_bf16(out, base, cols, rows, adapters, 2 * cols, 2 * cols * rows, kBox, box_rows);
 }
 
+constexpr int kShrinkStages = 4;
 constexpr int kHalfSmem = 115712, kFullSmem = 232448;     // two blocks an SM, or one
 
+// Blocks that share the long side: as many as leave all clusters resident at once (clusters of some sizes fit the GPU's SM groups worse than
+// others: a second wave for one more block costs twice the time), none with fewer than four stages.
 template <bool kFlip>
-sol_status_t launch_shrink(const Requests &q, const void *x, int64_t ldx, const void *factor, int64_t cols, int64_t r, const Plan &plan, float *partials,
-                           cudaStream_t stream) {
-    const int r16 = static_cast<int>(ceil_div(r, 16) * 16);
+int shrink_splits(int64_t items, int tiles, int smem) {
+    static int resident[kMaxCluster + 1] = {};
+    for (int n = kMaxCluster; n > 1; --n) {
+        if (n > tiles / 4) continue;
+        if (resident[n] == 0) {
+            cudaLaunchConfig_t cfg{};
+            cfg.gridDim = dim3(n * 1024);
+            cfg.blockDim = dim3(192);
+            cfg.dynamicSmemBytes = smem;
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = n;
+            attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&resident[n], shrink_kernel<kFlip>, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                resident[n] = 0;
+                continue;
+            }
+        }
+        if (items <= resident[n]) return n;
+    }
+    return 1;
+}
+template <bool kFlip>
+sol_status_t launch_shrink(const Requests &q, const void *x, int64_t ldx, const void *factor, int64_t cols, int64_t r, const Plan &plan,
+                           const float *scaling, void *parts, cudaStream_t stream) {
+    const int r16 = static_cast<int>(ceil_div(r, 16) * 16), tiles = static_cast<int>(ceil_div(cols, kBox)), smem = kControl + kShrinkStages * kStage;
     CUtensorMap tm_x, tm_f;
     if (!rows_map(&tm_x, x, cols, q.rows, ldx, kRows)) return SOL_ERR_CUDA;
     if (!(kFlip ? factor_map(&tm_f, factor, r, cols, q.adapters, kBox) : factor_map(&tm_f, factor, cols, r, q.adapters, r16))) return SOL_ERR_CUDA;
-    Shrink p{q, partials, device_status_word(), static_cast<int>(r), r16, plan.shrink_tiles, plan.shrink_per, plan.shrink_splits, (kHalfSmem - kControl) / kStage};
-    const sol_status_t st = configure(reinterpret_cast<const void *>(shrink_kernel<kFlip>), kControl + p.stages * kStage);
-    if (st != SOL_OK) return st;
-    shrink_kernel<kFlip><<<static_cast<unsigned>(plan.items * plan.shrink_splits), 192, kControl + p.stages * kStage, stream>>>(tm_x, tm_f, p);
-    return launch_status();
+    if (!allow_smem<shrink_kernel<kFlip>>(smem)) return SOL_ERR_CUDA;
+    const int per = static_cast<int>(ceil_div(tiles, shrink_splits<kFlip>(plan.items, tiles, smem))), splits = static_cast<int>(ceil_div(tiles, per));
+    const Shrink p{q, scaling, static_cast<uint16_t *>(parts), device_status_word(), static_cast<int>(r), r16, tiles, per, splits, kShrinkStages};
+    return launch<false>(shrink_kernel<kFlip>, plan.items * splits, 192, smem, splits, stream, tm_x, tm_f, p);
 }
-// y null: t's parts only
 template <bool kFlip>
-sol_status_t launch_expand(const Requests &q, const float *partials, const float *scaling, bool scale_t, void *parts, void *y, int64_t ldy,
-                           const void *factor, int64_t cols, int64_t r, const Plan &plan, cudaStream_t stream) {
+sol_status_t launch_expand(const Requests &q, const void *parts, const float *scaling, void *y, int64_t ldy, const void *factor, int64_t cols, int64_t r,
+                           const Plan &plan, cudaStream_t stream) {
     const int r16 = static_cast<int>(ceil_div(r, 16) * 16);
-    CUtensorMap tm_y{}, tm_out{}, tm_f{};
-    if (y != nullptr) {
-        if (!rows_map(&tm_y, y, cols, q.rows, ldy, kRows) || !rows_map(&tm_out, y, cols, q.rows, ldy, 32)) return SOL_ERR_CUDA;
-        if (!(kFlip ? factor_map(&tm_f, factor, cols, r, q.adapters, r16) : factor_map(&tm_f, factor, r, cols, q.adapters, kBox))) return SOL_ERR_CUDA;
-    }
+    CUtensorMap tm_y, tm_out, tm_f;
+    if (!rows_map(&tm_y, y, cols, q.rows, ldy, kRows) || !rows_map(&tm_out, y, cols, q.rows, ldy, 32)) return SOL_ERR_CUDA;
+    if (!(kFlip ? factor_map(&tm_f, factor, cols, r, q.adapters, r16) : factor_map(&tm_f, factor, r, cols, q.adapters, kBox))) return SOL_ERR_CUDA;
     const int t_bytes = static_cast<int>(ceil_div(2 * r16, kBox)) * kRowBox;
-    Expand p{q, partials, scaling, static_cast<uint16_t *>(parts), static_cast<uint16_t *>(y), device_status_word(), ldy, static_cast<int>(r), r16,
-             plan.shrink_splits, 0, scale_t, static_cast<int>(cols), y != nullptr ? plan.chunks : 0, plan.per_slice, y != nullptr ? plan.slices : 1};
-    // two blocks an SM with four stages up to rank 32, one with seven beyond
+    Expand p{q, static_cast<const uint16_t *>(parts), scaling, static_cast<uint16_t *>(y), device_status_word(), ldy, static_cast<int>(r), r16,
+             0, static_cast<int>(cols), plan.chunks, plan.per_slice, plan.slices};
+    // two blocks an SM with four stages up to rank 32, one with eight beyond
     p.stages = ((t_bytes == kRowBox ? kHalfSmem : kFullSmem) - kControl - t_bytes) / kStage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
-    const int smem = kControl + t_bytes + p.stages * kStage;
-    const sol_status_t st = configure(reinterpret_cast<const void *>(expand_kernel<kFlip>), smem);
-    if (st != SOL_OK) return st;
-    return launch_after(expand_kernel<kFlip>, plan.items * p.slices, 320, smem, stream, tm_y, tm_out, tm_f, p);
+    if (!allow_smem<expand_kernel<kFlip>>(kFullSmem)) return SOL_ERR_CUDA;
+    return launch<true>(expand_kernel<kFlip>, plan.items * p.slices, 320, kControl + t_bytes + p.stages * kStage, 1, stream, tm_y, tm_out, tm_f, p);
 }
 
 }  // namespace
@@ -697,32 +740,29 @@ int max_rank() { return kMaxRank; }
 int max_requests() { return kMaxRequests; }
 
 size_t workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, bool backward) {
-    if (!backward) return static_cast<size_t>(partial_bytes(plan_of(M, K, N, requests, adapters), M, r));
+    if (!backward) return static_cast<size_t>(parts_bytes(M, r));
     const Plan p = plan_of(M, N, K, requests, adapters);
-    return static_cast<size_t>(partial_bytes(p, M, r) + parts_bytes(M, r) + (p.outer_slices > 1 ? 4 * p.outer_slices * adapters * r * (K + N) : 0));
+    return static_cast<size_t>(parts_bytes(M, r) + (p.outer_slices > 1 ? 4 * p.outer_slices * adapters * r * (K + N) : 0));
 }
 
 sol_status_t launch_apply(const Call &c, const void *x, int64_t ldx, void *y, int64_t ldy, void *t_out, void *workspace, cudaStream_t stream) {
     const Requests q{c.offsets, c.ids, static_cast<int>(c.requests), static_cast<int>(c.adapters), static_cast<int>(c.M)};
     const Plan plan = plan_of(c.M, c.K, c.N, c.requests, c.adapters);
-    float *partials = static_cast<float *>(workspace);
-    const sol_status_t st = launch_shrink<false>(q, x, ldx, c.a, c.K, c.r, plan, partials, stream);
+    void *parts = t_out != nullptr ? t_out : workspace;
+    const sol_status_t st = launch_shrink<false>(q, x, ldx, c.a, c.K, c.r, plan, nullptr, parts, stream);
     if (st != SOL_OK) return st;
-    return launch_expand<false>(q, partials, c.scaling, false, t_out, y, ldy, c.b, c.N, c.r, plan, stream);
+    return launch_expand<false>(q, parts, c.scaling, y, ldy, c.b, c.N, c.r, plan, stream);
 }
 
 sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, const void *t, void *dx, int64_t ld_dx,
                              float *da, float *db, void *workspace, cudaStream_t stream) {
     const Requests q{c.offsets, c.ids, static_cast<int>(c.requests), static_cast<int>(c.adapters), static_cast<int>(c.M)};
     const Plan plan = plan_of(c.M, c.N, c.K, c.requests, c.adapters);
-    uint8_t *ws = static_cast<uint8_t *>(workspace);
-    float *partials = reinterpret_cast<float *>(ws);
-    void *dt = ws + partial_bytes(plan, c.M, c.r);
-    float *sums = reinterpret_cast<float *>(ws + partial_bytes(plan, c.M, c.r) + parts_bytes(c.M, c.r));
-    sol_status_t st = launch_shrink<true>(q, dy, ld_dy, c.b, c.N, c.r, plan, partials, stream);
+    uint8_t *dt = static_cast<uint8_t *>(workspace);
+    float *sums = reinterpret_cast<float *>(dt + parts_bytes(c.M, c.r));
+    sol_status_t st = launch_shrink<true>(q, dy, ld_dy, c.b, c.N, c.r, plan, c.scaling, dt, stream);
     if (st != SOL_OK) return st;
-    st = launch_expand<true>(q, partials, c.scaling, true, dt, dx, ld_dx, c.a, c.K, c.r, plan, stream);
-    if (st != SOL_OK) return st;
+    // the factors' gradients next, while L2 still holds a part of dy
     CUtensorMap tm_x, tm_dy, tm_dt, tm_t;
     if (!rows_map(&tm_x, x, c.K, c.M, ldx, kStepRows) || !rows_map(&tm_dy, dy, c.N, c.M, ld_dy, kStepRows) ||
         !rows_map(&tm_dt, dt, 2 * c.r, c.M, 2 * c.r, kStepRows) || !rows_map(&tm_t, t, 2 * c.r, c.M, 2 * c.r, kStepRows))
@@ -733,14 +773,17 @@ sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const
             static_cast<int>(c.K), static_cast<int>(c.N), plan.outer_tiles_x, plan.outer_tiles, plan.outer_slices, 0};
     const int stage = outer_stage(static_cast<int>(ceil_div(2 * c.r, kBox)));
     p.stages = (kHalfSmem - kControl - kRunBytes) / stage;
-    const int smem = kControl + kRunBytes + p.stages * stage;
-    st = configure(reinterpret_cast<const void *>(outer_kernel), smem);
+    if (!allow_smem<outer_kernel>(kHalfSmem)) return SOL_ERR_CUDA;
+    st = launch<true>(outer_kernel, static_cast<int64_t>(plan.outer_tiles) * plan.outer_slices * c.adapters, 192, kControl + kRunBytes + p.stages * stage, 1,
+                      stream, tm_x, tm_dy, tm_dt, tm_t, p);
     if (st != SOL_OK) return st;
-    st = launch_after(outer_kernel, static_cast<int64_t>(plan.outer_tiles) * plan.outer_slices * c.adapters, 192, smem, stream, tm_x, tm_dy, tm_dt, tm_t, p);
-    if (st != SOL_OK || !sliced) return st;
-    const int64_t slice4 = (da_floats + db_floats) / 4;
-    return launch_after(add_slices, ceil_div(slice4, 256), 256, 0, stream, reinterpret_cast<const float4 *>(sums), slice4, plan.outer_slices,
-                        da_floats / 4, reinterpret_cast<float4 *>(da), reinterpret_cast<float4 *>(db));
+    if (sliced) {
+        const int64_t slice4 = (da_floats + db_floats) / 4;
+        st = launch<true>(add_slices, ceil_div(slice4, 256), 256, 0, 1, stream, reinterpret_cast<const float4 *>(sums), slice4, plan.outer_slices,
+                          da_floats / 4, reinterpret_cast<float4 *>(da), reinterpret_cast<float4 *>(db));
+        if (st != SOL_OK) return st;
+    }
+    return dx != nullptr ? launch_expand<true>(q, dt, nullptr, dx, ld_dx, c.a, c.K, c.r, plan, stream) : SOL_OK;
 }
 
 }  // namespace lora
