@@ -45,7 +45,7 @@ struct Hyper {
     long long *state;                          // [0] steps done, [1] tickets
     uint64_t seed;
     uint32_t first_tensor, chunks;
-    int count, stochastic, advance, tiny_eps;
+    int count, advance, tiny_eps;
 };
 template <int kN>
 struct Table {
@@ -152,8 +152,8 @@ __device__ __forceinline__ bool finite_bits(uint32_t b) { return (b & 0x7F800000
 // By chance: y scaled down so that its FP32 bits are the code's, further down (exact but for subnormal codes, where what lies below
 // 2^-kDrop of a step is rounded), plus the noise's 16 bits below the code's, in the middle of what they leave open.  `odd`: some value
 // of the warp is not finite; such values become NaN and do not count for the block.
-template <int kMantissa>
-__device__ __forceinline__ uint2 encode(const float (&f)[kVec], uint32_t &e, const uint32_t (&noise)[kVec], bool stochastic, bool odd) {
+template <int kMantissa, bool kChance>
+__device__ __forceinline__ uint2 encode(const float (&f)[kVec], uint32_t &e, const uint32_t (&noise)[kVec], bool odd) {
     using F = Format<kMantissa>;
     float most = 0.0f;
     if (!odd) {
@@ -167,7 +167,7 @@ __device__ __forceinline__ uint2 encode(const float (&f)[kVec], uint32_t &e, con
     most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
     e = max(__float_as_uint(most) >> 23, F::kTop + 1u) - F::kTop;
     uint32_t c[kVec];                      // the code in the uppermost byte
-    if (stochastic) {
+    if constexpr (kChance) {
         // 2^(127 - e) and the format's 2^-120 (2^-112) in one factor where FP32 has it
         constexpr uint32_t kOne = kMantissa == 3 ? 134u : 142u;
         if (__all_sync(0xFFFFFFFFu, e < kOne)) {
@@ -212,13 +212,13 @@ __device__ __forceinline__ uint2 encode(const float (&f)[kVec], uint32_t &e, con
     return make_uint2(w[0], w[1]);
 }
 
-template <int kN, bool kP16, bool kG16, bool k8>
+template <int kN, bool kP16, bool kG16, bool k8, bool kChance>
 __global__ void __launch_bounds__(kThreads, 4)
 step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyper h) {
     using P = typename std::conditional<kP16, uint16_t, float>::type;
     using G = typename std::conditional<kG16, uint16_t, float>::type;
     using S = typename std::conditional<k8, uint8_t, float>::type;
-    constexpr bool kNoise = kP16 || k8;
+    constexpr bool kNoise = (kP16 || k8) && kChance, kOdd = kP16 || k8;
     __shared__ float coefficients[3];      // 1 - lr decay, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
     __shared__ uint32_t hash;              // of seed and step
     __shared__ uint16_t of_chunk[kThreads];
@@ -328,7 +328,7 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
                 unpack<false>(v, raw.v);
             }
             uint32_t noise[kVec] = {};
-            if (kNoise && h.stochastic) {
+            if (kNoise) {
                 uint32_t base = mix_word(hash, h.first_tensor + lo);
                 if (i0 >> 32) base = mix(base ^ static_cast<uint32_t>(i0 >> 32));
                 base ^= static_cast<uint32_t>(i0);
@@ -372,9 +372,9 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
                 if (k8) largest = max(largest, __float_as_uint(v[i]));         // a square's bits, or a NaN's of either sign
                 if (kP16) largest = max(largest, __float_as_uint(p[i]) & 0x7FFFFFFFu);
             }
-            const bool odd = kNoise && __any_sync(0xFFFFFFFFu, largest >= 0x7F800000u);
+            const bool odd = kOdd && __any_sync(0xFFFFFFFFu, largest >= 0x7F800000u);
             uint32_t packed_p[kVec / 2];
-            if (kP16 && h.stochastic) {
+            if (kP16 && kChance) {
                 uint32_t b[kVec];
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) b[i] = __float_as_uint(p[i]) + (noise[i] * 0x9E3779B1u >> 16);
@@ -395,8 +395,8 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
                     for (int i = 0; i < kVec; ++i)
                         if (i >= left) m[i] = v[i] = 0.0f;        // behind the end: nothing that counts for the block
                 }
-                cm = encode<3>(m, em, noise, h.stochastic, odd);
-                cv = encode<2>(v, ev, noise, h.stochastic, odd);
+                cm = encode<3, kChance>(m, em, noise, odd);
+                cv = encode<2, kChance>(v, ev, noise, odd);
                 if (left > 0 && (threadIdx.x & 3) == 0) {
                     static_cast<uint8_t *>(t.m_scale)[i0 >> 5] = static_cast<uint8_t>(em);
                     static_cast<uint8_t *>(t.v_scale)[i0 >> 5] = static_cast<uint8_t>(ev);
@@ -437,7 +437,7 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
     }
 }
 
-template <int kN, bool kP16, bool kG16, bool k8>
+template <int kN, bool kP16, bool kG16, bool k8, bool kChance>
 sol_status_t launch_table(const Tensor *tensors, Hyper h, cudaStream_t stream, const DeviceInfo *dev) {
     Table<kN> table;
     uint64_t chunks = 0;
@@ -451,25 +451,25 @@ sol_status_t launch_table(const Tensor *tensors, Hyper h, cudaStream_t stream, c
     for (int i = h.count; i < kN; ++i) table.t[i] = Tensor{};
     h.chunks = static_cast<uint32_t>(chunks);
     static int resident = 0;
-    if (resident == 0 && cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, step_kernel<kN, kP16, kG16, k8>, kThreads, 0) != cudaSuccess) {
+    if (resident == 0 && cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, step_kernel<kN, kP16, kG16, k8, kChance>, kThreads, 0) != cudaSuccess) {
         cudaGetLastError();
         return SOL_ERR_CUDA;
     }
     const int64_t most = static_cast<int64_t>(resident) * dev->sm_count;
     const int64_t grid = static_cast<int64_t>(chunks) < most ? static_cast<int64_t>(chunks) : most;
-    step_kernel<kN, kP16, kG16, k8><<<static_cast<unsigned>(grid < 1 ? 1 : grid), kThreads, 0, stream>>>(table, h);
+    step_kernel<kN, kP16, kG16, k8, kChance><<<static_cast<unsigned>(grid < 1 ? 1 : grid), kThreads, 0, stream>>>(table, h);
     return launch_status();
 }
 
-template <bool kP16, bool kG16, bool k8>
+template <bool kP16, bool kG16, bool k8, bool kChance>
 sol_status_t launch_all(const Tensor *tensors, int64_t count, Hyper h, cudaStream_t stream, const DeviceInfo *dev) {
     int64_t first = 0;
     do {
         h.first_tensor = static_cast<uint32_t>(first);
         h.count = static_cast<int>(count - first < kTable ? count - first : kTable);
         h.advance = first + h.count == count;
-        const sol_status_t st = h.count <= kSmallTable ? launch_table<kSmallTable, kP16, kG16, k8>(tensors + first, h, stream, dev)
-                                                       : launch_table<kTable, kP16, kG16, k8>(tensors + first, h, stream, dev);
+        const sol_status_t st = h.count <= kSmallTable ? launch_table<kSmallTable, kP16, kG16, k8, kChance>(tensors + first, h, stream, dev)
+                                                       : launch_table<kTable, kP16, kG16, k8, kChance>(tensors + first, h, stream, dev);
         if (st != SOL_OK) return st;
         first += h.count;
     } while (first < count);
@@ -488,14 +488,18 @@ sol_status_t launch_step(const Tensor *tensors, int64_t count, const sol_adamw_o
     h.tiny_eps = o.eps < 1e-12;              // the root of what FP32 flushes to 0 is below 2^-63
     h.lr_scale = o.lr_scale, h.grad_scale = o.grad_scale;
     h.state = reinterpret_cast<long long *>(state);
-    h.seed = o.seed, h.stochastic = o.stochastic != 0;
-    const bool e = o.state_bits == 8;
-    if (o.param_bf16) {
-        if (o.grad_bf16) return e ? launch_all<true, true, true>(tensors, count, h, stream, dev) : launch_all<true, true, false>(tensors, count, h, stream, dev);
-        return e ? launch_all<true, false, true>(tensors, count, h, stream, dev) : launch_all<true, false, false>(tensors, count, h, stream, dev);
-    }
-    if (o.grad_bf16) return e ? launch_all<false, true, true>(tensors, count, h, stream, dev) : launch_all<false, true, false>(tensors, count, h, stream, dev);
-    return e ? launch_all<false, false, true>(tensors, count, h, stream, dev) : launch_all<false, false, false>(tensors, count, h, stream, dev);
+    h.seed = o.seed;
+    auto all = [&](auto p16, auto g16, auto e8, auto chance) {
+        // rounding by chance is for what is held in fewer bits
+        constexpr bool kChance = decltype(chance)::value && (decltype(p16)::value || decltype(e8)::value);
+        return launch_all<decltype(p16)::value, decltype(g16)::value, decltype(e8)::value, kChance>(tensors, count, h, stream, dev);
+    };
+    auto pick = [](bool v, auto next) { return v ? next(std::true_type{}) : next(std::false_type{}); };
+    return pick(o.param_bf16 != 0, [&](auto p16) {
+        return pick(o.grad_bf16 != 0, [&](auto g16) {
+            return pick(o.state_bits == 8, [&](auto e8) { return pick(o.stochastic != 0, [&](auto chance) { return all(p16, g16, e8, chance); }); });
+        });
+    });
 }
 
 }  // namespace adamw

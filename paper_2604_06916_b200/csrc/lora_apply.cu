@@ -34,6 +34,7 @@ constexpr int kRowBox = kRows * 128;     // bytes of a [128][64] box
 constexpr int kFactorBox = 64 * 128;     // bytes of a [64][64] box
 constexpr int kStage = kRowBox + kFactorBox;
 constexpr int kMaxStages = 8;
+constexpr int kShrinkStage = 2 * kStage;    // 128 columns: rows of 256 bytes, which DRAM gives faster than twice 128
 constexpr int kMaxCluster = 8;
 constexpr int kSlots = 296;              // blocks that are resident at once: two on each of 148 SMs
 
@@ -141,8 +142,9 @@ __device__ __forceinline__ void end_block(volatile uint32_t *abort_flag, int war
 }
 
 // The tensor core adds to an FP32 sum with truncation, 2^-25 of it a step on average and always towards zero: a sum is taken out after so
-// many stages of 64 (32 steps, 2^-20) and goes on in a register, where additions are rounded.
-constexpr int kWindow = 8;
+// many stages (32 steps, 2^-20) and goes on in a register, where additions are rounded.
+constexpr int kWindow = 8;               // of 64 rows
+constexpr int kShrinkWindow = 4;         // of 128 columns
 
 // ------------------------------------------------------------------------------------------------ shrink
 struct Shrink {
@@ -151,7 +153,7 @@ struct Shrink {
     uint16_t *parts;          // [rows][2 r]: t's high and low parts
     uint32_t *status;
     int r, r16;               // rank, and the next multiple of 16
-    int tiles, per_split;     // 64-column tiles of the long side, and those of a block
+    int tiles, per_split;     // 128-column tiles of the long side, and those of a block
     int splits, stages;       // blocks of a cluster, which share the long side
 };
 __device__ __forceinline__ float4 ld_cluster(uint32_t cluster_addr) {
@@ -162,7 +164,7 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t cluster_addr) {
 
 // kFlip: the factor is [long side][r] (dy B: B is [N][r]) and not [r][long side].
 template <bool kFlip>
-__global__ void __launch_bounds__(192, 2)
+__global__ void __launch_bounds__(192)
 shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_f, const Shrink p) {
     extern __shared__ __align__(1024) uint8_t smem[];
     if (!aligned_block(smem, p.status)) return;
@@ -192,11 +194,16 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const uint32_t factor_bytes = kFlip ? kFactorBox : p.r16 * 128;
             for (int t = t0, s = 0, n = 0; t < t1; ++t, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
                 if (n >= p.stages && !wait_bounded(empty(s), ((n / p.stages) - 1) & 1u, abort_flag, p.status, 0xD00u | s)) break;
-                const uint32_t to = ring + s * kStage;
-                ptx::mbar_arrive_expect_tx(full(s), kRowBox + factor_bytes);
-                ptx::tma_load_2d(to, &tm_x, t * kBox, item.row0, full(s));
-                if (kFlip) ptx::tma_load_3d(to + kRowBox, &tm_f, 0, t * kBox, item.adapter, full(s));
-                else ptx::tma_load_3d(to + kRowBox, &tm_f, t * kBox, 0, item.adapter, full(s));
+                const uint32_t to = ring + s * kShrinkStage;
+                ptx::mbar_arrive_expect_tx(full(s), 2 * (kRowBox + factor_bytes));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) ptx::tma_load_2d(to + h * kRowBox, &tm_x, (2 * t + h) * kBox, item.row0, full(s));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t at = to + 2 * kRowBox + h * kFactorBox;
+                    if (kFlip) ptx::tma_load_3d(at, &tm_f, 0, (2 * t + h) * kBox, item.adapter, full(s));
+                    else ptx::tma_load_3d(at, &tm_f, (2 * t + h) * kBox, 0, item.adapter, full(s));
+                }
             }
         }
         __syncwarp();
@@ -204,20 +211,20 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         if (ptx::elect_one()) {
             const uint32_t idesc = idesc_of(p.r16, false, kFlip);
             for (int t = t0, s = 0, n = 0; t < t1; ++t, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
-                const int w = n / kWindow, d = w & 1;
-                if (n % kWindow == 0 && w >= 2 && !wait_bounded(bar(kSumEmpty + d), ((w >> 1) - 1) & 1u, abort_flag, p.status, 0xD18u | d)) break;
+                const int w = n / kShrinkWindow, d = w & 1;
+                if (n % kShrinkWindow == 0 && w >= 2 && !wait_bounded(bar(kSumEmpty + d), ((w >> 1) - 1) & 1u, abort_flag, p.status, 0xD18u | d)) break;
                 if (!wait_bounded(full(s), (n / p.stages) & 1u, abort_flag, p.status, 0xD10u | s)) break;
                 ptx::tc_fence_after_sync();
-                const uint32_t from = ring + s * kStage;
+                const uint32_t from = ring + s * kShrinkStage;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint64_t a = ptx::smem_desc_sw128(from) + 2u * i;
-                    const uint64_t b = kFlip ? ptx::smem_desc_sw128_mn(from + kRowBox + i * 2048, kFactorBox, 1024)
-                                             : ptx::smem_desc_sw128(from + kRowBox) + 2u * i;
-                    ptx::mma_bf16(tmem + d * kBox, a, b, idesc, n % kWindow > 0 || i > 0);
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t factor = from + 2 * kRowBox + (i >> 2) * kFactorBox;
+                    const uint64_t a = ptx::smem_desc_sw128(from + (i >> 2) * kRowBox) + 2u * (i & 3);
+                    const uint64_t b = kFlip ? ptx::smem_desc_sw128_mn(factor + (i & 3) * 2048, kFactorBox, 1024) : ptx::smem_desc_sw128(factor) + 2u * (i & 3);
+                    ptx::mma_bf16(tmem + d * kBox, a, b, idesc, n % kShrinkWindow > 0 || i > 0);
                 }
                 ptx::tc_commit(empty(s));
-                if (n % kWindow == kWindow - 1 || t + 1 == t1) ptx::tc_commit(bar(kSumFull + d));
+                if (n % kShrinkWindow == kShrinkWindow - 1 || t + 1 == t1) ptx::tc_commit(bar(kSumFull + d));
             }
         }
         __syncwarp();
@@ -226,7 +233,7 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         float sum[kMaxRank] = {};
         bool ok = true;
-        for (int w = 0; w * kWindow < t1 - t0; ++w) {
+        for (int w = 0; w * kShrinkWindow < t1 - t0; ++w) {
             const int d = w & 1;
             if (!(ok = warp_wait(bar(kSumFull + d), (w >> 1) & 1u, abort_flag, p.status, 0xD20u | d))) break;
             ptx::tc_fence_after_sync();
@@ -674,16 +681,16 @@ bool factor_map(CUtensorMap *out, const void *base, int64_t cols, int64_t rows, 
     return make_tmap_3d_bf16(out, base, cols, rows, adapters, 2 * cols, 2 * cols * rows, kBox, box_rows);
 }
 
-constexpr int kShrinkStages = 4;
+constexpr int kShrinkStages = 4;           // one block an SM
 constexpr int kHalfSmem = 115712, kFullSmem = 232448;     // two blocks an SM, or one
 
 // Blocks that share the long side: as many as leave all clusters resident at once (clusters of some sizes fit the GPU's SM groups worse than
-// others: a second wave for one more block costs twice the time), none with fewer than four stages.
+// others: a second wave for one more block costs twice the time), none with fewer than two tiles.
 template <bool kFlip>
 int shrink_splits(int64_t items, int tiles, int smem) {
     static int resident[kMaxCluster + 1] = {};
     for (int n = kMaxCluster; n > 1; --n) {
-        if (n > tiles / 4) continue;
+        if (n > tiles / 2) continue;
         if (resident[n] == 0) {
             cudaLaunchConfig_t cfg{};
             cfg.gridDim = dim3(n * 1024);
@@ -708,7 +715,7 @@ int shrink_splits(int64_t items, int tiles, int smem) {
 template <bool kFlip>
 sol_status_t launch_shrink(const Requests &q, const void *x, int64_t ldx, const void *factor, int64_t cols, int64_t r, const Plan &plan,
                            const float *scaling, void *parts, cudaStream_t stream) {
-    const int r16 = static_cast<int>(ceil_div(r, 16) * 16), tiles = static_cast<int>(ceil_div(cols, kBox)), smem = kControl + kShrinkStages * kStage;
+    const int r16 = static_cast<int>(ceil_div(r, 16) * 16), tiles = static_cast<int>(ceil_div(cols, 2 * kBox)), smem = kControl + kShrinkStages * kShrinkStage;
     CUtensorMap tm_x, tm_f;
     if (!rows_map(&tm_x, x, cols, q.rows, ldx, kRows)) return SOL_ERR_CUDA;
     if (!(kFlip ? factor_map(&tm_f, factor, r, cols, q.adapters, kBox) : factor_map(&tm_f, factor, cols, r, q.adapters, r16))) return SOL_ERR_CUDA;
