@@ -162,7 +162,7 @@ sol_status_t nvfp4_requantize_lora_batch(int64_t count, const void *const *w_lis
  *   K, N multiples of 8 up to 1048576;  r a multiple of 8, 8 <= r <= 64;  adapters, requests <= 1024
  *   workspace  sol_lora_workspace_bytes(M, K, N, r, adapters, requests, 0) bytes of device scratch, 256-byte aligned; two calls
  *              that may overlap need one each
- * Sums are FP32 in a fixed order; t enters the second product with 16 bits.  Two launches.  A wait that runs out (sol_last_device_status)
+ * Sums are FP32 in a fixed order; t enters the second product with 16 bits (the gradients' dt with 24).  Two launches.  A wait that runs out (sol_last_device_status)
  * leaves y incomplete or NaN.
  */
 size_t sol_lora_workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, int backward);

@@ -2,20 +2,30 @@
 //
 // A request is a run of rows with an adapter of its own (or none).  With t = x A^T (rank r <= 64 columns):
 //     y += s t B^T;     from dy:  dt = s dy B,  dx += dt A,  dA = dt^T x,  dB = s dy^T t
-// All products run on tcgen05 with FP32 sums.  t and dt are held in two BF16 parts, high and low (16 bits), side by side as one
-// operand of twice the width against the factor taken twice: what is lost is 2^-17 of a value and not 2^-9, at no more memory traffic.
+// All products run on tcgen05 with FP32 sums.  t is held in two BF16 parts (each what the one before left: 2^-17 of a value is lost and not
+// 2^-9), dt in three (its product with x is an FP32 result), side by side as one wider operand against the other one; the memory
+// traffic is that of x, y and dy all the same.
 //
 // HBM bound: the adapters' products are r / 2 operations a byte of x, y, dy, far below the tensor cores' rate.  Three kernels, each
-// of which streams one large operand through a ring of TMA stages once:
+// of which streams its large operands through a ring of TMA stages once:
 //   shrink  t = x A^T (or dy B): 128 rows a cluster, whose blocks share the columns and add up their sums over one another's shared
-//           memory; leaves t's two parts
+//           memory; leaves t's parts
+//   outer   dA and dB: 128 columns of x or dy by the columns of dt's or t's parts, summed over an adapter's rows (both operands have
+//           the row as their second index: MN-major); row slices of one adapter are added up in order by a last small launch
 //   expand  takes t as an operand and walks 64 columns at a time: a stage brings the columns of y and the factor's rows, the
 //           product is added to y in the stage's own memory, and a TMA store takes it back
-//   outer   dA and dB: 128 columns of x or dy by the 2r columns of dt or t, summed over an adapter's rows (both operands have the
-//           row as their second index: MN-major); row slices of one adapter are added up in order by a last small launch
 // Which rows and adapter a block has follows from the requests' offsets on the device: the host knows neither, the grid covers the most
 // that there can be (a tile of 128 rows for each 128 rows and one more per request) and blocks without a tile leave.
 // Everything is summed in a fixed order: equal inputs give equal bits.
+//
+// Measured (B200, inside a graph; bytes of the operands once, and each kernel by itself): 17003 rows, 3072 -> 9216, rank 32, 127 us = 5.2
+// TB/s, 80 % of the copy rate (shrink 25, expand 103: 6.1 TB/s); gradients of 9216 rows 104 us (shrink 39, outer 44, its sum 4, expand
+// 25): dy is read twice, which makes 78 us the floor of this form and 52 that of one that could keep dB's sums of all columns beside dt's (a
+// megabyte a row slice).  8 requests of one row, 3072 -> 18432, 17.3 us: latency, two launches of 7 to 9 us each.
+// What it was before: t's slices through the workspace and summed by every expanding block, 155 and 110 us (the sum over a
+// cluster: 127 and 117 with a cluster that left a second wave, 107 without); a stage held until the next store, 152; y written from registers
+// in place of TMA, 166.  Stages of 256 bytes a row in place of 128 in shrink are worth 1 us; another order of columns in every
+// block, against their reading the factor's same lines at the same time, nothing.
 #include "gemm_common.cuh"
 #include "quant_math.cuh"
 #include "sol_internal.h"
@@ -36,6 +46,7 @@ constexpr int kStage = kRowBox + kFactorBox;
 constexpr int kMaxStages = 8;
 constexpr int kShrinkStage = 2 * kStage;    // 128 columns: rows of 256 bytes, which DRAM gives faster than twice 128
 constexpr int kMaxCluster = 8;
+constexpr int kHalfSmem = 115712, kFullSmem = 232448;     // a block's shared memory where two fit an SM, or one
 constexpr int kSlots = 296;              // blocks that are resident at once: two on each of 148 SMs
 
 struct Requests {
@@ -150,8 +161,9 @@ constexpr int kShrinkWindow = 4;         // of 128 columns
 struct Shrink {
     Requests q;
     const float *scaling;     // [adapters]; null: t as it is
-    uint16_t *parts;          // [rows][2 r]: t's high and low parts
+    uint16_t *parts;          // [rows][n_parts r]: t's parts, each what the ones before it left
     uint32_t *status;
+    int n_parts;              // 2 or 3
     int r, r16;               // rank, and the next multiple of 16
     int tiles, per_split;     // 128-column tiles of the long side, and those of a block
     int splits, stages;       // blocks of a cluster, which share the long side
@@ -272,16 +284,18 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             const float4 a = ld_cluster(from), b = ld_cluster(from + 16);
             t[0] += a.x, t[1] += a.y, t[2] += a.z, t[3] += a.w, t[4] += b.x, t[5] += b.y, t[6] += b.z, t[7] += b.w;
         }
-        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float a = t[2 * e] * factor, b = t[2 * e + 1] * factor;
-            hi[e] = pack_bf16(a, b);
-            lo[e] = pack_bf16(a - qmath::bf16_lo(hi[e]), b - qmath::bf16_hi(hi[e]));
+        for (int e = 0; e < 8; ++e) t[e] *= factor;
+        uint16_t *out = p.parts + static_cast<int64_t>(item.row0 + r) * p.n_parts * p.r + c;
+        for (int part = 0; part < p.n_parts; ++part, out += p.r) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = pack_bf16(t[2 * e], t[2 * e + 1]);
+                t[2 * e] -= qmath::bf16_lo(w[e]), t[2 * e + 1] -= qmath::bf16_hi(w[e]);
+            }
+            *reinterpret_cast<uint4 *>(out) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-        uint16_t *out = p.parts + static_cast<int64_t>(item.row0 + r) * 2 * p.r + c;
-        *reinterpret_cast<uint4 *>(out) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4 *>(out + p.r) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
     ptx::cluster_sync();                   // nobody leaves while others read its memory
     end_block<128>(abort_flag, warp, tmem);
@@ -290,8 +304,9 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
 // ------------------------------------------------------------------------------------------------ expand
 struct Expand {
     Requests q;
-    const uint16_t *parts;    // [rows][2 r]: t's high and low parts
+    const uint16_t *parts;    // [rows][n_parts r]: t's parts, of which the first two are used
     const float *scaling;     // [adapters]; null: it is on t already
+    int n_parts;
     uint16_t *y;
     uint32_t *status;
     int64_t ldy;
@@ -380,7 +395,7 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
             if (c >= p.r16) continue;
             uint4 h = make_uint4(0, 0, 0, 0), l = h;
             if (there && c < p.r) {
-                const uint16_t *from = p.parts + static_cast<int64_t>(row) * 2 * p.r + c;
+                const uint16_t *from = p.parts + static_cast<int64_t>(row) * p.n_parts * p.r + c;
                 h = __ldcg(reinterpret_cast<const uint4 *>(from));
                 l = __ldcg(reinterpret_cast<const uint4 *>(from + p.r));
             }
@@ -455,11 +470,14 @@ struct Outer {
     int64_t slice_floats;     // from one row slice's sums to the next's
     uint32_t *status;
     int r, K, N, tiles_x, tiles;    // 128-column tiles of x, and of x and dy
-    int slices, stages;       // row slices of an adapter
+    int slices;               // row slices of an adapter
+    int parts_x, parts_dy;    // parts of dt (with x) and of t (with dy)
 };
 constexpr int kStepRows = 64;
 constexpr int kRunBytes = kMaxRequests * 8;
-constexpr int outer_stage(int u_boxes) { return (2 + u_boxes) * kFactorBox; }     // 128 columns of x or dy, 64 or 128 of t's parts
+// A stage: 128 columns of x or dy and all parts' columns of dt or t; two blocks an SM.
+__host__ __device__ constexpr int outer_stage(int r, int parts) { return (2 + (parts * r + kBox - 1) / kBox) * kFactorBox; }
+__host__ __device__ constexpr int outer_stages(int r, int parts) { return (kHalfSmem - kControl - kRunBytes) / outer_stage(r, parts); }
 
 __global__ void __launch_bounds__(192, 2)
 outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_dt,
@@ -486,9 +504,11 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
         }
         if (lane == 0) control.n_runs = n;
     }
-    // full, empty: [stage]; sum full, sum empty: [accumulator]
-    constexpr int kSumFull = 2 * kMaxStages, kSumEmpty = kSumFull + 2, kSumColumns = 2 * kMaxRank;
-    begin_block<2 * kSumColumns>(control, kSumEmpty + 2, [](int i) { return i >= kSumEmpty ? 4 : 1; }, warp);
+    // full, empty: [stage]; sum full, sum empty: [accumulator].  A sum has a column for every part's; two take turns where they fit
+    constexpr int kSumFull = 2 * kMaxStages, kSumEmpty = kSumFull + 2, kColumns = 256;
+    const int parts = of_x ? p.parts_x : p.parts_dy, n_columns = (parts * p.r + 15) / 16 * 16, sums = n_columns <= kColumns / 2 ? 2 : 1;
+    const int stage_bytes = outer_stage(p.r, parts), stages = outer_stages(p.r, parts);
+    begin_block<kColumns>(control, kSumEmpty + 2, [](int i) { return i >= kSumEmpty ? 4 : 1; }, warp);
     ptx::grid_launch_dependents();
     const uint32_t bars = ptx::smem_u32(control.bars), tmem = control.tmem, ring = ptx::smem_u32(smem) + kControl + kRunBytes;
     volatile uint32_t *abort_flag = &control.abort;
@@ -498,7 +518,7 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
     auto bar = [&](int i) { return bars + 8u * i; };
     int steps = 0;                        // of 64 rows
     for (int run = 0; run < n_runs; ++run) steps += (runs[run].y - runs[run].x + kStepRows - 1) / kStepRows;
-    const int u_boxes = (2 * p.r + kBox - 1) / kBox, stage_bytes = (2 + u_boxes) * kFactorBox;
+    const int u_boxes = (parts * p.r + kBox - 1) / kBox;
     if (warp == 0) {
         ptx::grid_dependency_wait();
         if (ptx::elect_one() && !loads_held(p.status)) {
@@ -506,8 +526,8 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
             int s = 0, n = 0;
             bool ok = true;
             for (int run = 0; ok && run < n_runs; ++run) {
-                for (int row = runs[run].x; row < runs[run].y; row += kStepRows, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
-                    if (n >= p.stages && !(ok = wait_bounded(empty(s), ((n / p.stages) - 1) & 1u, abort_flag, p.status, 0xD90u | s))) break;
+                for (int row = runs[run].x; row < runs[run].y; row += kStepRows, ++n, s = s + 1 == stages ? 0 : s + 1) {
+                    if (n >= stages && !(ok = wait_bounded(empty(s), ((n / stages) - 1) & 1u, abort_flag, p.status, 0xD90u | s))) break;
                     const uint32_t to = ring + s * stage_bytes;
                     ptx::mbar_arrive_expect_tx(full(s), (2 + u_boxes) * kFactorBox);
                     ptx::tma_load_2d(to, tm_z, column, row, full(s));
@@ -518,14 +538,14 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
         }
         __syncwarp();
     } else if (warp == 1) {
-        const uint32_t idesc = idesc_of(2 * p.r, true, true);
+        const uint32_t idesc = idesc_of(n_columns, true, true);
         int s = 0, n = 0;
         bool ok = true;
         for (int run = 0; ok && run < n_runs; ++run) {
-            for (int row = runs[run].x; row < runs[run].y; row += kStepRows, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
-                const int w = n / kWindow, d = w & 1;
-                if (n % kWindow == 0 && w >= 2 && !(ok = warp_wait(bar(kSumEmpty + d), ((w >> 1) - 1) & 1u, abort_flag, p.status, 0xDA8u | d))) break;
-                if (!(ok = warp_wait(full(s), (n / p.stages) & 1u, abort_flag, p.status, 0xDA0u | s))) break;
+            for (int row = runs[run].x; row < runs[run].y; row += kStepRows, ++n, s = s + 1 == stages ? 0 : s + 1) {
+                const int w = n / kWindow, d = w % sums;
+                if (n % kWindow == 0 && w >= sums && !(ok = warp_wait(bar(kSumEmpty + d), (w / sums - 1) & 1u, abort_flag, p.status, 0xDA8u | d))) break;
+                if (!(ok = warp_wait(full(s), (n / stages) & 1u, abort_flag, p.status, 0xDA0u | s))) break;
                 const uint32_t from = ring + s * stage_bytes;
                 const int rows = runs[run].y - row;
                 if (rows < kStepRows) {       // rows that belong to somebody else may hold anything: zeros in their place
@@ -538,7 +558,7 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
                     ptx::tc_fence_after_sync();
 #pragma unroll
                     for (int i = 0; i < kStepRows / 16; ++i)
-                        ptx::mma_bf16(tmem + d * kSumColumns, ptx::smem_desc_sw128_mn(from + i * 2048, kFactorBox, 1024),
+                        ptx::mma_bf16(tmem + d * (kColumns / 2), ptx::smem_desc_sw128_mn(from + i * 2048, kFactorBox, 1024),
                                       ptx::smem_desc_sw128_mn(from + 2 * kFactorBox + i * 2048, kFactorBox, 1024), idesc, n % kWindow > 0 || i > 0);
                     ptx::tc_commit(empty(s));
                     if (n % kWindow == kWindow - 1 || n + 1 == steps) ptx::tc_commit(bar(kSumFull + d));
@@ -552,18 +572,22 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
         float v[kMaxRank] = {};
         bool ok = true;
         for (int w = 0; w * kWindow < steps; ++w) {
-            const int d = w & 1;
-            if (!(ok = warp_wait(bar(kSumFull + d), (w >> 1) & 1u, abort_flag, p.status, 0xDB0u | d))) break;
+            const int d = w % sums;
+            if (!(ok = warp_wait(bar(kSumFull + d), (w / sums) & 1u, abort_flag, p.status, 0xDB0u | d))) break;
             ptx::tc_fence_after_sync();
 #pragma unroll
             for (int j = 0; j < kMaxRank; j += 8) {
                 if (j >= p.r) continue;
-                uint32_t hi[8], lo[8];
-                ptx::tmem_ld_32x8(lanes_at + d * kSumColumns + j, hi);
-                ptx::tmem_ld_32x8(lanes_at + d * kSumColumns + p.r + j, lo);
+                uint32_t part[3][8];
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+                    if (k < parts) ptx::tmem_ld_32x8(lanes_at + d * (kColumns / 2) + k * p.r + j, part[k]);
                 ptx::tmem_ld_wait();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[j + e] += __uint_as_float(hi[e]) + __uint_as_float(lo[e]);
+                for (int e = 0; e < 8; ++e) {
+                    const float low = parts > 2 ? __uint_as_float(part[1][e]) + __uint_as_float(part[2][e]) : __uint_as_float(part[1][e]);
+                    v[j + e] += __uint_as_float(part[0][e]) + low;
+                }
             }
             ptx::tc_fence_before_sync();
             __syncwarp();
@@ -585,7 +609,7 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
             }
         }
     }
-    end_block<2 * kSumColumns>(abort_flag, warp, tmem);
+    end_block<kColumns>(abort_flag, warp, tmem);
 }
 
 // The row slices' sums, in order: dA's values, then dB's.
@@ -635,7 +659,9 @@ Plan plan_of(int64_t M, int64_t from, int64_t to, int64_t requests, int64_t adap
     return p;
 }
 int64_t pad256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-int64_t parts_bytes(int64_t M, int64_t r) { return pad256(4 * M * r); }
+// t in two parts; dt in three, since the gradient of lora_a is FP32 and two would be what limits it
+constexpr int kTParts = 2, kDtParts = 3;
+int64_t parts_bytes(int64_t M, int64_t r, int parts) { return pad256(2 * parts * M * r); }
 
 // Allows kernel `kern` `smem` bytes of dynamic shared memory on the current device (asked for once).
 template <auto kern>
@@ -682,7 +708,6 @@ bool factor_map(CUtensorMap *out, const void *base, int64_t cols, int64_t rows, 
 }
 
 constexpr int kShrinkStages = 4;           // one block an SM
-constexpr int kHalfSmem = 115712, kFullSmem = 232448;     // two blocks an SM, or one
 
 // Blocks that share the long side: as many as leave all clusters resident at once (clusters of some sizes fit the GPU's SM groups worse than
 // others: a second wave for one more block costs twice the time), none with fewer than two tiles.
@@ -714,25 +739,25 @@ int shrink_splits(int64_t items, int tiles, int smem) {
 }
 template <bool kFlip>
 sol_status_t launch_shrink(const Requests &q, const void *x, int64_t ldx, const void *factor, int64_t cols, int64_t r, const Plan &plan,
-                           const float *scaling, void *parts, cudaStream_t stream) {
+                           const float *scaling, void *parts, int n_parts, cudaStream_t stream) {
     const int r16 = static_cast<int>(ceil_div(r, 16) * 16), tiles = static_cast<int>(ceil_div(cols, 2 * kBox)), smem = kControl + kShrinkStages * kShrinkStage;
     CUtensorMap tm_x, tm_f;
     if (!rows_map(&tm_x, x, cols, q.rows, ldx, kRows)) return SOL_ERR_CUDA;
     if (!(kFlip ? factor_map(&tm_f, factor, r, cols, q.adapters, kBox) : factor_map(&tm_f, factor, cols, r, q.adapters, r16))) return SOL_ERR_CUDA;
     if (!allow_smem<shrink_kernel<kFlip>>(smem)) return SOL_ERR_CUDA;
     const int per = static_cast<int>(ceil_div(tiles, shrink_splits<kFlip>(plan.items, tiles, smem))), splits = static_cast<int>(ceil_div(tiles, per));
-    const Shrink p{q, scaling, static_cast<uint16_t *>(parts), device_status_word(), static_cast<int>(r), r16, tiles, per, splits, kShrinkStages};
+    const Shrink p{q, scaling, static_cast<uint16_t *>(parts), device_status_word(), n_parts, static_cast<int>(r), r16, tiles, per, splits, kShrinkStages};
     return launch<false>(shrink_kernel<kFlip>, plan.items * splits, 192, smem, splits, stream, tm_x, tm_f, p);
 }
 template <bool kFlip>
-sol_status_t launch_expand(const Requests &q, const void *parts, const float *scaling, void *y, int64_t ldy, const void *factor, int64_t cols, int64_t r,
+sol_status_t launch_expand(const Requests &q, const void *parts, int n_parts, const float *scaling, void *y, int64_t ldy, const void *factor, int64_t cols, int64_t r,
                            const Plan &plan, cudaStream_t stream) {
     const int r16 = static_cast<int>(ceil_div(r, 16) * 16);
     CUtensorMap tm_y, tm_out, tm_f;
     if (!rows_map(&tm_y, y, cols, q.rows, ldy, kRows) || !rows_map(&tm_out, y, cols, q.rows, ldy, 32)) return SOL_ERR_CUDA;
     if (!(kFlip ? factor_map(&tm_f, factor, cols, r, q.adapters, r16) : factor_map(&tm_f, factor, r, cols, q.adapters, kBox))) return SOL_ERR_CUDA;
     const int t_bytes = static_cast<int>(ceil_div(2 * r16, kBox)) * kRowBox;
-    Expand p{q, static_cast<const uint16_t *>(parts), scaling, static_cast<uint16_t *>(y), device_status_word(), ldy, static_cast<int>(r), r16,
+    Expand p{q, static_cast<const uint16_t *>(parts), scaling, n_parts, static_cast<uint16_t *>(y), device_status_word(), ldy, static_cast<int>(r), r16,
              0, static_cast<int>(cols), plan.chunks, plan.per_slice, plan.slices};
     // two blocks an SM with four stages up to rank 32, one with eight beyond
     p.stages = ((t_bytes == kRowBox ? kHalfSmem : kFullSmem) - kControl - t_bytes) / kStage;
@@ -747,18 +772,18 @@ int max_rank() { return kMaxRank; }
 int max_requests() { return kMaxRequests; }
 
 size_t workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, bool backward) {
-    if (!backward) return static_cast<size_t>(parts_bytes(M, r));
+    if (!backward) return static_cast<size_t>(parts_bytes(M, r, kTParts));
     const Plan p = plan_of(M, N, K, requests, adapters);
-    return static_cast<size_t>(parts_bytes(M, r) + (p.outer_slices > 1 ? 4 * p.outer_slices * adapters * r * (K + N) : 0));
+    return static_cast<size_t>(parts_bytes(M, r, kDtParts) + (p.outer_slices > 1 ? 4 * p.outer_slices * adapters * r * (K + N) : 0));
 }
 
 sol_status_t launch_apply(const Call &c, const void *x, int64_t ldx, void *y, int64_t ldy, void *t_out, void *workspace, cudaStream_t stream) {
     const Requests q{c.offsets, c.ids, static_cast<int>(c.requests), static_cast<int>(c.adapters), static_cast<int>(c.M)};
     const Plan plan = plan_of(c.M, c.K, c.N, c.requests, c.adapters);
     void *parts = t_out != nullptr ? t_out : workspace;
-    const sol_status_t st = launch_shrink<false>(q, x, ldx, c.a, c.K, c.r, plan, nullptr, parts, stream);
+    const sol_status_t st = launch_shrink<false>(q, x, ldx, c.a, c.K, c.r, plan, nullptr, parts, kTParts, stream);
     if (st != SOL_OK) return st;
-    return launch_expand<false>(q, parts, c.scaling, y, ldy, c.b, c.N, c.r, plan, stream);
+    return launch_expand<false>(q, parts, kTParts, c.scaling, y, ldy, c.b, c.N, c.r, plan, stream);
 }
 
 sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, const void *t, void *dx, int64_t ld_dx,
@@ -766,22 +791,20 @@ sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const
     const Requests q{c.offsets, c.ids, static_cast<int>(c.requests), static_cast<int>(c.adapters), static_cast<int>(c.M)};
     const Plan plan = plan_of(c.M, c.N, c.K, c.requests, c.adapters);
     uint8_t *dt = static_cast<uint8_t *>(workspace);
-    float *sums = reinterpret_cast<float *>(dt + parts_bytes(c.M, c.r));
-    sol_status_t st = launch_shrink<true>(q, dy, ld_dy, c.b, c.N, c.r, plan, c.scaling, dt, stream);
+    float *sums = reinterpret_cast<float *>(dt + parts_bytes(c.M, c.r, kDtParts));
+    sol_status_t st = launch_shrink<true>(q, dy, ld_dy, c.b, c.N, c.r, plan, c.scaling, dt, kDtParts, stream);
     if (st != SOL_OK) return st;
     // the factors' gradients next, while L2 still holds a part of dy
     CUtensorMap tm_x, tm_dy, tm_dt, tm_t;
     if (!rows_map(&tm_x, x, c.K, c.M, ldx, kStepRows) || !rows_map(&tm_dy, dy, c.N, c.M, ld_dy, kStepRows) ||
-        !rows_map(&tm_dt, dt, 2 * c.r, c.M, 2 * c.r, kStepRows) || !rows_map(&tm_t, t, 2 * c.r, c.M, 2 * c.r, kStepRows))
+        !rows_map(&tm_dt, dt, kDtParts * c.r, c.M, kDtParts * c.r, kStepRows) || !rows_map(&tm_t, t, kTParts * c.r, c.M, kTParts * c.r, kStepRows))
         return SOL_ERR_CUDA;
     const int64_t da_floats = c.adapters * c.r * c.K, db_floats = c.adapters * c.r * c.N;
     const bool sliced = plan.outer_slices > 1;
-    Outer p{q, c.scaling, sliced ? sums : da, sliced ? sums + da_floats : db, da_floats + db_floats, device_status_word(), static_cast<int>(c.r),
-            static_cast<int>(c.K), static_cast<int>(c.N), plan.outer_tiles_x, plan.outer_tiles, plan.outer_slices, 0};
-    const int stage = outer_stage(static_cast<int>(ceil_div(2 * c.r, kBox)));
-    p.stages = (kHalfSmem - kControl - kRunBytes) / stage;
+    const Outer p{q, c.scaling, sliced ? sums : da, sliced ? sums + da_floats : db, da_floats + db_floats, device_status_word(), static_cast<int>(c.r),
+                  static_cast<int>(c.K), static_cast<int>(c.N), plan.outer_tiles_x, plan.outer_tiles, plan.outer_slices, kDtParts, kTParts};
     if (!allow_smem<outer_kernel>(kHalfSmem)) return SOL_ERR_CUDA;
-    st = launch<true>(outer_kernel, static_cast<int64_t>(plan.outer_tiles) * plan.outer_slices * c.adapters, 192, kControl + kRunBytes + p.stages * stage, 1,
+    st = launch<true>(outer_kernel, static_cast<int64_t>(plan.outer_tiles) * plan.outer_slices * c.adapters, 192, kHalfSmem, 1,
                       stream, tm_x, tm_dy, tm_dt, tm_t, p);
     if (st != SOL_OK) return st;
     if (sliced) {
@@ -790,7 +813,7 @@ sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const
                           da_floats / 4, reinterpret_cast<float4 *>(da), reinterpret_cast<float4 *>(db));
         if (st != SOL_OK) return st;
     }
-    return dx != nullptr ? launch_expand<true>(q, dt, nullptr, dx, ld_dx, c.a, c.K, c.r, plan, stream) : SOL_OK;
+    return dx != nullptr ? launch_expand<true>(q, dt, kDtParts, nullptr, dx, ld_dx, c.a, c.K, c.r, plan, stream) : SOL_OK;
 }
 
 }  // namespace lora
