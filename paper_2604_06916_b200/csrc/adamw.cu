@@ -485,7 +485,7 @@ sol_status_t launch_step(const Tensor *tensors, int64_t count, const sol_adamw_o
     h.b1 = static_cast<float>(o.beta1), h.c1 = static_cast<float>(1.0 - o.beta1);
     h.b2 = static_cast<float>(o.beta2), h.c2 = static_cast<float>(1.0 - o.beta2);
     h.eps = static_cast<float>(o.eps);
-    h.tiny_eps = o.eps < 1e-12;              // the root of what FP32 flushes to 0 is below 2^-63
+    h.tiny_eps = o.eps < 1e-9;               // a root below 2^-63 (times its bias correction) is then more than eps' last place
     h.lr_scale = o.lr_scale, h.grad_scale = o.grad_scale;
     h.state = reinterpret_cast<long long *>(state);
     h.seed = o.seed;

@@ -147,6 +147,14 @@ def test_tiny_and_huge_values(B):
     run.check_step(5, eps=1e-3)
 
 
+@pytest.mark.parametrize("eps", [1e-9, 2e-10, 1e-12, 1e-16])
+def test_squares_below_the_normal_range(B, eps):
+    run = Run(B, [256], 32, False, False, False, 12, warm=False)
+    run.gs[0].copy_(torch.logspace(-21, -15, 256, device="cuda"))       # squares from 1e-42 on, times 1 - beta2
+    run.check_step(None, eps=eps, weight_decay=0.0)
+    run.check_step(None, eps=eps, weight_decay=0.0, beta2=0.9999)
+
+
 def test_factors_on_the_device_capture_and_replay(B):
     run = Run(B, [5000, 321], 8, False, False, True, 9)
     lr_scale, grad_scale = torch.tensor([0.5], device="cuda"), torch.tensor(0.25, device="cuda")
