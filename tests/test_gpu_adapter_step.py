@@ -157,3 +157,25 @@ def test_policies_unmerged_beside_a_quantized_projection(B):
     one = B.sol_lora_apply(step.x[:1], step.a16, step.b16, step.scaling, step.offsets[:2].clamp(max=1), step.ids[:1], base[:1].clone())
     assert torch.equal(one, y[:1])
     assert torch.equal(y[290], base[290])
+
+
+def test_two_streams_at_once(B):
+    """Two steps that overlap, each with its own tensors and workspaces, give what they give alone."""
+    alone = [Step(B, seed, 8).run() for seed in (7, 8)]
+    torch.cuda.synchronize()
+    steps = [Step(B, seed, 8) for seed in (7, 8)]
+    streams = [torch.cuda.Stream() for _ in steps]
+    torch.cuda.synchronize()
+    got = []
+    for step, stream in zip(steps, streams):
+        with torch.cuda.stream(stream):
+            got.append(step.run())
+    torch.cuda.synchronize()
+    for a, b in zip(alone, got):
+        for name in a:
+            if name == "t":        # the request without an adapter leaves its rows as they are
+                rows = torch.ones(ROWS, dtype=torch.bool, device="cuda")
+                rows[290] = False
+                assert torch.equal(a[name][rows], b[name][rows])
+            else:
+                assert torch.equal(a[name], b[name]), name
