@@ -182,7 +182,6 @@ struct Backward {
 
 constexpr int kMaxWarps = 16;           // of a block, at most (twelve where 168 registers a thread are wanted: up to 12288 columns)
 constexpr int kGroupColumns = 256;      // columns of a warp and piece
-__host__ __device__ constexpr int rows_of(int chunks) { return chunks == 1 ? 4 : chunks == 2 ? 2 : 1; }   // rows of a group's step
 // Sums of kValues (a power of two up to 32) values over the warp: lane l ends up with that of value l >> (5 - log2 kValues).
 template <int kValues>
 __device__ __forceinline__ float transpose_sum(float (&v)[kValues], int lane) {
@@ -205,10 +204,11 @@ __device__ __forceinline__ float transpose_sum(float (&v)[kValues], int lane) {
     return v[0];
 }
 
-template <int kChunks, int kWarps>
+// kRows rows a step of a group; kAhead: the next step's rows are under way meanwhile.
+template <int kChunks, int kRows, int kWarps, bool kAhead>
 __global__ void __launch_bounds__(32 * kWarps, 1)
 backward_kernel(const Backward p) {
-    constexpr int kRows = rows_of(kChunks), kValues = 2 * kRows;
+    constexpr int kValues = 2 * kRows;
     constexpr int kLanesPer = 32 / kValues;                   // lanes that hold one value after the warp's sum
     __shared__ float part[2][kMaxWarps][kValues];             // [buffer][warp]
     __shared__ __align__(16) float across[kMaxWarps * kGroupColumns];   // the groups' sums: eight columns a thread
@@ -315,17 +315,22 @@ backward_kernel(const Backward p) {
                 }
             }
         };
-        // whole steps, each one's rows asked for while the one before is worked on
+        // whole steps, each one's rows asked for while the one before is worked on (where the registers hold both)
         uint32_t base = s0 + t0 * stride + group * kRows, left = t1 - t0;
         const bool tail = left > 0 && base + (left - 1) * stride + kRows > end;     // this group's last step
         if (tail) --left;
         Step next;
-        if (left > 0) fetch(next, base, std::true_type{});
+        if (kAhead && left > 0) fetch(next, base, std::true_type{});
 #pragma unroll 1
         for (; left > 0; --left, base += stride) {
-            const Step now = next;
-            if (left > 1) fetch(next, base + stride, std::true_type{});
-            work(now, base, std::true_type{});
+            if constexpr (kAhead) {
+                const Step now = next;
+                if (left > 1) fetch(next, base + stride, std::true_type{});
+                work(now, base, std::true_type{});
+            } else {
+                fetch(next, base, std::true_type{});
+                work(next, base, std::true_type{});
+            }
         }
         if (tail) {
             fetch(next, base, std::false_type{});
@@ -392,21 +397,28 @@ reduce_kernel(const float *__restrict__ partials, int K, int pieces, float *dsca
 constexpr int kMaxItems = 512;      // pieces in all, where a sample has more than one
 
 struct Shape {
-    int chunks, warps_per_row, groups;
+    int variant, chunks, rows, warps_per_row, groups;
 };
-// A thread holds one piece of eight columns of a row up to 3072 columns, two up to 6144, four beyond; as many groups of warps as twelve
-// warps make.
+// A thread holds `chunks` pieces of eight columns of `rows` rows, and as many again of the next ones, in what a block of twelve (168
+// registers a thread) or sixteen warps (128) leaves it beside the sums and the gain.  Up to 3072 columns as many groups as twelve
+// warps make; beyond, one.  Measured (gradients of 28 to 34 M values, us; in brackets another form): 4096 columns 42.4 (two pieces, eight
+// warps: 51.9), 6144 42, 8192 47 (two rows with spills: 78; four pieces: 98), 12288 57 (with the next row: 69; four pieces: 66), 16384 82
+// (twelve warps and the next row: 118): there the sums alone take half the registers.
+constexpr int kVariants = 6;
+constexpr int kLimit[kVariants] = {3072, 4096, 6144, 8192, 12288, 16384}, kChunksOf[kVariants] = {1, 1, 2, 2, 3, 4}, kRowsOf[kVariants] = {4, 2, 2, 1, 1, 1};
 Shape shape_of(int64_t K) {
-    Shape s;
-    s.chunks = K <= 3072 ? 1 : K <= 6144 ? 2 : 4;
+    Shape s{};
+    while (K > kLimit[s.variant]) ++s.variant;
+    s.chunks = kChunksOf[s.variant];
+    s.rows = kRowsOf[s.variant];
     s.warps_per_row = static_cast<int>(ceil_div(K, kGroupColumns * s.chunks));
-    s.groups = s.warps_per_row > 12 ? 1 : 12 / s.warps_per_row;
+    s.groups = s.variant == 0 ? 12 / s.warps_per_row : 1;
     return s;
 }
 // Pieces of a sample: so many that the blocks all have one, none of fewer rows than the groups take in a step.
 int pieces_of(int64_t M, int64_t rows_per_sample, const Shape &s, int blocks) {
     const int64_t samples = ceil_div(M, rows_per_sample);
-    const int64_t most = ceil_div(rows_per_sample < M ? rows_per_sample : M, s.groups * rows_of(s.chunks));
+    const int64_t most = ceil_div(rows_per_sample < M ? rows_per_sample : M, s.groups * s.rows);
     int64_t pieces = blocks / samples;
     if (pieces > most) pieces = most;
     return pieces < 1 ? 1 : static_cast<int>(pieces);
@@ -472,10 +484,14 @@ sol_status_t launch_backward(const void *dy, int64_t ld_dy, const void *x, int64
     const int64_t items = samples * p.pieces;
     const unsigned grid = static_cast<unsigned>(items < blocks ? items : blocks), threads = 32u * s.warps_per_row * s.groups;
     auto launch = [&](auto kern) { kern<<<grid, threads, 0, stream>>>(p); };
-    if (s.chunks == 1) launch(backward_kernel<1, 12>);
-    else if (s.chunks == 2) launch(backward_kernel<2, 12>);
-    else if (s.warps_per_row <= 12) launch(backward_kernel<4, 12>);
-    else launch(backward_kernel<4, 16>);
+    switch (s.variant) {
+        case 0: launch(backward_kernel<1, 4, 12, true>); break;
+        case 1: launch(backward_kernel<1, 2, 16, true>); break;
+        case 2: launch(backward_kernel<2, 2, 12, true>); break;
+        case 3: launch(backward_kernel<2, 1, 16, true>); break;
+        case 4: launch(backward_kernel<3, 1, 16, false>); break;
+        default: launch(backward_kernel<4, 1, 16, false>); break;
+    }
     const sol_status_t st = launch_status();
     if (st != SOL_OK || p.pieces == 1 || (dscale == nullptr && dshift == nullptr)) return st;
     cudaLaunchConfig_t cfg{};

@@ -189,3 +189,11 @@ def test_refused_tensors(B):
         B.sol_layernorm(x[:, 1:57])
     with pytest.raises(B.SolError):
         B.sol_layernorm(x, rows_per_sample=0)
+
+
+@pytest.mark.parametrize("M,K,rows", [(41, 3080, 20), (37, 4096, 37), (33, 4608, 11), (29, 6144, 29), (50, 6152, 25), (31, 8192, 31), (23, 10000, 8), (21, 12288, 21), (600, 4000, 600)])
+def test_every_form_of_the_gradients(B, M, K, rows):
+    x, dy, scale, shift = make(M, K, rows, M + K)
+    stats = B.sol_layernorm(x, scale, shift, rows, with_stats=True)[1]
+    dx, dscale, dshift = B.sol_layernorm_backward(dy, x, stats, scale, rows)
+    check_backward(dy, x, scale, rows, 1.0, 1e-6, dx, dscale, dshift)
