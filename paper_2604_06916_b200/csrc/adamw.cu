@@ -13,12 +13,14 @@
 // The new parameter comes from m and v before they are rounded.
 //
 // HBM bound in FP32: 28 bytes per element (30 with the BF16 copy); 18.1 with 8-bit states and a copy; 10.1 with BF16 parameters and
-// gradients as well, where issuing is the bound (67 instructions a value).  A thread takes eight neighbouring values (a block of 32 is
-// four lanes); FP32 goes in 32-byte accesses where the addresses allow it (304 tensors of 60 M values 304 us, with 16-byte ones 324).
-// Measured (B200, inside a graph): 60 M FP32 values in 304 tensors with the BF16 copy 306 us = 5.9 TB/s, 90 % of the copy
-// rate; 8-bit states 197 us = 5.5 TB/s; 71 M BF16 values with 8-bit states 187 us = 3.9 TB/s.  Neighbouring chunks for a block in place
-// of every gridDim-th one: 226 and 180 us; loads a chunk ahead: 194 and 200 us (fewer blocks fit); every operation and conversion by
-// itself, without the hardware's 8-bit conversions and byte permutes: 259 and 310 us.
+// gradients as well, where issuing is the bound (62 instructions a value: hash 9, encoding 14, decoding and the parameter's rounding 3,
+// the update 9).  A thread takes eight neighbouring values (a block of 32 is four lanes); FP32 goes in 32-byte accesses where the addresses
+// allow it (304 tensors of 60 M values 304 us, with 16-byte ones 324).
+// Measured (B200, inside a graph): 60 M FP32 values in 304 tensors with the BF16 copy 301 us = 6.0 TB/s, 91 % of the copy
+// rate; 8-bit states 193 us = 5.6 TB/s; 71 M BF16 values with 8-bit states 179 us = 4.0 TB/s; 2 tensors of 98304 values 3.7 us.
+// Neighbouring chunks for a block in place of every gridDim-th one: 226 us (8-bit states); loads a chunk ahead: 194 and 200 us (fewer
+// blocks fit); every operation and conversion by itself, without the hardware's 8-bit conversions and byte permutes: 259 and 310 us;
+// products one an instruction: 186 us on BF16 values; steps two by two 176 us, four by four 202 us.
 #include "ptx.cuh"
 #include "quant_math.cuh"
 #include "sol_internal.h"
@@ -35,7 +37,8 @@ using qmath::mul2;
 
 constexpr int kThreads = 256;
 constexpr int kVec = 8;                        // values of a thread
-constexpr int kChunk = kThreads * kVec;        // values of a block at a time
+constexpr int kStep = kThreads * kVec;         // values of a block at a time
+constexpr int kSteps = 4;                      // of a chunk, where it has more than one
 constexpr int kTable = 448, kSmallTable = 16;  // tensors of a launch
 
 struct Hyper {
@@ -45,6 +48,7 @@ struct Hyper {
     long long *state;                          // [0] steps done, [1] tickets
     uint64_t seed;
     uint32_t first_tensor, chunks;
+    int steps;                                 // of a chunk: a power of two
     int count, advance, tiny_eps;
 };
 template <int kN>
@@ -221,7 +225,6 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
     constexpr bool kNoise = (kP16 || k8) && kChance, kOdd = kP16 || k8;
     __shared__ float coefficients[3];      // 1 - lr decay, lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
     __shared__ uint32_t hash;              // of seed and step
-    __shared__ uint16_t of_chunk[kThreads];
     if (threadIdx.x == 0) {
         const long long t = *reinterpret_cast<volatile long long *>(h.state) + 1;
         // b^t by squaring, in FP64
@@ -249,92 +252,66 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
     const float keep = coefficients[0], size = coefficients[1], root = coefficients[2];
     const float grad_scale = h.grad_scale != nullptr ? __ldg(h.grad_scale) : 1.0f;
     const uint64_t gs2 = f32x2(grad_scale, grad_scale), b1 = f32x2(h.b1, h.b1), c1 = f32x2(h.c1, h.c1), b2 = f32x2(h.b2, h.b2), c2 = f32x2(h.c2, h.c2);
-    for (uint64_t first = blockIdx.x; first < h.chunks; first += static_cast<uint64_t>(kThreads) * gridDim.x) {
-        // the tensors of this block's next chunks, one looked for by each thread: the last tensor that begins at or before the chunk
-        if (first != blockIdx.x) __syncthreads();
-        const uint64_t mine = first + static_cast<uint64_t>(threadIdx.x) * gridDim.x;
-        if (mine < h.chunks) {
-            int lo = 0, hi = h.count;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (table.first[mid] <= mine) lo = mid;
-                else hi = mid;
-            }
-            of_chunk[threadIdx.x] = static_cast<uint16_t>(lo);
+    for (uint32_t chunk = blockIdx.x; chunk < h.chunks; chunk += gridDim.x) {
+        int lo = 0, hi = h.count;          // the last tensor that begins at or before the chunk
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (table.first[mid] <= chunk) lo = mid;
+            else hi = mid;
         }
-        __syncthreads();
-        // a thread's values of the block's k-th chunk, as they lie in memory; 0 behind the tensor's end
-        struct Raw {
-            uint32_t p[kVec * sizeof(P) / 4], g[kVec * sizeof(G) / 4], m[kVec * sizeof(S) / 4], v[kVec * sizeof(S) / 4];
-            uint32_t em, ev;
-        };
-        auto place = [&](int k, int &lo) {
-            lo = of_chunk[k];
-            return static_cast<int64_t>(first + static_cast<uint64_t>(k) * gridDim.x - table.first[lo]) * kChunk + threadIdx.x * kVec;
-        };
-        auto aligned32 = [](const Tensor &t) {
-            uintptr_t all = 0;
-            if (!kP16) all |= reinterpret_cast<uintptr_t>(t.param);
-            if (!kG16) all |= reinterpret_cast<uintptr_t>(t.grad);
-            if (!k8) all |= reinterpret_cast<uintptr_t>(t.m) | reinterpret_cast<uintptr_t>(t.v);
-            return (all & 31u) == 0;
-        };
-        auto fetch = [&](Raw &r, int k) {
-            int lo;
-            const int64_t i0 = place(k, lo);
-            const Tensor &t = table.t[lo];
-            const int64_t left = t.n - i0;
-            const P *pp = static_cast<const P *>(t.param) + i0;
-            const G *gp = static_cast<const G *>(t.grad) + i0;
-            const S *mp = static_cast<const S *>(t.m) + i0, *vp = static_cast<const S *>(t.v) + i0;
-            if (left >= kVec) {
-                const bool wide = aligned32(t);
-                load(r.p, pp, wide);
-                load(r.g, gp, wide);
-                load(r.m, mp, wide);
-                load(r.v, vp, wide);
+        // everything that is the block's: addresses of the chunk, so that a thread has 32-bit offsets only
+        const Tensor &t = table.t[lo];
+        const int64_t base = static_cast<int64_t>(chunk - table.first[lo]) * kStep * h.steps;
+        P *const p0 = static_cast<P *>(t.param) + base;
+        const G *const g0 = static_cast<const G *>(t.grad) + base;
+        S *const m0 = static_cast<S *>(t.m) + base, *const v0 = static_cast<S *>(t.v) + base;
+        uint8_t *const ms0 = k8 ? static_cast<uint8_t *>(t.m_scale) + (base >> 5) : nullptr, *const vs0 = k8 ? static_cast<uint8_t *>(t.v_scale) + (base >> 5) : nullptr;
+        uint16_t *const copy0 = kP16 || t.copy == nullptr ? nullptr : static_cast<uint16_t *>(t.copy) + base;
+        const int here = static_cast<int>(min(t.n - base, static_cast<int64_t>(kStep) * h.steps));
+        const bool wide = ((kP16 ? 0 : reinterpret_cast<uintptr_t>(p0)) | (kG16 ? 0 : reinterpret_cast<uintptr_t>(g0)) |
+                           (k8 ? 0 : reinterpret_cast<uintptr_t>(m0) | reinterpret_cast<uintptr_t>(v0))) % 32 == 0;
+        uint32_t noise_base = 0;
+        if (kNoise) {
+            noise_base = mix_word(hash, h.first_tensor + lo);
+            if (base >> 32) noise_base = mix(noise_base ^ static_cast<uint32_t>(base >> 32));
+            noise_base ^= static_cast<uint32_t>(base);
+        }
+        // kWhole: all threads have eight values; the others' way, value by value, is compiled apart
+        auto step = [&](auto whole, uint32_t i0) {
+            constexpr bool kWhole = decltype(whole)::value;
+            const int left = here - static_cast<int>(i0);      // a thread without values still takes part in its block's maximum
+            uint32_t rp[kVec * sizeof(P) / 4], rg[kVec * sizeof(G) / 4], rm[kVec * sizeof(S) / 4], rv[kVec * sizeof(S) / 4];
+            uint32_t em = 0, ev = 0;
+            if (kWhole || left >= kVec) {
+                load(rp, p0 + i0, wide);
+                load(rg, g0 + i0, wide);
+                load(rm, m0 + i0, wide);
+                load(rv, v0 + i0, wide);
             } else {
-                load_some(r.p, pp, left);
-                load_some(r.g, gp, left);
-                load_some(r.m, mp, left);
-                load_some(r.v, vp, left);
+                load_some(rp, p0 + i0, left);
+                load_some(rg, g0 + i0, left);
+                load_some(rm, m0 + i0, left);
+                load_some(rv, v0 + i0, left);
             }
-            r.em = r.ev = 0;
-            if (k8 && left > 0) {
-                r.em = static_cast<const uint8_t *>(t.m_scale)[i0 >> 5];
-                r.ev = static_cast<const uint8_t *>(t.v_scale)[i0 >> 5];
-            }
-        };
-        const int chunks = static_cast<int>(min(static_cast<uint64_t>(kThreads), (h.chunks - first + gridDim.x - 1) / gridDim.x));
-        for (int k = 0; k < chunks; ++k) {
-            Raw raw;
-            fetch(raw, k);
-            int lo;
-            const int64_t i0 = place(k, lo);
-            const Tensor &t = table.t[lo];
-            const int64_t left = t.n - i0;     // a thread without values still takes part in its block's maximum
-            P *pp = static_cast<P *>(t.param) + i0;
-            S *mp = static_cast<S *>(t.m) + i0, *vp = static_cast<S *>(t.v) + i0;
+            if (k8 && (kWhole || left > 0)) em = ms0[i0 >> 5], ev = vs0[i0 >> 5];
             float p[kVec], g[kVec], m[kVec], v[kVec];
-            unpack<kP16>(p, raw.p);
-            unpack<kG16>(g, raw.g);
-            uint2 cm = make_uint2(raw.m[0], raw.m[1]), cv = make_uint2(raw.v[0], raw.v[1]);
-            uint32_t em = raw.em, ev = raw.ev;
+            unpack<kP16>(p, rp);
+            unpack<kG16>(g, rg);
+            uint2 cm = make_uint2(rm[0], rm[1]), cv = make_uint2(rv[0], rv[1]);
             if constexpr (k8) {
                 decode<3>(m, cm, em);
                 decode<2>(v, cv, ev);
             } else {
-                unpack<false>(m, raw.m);
-                unpack<false>(v, raw.v);
+                unpack<false>(m, rm);
+                unpack<false>(v, rv);
             }
             uint32_t noise[kVec] = {};
             if (kNoise) {
-                uint32_t base = mix_word(hash, h.first_tensor + lo);
-                if (i0 >> 32) base = mix(base ^ static_cast<uint32_t>(i0 >> 32));
-                base ^= static_cast<uint32_t>(i0);
-                base ^= base >> 16;            // mix's first step: i0 is a multiple of eight, so i changes none of the bits that it moves
+                // the place's bits are the chunk's, the thread's and i's; mix's first step moves none of i's
+                uint32_t x = noise_base ^ i0;
+                x ^= x >> 16;
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) noise[i] = mix_rest(base ^ i);
+                for (int i = 0; i < kVec; ++i) noise[i] = mix_rest(x ^ i);
             }
             // products two an instruction, sums one by one: a two-lane sum behind two-lane products would be made one operation with one
             // rounding, and the definition has two
@@ -390,72 +367,77 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
                 for (int i = 0; i < kVec; i += 2) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(packed_p[i / 2]) : "f"(p[i + 1]), "f"(p[i]));
             }
             if constexpr (k8) {
-                if (left < kVec) {
+                if (!kWhole && left < kVec) {
 #pragma unroll
                     for (int i = 0; i < kVec; ++i)
                         if (i >= left) m[i] = v[i] = 0.0f;        // behind the end: nothing that counts for the block
                 }
                 cm = encode<3, kChance>(m, em, noise, odd);
                 cv = encode<2, kChance>(v, ev, noise, odd);
-                if (left > 0 && (threadIdx.x & 3) == 0) {
-                    static_cast<uint8_t *>(t.m_scale)[i0 >> 5] = static_cast<uint8_t>(em);
-                    static_cast<uint8_t *>(t.v_scale)[i0 >> 5] = static_cast<uint8_t>(ev);
-                }
+                if ((kWhole || left > 0) && (threadIdx.x & 3) == 0) ms0[i0 >> 5] = static_cast<uint8_t>(em), vs0[i0 >> 5] = static_cast<uint8_t>(ev);
             }
-            uint16_t *copy = kP16 ? nullptr : static_cast<uint16_t *>(t.copy);
-            if (left >= kVec) {
-                const bool wide = aligned32(t);
+            if (kWhole || left >= kVec) {
                 const uint4 packed = make_uint4(packed_p[0], packed_p[1], packed_p[2], packed_p[3]);
-                if constexpr (kP16) *reinterpret_cast<uint4 *>(pp) = packed;
-                else store(pp, p, wide);
-                if (copy != nullptr) *reinterpret_cast<uint4 *>(copy + i0) = packed;
+                if constexpr (kP16) *reinterpret_cast<uint4 *>(p0 + i0) = packed;
+                else store(p0 + i0, p, wide);
+                if (copy0 != nullptr) *reinterpret_cast<uint4 *>(copy0 + i0) = packed;
                 if constexpr (k8) {
-                    *reinterpret_cast<uint2 *>(mp) = cm;
-                    *reinterpret_cast<uint2 *>(vp) = cv;
+                    *reinterpret_cast<uint2 *>(m0 + i0) = cm;
+                    *reinterpret_cast<uint2 *>(v0 + i0) = cv;
                 } else {
-                    store(mp, m, wide);
-                    store(vp, v, wide);
+                    store(m0 + i0, m, wide);
+                    store(v0 + i0, v, wide);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
                     if (i >= left) continue;
                     const uint16_t short_p = static_cast<uint16_t>(packed_p[i / 2] >> (16 * (i & 1)));
-                    if constexpr (kP16) pp[i] = short_p;
-                    else pp[i] = p[i];
-                    if (copy != nullptr) copy[i0 + i] = short_p;
+                    if constexpr (kP16) p0[i0 + i] = short_p;
+                    else p0[i0 + i] = p[i];
+                    if (copy0 != nullptr) copy0[i0 + i] = short_p;
                     if constexpr (k8) {
-                        mp[i] = static_cast<uint8_t>((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
-                        vp[i] = static_cast<uint8_t>((i < 4 ? cv.x : cv.y) >> (8 * (i & 3)));
+                        m0[i0 + i] = static_cast<uint8_t>((i < 4 ? cm.x : cm.y) >> (8 * (i & 3)));
+                        v0[i0 + i] = static_cast<uint8_t>((i < 4 ? cv.x : cv.y) >> (8 * (i & 3)));
                     } else {
-                        mp[i] = m[i];
-                        vp[i] = v[i];
+                        m0[i0 + i] = m[i];
+                        v0[i0 + i] = v[i];
                     }
                 }
             }
+        };
+#pragma unroll 1
+        for (int from = 0; from < here; from += kStep) {
+            if (from + kStep <= here) step(std::true_type{}, from + threadIdx.x * kVec);
+            else step(std::false_type{}, from + threadIdx.x * kVec);
         }
     }
 }
 
 template <int kN, bool kP16, bool kG16, bool k8, bool kChance>
 sol_status_t launch_table(const Tensor *tensors, Hyper h, cudaStream_t stream, const DeviceInfo *dev) {
-    Table<kN> table;
-    uint64_t chunks = 0;
-    for (int i = 0; i < h.count; ++i) {
-        table.t[i] = tensors[i];
-        table.first[i] = static_cast<uint32_t>(chunks);
-        chunks += static_cast<uint64_t>(ceil_div(tensors[i].n, kChunk));
-        if (chunks > 0xFFFFFFFFull) return SOL_ERR_BAD_SHAPE;
-    }
-    for (int i = h.count; i <= kN; ++i) table.first[i] = static_cast<uint32_t>(chunks);
-    for (int i = h.count; i < kN; ++i) table.t[i] = Tensor{};
-    h.chunks = static_cast<uint32_t>(chunks);
     static int resident = 0;
     if (resident == 0 && cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, step_kernel<kN, kP16, kG16, k8, kChance>, kThreads, 0) != cudaSuccess) {
         cudaGetLastError();
         return SOL_ERR_CUDA;
     }
     const int64_t most = static_cast<int64_t>(resident) * dev->sm_count;
+    // chunks of four steps share the looking for the tensor and its addresses (71 M BF16 values 179 us, with one step 184); with FP32
+    // parameters and 8-bit states one step is faster all the same (193 us, four 213), and where blocks would not get eight chunks each
+    int64_t values = 0;
+    for (int i = 0; i < h.count; ++i) values += tensors[i].n;
+    h.steps = !(k8 && !kP16) && values >= 8 * most * kSteps * kStep ? kSteps : 1;
+    Table<kN> table;
+    uint64_t chunks = 0;
+    for (int i = 0; i < h.count; ++i) {
+        table.t[i] = tensors[i];
+        table.first[i] = static_cast<uint32_t>(chunks);
+        chunks += static_cast<uint64_t>(ceil_div(tensors[i].n, kStep * h.steps));
+        if (chunks > 0xFFFF0000ull) return SOL_ERR_BAD_SHAPE;
+    }
+    for (int i = h.count; i <= kN; ++i) table.first[i] = static_cast<uint32_t>(chunks);
+    for (int i = h.count; i < kN; ++i) table.t[i] = Tensor{};
+    h.chunks = static_cast<uint32_t>(chunks);
     const int64_t grid = static_cast<int64_t>(chunks) < most ? static_cast<int64_t>(chunks) : most;
     step_kernel<kN, kP16, kG16, k8, kChance><<<static_cast<unsigned>(grid < 1 ? 1 : grid), kThreads, 0, stream>>>(table, h);
     return launch_status();

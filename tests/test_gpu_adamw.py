@@ -240,3 +240,33 @@ def test_refused_plans(B):
         B.sol_adamw_step(plan, 1e-3)
     with pytest.raises(B.SolError):
         B.sol_adamw_step(B.sol_adamw_plan([p], [g]), -1.0)
+
+
+def test_large_steps_in_chunks_of_several(B):
+    run = Run(B, [39000037, 5, 8191, 8193, 8192, 100], 32, False, True, True, 14)
+    run.check_step(None)
+
+
+@pytest.mark.parametrize("p16", [True, False])
+def test_large_and_small_plans_agree(B, p16):
+    """To nearest the place in a tensor does not count: a large tensor's slices (on blocks of 32) give what it gives."""
+    n, cut = 40000007, 1000000
+    g = torch.Generator(device="cuda").manual_seed(15)
+    p = (0.05 * torch.randn(n, generator=g, device="cuda")).to(torch.bfloat16 if p16 else torch.float32)
+    grad = (1e-3 * torch.randn(n, generator=g, device="cuda")).to(torch.bfloat16 if p16 else torch.float32)
+    other = p.clone()
+    whole = B.sol_adamw_plan([p], [grad], state_bits=8)
+    for _ in range(2):
+        B.sol_adamw_step(whole, 1e-3)
+    for first in (0, 17 * cut, 39 * cut, 40 * cut - cut):
+        part = slice(first, min(n, first + cut))
+        small = B.sol_adamw_plan([other[part].clone()], [grad[part].clone()], state_bits=8)
+        for _ in range(2):
+            B.sol_adamw_step(small, 1e-3)
+        assert torch.equal(small.params[0], p[part]) and torch.equal(small.m[0], whole.m[0][part]) and torch.equal(small.v[0], whole.v[0][part])
+        assert torch.equal(small.m_scale[0], whole.m_scale[0][first // 32:first // 32 + small.m_scale[0].numel()])
+    last = slice(40 * cut, n)
+    small = B.sol_adamw_plan([other[last].clone()], [grad[last].clone()], state_bits=8)
+    for _ in range(2):
+        B.sol_adamw_step(small, 1e-3)
+    assert torch.equal(small.params[0], p[last]) and torch.equal(small.v[0], whole.v[0][last])
