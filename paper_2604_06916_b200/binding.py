@@ -850,7 +850,7 @@ def sol_layernorm(x, scale=None, shift=None, rows_per_sample: int | None = None,
     scale_ptr = None if scale is None else _dense("scale", scale, torch.bfloat16, (samples, K), index)
     shift_ptr = None if shift is None else _dense("shift", shift, torch.bfloat16, (samples, K), index)
     if out is None:
-        out, ldy = _new(x, (M, K)), K
+        out, ldy = _like(x), K
     else:
         ldy = _rows_view("out", out, index, x.shape)
     stats = _new(x, (M, 2), torch.float32) if with_stats else None
@@ -879,12 +879,12 @@ def sol_layernorm_backward(dy, x, stats, scale=None, rows_per_sample: int | None
     stats_ptr = _dense("stats", stats, torch.float32, (M, 2), index)
     scale_ptr = None if scale is None else _dense("scale", scale, torch.bfloat16, (samples, K), index)
     if out is None:
-        out, ld_dx = _new(dy, (M, K)), K
+        out, ld_dx = _like(dy), K
     else:
         ld_dx = _rows_view("out", out, index, dy.shape)
     dscale = _new(dy, (samples, K), torch.float32) if with_scale else None
     dshift = _new(dy, (samples, K), torch.float32) if with_shift else None
-    need = lib().sol_layernorm_backward_workspace_bytes(M, K, rows) if with_scale or with_shift else 0
+    need = lib().sol_layernorm_backward_workspace_bytes(M, K, rows) if workspace is None and (with_scale or with_shift) else 0
     workspace, ws_ptr, ws_bytes = _scratch(workspace, need, dy, index)
     code = lib().sol_layernorm_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ldx, stats_ptr, scale_ptr, M, K, rows, scale_offset,
                                         out.data_ptr(), ld_dx, _ptr(dscale), _ptr(dshift), ws_ptr, ws_bytes, _raw_stream(index))
@@ -920,7 +920,8 @@ def sol_lora_apply(x, lora_a, lora_b, scaling, offsets, ids, y, with_t: bool = F
         raise ValueError("x and y must have the same rows")
     n, r, requests, a_ptr, b_ptr, s_ptr, o_ptr, i_ptr = _lora_stacks(lora_a, lora_b, scaling, offsets, ids, K, N, index)
     t = _new(x, (M, 2 * r)) if with_t else None
-    workspace, ws_ptr, ws_bytes = _scratch(workspace, lib().sol_lora_workspace_bytes(M, K, N, r, n, requests, 0), x, index)
+    need = 0 if workspace is not None else lib().sol_lora_workspace_bytes(M, K, N, r, n, requests, 0)
+    workspace, ws_ptr, ws_bytes = _scratch(workspace, need, x, index)
     code = lib().sol_lora_apply(x.data_ptr(), ldx, a_ptr, b_ptr, s_ptr, o_ptr, i_ptr, requests, n, y.data_ptr(), ldy, _ptr(t), M, K, N, r,
                                 ws_ptr, ws_bytes, _raw_stream(index))
     if code:
@@ -946,7 +947,8 @@ def sol_lora_backward(dy, x, t, lora_a, lora_b, scaling, offsets, ids, dx: torch
     t_ptr = _dense("t", t, torch.bfloat16, (M, 2 * r), index)
     ld_dx = K if dx is None else _rows_view("dx", dx, index, x.shape)
     da, db = _new(dy, (n, r, K), torch.float32), _new(dy, (n, N, r), torch.float32)
-    workspace, ws_ptr, ws_bytes = _scratch(workspace, lib().sol_lora_workspace_bytes(M, K, N, r, n, requests, 1), dy, index)
+    need = 0 if workspace is not None else lib().sol_lora_workspace_bytes(M, K, N, r, n, requests, 1)
+    workspace, ws_ptr, ws_bytes = _scratch(workspace, need, dy, index)
     code = lib().sol_lora_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ldx, t_ptr, a_ptr, b_ptr, s_ptr, o_ptr, i_ptr, requests, n, _ptr(dx), ld_dx,
                                    da.data_ptr(), db.data_ptr(), M, K, N, r, ws_ptr, ws_bytes, _raw_stream(index))
     if code:

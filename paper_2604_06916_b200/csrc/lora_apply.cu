@@ -629,33 +629,34 @@ add_slices(const float4 *__restrict__ from, int64_t slice4, int slices, int64_t 
 }
 
 // ------------------------------------------------------------------------------------------------ host side
-// How a call's work is shared out: from its sizes alone, so that the workspace's size follows from them too.
-struct Plan {
-    int64_t items;                         // tiles of rows, at most
-    int chunks, slices, per_slice;         // of expand
-    int outer_tiles, outer_tiles_x, outer_slices;
+// How a call's work is shared out: from its sizes alone.
+int64_t items_of(int64_t M, int64_t requests) { return ceil_div(M, kRows) + requests; }     // tiles of rows, at most
+struct Slices {
+    int chunks, slices, per_slice;         // 64-column chunks of expand's y, and how blocks share them
 };
-Plan plan_of(int64_t M, int64_t from, int64_t to, int64_t requests, int64_t adapters) {     // shrink over `from` columns, expand to `to`
-    Plan p;
-    p.items = ceil_div(M, kRows) + requests;
+Slices expand_slices(int64_t items, int64_t columns) {
     // the number of slices with the least (waves + 1/2) (chunks of a block + 4): a block's way in and out is worth some four chunks, and half
-    // a wave stands for slots that stay empty at the end and behind short requests
-    p.chunks = static_cast<int>(ceil_div(to, kBox));
-    int64_t slices = 1;
+    // a wave stands for slots that stay empty at the end and behind short requests.  Every number of slices once, with the fewest chunks
+    Slices best{static_cast<int>(ceil_div(columns, kBox)), 1, 0};
     double least = 0.0;
-    for (int64_t per = p.chunks; per >= 1; --per) {
-        const int64_t n = ceil_div(p.chunks, per);
-        const double waves = static_cast<double>(p.items * n) / kSlots, cost = ((waves < 1.0 ? 1.0 : waves) + 0.5) * static_cast<double>(per + 4);
-        if (per == p.chunks || cost < least) least = cost, slices = n;
+    for (int64_t per = best.chunks; per >= 1; --per) {
+        const int64_t n = ceil_div(best.chunks, per);
+        per = ceil_div(best.chunks, n);
+        const double waves = static_cast<double>(items * n) / kSlots, cost = ((waves < 1.0 ? 1.0 : waves) + 0.5) * static_cast<double>(per + 4);
+        if (best.per_slice == 0 || cost < least) least = cost, best.slices = static_cast<int>(n), best.per_slice = static_cast<int>(per);
     }
-    p.per_slice = static_cast<int>(ceil_div(p.chunks, slices));
-    p.slices = static_cast<int>(ceil_div(p.chunks, p.per_slice));
-    // gradients of the factors: `from` is dy's width, `to` that of x
-    p.outer_tiles_x = static_cast<int>(ceil_div(to, 128));
-    p.outer_tiles = p.outer_tiles_x + static_cast<int>(ceil_div(from, 128));
-    int64_t rows = kSlots / (p.outer_tiles * adapters);
-    if (rows > ceil_div(M, 512)) rows = ceil_div(M, 512);
-    p.outer_slices = rows < 1 ? 1 : static_cast<int>(rows);
+    return best;
+}
+struct OuterPlan {
+    int tiles, tiles_x, slices;
+};
+OuterPlan outer_plan(int64_t M, int64_t K, int64_t N, int64_t adapters) {
+    OuterPlan p;
+    p.tiles_x = static_cast<int>(ceil_div(K, 128));
+    p.tiles = p.tiles_x + static_cast<int>(ceil_div(N, 128));
+    int64_t slices = kSlots / (p.tiles * adapters);
+    if (slices > ceil_div(M, 512)) slices = ceil_div(M, 512);
+    p.slices = slices < 1 ? 1 : static_cast<int>(slices);
     return p;
 }
 int64_t pad256(int64_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -738,24 +739,26 @@ int shrink_splits(int64_t items, int tiles, int smem) {
     return 1;
 }
 template <bool kFlip>
-sol_status_t launch_shrink(const Requests &q, const void *x, int64_t ldx, const void *factor, int64_t cols, int64_t r, const Plan &plan,
-                           const float *scaling, void *parts, int n_parts, cudaStream_t stream) {
+sol_status_t launch_shrink(const Requests &q, const void *x, int64_t ldx, const void *factor, int64_t cols, int64_t r, const float *scaling,
+                           void *parts, int n_parts, cudaStream_t stream) {
     const int r16 = static_cast<int>(ceil_div(r, 16) * 16), tiles = static_cast<int>(ceil_div(cols, 2 * kBox)), smem = kControl + kShrinkStages * kShrinkStage;
     CUtensorMap tm_x, tm_f;
     if (!rows_map(&tm_x, x, cols, q.rows, ldx, kRows)) return SOL_ERR_CUDA;
     if (!(kFlip ? factor_map(&tm_f, factor, r, cols, q.adapters, kBox) : factor_map(&tm_f, factor, cols, r, q.adapters, r16))) return SOL_ERR_CUDA;
     if (!allow_smem<shrink_kernel<kFlip>>(smem)) return SOL_ERR_CUDA;
-    const int per = static_cast<int>(ceil_div(tiles, shrink_splits<kFlip>(plan.items, tiles, smem))), splits = static_cast<int>(ceil_div(tiles, per));
+    const int64_t items = items_of(q.rows, q.requests);
+    const int per = static_cast<int>(ceil_div(tiles, shrink_splits<kFlip>(items, tiles, smem))), splits = static_cast<int>(ceil_div(tiles, per));
     const Shrink p{q, scaling, static_cast<uint16_t *>(parts), device_status_word(), n_parts, static_cast<int>(r), r16, tiles, per, splits, kShrinkStages};
-    return launch<false>(shrink_kernel<kFlip>, plan.items * splits, 192, smem, splits, stream, tm_x, tm_f, p);
+    return launch<false>(shrink_kernel<kFlip>, items * splits, 192, smem, splits, stream, tm_x, tm_f, p);
 }
 template <bool kFlip>
-sol_status_t launch_expand(const Requests &q, const void *parts, int n_parts, const float *scaling, void *y, int64_t ldy, const void *factor, int64_t cols, int64_t r,
-                           const Plan &plan, cudaStream_t stream) {
+sol_status_t launch_expand(const Requests &q, const void *parts, int n_parts, const float *scaling, void *y, int64_t ldy, const void *factor, int64_t cols, int64_t r, cudaStream_t stream) {
     const int r16 = static_cast<int>(ceil_div(r, 16) * 16);
     CUtensorMap tm_y, tm_out, tm_f;
     if (!rows_map(&tm_y, y, cols, q.rows, ldy, kRows) || !rows_map(&tm_out, y, cols, q.rows, ldy, 32)) return SOL_ERR_CUDA;
     if (!(kFlip ? factor_map(&tm_f, factor, cols, r, q.adapters, r16) : factor_map(&tm_f, factor, r, cols, q.adapters, kBox))) return SOL_ERR_CUDA;
+    const int64_t items = items_of(q.rows, q.requests);
+    const Slices plan = expand_slices(items, cols);
     const int t_bytes = static_cast<int>(ceil_div(2 * r16, kBox)) * kRowBox;
     Expand p{q, static_cast<const uint16_t *>(parts), scaling, n_parts, static_cast<uint16_t *>(y), device_status_word(), ldy, static_cast<int>(r), r16,
              0, static_cast<int>(cols), plan.chunks, plan.per_slice, plan.slices};
@@ -763,7 +766,7 @@ sol_status_t launch_expand(const Requests &q, const void *parts, int n_parts, co
     p.stages = ((t_bytes == kRowBox ? kHalfSmem : kFullSmem) - kControl - t_bytes) / kStage;
     if (p.stages > kMaxStages) p.stages = kMaxStages;
     if (!allow_smem<expand_kernel<kFlip>>(kFullSmem)) return SOL_ERR_CUDA;
-    return launch<true>(expand_kernel<kFlip>, plan.items * p.slices, 320, kControl + t_bytes + p.stages * kStage, 1, stream, tm_y, tm_out, tm_f, p);
+    return launch<true>(expand_kernel<kFlip>, items * p.slices, 320, kControl + t_bytes + p.stages * kStage, 1, stream, tm_y, tm_out, tm_f, p);
 }
 
 }  // namespace
@@ -773,26 +776,26 @@ int max_requests() { return kMaxRequests; }
 
 size_t workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, bool backward) {
     if (!backward) return static_cast<size_t>(parts_bytes(M, r, kTParts));
-    const Plan p = plan_of(M, N, K, requests, adapters);
-    return static_cast<size_t>(parts_bytes(M, r, kDtParts) + (p.outer_slices > 1 ? 4 * p.outer_slices * adapters * r * (K + N) : 0));
+    (void)requests;
+    const int slices = outer_plan(M, K, N, adapters).slices;
+    return static_cast<size_t>(parts_bytes(M, r, kDtParts) + (slices > 1 ? 4 * slices * adapters * r * (K + N) : 0));
 }
 
 sol_status_t launch_apply(const Call &c, const void *x, int64_t ldx, void *y, int64_t ldy, void *t_out, void *workspace, cudaStream_t stream) {
     const Requests q{c.offsets, c.ids, static_cast<int>(c.requests), static_cast<int>(c.adapters), static_cast<int>(c.M)};
-    const Plan plan = plan_of(c.M, c.K, c.N, c.requests, c.adapters);
     void *parts = t_out != nullptr ? t_out : workspace;
-    const sol_status_t st = launch_shrink<false>(q, x, ldx, c.a, c.K, c.r, plan, nullptr, parts, kTParts, stream);
+    const sol_status_t st = launch_shrink<false>(q, x, ldx, c.a, c.K, c.r, nullptr, parts, kTParts, stream);
     if (st != SOL_OK) return st;
-    return launch_expand<false>(q, parts, kTParts, c.scaling, y, ldy, c.b, c.N, c.r, plan, stream);
+    return launch_expand<false>(q, parts, kTParts, c.scaling, y, ldy, c.b, c.N, c.r, stream);
 }
 
 sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const void *x, int64_t ldx, const void *t, void *dx, int64_t ld_dx,
                              float *da, float *db, void *workspace, cudaStream_t stream) {
     const Requests q{c.offsets, c.ids, static_cast<int>(c.requests), static_cast<int>(c.adapters), static_cast<int>(c.M)};
-    const Plan plan = plan_of(c.M, c.N, c.K, c.requests, c.adapters);
+    const OuterPlan plan = outer_plan(c.M, c.K, c.N, c.adapters);
     uint8_t *dt = static_cast<uint8_t *>(workspace);
     float *sums = reinterpret_cast<float *>(dt + parts_bytes(c.M, c.r, kDtParts));
-    sol_status_t st = launch_shrink<true>(q, dy, ld_dy, c.b, c.N, c.r, plan, c.scaling, dt, kDtParts, stream);
+    sol_status_t st = launch_shrink<true>(q, dy, ld_dy, c.b, c.N, c.r, c.scaling, dt, kDtParts, stream);
     if (st != SOL_OK) return st;
     // the factors' gradients next, while L2 still holds a part of dy
     CUtensorMap tm_x, tm_dy, tm_dt, tm_t;
@@ -800,20 +803,20 @@ sol_status_t launch_backward(const Call &c, const void *dy, int64_t ld_dy, const
         !rows_map(&tm_dt, dt, kDtParts * c.r, c.M, kDtParts * c.r, kStepRows) || !rows_map(&tm_t, t, kTParts * c.r, c.M, kTParts * c.r, kStepRows))
         return SOL_ERR_CUDA;
     const int64_t da_floats = c.adapters * c.r * c.K, db_floats = c.adapters * c.r * c.N;
-    const bool sliced = plan.outer_slices > 1;
+    const bool sliced = plan.slices > 1;
     const Outer p{q, c.scaling, sliced ? sums : da, sliced ? sums + da_floats : db, da_floats + db_floats, device_status_word(), static_cast<int>(c.r),
-                  static_cast<int>(c.K), static_cast<int>(c.N), plan.outer_tiles_x, plan.outer_tiles, plan.outer_slices, kDtParts, kTParts};
+                  static_cast<int>(c.K), static_cast<int>(c.N), plan.tiles_x, plan.tiles, plan.slices, kDtParts, kTParts};
     if (!allow_smem<outer_kernel>(kHalfSmem)) return SOL_ERR_CUDA;
-    st = launch<true>(outer_kernel, static_cast<int64_t>(plan.outer_tiles) * plan.outer_slices * c.adapters, 192, kHalfSmem, 1,
+    st = launch<true>(outer_kernel, static_cast<int64_t>(plan.tiles) * plan.slices * c.adapters, 192, kHalfSmem, 1,
                       stream, tm_x, tm_dy, tm_dt, tm_t, p);
     if (st != SOL_OK) return st;
     if (sliced) {
         const int64_t slice4 = (da_floats + db_floats) / 4;
-        st = launch<true>(add_slices, ceil_div(slice4, 256), 256, 0, 1, stream, reinterpret_cast<const float4 *>(sums), slice4, plan.outer_slices,
+        st = launch<true>(add_slices, ceil_div(slice4, 256), 256, 0, 1, stream, reinterpret_cast<const float4 *>(sums), slice4, plan.slices,
                           da_floats / 4, reinterpret_cast<float4 *>(da), reinterpret_cast<float4 *>(db));
         if (st != SOL_OK) return st;
     }
-    return dx != nullptr ? launch_expand<true>(q, dt, kDtParts, nullptr, dx, ld_dx, c.a, c.K, c.r, plan, stream) : SOL_OK;
+    return dx != nullptr ? launch_expand<true>(q, dt, kDtParts, nullptr, dx, ld_dx, c.a, c.K, c.r, stream) : SOL_OK;
 }
 
 }  // namespace lora
