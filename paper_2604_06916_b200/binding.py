@@ -972,6 +972,8 @@ class AdamWPlan:
             raise ValueError("no parameters")
         if state_bits not in _ADAMW_STATES:
             raise ValueError("state_bits must be 32 or 8")
+        if step < 0:
+            raise ValueError("step: the steps that the states have behind them, 0 or more")
         self.index, self.state_bits, self.params = params[0].get_device(), state_bits, params
         if self.index < 0:
             raise TypeError("sol_adamw_plan: expected CUDA tensors")

@@ -351,6 +351,7 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
         if (ptx::elect_one() && !loads_held(p.status)) {
             const uint32_t factor_bytes = kFlip ? p.r16 * 128 : kFactorBox;
             for (int c = c0, s = 0, n = 0; c < c1; ++c, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
+                if (n == p.stages) ptx::grid_dependency_wait();      // a wait's limit counts from when what it waits for can come
                 if (n >= p.stages && !wait_bounded(bar(kMaxStages + s), ((n / p.stages) - 1) & 1u, abort_flag, p.status, 0xD30u | s)) break;
                 const uint32_t to = ring + s * kStage;
                 ptx::mbar_arrive_expect_tx(bar(s), kRowBox + factor_bytes);
@@ -364,6 +365,7 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
         if (ptx::elect_one()) {
             const uint32_t idesc = idesc_of(kBox, false, kFlip);
             const int half = p.r16 >> 4;          // products for each of t's parts
+            ptx::grid_dependency_wait();
             bool ok = wait_bounded(bar(kReady), 0, abort_flag, p.status, 0xD40u);
             for (int c = c0, s = 0, n = 0; ok && c < c1; ++c, ++n, s = s + 1 == p.stages ? 0 : s + 1) {
                 const int d = n % kSums;
@@ -538,6 +540,7 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
         }
         __syncwarp();
     } else if (warp == 1) {
+        ptx::grid_dependency_wait();          // the waits' limits count from here
         const uint32_t idesc = idesc_of(n_columns, true, true);
         int s = 0, n = 0;
         bool ok = true;
@@ -567,6 +570,7 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
             }
         }
     } else {
+        ptx::grid_dependency_wait();
         const int quad = warp & 3, c = column + quad * 32 + lane;
         const uint32_t lanes_at = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         float v[kMaxRank] = {};

@@ -228,7 +228,7 @@ def test_refused_plans(B):
     p, g = torch.zeros(64, device="cuda"), torch.zeros(64, device="cuda")
     for bad in (lambda: B.sol_adamw_plan([p, p], [g, g]), lambda: B.sol_adamw_plan([p], [g[:32]]), lambda: B.sol_adamw_plan([p], [g, g]),
                 lambda: B.sol_adamw_plan([p.half()], [g]), lambda: B.sol_adamw_plan([p], [g.half()]), lambda: B.sol_adamw_plan([p[::2]], [g[:32]]),
-                lambda: B.sol_adamw_plan([p], [g], state_bits=16), lambda: B.sol_adamw_plan([p], [g], copies=[p]),
+                lambda: B.sol_adamw_plan([p], [g], state_bits=16), lambda: B.sol_adamw_plan([p], [g], step=-1), lambda: B.sol_adamw_plan([p], [g], copies=[p]),
                 lambda: B.sol_adamw_plan([p.bfloat16()], [g], copies=[p.bfloat16()]), lambda: B.sol_adamw_plan([p], [g.cpu()]),
                 lambda: B.sol_adamw_plan([p], [g], states={"m": [p], "v": [p[:3]]})):
         with pytest.raises((TypeError, ValueError)):
