@@ -307,18 +307,19 @@ sol_status_t nvfp4_layernorm_quantize(const void *x_bf16, int64_t M, int64_t K, 
  *     xhat = (x - mean) rstd,  rstd = 1 / sqrt(var + eps);   y[m,k] = bf16_rne( xhat (scale_offset + scale[s,k]) + shift[s,k] )
  *     s = m / rows_per_sample:  scale_offset = 1 is the modulation above, 0 a plain weight (one sample: rows_per_sample >= M)
  *   x_bf16       [M, K] BF16, pitch ldx;  K % 8 == 0, K <= 16384;  y_bf16  [M, K], pitch ldy; may be x with the same pitch
- *   scale, shift [ceil(M / rows_per_sample), K] BF16, dense; either may be NULL (gain 1, shift 0)
+ *   scale, shift [ceil(M / rows_per_sample), K] BF16, pitch ld_mod (slices of one modulation vector per sample will do); either may
+ *                be NULL (gain 1, shift 0)
  *   stats_out    [M, 2] FP32 (mean, rstd), 8-byte aligned, or NULL;  eps >= 0 (with eps = 0 a constant row gives NaN)
  */
 sol_status_t sol_layernorm(const void *x_bf16, int64_t M, int64_t K, int64_t ldx, const void *scale_bf16, const void *shift_bf16,
-                           int64_t rows_per_sample, float scale_offset, float eps, void *y_bf16, int64_t ldy, float *stats_out,
+                           int64_t ld_mod, int64_t rows_per_sample, float scale_offset, float eps, void *y_bf16, int64_t ldy, float *stats_out,
                            void *stream);
 
 /*
  * Gradients of sol_layernorm from dy = d loss / d y, with w = dy (scale_offset + scale):
  *     dx = rstd (w - mean(w) - xhat mean(w xhat)),   dscale[s] = sum over the sample's rows of dy xhat,   dshift[s] = sum of dy
  *   dy, x, dx      [M, K] BF16 with pitches; x and stats [M, 2] are the forward call's; dx may be dy or x, with the same pitch
- *   scale          the forward call's, or NULL
+ *   scale          the forward call's, pitch ld_scale, or NULL
  *   dscale, dshift [ceil(M / rows_per_sample), K] FP32, dense, 16-byte aligned, overwritten; either may be NULL
  *   workspace      sol_layernorm_backward_workspace_bytes(...) bytes of device scratch, 256-byte aligned (the size may be 0:
  *                  NULL will do).  Two calls that may overlap need one each.
@@ -326,8 +327,8 @@ sol_status_t sol_layernorm(const void *x_bf16, int64_t M, int64_t K, int64_t ldx
  */
 size_t sol_layernorm_backward_workspace_bytes(int64_t M, int64_t K, int64_t rows_per_sample);
 sol_status_t sol_layernorm_backward(const void *dy_bf16, int64_t ld_dy, const void *x_bf16, int64_t ldx, const float *stats,
-                                    const void *scale_bf16, int64_t M, int64_t K, int64_t rows_per_sample, float scale_offset,
-                                    void *dx_bf16, int64_t ld_dx, float *dscale, float *dshift, void *workspace,
+                                    const void *scale_bf16, int64_t ld_scale, int64_t M, int64_t K, int64_t rows_per_sample,
+                                    float scale_offset, void *dx_bf16, int64_t ld_dx, float *dscale, float *dshift, void *workspace,
                                     size_t workspace_bytes, void *stream);
 
 /*

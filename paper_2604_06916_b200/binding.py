@@ -132,9 +132,9 @@ def lib() -> ctypes.CDLL:
     L.sol_rotary_frequencies.restype = i32
     L.sol_rotary_frequencies.argtypes = [i64, f64, i32, f64, f64, f64, f64, vp, vp]
     L.sol_layernorm.restype = i32
-    L.sol_layernorm.argtypes = [vp, i64, i64, i64, vp, vp, i64, f32, f32, vp, i64, vp, vp]
+    L.sol_layernorm.argtypes = [vp, i64, i64, i64, vp, vp, i64, i64, f32, f32, vp, i64, vp, vp]
     L.sol_layernorm_backward.restype = i32
-    L.sol_layernorm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, f32, vp, i64, vp, vp, vp, sz, vp]
+    L.sol_layernorm_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, f32, vp, i64, vp, vp, vp, sz, vp]
     L.sol_layernorm_backward_workspace_bytes.restype = sz
     L.sol_layernorm_backward_workspace_bytes.argtypes = [i64, i64, i64]
     L.sol_adamw_step.restype, L.sol_adamw_step.argtypes = i32, [vp, i64, vp, vp, vp]
@@ -839,22 +839,24 @@ def sol_layernorm(x, scale=None, shift=None, rows_per_sample: int | None = None,
                   out: torch.Tensor | None = None, with_stats: bool = False):
     """LN(x) * (scale_offset + scale[sample]) + shift[sample] in BF16; scale_offset 1: modulation, 0: a weight and a bias.
 
-    x [M, K] (a view with a row pitch will do); scale and shift [samples, K] or None, a sample being `rows_per_sample` rows (default:
-    all).  Returns y, or (y, stats) `with_stats`: FP32 [M, 2] mean and 1 / sqrt(var + eps) for sol_layernorm_backward.
+    x [M, K] (a view with a row pitch will do); scale and shift [samples, K] or None (slices of one modulation tensor will do, both
+    with its pitch), a sample being `rows_per_sample` rows (default: all).  Returns y, or (y, stats) `with_stats`: FP32 [M, 2] mean and 1 / sqrt(var + eps) for sol_layernorm_backward.
     """
     index = x.get_device()
     ldx = _rows_view("x", x, index)
     M, K = x.shape
     rows = M if rows_per_sample is None else rows_per_sample
     samples = -(-M // rows) if rows > 0 else 0
-    scale_ptr = None if scale is None else _dense("scale", scale, torch.bfloat16, (samples, K), index)
-    shift_ptr = None if shift is None else _dense("shift", shift, torch.bfloat16, (samples, K), index)
+    ld_scale = None if scale is None else _rows_view("scale", scale, index, (samples, K))
+    ld_mod = ld_scale if shift is None else _rows_view("shift", shift, index, (samples, K))
+    if ld_scale is not None and ld_scale != ld_mod:
+        raise ValueError("scale and shift must have the same row pitch")
     if out is None:
         out, ldy = _like(x), K
     else:
         ldy = _rows_view("out", out, index, x.shape)
     stats = _new(x, (M, 2), torch.float32) if with_stats else None
-    code = lib().sol_layernorm(x.data_ptr(), M, K, ldx, scale_ptr, shift_ptr, rows, scale_offset, eps, out.data_ptr(), ldy,
+    code = lib().sol_layernorm(x.data_ptr(), M, K, ldx, _ptr(scale), _ptr(shift), ld_mod or K, rows, scale_offset, eps, out.data_ptr(), ldy,
                                None if stats is None else stats.data_ptr(), _raw_stream(index))
     if code:
         raise SolError(code, "sol_layernorm")
@@ -877,7 +879,7 @@ def sol_layernorm_backward(dy, x, stats, scale=None, rows_per_sample: int | None
     rows = M if rows_per_sample is None else rows_per_sample
     samples = -(-M // rows) if rows > 0 else 0
     stats_ptr = _dense("stats", stats, torch.float32, (M, 2), index)
-    scale_ptr = None if scale is None else _dense("scale", scale, torch.bfloat16, (samples, K), index)
+    ld_scale = K if scale is None else _rows_view("scale", scale, index, (samples, K))
     if out is None:
         out, ld_dx = _like(dy), K
     else:
@@ -886,7 +888,7 @@ def sol_layernorm_backward(dy, x, stats, scale=None, rows_per_sample: int | None
     dshift = _new(dy, (samples, K), torch.float32) if with_shift else None
     need = lib().sol_layernorm_backward_workspace_bytes(M, K, rows) if workspace is None and (with_scale or with_shift) else 0
     workspace, ws_ptr, ws_bytes = _scratch(workspace, need, dy, index)
-    code = lib().sol_layernorm_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ldx, stats_ptr, scale_ptr, M, K, rows, scale_offset,
+    code = lib().sol_layernorm_backward(dy.data_ptr(), ld_dy, x.data_ptr(), ldx, stats_ptr, _ptr(scale), ld_scale, M, K, rows, scale_offset,
                                         out.data_ptr(), ld_dx, _ptr(dscale), _ptr(dshift), ws_ptr, ws_bytes, _raw_stream(index))
     if code:
         raise SolError(code, "sol_layernorm_backward")

@@ -805,16 +805,19 @@ static bool norm_shape_ok(int64_t M, int64_t K, int64_t rows_per_sample) {
     return M > 0 && M <= 0x7FFFFFFFLL && K > 0 && K % 8 == 0 && K <= norm::max_k() && rows_per_sample > 0;
 }
 
-sol_status_t sol_layernorm(const void *x, int64_t M, int64_t K, int64_t ldx, const void *scale, const void *shift,
+sol_status_t sol_layernorm(const void *x, int64_t M, int64_t K, int64_t ldx, const void *scale, const void *shift, int64_t ld_mod,
                            int64_t rows_per_sample, float scale_offset, float eps, void *y, int64_t ldy, float *stats, void *stream) {
     if (x == nullptr || y == nullptr) return SOL_ERR_NULL_POINTER;
-    if (!norm_shape_ok(M, K, rows_per_sample) || ldx < K || ldy < K || !(eps >= 0.0f) || !std::isfinite(scale_offset)) return SOL_ERR_BAD_SHAPE;
-    if (!aligned16(x) || !aligned16(y) || !aligned16(scale) || !aligned16(shift) || ldx % 8 != 0 || ldy % 8 != 0 || !aligned8(stats))
+    if (!norm_shape_ok(M, K, rows_per_sample) || ldx < K || ldy < K || !(eps >= 0.0f) || !std::isfinite(scale_offset) ||
+        ((scale != nullptr || shift != nullptr) && ld_mod < K))
+        return SOL_ERR_BAD_SHAPE;
+    if (!aligned16(x) || !aligned16(y) || !aligned16(scale) || !aligned16(shift) || ldx % 8 != 0 || ldy % 8 != 0 || !aligned8(stats) ||
+        ((scale != nullptr || shift != nullptr) && ld_mod % 8 != 0))
         return SOL_ERR_ALIGNMENT;
     const DeviceInfo *dev = nullptr;
     const sol_status_t st = check_arch(&dev);
     if (st != SOL_OK) return st;
-    return norm::launch_forward(x, M, K, ldx, scale, shift, rows_per_sample < M ? rows_per_sample : M, scale_offset, eps, y, ldy, stats,
+    return norm::launch_forward(x, M, K, ldx, scale, shift, ld_mod, rows_per_sample < M ? rows_per_sample : M, scale_offset, eps, y, ldy, stats,
                                 static_cast<cudaStream_t>(stream), dev);
 }
 
@@ -823,12 +826,13 @@ size_t sol_layernorm_backward_workspace_bytes(int64_t M, int64_t K, int64_t rows
 }
 
 sol_status_t sol_layernorm_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ldx, const float *stats, const void *scale,
-                                    int64_t M, int64_t K, int64_t rows_per_sample, float scale_offset, void *dx, int64_t ld_dx,
+                                    int64_t ld_scale, int64_t M, int64_t K, int64_t rows_per_sample, float scale_offset, void *dx, int64_t ld_dx,
                                     float *dscale, float *dshift, void *workspace, size_t workspace_bytes, void *stream) {
     if (dy == nullptr || x == nullptr || stats == nullptr || dx == nullptr) return SOL_ERR_NULL_POINTER;
-    if (!norm_shape_ok(M, K, rows_per_sample) || ld_dy < K || ldx < K || ld_dx < K || !std::isfinite(scale_offset)) return SOL_ERR_BAD_SHAPE;
+    if (!norm_shape_ok(M, K, rows_per_sample) || ld_dy < K || ldx < K || ld_dx < K || !std::isfinite(scale_offset) || (scale != nullptr && ld_scale < K))
+        return SOL_ERR_BAD_SHAPE;
     if (!aligned16(dy) || !aligned16(x) || !aligned16(dx) || !aligned16(scale) || !aligned16(dscale) || !aligned16(dshift) ||
-        !aligned8(stats) || ld_dy % 8 != 0 || ldx % 8 != 0 || ld_dx % 8 != 0)
+        !aligned8(stats) || ld_dy % 8 != 0 || ldx % 8 != 0 || ld_dx % 8 != 0 || (scale != nullptr && ld_scale % 8 != 0))
         return SOL_ERR_ALIGNMENT;
     if (rows_per_sample > M) rows_per_sample = M;
     const size_t need = dscale != nullptr || dshift != nullptr ? norm::backward_workspace_bytes(M, K, rows_per_sample) : 0;
@@ -840,7 +844,7 @@ sol_status_t sol_layernorm_backward(const void *dy, int64_t ld_dy, const void *x
     const DeviceInfo *dev = nullptr;
     const sol_status_t st = check_arch(&dev);
     if (st != SOL_OK) return st;
-    return norm::launch_backward(dy, ld_dy, x, ldx, stats, scale, M, K, rows_per_sample, scale_offset, dx, ld_dx, dscale, dshift,
+    return norm::launch_backward(dy, ld_dy, x, ldx, stats, scale, ld_scale, M, K, rows_per_sample, scale_offset, dx, ld_dx, dscale, dshift,
                                  static_cast<float *>(workspace), static_cast<cudaStream_t>(stream), dev);
 }
 

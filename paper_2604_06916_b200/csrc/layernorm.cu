@@ -66,10 +66,10 @@ __device__ __forceinline__ uint4 load8(const uint16_t *p) { return __ldcs(reinte
 __device__ __forceinline__ uint4 cached8(const uint16_t *p) { return __ldg(reinterpret_cast<const uint4 *>(p)); }
 
 struct Forward {
-    const uint16_t *x, *scale, *shift;   // scale, shift: [samples, K] or null
+    const uint16_t *x, *scale, *shift;   // scale, shift: [samples, K], pitch ld_mod, or null
     uint16_t *y;
     float2 *stats;                       // [M] (mean, rstd) or null
-    int64_t ldx, ldy;
+    int64_t ldx, ldy, ld_mod;
     uint32_t rows, rows_per_sample;
     int K;
     float offset, eps, inv_k;
@@ -114,7 +114,7 @@ forward_kernel(const Forward p) {
         if (left == 0) {
             const uint32_t sample = m / p.rows_per_sample;
             left = p.rows_per_sample - (m - sample * p.rows_per_sample);
-            const int64_t s = static_cast<int64_t>(sample) * p.K;
+            const int64_t s = static_cast<int64_t>(sample) * p.ld_mod;
 #pragma unroll
             for (int i = 0; i < kChunks; ++i) {
                 const int c = 8 * (lane + i * kLanes);
@@ -173,7 +173,7 @@ struct Backward {
     uint16_t *dx;
     float *dscale, *dshift;     // [samples, K] or null
     float *partials;            // [items][2][K] where a sample has several pieces
-    int64_t ld_dy, ld_x, ld_dx;
+    int64_t ld_dy, ld_x, ld_dx, ld_scale;
     uint32_t rows, rows_per_sample;
     int K, samples, pieces;     // pieces of a sample
     int warps_per_row;
@@ -238,7 +238,7 @@ backward_kernel(const Backward p) {
         for (int i = 0; i < kChunks; ++i) {
             uint4 g = make_uint4(0, 0, 0, 0);
             const bool there = at + i * lanes < columns8;
-            if (p.scale != nullptr && there) g = cached8(p.scale + static_cast<int64_t>(sample) * p.K + 8 * (at + i * lanes));
+            if (p.scale != nullptr && there) g = cached8(p.scale + static_cast<int64_t>(sample) * p.ld_scale + 8 * (at + i * lanes));
             const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -451,11 +451,11 @@ sol_status_t forward_by_chunks(const Forward &p, cudaStream_t stream, const Devi
 
 int max_k() { return kMaxK; }
 
-sol_status_t launch_forward(const void *x, int64_t M, int64_t K, int64_t ldx, const void *scale, const void *shift,
+sol_status_t launch_forward(const void *x, int64_t M, int64_t K, int64_t ldx, const void *scale, const void *shift, int64_t ld_mod,
                             int64_t rows_per_sample, float offset, float eps, void *y, int64_t ldy, float *stats, cudaStream_t stream,
                             const DeviceInfo *dev) {
     const Forward p{static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(scale), static_cast<const uint16_t *>(shift),
-                    static_cast<uint16_t *>(y), reinterpret_cast<float2 *>(stats), ldx, ldy, static_cast<uint32_t>(M),
+                    static_cast<uint16_t *>(y), reinterpret_cast<float2 *>(stats), ldx, ldy, ld_mod, static_cast<uint32_t>(M),
                     static_cast<uint32_t>(rows_per_sample), static_cast<int>(K), scale != nullptr ? offset : 1.0f, eps,
                     1.0f / static_cast<float>(K)};
     if (K <= 768) return forward_by_chunks<1>(p, stream, dev);
@@ -470,15 +470,15 @@ size_t backward_workspace_bytes(int64_t M, int64_t K, int64_t rows_per_sample) {
     return pieces == 1 ? 0 : sizeof(float) * 2 * static_cast<size_t>(K) * static_cast<size_t>(pieces) * static_cast<size_t>(ceil_div(M, rows_per_sample));
 }
 
-sol_status_t launch_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const float *stats, const void *scale, int64_t M,
-                             int64_t K, int64_t rows_per_sample, float offset, void *dx, int64_t ld_dx, float *dscale, float *dshift,
+sol_status_t launch_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const float *stats, const void *scale,
+                             int64_t ld_scale, int64_t M, int64_t K, int64_t rows_per_sample, float offset, void *dx, int64_t ld_dx, float *dscale, float *dshift,
                              float *partials, cudaStream_t stream, const DeviceInfo *dev) {
     const Shape s = shape_of(K);
     const int64_t samples = ceil_div(M, rows_per_sample);
     const int blocks = dev->sm_count < kMaxItems ? dev->sm_count : kMaxItems;
     const Backward p{static_cast<const uint16_t *>(dy), static_cast<const uint16_t *>(x), static_cast<const uint16_t *>(scale),
                      reinterpret_cast<const float2 *>(stats), static_cast<uint16_t *>(dx), dscale, dshift, partials,
-                     ld_dy, ld_x, ld_dx, static_cast<uint32_t>(M), static_cast<uint32_t>(rows_per_sample),
+                     ld_dy, ld_x, ld_dx, ld_scale, static_cast<uint32_t>(M), static_cast<uint32_t>(rows_per_sample),
                      static_cast<int>(K), static_cast<int>(samples), pieces_of(M, rows_per_sample, s, blocks), s.warps_per_row,
                      scale != nullptr ? offset : 1.0f, 1.0f / static_cast<float>(K)};
     const int64_t items = samples * p.pieces;

@@ -205,12 +205,12 @@ sol_status_t launch_backward(const Grads2 &g, const Turn &t, int64_t rows, int64
 // Layer norm with modulation or a weight in BF16, and its gradients (scale null: gain 1).
 namespace norm {
 int max_k();
-sol_status_t launch_forward(const void *x, int64_t M, int64_t K, int64_t ldx, const void *scale, const void *shift,
+sol_status_t launch_forward(const void *x, int64_t M, int64_t K, int64_t ldx, const void *scale, const void *shift, int64_t ld_mod,
                             int64_t rows_per_sample, float offset, float eps, void *y, int64_t ldy, float *stats, cudaStream_t stream,
                             const DeviceInfo *dev);
 size_t backward_workspace_bytes(int64_t M, int64_t K, int64_t rows_per_sample);
-sol_status_t launch_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const float *stats, const void *scale, int64_t M,
-                             int64_t K, int64_t rows_per_sample, float offset, void *dx, int64_t ld_dx, float *dscale, float *dshift,
+sol_status_t launch_backward(const void *dy, int64_t ld_dy, const void *x, int64_t ld_x, const float *stats, const void *scale,
+                             int64_t ld_scale, int64_t M, int64_t K, int64_t rows_per_sample, float offset, void *dx, int64_t ld_dx, float *dscale, float *dshift,
                              float *partials, cudaStream_t stream, const DeviceInfo *dev);
 }
 

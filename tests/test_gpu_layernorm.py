@@ -197,3 +197,18 @@ def test_every_form_of_the_gradients(B, M, K, rows):
     stats = B.sol_layernorm(x, scale, shift, rows, with_stats=True)[1]
     dx, dscale, dshift = B.sol_layernorm_backward(dy, x, stats, scale, rows)
     check_backward(dy, x, scale, rows, 1.0, 1e-6, dx, dscale, dshift)
+
+
+def test_slices_of_one_modulation_tensor(B):
+    """Scale and shift as columns of the modulation linear's output, six chunks a sample."""
+    x, dy, _, _ = make(300, 328, 75, 21)
+    g = torch.Generator(device="cuda").manual_seed(22)
+    mod = (0.3 * torch.randn((4, 6 * 328), generator=g, device="cuda")).to(torch.bfloat16)
+    shift, scale = mod.chunk(6, dim=1)[:2]
+    y, stats = B.sol_layernorm(x, scale, shift, 75, with_stats=True)
+    check_forward(x, scale, shift, 75, 1.0, 1e-6, y, stats)
+    assert torch.equal(y, B.sol_layernorm(x, scale.contiguous(), shift.contiguous(), 75))
+    got = B.sol_layernorm_backward(dy, x, stats, scale, 75)
+    check_backward(dy, x, scale, 75, 1.0, 1e-6, *got)
+    with pytest.raises(ValueError, match="pitch"):
+        B.sol_layernorm(x, scale, shift.contiguous(), 75)

@@ -52,27 +52,27 @@ def test_refusals(B):
     p = (ctypes.addressof(buf) + 255) & ~255
     NULLP, SHAPE, ALIGN, WS = 1, 2, 3, 4
 
-    def forward(x=p, M=4, K=64, ldx=64, scale=p, shift=p, rows=4, offset=1.0, eps=1e-6, y=p, ldy=64, stats=p):
-        return L.sol_layernorm(x, M, K, ldx, scale, shift, rows, offset, eps, y, ldy, stats, None)
+    def forward(x=p, M=4, K=64, ldx=64, scale=p, shift=p, ld_mod=64, rows=4, offset=1.0, eps=1e-6, y=p, ldy=64, stats=p):
+        return L.sol_layernorm(x, M, K, ldx, scale, shift, ld_mod, rows, offset, eps, y, ldy, stats, None)
 
     assert forward(x=None) == NULLP and forward(y=None) == NULLP
-    for bad in (dict(M=0), dict(K=0), dict(K=60), dict(K=16392, ldx=16392, ldy=16392), dict(ldx=56), dict(ldy=56), dict(rows=0), dict(eps=-1.0),
+    for bad in (dict(M=0), dict(K=0), dict(K=60), dict(K=16392, ldx=16392, ldy=16392, ld_mod=16392), dict(ld_mod=56), dict(ldx=56), dict(ldy=56), dict(rows=0), dict(eps=-1.0),
                 dict(eps=float("nan")), dict(offset=float("inf")), dict(M=2 ** 31)):
         assert forward(**bad) == SHAPE, bad
-    for bad in (dict(x=p + 8), dict(y=p + 8), dict(scale=p + 2), dict(shift=p + 8), dict(stats=p + 4), dict(ldx=68), dict(ldy=66)):
+    for bad in (dict(x=p + 8), dict(y=p + 8), dict(scale=p + 2), dict(shift=p + 8), dict(stats=p + 4), dict(ldx=68), dict(ldy=66), dict(ld_mod=76)):
         assert forward(**bad) == ALIGN, bad
 
-    def backward(dy=p, ld_dy=64, x=p, ldx=64, stats=p, scale=p, M=400, K=64, rows=400, offset=1.0, dx=p, ld_dx=64, ds=p, db=p, ws=p, size=1 << 22):
-        return L.sol_layernorm_backward(dy, ld_dy, x, ldx, stats, scale, M, K, rows, offset, dx, ld_dx, ds, db, ws, size, None)
+    def backward(dy=p, ld_dy=64, x=p, ldx=64, stats=p, scale=p, ld_scale=64, M=400, K=64, rows=400, offset=1.0, dx=p, ld_dx=64, ds=p, db=p, ws=p, size=1 << 22):
+        return L.sol_layernorm_backward(dy, ld_dy, x, ldx, stats, scale, ld_scale, M, K, rows, offset, dx, ld_dx, ds, db, ws, size, None)
 
     need = L.sol_layernorm_backward_workspace_bytes(400, 64, 400)
     assert need > 0 and L.sol_layernorm_backward_workspace_bytes(400, 60, 400) == 0
     assert L.sol_layernorm_backward_workspace_bytes(8192, 64, 1) == 0            # a sample to a row: nothing to add up
     for bad in (dict(dy=None), dict(x=None), dict(stats=None), dict(dx=None), dict(ws=None)):
         assert backward(**bad) == NULLP, bad
-    for bad in (dict(M=0), dict(K=4), dict(ld_dy=32), dict(ldx=32), dict(ld_dx=32), dict(rows=-1), dict(offset=float("nan"))):
+    for bad in (dict(M=0), dict(K=4), dict(ld_dy=32), dict(ldx=32), dict(ld_dx=32), dict(ld_scale=8), dict(rows=-1), dict(offset=float("nan"))):
         assert backward(**bad) == SHAPE, bad
-    for bad in (dict(dy=p + 8), dict(x=p + 2), dict(dx=p + 8), dict(scale=p + 8), dict(ds=p + 8), dict(db=p + 4), dict(stats=p + 4), dict(ld_dx=68),
+    for bad in (dict(dy=p + 8), dict(x=p + 2), dict(dx=p + 8), dict(scale=p + 8), dict(ds=p + 8), dict(db=p + 4), dict(stats=p + 4), dict(ld_dx=68), dict(ld_scale=68),
                 dict(ws=p + 16)):
         assert backward(**bad) == ALIGN, bad
     assert backward(size=need - 1) == WS
