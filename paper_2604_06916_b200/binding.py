@@ -840,7 +840,8 @@ def sol_layernorm(x, scale=None, shift=None, rows_per_sample: int | None = None,
     """LN(x) * (scale_offset + scale[sample]) + shift[sample] in BF16; scale_offset 1: modulation, 0: a weight and a bias.
 
     x [M, K] (a view with a row pitch will do); scale and shift [samples, K] or None (slices of one modulation tensor will do, both
-    with its pitch), a sample being `rows_per_sample` rows (default: all).  Returns y, or (y, stats) `with_stats`: FP32 [M, 2] mean and 1 / sqrt(var + eps) for sol_layernorm_backward.
+    with its pitch; one vector expanded over the samples is refused), a sample being `rows_per_sample` rows (default: all).
+    Returns y, or (y, stats) `with_stats`: FP32 [M, 2] mean and 1 / sqrt(var + eps) for sol_layernorm_backward.
     """
     index = x.get_device()
     ldx = _rows_view("x", x, index)
@@ -856,7 +857,7 @@ def sol_layernorm(x, scale=None, shift=None, rows_per_sample: int | None = None,
     else:
         ldy = _rows_view("out", out, index, x.shape)
     stats = _new(x, (M, 2), torch.float32) if with_stats else None
-    code = lib().sol_layernorm(x.data_ptr(), M, K, ldx, _ptr(scale), _ptr(shift), ld_mod or K, rows, scale_offset, eps, out.data_ptr(), ldy,
+    code = lib().sol_layernorm(x.data_ptr(), M, K, ldx, _ptr(scale), _ptr(shift), K if ld_mod is None else ld_mod, rows, scale_offset, eps, out.data_ptr(), ldy,
                                None if stats is None else stats.data_ptr(), _raw_stream(index))
     if code:
         raise SolError(code, "sol_layernorm")
