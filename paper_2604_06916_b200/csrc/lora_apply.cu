@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(320, 2)
 expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ CUtensorMap tm_out, const __grid_constant__ CUtensorMap tm_f,
               const Expand p) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    if (!aligned_block(smem, p.status)) return;
+    if (!aligned_block(smem, p.status)) return ptx::grid_dependency_wait();
     Control &control = *reinterpret_cast<Control *>(smem);
     constexpr int kSums = 4;              // accumulators of 64 columns
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -331,7 +331,7 @@ expand_kernel(const __grid_constant__ CUtensorMap tm_y, const __grid_constant__ 
         if (lane == 0) control.item = it, control.found = there;
     }
     __syncthreads();
-    if (!control.found) return;
+    if (!control.found) return ptx::grid_dependency_wait();       // a grid without a tile ends behind the one in front of it all the same
     const Item item = control.item;
     // full, empty: [stage]; sum full, sum empty: [accumulator]; t ready
     constexpr int kSumFull = 2 * kMaxStages, kSumEmpty = kSumFull + kSums, kReady = kSumEmpty + kSums, kBars = kReady + 1;
@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(192, 2)
 outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_dt,
              const __grid_constant__ CUtensorMap tm_t, const Outer p) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    if (!aligned_block(smem, p.status)) return;
+    if (!aligned_block(smem, p.status)) return ptx::grid_dependency_wait();
     Control &control = *reinterpret_cast<Control *>(smem);
     int2 *runs = reinterpret_cast<int2 *>(smem + kControl);       // this block's rows: [begin, end) of each request of its adapter, cut to the slice
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
