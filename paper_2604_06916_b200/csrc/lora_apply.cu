@@ -597,7 +597,7 @@ outer_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ C
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(bar(kSumEmpty + d));
         }
-        const float scale = of_x ? 1.0f : __ldg(p.scaling + adapter);
+        const float scale = of_x || steps == 0 ? 1.0f : __ldg(p.scaling + adapter);     // no rows: zeros, whatever the scaling holds
         float *out = (of_x ? p.da : p.db) + slice * p.slice_floats;
         if (ok && c < (of_x ? p.K : p.N)) {
 #pragma unroll
