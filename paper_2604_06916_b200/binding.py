@@ -1009,6 +1009,14 @@ class AdamWPlan:
                 self._check_all(name, parts, dtype, unit)
             setattr(self, name, parts)
         self.step = torch.tensor([step, 0], dtype=torch.int64, device=self.device)
+        # a view of each: the memory stays as long as the plan, whatever the caller does to the tensors
+        columns = [params, copies or [None] * len(params)] + [getattr(self, s[0]) for s in _ADAMW_STATES[state_bits]]
+        self._memory = [[None if t is None else t.detach() for t in column] for column in columns]
+        self._columns = [[0 if t is None else t.data_ptr() for t in column] for column in self._memory]
+        self._sizes = [p.numel() for p in params]
+        # what a step compares: where the tensors are that it writes, and where they were
+        self._pointers = [t.data_ptr for t in (*params, *(copies or []))]
+        self._addresses = [f() for f in self._pointers]
         self.set_grads(grads)
 
     def _check(self, name, t, dtype, numel):
@@ -1029,17 +1037,22 @@ class AdamWPlan:
         dtypes = {g.dtype for g in grads if g is not None}
         if len(dtypes) > 1 or not dtypes <= {torch.float32, torch.bfloat16}:
             raise TypeError("grads: expected float32 or bfloat16, the same for all")
-        for g, p in zip(grads, self.params):
+        for g, n in zip(grads, self._sizes):
             if g is not None:
-                self._check("grads", g, g.dtype, p.numel())
+                self._check("grads", g, g.dtype, n)
         self.grads = grads
         self.grad_bf16 = torch.bfloat16 in dtypes
-        scales = self.state_bits == 8
-        self._packed = b"".join(
-            _ADAMW_TENSOR.pack(p.data_ptr(), 0 if self.copies is None else self.copies[i].data_ptr(), 0 if g is None else g.data_ptr(),
-                               self.m[i].data_ptr(), self.v[i].data_ptr(), self.m_scale[i].data_ptr() if scales else 0,
-                               self.v_scale[i].data_ptr() if scales else 0, 0 if g is None else p.numel())
-            for i, (p, g) in enumerate(zip(self.params, grads)))
+        self._grads_memory = [None if g is None else g.detach() for g in grads]
+        param, copy, m, v, *scales = self._columns
+        m_scale, v_scale = scales or ([0] * len(param),) * 2
+        grad = [0 if g is None else g.data_ptr() for g in grads]
+        sizes = [0 if g is None else n for g, n in zip(grads, self._sizes)]
+        self._packed = b"".join(map(_ADAMW_TENSOR.pack, param, copy, grad, m, v, m_scale, v_scale, sizes))
+
+    def _refuse_moved(self) -> None:
+        moved = next(i for i, (f, a) in enumerate(zip(self._pointers, self._addresses)) if f() != a)
+        name = "params" if moved < len(self._sizes) else "copies"
+        raise ValueError(f"{name}[{moved % len(self._sizes)}]: its memory is not that of the plan any more; make a plan of the tensors as they are")
 
 
 def sol_adamw_plan(params, grads, copies=None, state_bits: int = 32, states=None, step: int = 0) -> AdamWPlan:
@@ -1048,7 +1061,9 @@ def sol_adamw_plan(params, grads, copies=None, state_bits: int = 32, states=None
     `copies`: BF16 tensors that receive the rounded FP32 parameters (what the linears read).  `state_bits` 32: FP32 moments;
     8: E4M3 and E5M2 codes under one power of two per 32 values.  The states are new and zero, or `states`' lists ("m", "v" and, in
     8 bits, "m_scale", "v_scale"); `step` is the number of steps that they have behind them.  The plan keeps the tensors and
-    offers them as attributes: params, grads, copies, m, v, m_scale, v_scale, step ([0] on the device).
+    offers them as attributes: params, grads, copies, m, v, m_scale, v_scale, step ([0] on the device).  It is laid out for the memory
+    that they have now: once the `data` of a parameter or a copy has been replaced a step is refused (a captured one cannot be, and
+    goes on with the memory of before), and a gradient whose `data` has been replaced is given again with set_grads.  No two of the tensors may overlap.
     """
     return AdamWPlan(params, grads, copies, state_bits, states, step)
 
@@ -1067,9 +1082,11 @@ def sol_adamw_step(plan: AdamWPlan, lr: float, beta1: float = 0.9, beta2: float 
     for i, (name, t) in enumerate((("lr_scale", lr_scale), ("grad_scale", grad_scale))):
         if t is not None:
             scales[i] = _dense(name, t.reshape(-1), torch.float32, (1,), index)
+    if [f() for f in plan._pointers] != plan._addresses:
+        plan._refuse_moved()
     options = _ADAMW_OPTIONS.pack(lr, beta1, beta2, eps, weight_decay, *scales, 0 if seed is None else seed & (2 ** 64 - 1), seed is not None,
                                   plan.param_dtype is torch.bfloat16, plan.grad_bf16, plan.state_bits)
-    packed, count = plan._packed, len(plan.params)
+    packed, count = plan._packed, len(plan._sizes)
     if index == torch._C._cuda_getDevice():
         code = lib().sol_adamw_step(packed, count, options, plan.step.data_ptr(), _raw_stream(index))
     else:
