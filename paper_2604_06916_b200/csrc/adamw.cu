@@ -25,6 +25,7 @@
 #include "quant_math.cuh"
 #include "sol_internal.h"
 
+#include <atomic>
 #include <type_traits>
 
 namespace sol {
@@ -416,10 +417,14 @@ step_kernel(const __grid_constant__ Table<kN> table, const __grid_constant__ Hyp
 
 template <int kN, bool kP16, bool kG16, bool k8, bool kChance>
 sol_status_t launch_table(const Tensor *tensors, Hyper h, cudaStream_t stream, const DeviceInfo *dev) {
-    static int resident = 0;
-    if (resident == 0 && cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, step_kernel<kN, kP16, kG16, k8, kChance>, kThreads, 0) != cudaSuccess) {
-        cudaGetLastError();
-        return SOL_ERR_CUDA;
+    static std::atomic<int> known[64];     // by device: blocks per SM
+    int resident = known[dev->device].load(std::memory_order_relaxed);
+    if (resident == 0) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, step_kernel<kN, kP16, kG16, k8, kChance>, kThreads, 0) != cudaSuccess) {
+            cudaGetLastError();
+            return SOL_ERR_CUDA;
+        }
+        known[dev->device].store(resident, std::memory_order_relaxed);
     }
     const int64_t most = static_cast<int64_t>(resident) * dev->sm_count;
     // chunks of four steps share the looking for the tensor and its addresses (71 M BF16 values 179 us, with one step 184); with FP32

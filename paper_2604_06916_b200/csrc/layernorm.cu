@@ -24,6 +24,7 @@
 #include "quant_math.cuh"
 #include "sol_internal.h"
 
+#include <atomic>
 #include <type_traits>
 
 namespace sol {
@@ -427,10 +428,14 @@ int pieces_of(int64_t M, int64_t rows_per_sample, const Shape &s, int blocks) {
 template <int kWarps, int kChunks>
 sol_status_t forward_of(const Forward &p, cudaStream_t stream, const DeviceInfo *dev) {
     constexpr int kBlockWarps = kWarps > kForwardWarps ? kWarps : kForwardWarps;
-    static int resident = 0;            // blocks per SM that the kernel's registers allow
-    if (resident == 0 && cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, forward_kernel<kWarps, kChunks>, 32 * kBlockWarps, 0) != cudaSuccess) {
-        cudaGetLastError();
-        return SOL_ERR_CUDA;
+    static std::atomic<int> known[64];  // by device: blocks per SM that the kernel's registers allow
+    int resident = known[dev->device].load(std::memory_order_relaxed);
+    if (resident == 0) {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, forward_kernel<kWarps, kChunks>, 32 * kBlockWarps, 0) != cudaSuccess) {
+            cudaGetLastError();
+            return SOL_ERR_CUDA;
+        }
+        known[dev->device].store(resident, std::memory_order_relaxed);
     }
     const int64_t most = static_cast<int64_t>(resident) * dev->sm_count, want = ceil_div(p.rows, kBlockWarps / kWarps);
     forward_kernel<kWarps, kChunks><<<static_cast<unsigned>(want < most ? want : most), 32 * kBlockWarps, 0, stream>>>(p);

@@ -30,6 +30,8 @@
 #include "quant_math.cuh"
 #include "sol_internal.h"
 
+#include <atomic>
+
 namespace sol {
 namespace lora {
 namespace {
@@ -718,10 +720,13 @@ constexpr int kShrinkStages = 4;           // one block an SM
 // others: a second wave for one more block costs twice the time), none with fewer than two tiles.
 template <bool kFlip>
 int shrink_splits(int64_t items, int tiles, int smem) {
-    static int resident[kMaxCluster + 1] = {};
+    static std::atomic<int> known[64][kMaxCluster + 1];     // by device: clusters of so many blocks that run at once
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 1;
     for (int n = kMaxCluster; n > 1; --n) {
         if (n > tiles / 2) continue;
-        if (resident[n] == 0) {
+        int resident = known[dev][n].load(std::memory_order_relaxed);
+        if (resident == 0) {
             cudaLaunchConfig_t cfg{};
             cfg.gridDim = dim3(n * 1024);
             cfg.blockDim = dim3(192);
@@ -732,13 +737,13 @@ int shrink_splits(int64_t items, int tiles, int smem) {
             attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
             cfg.attrs = attr;
             cfg.numAttrs = 1;
-            if (cudaOccupancyMaxActiveClusters(&resident[n], shrink_kernel<kFlip>, &cfg) != cudaSuccess) {
+            if (cudaOccupancyMaxActiveClusters(&resident, shrink_kernel<kFlip>, &cfg) != cudaSuccess) {
                 cudaGetLastError();
-                resident[n] = 0;
                 continue;
             }
+            known[dev][n].store(resident, std::memory_order_relaxed);
         }
-        if (items <= resident[n]) return n;
+        if (items <= resident) return n;
     }
     return 1;
 }
