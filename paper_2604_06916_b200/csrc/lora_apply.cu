@@ -264,6 +264,7 @@ shrink_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ 
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(bar(kSumEmpty + d));
         }
+        if (!ok) __nanosleep(2000000);     // copies already in flight land where the sums go, before them
         // this slice's sums, for the cluster: rows of r floats and four that keep them off one another's banks, where the ring was
         const float nan = __uint_as_float(0x7FC00000u);       // what reads a sum that is not whole shall not take it for a result
         float *mine = reinterpret_cast<float *>(smem + kControl) + (quad * 32 + lane) * (p.r + 4);
