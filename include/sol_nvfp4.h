@@ -162,8 +162,9 @@ sol_status_t nvfp4_requantize_lora_batch(int64_t count, const void *const *w_lis
  *   K, N multiples of 8 up to 1048576;  r a multiple of 8, 8 <= r <= 64;  adapters, requests <= 1024
  *   workspace  sol_lora_workspace_bytes(M, K, N, r, adapters, requests, 0) bytes of device scratch, 256-byte aligned; two calls
  *              that may overlap need one each
- * Sums are FP32 in a fixed order; t enters the second product with 16 bits (the gradients' dt with 24).  Two launches.  A wait that runs out (sol_last_device_status)
- * leaves y incomplete or NaN.
+ * Sums are FP32 in a fixed order; t enters the second product with 16 bits.  Two launches.  A wait that runs out
+ * (sol_last_device_status) leaves y incomplete or NaN.  Where a value of t is infinite its row of y is NaN, also where the formula has
+ * an infinity: the part that its rounding leaves is a difference of infinities.  No other request's rows see it.
  */
 size_t sol_lora_workspace_bytes(int64_t M, int64_t K, int64_t N, int64_t r, int64_t adapters, int64_t requests, int backward);
 sol_status_t sol_lora_apply(const void *x_bf16, int64_t ldx, const void *lora_a, const void *lora_b, const float *scaling,
@@ -177,7 +178,8 @@ sol_status_t sol_lora_apply(const void *x_bf16, int64_t ldx, const void *lora_a,
  *   t        [M, 2 r] as sol_lora_apply left it;  dx_bf16  [M, K], pitch ld_dx, in place: the gradient that x has from the shared
  *            projection, or NULL
  *   dlora_a, dlora_b  FP32, shaped as the factors, 16-byte aligned, overwritten (zeros for an adapter without rows)
- *   workspace  sol_lora_workspace_bytes(..., 1) bytes.  Everything else as there.  Three or four launches.
+ *   workspace  sol_lora_workspace_bytes(..., 1) bytes.  Everything else as there (dt in t's place).  Three or four launches.
+ * dt enters dlora_a with 24 bits and dx, which is BF16, with 16.
  */
 sol_status_t sol_lora_backward(const void *dy_bf16, int64_t ld_dy, const void *x_bf16, int64_t ldx, const void *t, const void *lora_a,
                                const void *lora_b, const float *scaling, const int32_t *offsets, const int32_t *ids, int64_t requests,
