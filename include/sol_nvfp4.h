@@ -190,6 +190,8 @@ sol_status_t sol_lora_backward(const void *dy_bf16, int64_t ld_dy, const void *x
  * One AdamW step over many tensors (the policy update in front of that refresh), in place.  Per element, FP32, with t the step:
  *     g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;   v = beta2 v + (1 - beta2) g^2       (every operation rounded)
  *     param = param (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * Root and quotient are the hardware's approximate ones, products and sums of the second line are fused: param is off by at most 2^-24
+ * (2 |param| + 16 |update|) before it is rounded to its type.
  *   tensors     HOST array of `count` descriptions (read during the call only) of device tensors of n >= 0 dense elements, 16-byte
  *               aligned, no two of them overlapping:  param FP32 or BF16;  copy BF16 or NULL, receives bf16_rne(param) beside an FP32
  *               param;  grad FP32 or BF16, of the same types for all;  m, v the states
@@ -201,8 +203,10 @@ sol_status_t sol_lora_backward(const void *dy_bf16, int64_t ld_dy, const void *x
  *   step_state  two 64-bit words (device, 8-byte aligned): [0] steps done so far, read and advanced by this call (t is one more),
  *               [1] scratch, 0 between calls.  The same for all tensors of a call
  *   lr_scale, grad_scale  one float each (device) or NULL (1): factors that change between the replays of a captured call
- * lr and weight_decay >= 0, 0 <= beta < 1, eps >= 0.  An element whose gradient is not finite becomes NaN, with its states; its
- * block's other elements do not.  One launch for up to 448 tensors.
+ * lr and weight_decay >= 0, 0 <= beta < 1, eps >= 0.  An element whose g is not finite becomes NaN; its 8-bit states too, its FP32 ones
+ * are what the formulas give (infinite, or NaN).  Where g is finite and its square is not (|g| above 1.8e19) v is infinite, and the element
+ * keeps its value but for the decay; an 8-bit v is NaN then, and the element is NaN from the next step on.  The other elements
+ * of a block are not affected.  One launch for up to 448 tensors.
  */
 typedef struct {
     void *param, *copy;

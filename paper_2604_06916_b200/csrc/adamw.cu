@@ -1,6 +1,8 @@
-// One AdamW step over many tensors (sm_100a).  Per element, with t the step and every operation rounded in FP32:
-//     m = b1 m + (1 - b1) g;   v = b2 v + (1 - b2) g^2
+// One AdamW step over many tensors (sm_100a).  Per element in FP32, with t the step:
+//     m = b1 m + (1 - b1) g;   v = b2 v + (1 - b2) g^2          (every operation rounded)
 //     p = p (1 - lr decay) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+// In the second line root and quotient are approximate instructions (2^-22 each) and products are fused with their sums: that touches the
+// last places of an update, which is itself far below the parameter; the moments, which are compared bit for bit, are not approximate.
 // The tensors' addresses are the kernel's parameter (up to kTable of them a launch), so a step over a few hundred adapters is one
 // launch, from host arrays, and can be captured; the step counter is on the device and counts replays too: every block takes a
 // ticket when it has read it, the one with the last ticket writes it back.
