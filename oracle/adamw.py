@@ -53,6 +53,7 @@ def encode(v, mantissa: int, noise):
 
 
 def mix(x):
+    """The published 32-bit mixer lowbias32 (C. Wellons' hash-prospector): two products, three shifts."""
     x = np.asarray(x, np.uint64) & np.uint64(0xFFFFFFFF)
     w = np.uint64(0xFFFFFFFF)
     x = x ^ (x >> np.uint64(16))

@@ -10,8 +10,9 @@
 // States in 8 bits: blocks of 32 values under a power of two (E8M0, as in the MXFP4 tensors), m in E4M3, v in E5M2 (it is a
 // square: twice the exponents).  A value keeps three or two mantissa bits, which is coarser than what a step adds to v at b2 = 0.999:
 // rounded to nearest, v would stay where it is.  So it is rounded up or down by chance, in proportion (16 random bits a value, by
-// hashing seed, step, tensor and place): the average moves as the 32-bit state does.  The powers of two put the block's largest value
-// at [2^7, 2^8) of E4M3, [2^14, 2^15) of E5M2, so rounding up never leaves the format.
+// hashing seed, step, tensor and place): the average moves as the 32-bit state does.  The hash's mixer is a published one of two products
+// and three shifts, lowbias32 (C. Wellons' hash-prospector).  The powers of two put the block's largest value at [2^7, 2^8) of E4M3,
+// [2^14, 2^15) of E5M2, so rounding up never leaves the format.
 // The new parameter comes from m and v before they are rounded.
 //
 // HBM bound in FP32: 28 bytes per element (30 with the BF16 copy); 18.1 with 8-bit states and a copy; 10.1 with BF16 parameters and
