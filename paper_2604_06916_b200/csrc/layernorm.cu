@@ -15,9 +15,11 @@
 // Gradients: a thread owns the same eight columns of every row that its block walks, so that the sums over rows stay in its
 // registers; the two row means go over the block (a group of warps per row, as many groups as fit the block) once per four
 // rows, whose successors are under way meanwhile.  A block's sums leave as FP32 partials, which a second launch adds up in FP64 in
-// a fixed order: equal inputs give equal bits.  Measured: 9216 x 3072, two samples, 33.3 us = 5.1 TB/s, 78 %; 13287 x 2432 43.2 us.
-// Bound by issuing: some 560 instructions a warp and four rows, half of them taking BF16 apart and putting it together; twelve warps a
-// block with 168 registers issue every second cycle.  The sum over the blocks is 4 us of it.  Rows through a ring in shared
+// a fixed order: equal inputs give equal bits.  Measured: 9216 x 3072, two samples, 33.5 us = 5.1 TB/s, 77 %; 13287 x 2432 43.2 us.
+// Bound by dependences: three warps a scheduler (168 registers a thread) issue every second cycle (at 2432 columns, ten warps, 44 % of
+// them), and per instruction a warp waits 1.2 cycles for its own last result, 0.8 for shuffles and shared memory, 0.8 for the arithmetic
+// pipe, 0.3 (0.6) at the barrier, 0.4 (0.2) for memory.  A step of four rows is some 560 instructions a warp, half of them taking BF16
+// apart and putting it together.  The sum over the blocks is 4 us of it.  Rows through a ring in shared
 // memory (24 warps, bulk copies) took 43.6 us: the same instructions and the second reads; without loads ahead 41 us, two
 // sets of registers in turn spill (51 us), two blocks an SM with fewer rows a step 43 us.
 #include "ptx.cuh"
@@ -181,7 +183,7 @@ struct Backward {
     float offset, inv_k;
 };
 
-constexpr int kMaxWarps = 16;           // of a block, at most (twelve where 168 registers a thread are wanted: up to 12288 columns)
+constexpr int kMaxWarps = 16;           // of a block, at most (twelve where 168 registers a thread are wanted: up to 3072 columns and from 4097 to 6144)
 constexpr int kGroupColumns = 256;      // columns of a warp and piece
 // Sums of kValues (a power of two up to 32) values over the warp: lane l ends up with that of value l >> (5 - log2 kValues).
 template <int kValues>
@@ -402,9 +404,9 @@ struct Shape {
 };
 // A thread holds `chunks` pieces of eight columns of `rows` rows, and as many again of the next ones, in what a block of twelve (168
 // registers a thread) or sixteen warps (128) leaves it beside the sums and the gain.  Up to 3072 columns as many groups as twelve
-// warps make; beyond, one.  Measured (gradients of 28 to 34 M values, us; in brackets another form): 4096 columns 42.4 (two pieces, eight
-// warps: 51.9), 6144 42, 8192 47 (two rows with spills: 78; four pieces: 98), 12288 57 (with the next row: 69; four pieces: 66), 16384 82
-// (twelve warps and the next row: 118): there the sums alone take half the registers.
+// warps make; beyond, one.  Measured (gradients of 28.3 M values, two samples; in brackets other forms' time in terms of this one's, taken at
+// 25 to 34 M): 4096 columns 35 us (two pieces, eight warps: 1.2), 6144 43, 8192 41 (two rows with spills: 1.7; four pieces: 2.1), 12288 65 (with
+// the next row: 1.2; four pieces: 1.15), 16384 84 (twelve warps and the next row: 1.4): there the sums alone take half the registers.
 constexpr int kVariants = 6;
 constexpr int kLimit[kVariants] = {3072, 4096, 6144, 8192, 12288, 16384}, kChunksOf[kVariants] = {1, 1, 2, 2, 3, 4}, kRowsOf[kVariants] = {4, 2, 2, 1, 1, 1};
 Shape shape_of(int64_t K) {
@@ -416,7 +418,8 @@ Shape shape_of(int64_t K) {
     s.groups = s.variant == 0 ? 12 / s.warps_per_row : 1;
     return s;
 }
-// Pieces of a sample: so many that the blocks all have one, none of fewer rows than the groups take in a step.
+// Pieces of a sample: as many as there are blocks for each sample (rounded down, at least one: where samples are more than half as many as
+// blocks, and no multiple of them, some blocks have less to do), none of fewer rows than the groups take in a step.
 int pieces_of(int64_t M, int64_t rows_per_sample, const Shape &s, int blocks) {
     const int64_t samples = ceil_div(M, rows_per_sample);
     const int64_t most = ceil_div(rows_per_sample < M ? rows_per_sample : M, s.groups * s.rows);

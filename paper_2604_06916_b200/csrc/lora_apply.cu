@@ -49,7 +49,7 @@ constexpr int kMaxStages = 8;
 constexpr int kShrinkStage = 2 * kStage;    // 128 columns: rows of 256 bytes, which DRAM gives faster than twice 128
 constexpr int kMaxCluster = 8;
 constexpr int kHalfSmem = 115712, kFullSmem = 232448;     // a block's shared memory where two fit an SM, or one
-constexpr int kSlots = 296;              // blocks that are resident at once: two on each of 148 SMs
+constexpr int kSlots = 296;              // blocks that are taken to be resident at once: two on each of 148 SMs (above rank 32 expand has one)
 
 struct Requests {
     const int32_t *offsets;    // [requests + 1]
